@@ -201,6 +201,55 @@ kvs_status_t kvs_evict_attn_fwd_noalloc(const void* Q, const void* K, const void
                                         int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D,
                                         float softmax_scale, void* stream);
 
+/* ---------------------------------------------------------------- sliding window with sinks
+ * Attention of a layer with a sliding window in which the first tokens of a
+ * trace stay visible (sinks), on top of the evictions: query i sees key j iff
+ *
+ *        j <= i < evict_at[j]   and   (i - j < window  or  j < sinks)
+ *
+ * (trace-local indices; window >= 1 counts the query's own token, sinks >= 0).
+ * evict_at may be NULL: nothing is evicted.  Everything else - outputs,
+ * gradients, layouts, checks - is as in kvs_evict_attn_{fwd,bwd}_ex without
+ * flags: cu_seqlens NULL means B fixed-length traces of max_seqlen tokens.
+ * Workspaces come from the queries below; the backward's may be smaller in
+ * the way kvs_evict_attn_bwd's may.  Every query sees itself, so no row is empty.
+ */
+size_t kvs_window_attn_fwd_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D);
+kvs_status_t kvs_window_attn_fwd(const void* Q, const void* K, const void* V,
+                                 const int32_t* evict_at, const int32_t* cu_seqlens,
+                                 void* O, float* LSE,
+                                 int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D,
+                                 float softmax_scale, int window, int sinks,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+size_t kvs_window_attn_bwd_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D);
+kvs_status_t kvs_window_attn_bwd(const void* dO, const void* Q, const void* K, const void* V,
+                                 const void* O, const float* LSE,
+                                 const int32_t* evict_at, const int32_t* cu_seqlens,
+                                 void* dQ, void* dK, void* dV,
+                                 int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D,
+                                 float softmax_scale, int window, int sinks,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------- attention weights of the keys
+ * What every key of a trace has received from the softmax, over all q-heads:
+ *
+ *        W_j = sum_h sum_{i sees j} exp(s_ij^h - LSE_i^h)
+ *
+ * W is fp32, [B][T] (fixed) or [Ntot] (varlen); LSE is the forward's, of the
+ * same inputs and the same mask.  Only the last last_rows queries of each
+ * trace count if last_rows > 0, all of them if it is 0.  window 0: no window
+ * (sinks is then without effect); evict_at NULL: nothing is evicted.  A key no
+ * counted query sees gets 0; tokens behind the last trace keep what W held.
+ * These are the weights a cache starts from (kvs_paged_append_weighted) when
+ * the trace's keys enter it.
+ */
+size_t kvs_key_weights_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D, int last_rows);
+kvs_status_t kvs_key_weights(const void* Q, const void* K, const float* LSE,
+                             const int32_t* evict_at, const int32_t* cu_seqlens, float* W,
+                             int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D,
+                             float softmax_scale, int window, int sinks, int last_rows,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------- tile classes
  * Class of every BM x BN tile of the mask: 0 = EMPTY (no visible element,
  * skipped), 1 = PARTIAL (per-element mask), 2 = FULL (every element
@@ -234,7 +283,7 @@ kvs_status_t kvs_check_evict_at(const int32_t* evict_at, const int32_t* cu_seqle
  * Per-kernel timing for benchmarks.  While enabled, each call brackets every
  * kernel it launches with HIP events on the call's stream.  kvs_prof_read
  * waits for the recorded events and returns, for the kernel named `name`
- * ("classify", "fwd", "bwd_pre", "bwd_dkdv", "bwd_dq", "paged_decode"), the
+ * ("classify", "fwd", "bwd_pre", "bwd_dkdv", "bwd_dq", "key_weights", "paged_decode", "paged_evict_lowest"), the
  * number of launches and their total duration in milliseconds.  The records
  * are process-wide (every thread's launches land in one list, guarded by a
  * lock), so enable timing only while the calls to be timed are the only
@@ -335,6 +384,40 @@ kvs_status_t kvs_paged_append_host(const void* K_new, const void* V_new, const i
 kvs_status_t kvs_paged_evict_host(const int32_t* slots, int n, int32_t* slot_pos, int num_blocks, int block_size,
                                   void* stream);
 
+/* ---- weights of the entries
+ * A cache may keep a weight for every entry, fp32 slot_weight [num_blocks *
+ * block_size]: the attention weight the entry has received so far.  It is set
+ * when the entry is appended, added to by kvs_paged_decode_ex and read by
+ * kvs_paged_evict_lowest; what it holds for a slot without an entry is without
+ * meaning.  Caches of several layers that share one block manager may share
+ * one slot_weight (each layer's decode then adds to the sum), on one stream.
+ * Calls that take it expect every block in the table of at most one sequence,
+ * once; otherwise the weights are unspecified (nothing else is). */
+
+/* kvs_paged_append and kvs_paged_append_host for such a cache: also
+ * slot_weight[slots[t]] = W_new[t] (device fp32 [n], e.g. from kvs_key_weights), or 0 if W_new is NULL. */
+kvs_status_t kvs_paged_append_weighted(const void* K_new, const void* V_new, const float* W_new,
+                                       const int32_t* positions, const int32_t* slots, int n,
+                                       void* K_cache, void* V_cache, int32_t* slot_pos, float* slot_weight,
+                                       int num_blocks, int block_size, int Hkv, int D, void* stream);
+kvs_status_t kvs_paged_append_weighted_host(const void* K_new, const void* V_new, const float* W_new,
+                                            const int32_t* positions, const int32_t* slots, int n,
+                                            void* K_cache, void* V_cache, int32_t* slot_pos, float* slot_weight,
+                                            int num_blocks, int block_size, int Hkv, int D, void* stream);
+
+/* Evict the entries of lowest weight: of sequence s, as many as its live
+ * entries exceed keep[s] (device int32 [num_seqs]; negative counts as 0), but at
+ * most max_out, and only entries at trace positions that are >= sinks and <=
+ * (newest live position) - recent.  Lowest weights first; NaN counts as the
+ * highest weight, equal weights leave in the table's order.  slot_pos of the
+ * evicted slots becomes -1; their positions go to positions[s][0..counts[s])
+ * (device int32 [num_seqs][max_out], in the table's order, the rest -1), for
+ * kvs_bm_evict.  Tables are clamped as in the decode. */
+kvs_status_t kvs_paged_evict_lowest(const float* slot_weight, int32_t* slot_pos, const int32_t* block_table,
+                                    const int32_t* seq_blocks, const int32_t* keep, int32_t* positions,
+                                    int32_t* counts, int num_seqs, int num_blocks, int block_size, int max_blocks,
+                                    int sinks, int recent, int max_out, void* stream);
+
 /* ---- decode attention over the live cache
  * One query token per sequence: Q, O bf16 [num_seqs][Hq][D], LSE fp32
  * [num_seqs][Hq] (natural log).  Sequence s attends over every slot of its
@@ -352,6 +435,25 @@ kvs_status_t kvs_paged_decode(const void* Q, const void* K_cache, const void* V_
                               int num_seqs, int Hq, int Hkv, int D, int num_blocks, int block_size,
                               int max_blocks, float softmax_scale, void* workspace, size_t workspace_bytes,
                               void* stream);
+
+/* The decode of a layer with a sliding window, and the decode that keeps the entries' weights; both, or neither.
+ * window > 0: the query of sequence s, at trace position q_pos[s] (device int32
+ * [num_seqs]), sees of the live entries those at positions p <= q_pos[s] with
+ * q_pos[s] - p < window or p < sinks: row q_pos[s] of kvs_window_attn_fwd.
+ * Positions within a sequence are distinct (as a block manager has them); of
+ * one with repeated positions at most window + sinks entries are seen.
+ * window 0: every live entry, q_pos (may be NULL) and sinks without effect.
+ * slot_weight not NULL: slot_weight[slot] += sum_h exp(s_h - LSE_h) over all
+ * q-heads, for every entry the query sees.  Limits and layouts are those of
+ * kvs_paged_decode (under a window at most 65535 sequences); the workspace is
+ * the query's, `weights` nonzero for calls with slot_weight. */
+size_t kvs_paged_decode_ex_workspace(int num_seqs, int Hq, int Hkv, int D, int num_blocks, int max_blocks,
+                                     int block_size, int window, int sinks, int weights);
+kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
+                                 float* slot_weight, const int32_t* block_table, const int32_t* seq_blocks,
+                                 const int32_t* q_pos, void* O, float* LSE, int num_seqs, int Hq, int Hkv, int D,
+                                 int num_blocks, int block_size, int max_blocks, float softmax_scale, int window,
+                                 int sinks, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

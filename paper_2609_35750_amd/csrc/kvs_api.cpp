@@ -351,6 +351,135 @@ kvs_status_t kvs_evict_attn_fwd_noalloc(const void* Q, const void* K, const void
                     scratch, kvs::kNoAllocScratchBytes, stream);
 }
 
+// ---------------------------------------------------------------- sliding window with sinks, attention weights
+// Workspace: the keys' last visible queries, then what the call without a window takes.
+static size_t until_bytes(long long ntok) { return ((size_t)ntok * sizeof(int32_t) + 255) & ~(size_t)255; }
+
+// Shapes of a call in either layout, its window and its scale.
+static kvs_status_t window_dims(const int32_t* cu, int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D, float scale,
+                                int window, int least, int sinks) {
+  if (kvs_status_t st = ex_dims(cu, B, Ntot, max_seqlen)) return st;
+  if (kvs_status_t st = check_dims(B, max_seqlen, Ntot, Hq, Hkv, D)) return st;
+  if (!(scale > 0.f) || scale != scale) return fail(KVS_ERR_SHAPE, "softmax_scale must be positive and finite");
+  if (window < least) return fail(KVS_ERR_SHAPE, "window must be >= %d (got %d)", least, window);
+  if (sinks < 0) return fail(KVS_ERR_SHAPE, "sinks must be >= 0 (got %d)", sinks);
+  return KVS_OK;
+}
+
+// The problem of a windowed call: every trace is shorter than kMaxSeq, so a wider window is as good as that.
+static kvs::Problem window_problem(const void* Q, const void* K, const void* V, const int32_t* evict_at,
+                                   const int32_t* cu, int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D,
+                                   float scale, int window, int sinks, void* ws, size_t ws_bytes, void* stream) {
+  kvs::Problem p{};
+  p.q = Q; p.k = K; p.v = V; p.evict = evict_at; p.cu = cu;
+  p.B = B; p.T = max_seqlen; p.ntok = Ntot; p.Hq = Hq; p.Hkv = Hkv; p.D = D; p.G = Hq / Hkv; p.scale = scale;
+  p.window = std::min(window, kMaxSeq);
+  p.sinks = std::min(sinks, kMaxSeq);
+  p.until = (int32_t*)ws;
+  p.ws = (char*)ws + until_bytes(Ntot);
+  p.ws_bytes = ws_bytes - until_bytes(Ntot);
+  p.stream = (hipStream_t)stream;
+  return p;
+}
+
+size_t kvs_window_attn_fwd_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D) {
+  if (B < 1 || Ntot < 0) return 0;
+  (void)max_seqlen; (void)Hq; (void)Hkv; (void)D;
+  return until_bytes(Ntot) + fwd_ws(B, Ntot);
+}
+
+kvs_status_t kvs_window_attn_fwd(const void* Q, const void* K, const void* V, const int32_t* evict_at,
+                                 const int32_t* cu_seqlens, void* O, float* LSE, int B, int Ntot, int max_seqlen,
+                                 int Hq, int Hkv, int D, float softmax_scale, int window, int sinks, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  t_err.clear();
+  if (kvs_status_t st = window_dims(cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale, window, 1, sinks))
+    return st;
+  if (Ntot == 0) return KVS_OK;  // empty batch: pointers and workspace are not looked at
+  REQUIRE_PTR(Q, "Q");
+  REQUIRE_PTR(K, "K");
+  REQUIRE_PTR(V, "V");
+  REQUIRE_PTR(O, "O");
+  REQUIRE_PTR(LSE, "LSE");
+  if (kvs_status_t st = check_ws(workspace, workspace_bytes, until_bytes(Ntot) + fwd_ws(B, Ntot))) return st;
+  kvs::Problem p = window_problem(Q, K, V, evict_at, cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale, window,
+                                  sinks, workspace, workspace_bytes, stream);
+  p.o = O; p.lse = LSE;
+  return run_fwd(p);
+}
+
+size_t kvs_window_attn_bwd_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D) {
+  if (B < 1 || Ntot < 0 || Hq < 1 || Hkv < 1 || max_seqlen < 1) return 0;
+  return until_bytes(Ntot) + bwd_ws(B, max_seqlen, Ntot, Hq, Hkv, D);
+}
+
+kvs_status_t kvs_window_attn_bwd(const void* dO, const void* Q, const void* K, const void* V, const void* O,
+                                 const float* LSE, const int32_t* evict_at, const int32_t* cu_seqlens, void* dQ,
+                                 void* dK, void* dV, int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D,
+                                 float softmax_scale, int window, int sinks, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  t_err.clear();
+  if (kvs_status_t st = window_dims(cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale, window, 1, sinks))
+    return st;
+  if (Ntot == 0) return KVS_OK;
+  REQUIRE_PTR(dO, "dO");
+  REQUIRE_PTR(Q, "Q");
+  REQUIRE_PTR(K, "K");
+  REQUIRE_PTR(V, "V");
+  REQUIRE_PTR(O, "O");
+  REQUIRE_PTR(LSE, "LSE");
+  REQUIRE_PTR(dQ, "dQ");
+  REQUIRE_PTR(dK, "dK");
+  REQUIRE_PTR(dV, "dV");
+  if (kvs_status_t st = check_ws(workspace, workspace_bytes,
+                                 until_bytes(Ntot) + bwd_ws_least(B, max_seqlen, Ntot, Hq, Hkv, D)))
+    return st;
+  kvs::Problem p = window_problem(Q, K, V, evict_at, cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale, window,
+                                  sinks, workspace, workspace_bytes, stream);
+  p.o_in = O; p.dout = dO; p.lse_in = LSE; p.dq = dQ; p.dk = dK; p.dv = dV;
+  return run_bwd(p);
+}
+
+static int rows_counted(int last_rows, int max_seqlen) {
+  return last_rows > 0 ? std::min(last_rows, max_seqlen) : max_seqlen;
+}
+
+size_t kvs_key_weights_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D, int last_rows) {
+  if (B < 1 || Ntot < 0 || Hkv < 1 || max_seqlen < 1) return 0;
+  (void)Hq; (void)D;
+  return until_bytes(Ntot) + fwd_ws(B, Ntot) +
+         kvs::ws_weights_bytes(B, max_seqlen, Ntot, Hkv, rows_counted(last_rows, max_seqlen));
+}
+
+kvs_status_t kvs_key_weights(const void* Q, const void* K, const float* LSE, const int32_t* evict_at,
+                             const int32_t* cu_seqlens, float* W, int B, int Ntot, int max_seqlen, int Hq, int Hkv,
+                             int D, float softmax_scale, int window, int sinks, int last_rows, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  t_err.clear();
+  if (kvs_status_t st = window_dims(cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale, window, 0, sinks))
+    return st;
+  if (last_rows < 0) return fail(KVS_ERR_SHAPE, "last_rows must be >= 0 (got %d)", last_rows);
+  const int rows = rows_counted(last_rows, max_seqlen);
+  if (kvs::weights_grid(B, max_seqlen, Hkv, rows) * 256 > 0xffffffffll)
+    return fail(KVS_ERR_UNSUPPORTED, "key weights grid too large");
+  if (Ntot == 0) return KVS_OK;
+  REQUIRE_PTR(Q, "Q");
+  REQUIRE_PTR(K, "K");
+  REQUIRE_PTR(LSE, "LSE");
+  REQUIRE_PTR(W, "W");
+  if (kvs_status_t st = check_ws(workspace, workspace_bytes,
+                                 kvs_key_weights_workspace(B, Ntot, max_seqlen, Hq, Hkv, D, last_rows)))
+    return st;
+  kvs::Problem p = window_problem(Q, K, nullptr, evict_at, cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale,
+                                  window, sinks, workspace, workspace_bytes, stream);
+  p.lse_in = LSE;
+  int2* kstats = (int2*)p.ws;
+  hipError_t e = kvs::launch_kstats(p, kstats);
+  if (e != hipSuccess) return hip_fail(e, "key-tile statistics launch");
+  e = kvs::launch_key_weights(p, kstats, rows, (float*)((char*)p.ws + fwd_ws(B, Ntot)), W);
+  return e == hipSuccess ? KVS_OK : hip_fail(e, "key weights launch");
+}
+
 kvs_status_t kvs_classify_tiles(const int32_t* evict_at, const int32_t* cu_seqlens, int B, int T, int BM, int BN,
                                 uint8_t* tile_class, void* stream) {
   t_err.clear();
@@ -498,23 +627,52 @@ static kvs_status_t check_cache_dims(int num_blocks, int block_size) {
   return KVS_OK;
 }
 
-kvs_status_t kvs_paged_append(const void* K_new, const void* V_new, const int32_t* positions, const int32_t* slots,
-                              int n, void* K_cache, void* V_cache, int32_t* slot_pos, int num_blocks,
-                              int block_size, int Hkv, int D, void* stream) {
-  t_err.clear();
+// W_new (may be NULL) and slot_weight: the weights of a cache that keeps some; `weighted` requires slot_weight.
+static kvs_status_t append_checks(const void* K_new, const void* V_new, const int32_t* positions, const int32_t* slots,
+                                  int n, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
+                                  const float* slot_weight, bool weighted, int num_blocks, int block_size, int Hkv,
+                                  int D) {
   if (kvs_status_t st = check_cache_dims(num_blocks, block_size)) return st;
   if (n < 0 || Hkv < 1) return fail(KVS_ERR_SHAPE, "n must be >= 0 and Hkv >= 1");
   if (D != 64 && D != 128) return fail(KVS_ERR_SHAPE, "head dim D must be 64 or 128 (got %d)", D);
   REQUIRE_PTR(K_cache, "K_cache");
   REQUIRE_PTR(V_cache, "V_cache");
   if (!slot_pos) return fail(KVS_ERR_NULL, "slot_pos is NULL");
+  if (weighted && !slot_weight) return fail(KVS_ERR_NULL, "slot_weight is NULL");
   if (n == 0) return KVS_OK;
   REQUIRE_PTR(K_new, "K_new");
   REQUIRE_PTR(V_new, "V_new");
   if (!positions || !slots) return fail(KVS_ERR_NULL, "positions or slots is NULL");
+  return KVS_OK;
+}
+
+static kvs_status_t append_common(const void* K_new, const void* V_new, const float* W_new, const int32_t* positions,
+                                  const int32_t* slots, int n, void* K_cache, void* V_cache, int32_t* slot_pos,
+                                  float* slot_weight, bool weighted, int num_blocks, int block_size, int Hkv, int D,
+                                  void* stream) {
+  t_err.clear();
+  kvs_status_t st = append_checks(K_new, V_new, positions, slots, n, K_cache, V_cache, slot_pos, slot_weight, weighted,
+                                  num_blocks, block_size, Hkv, D);
+  if (st != KVS_OK || n == 0) return st;
   hipError_t e = kvs::launch_paged_append(K_new, V_new, positions, slots, n, K_cache, V_cache, slot_pos,
-                                          num_blocks * block_size, block_size, Hkv, D, (hipStream_t)stream);
+                                          num_blocks * block_size, block_size, Hkv, D, {W_new, slot_weight},
+                                          (hipStream_t)stream);
   return e == hipSuccess ? KVS_OK : hip_fail(e, "paged append launch");
+}
+
+kvs_status_t kvs_paged_append(const void* K_new, const void* V_new, const int32_t* positions, const int32_t* slots,
+                              int n, void* K_cache, void* V_cache, int32_t* slot_pos, int num_blocks,
+                              int block_size, int Hkv, int D, void* stream) {
+  return append_common(K_new, V_new, nullptr, positions, slots, n, K_cache, V_cache, slot_pos, nullptr, false,
+                       num_blocks, block_size, Hkv, D, stream);
+}
+
+kvs_status_t kvs_paged_append_weighted(const void* K_new, const void* V_new, const float* W_new,
+                                       const int32_t* positions, const int32_t* slots, int n, void* K_cache,
+                                       void* V_cache, int32_t* slot_pos, float* slot_weight, int num_blocks,
+                                       int block_size, int Hkv, int D, void* stream) {
+  return append_common(K_new, V_new, W_new, positions, slots, n, K_cache, V_cache, slot_pos, slot_weight, true,
+                       num_blocks, block_size, Hkv, D, stream);
 }
 
 kvs_status_t kvs_paged_evict(const int32_t* slots, int n, int32_t* slot_pos, int num_blocks, int block_size,
@@ -564,30 +722,40 @@ static bool capturing(void* stream) {
   return hipStreamIsCapturing((hipStream_t)stream, &st) == hipSuccess && st != hipStreamCaptureStatusNone;
 }
 
-kvs_status_t kvs_paged_append_host(const void* K_new, const void* V_new, const int32_t* positions,
-                                   const int32_t* slots, int n, void* K_cache, void* V_cache, int32_t* slot_pos,
-                                   int num_blocks, int block_size, int Hkv, int D, void* stream) {
+static kvs_status_t append_host_common(const void* K_new, const void* V_new, const float* W_new,
+                                       const int32_t* positions, const int32_t* slots, int n, void* K_cache,
+                                       void* V_cache, int32_t* slot_pos, float* slot_weight, bool weighted,
+                                       int num_blocks, int block_size, int Hkv, int D, void* stream) {
   t_err.clear();
-  if (kvs_status_t st = check_cache_dims(num_blocks, block_size)) return st;
-  if (n < 0 || Hkv < 1) return fail(KVS_ERR_SHAPE, "n must be >= 0 and Hkv >= 1");
-  if (D != 64 && D != 128) return fail(KVS_ERR_SHAPE, "head dim D must be 64 or 128 (got %d)", D);
-  REQUIRE_PTR(K_cache, "K_cache");
-  REQUIRE_PTR(V_cache, "V_cache");
-  if (!slot_pos) return fail(KVS_ERR_NULL, "slot_pos is NULL");
-  if (n == 0) return KVS_OK;
-  REQUIRE_PTR(K_new, "K_new");
-  REQUIRE_PTR(V_new, "V_new");
-  if (!positions || !slots) return fail(KVS_ERR_NULL, "positions or slots is NULL");
+  kvs_status_t st = append_checks(K_new, V_new, positions, slots, n, K_cache, V_cache, slot_pos, slot_weight, weighted,
+                                  num_blocks, block_size, Hkv, D);
+  if (st != KVS_OK || n == 0) return st;
   if (capturing(stream)) return fail(KVS_ERR_UNSUPPORTED, "host lists are not captured");
   if (!count_runs(positions, slots, n)) return fail(KVS_ERR_UNSUPPORTED, "slots lie in too many runs");
   kvs::SlotRuns runs;
   for (int t = 0; t < n;) {
     next_runs(positions, slots, n, &t, &runs);
     hipError_t e = kvs::launch_paged_append_runs(K_new, V_new, runs, K_cache, V_cache, slot_pos,
-                                                 num_blocks * block_size, block_size, Hkv, D, (hipStream_t)stream);
+                                                 num_blocks * block_size, block_size, Hkv, D, {W_new, slot_weight},
+                                                 (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "paged append launch");
   }
   return KVS_OK;
+}
+
+kvs_status_t kvs_paged_append_host(const void* K_new, const void* V_new, const int32_t* positions,
+                                   const int32_t* slots, int n, void* K_cache, void* V_cache, int32_t* slot_pos,
+                                   int num_blocks, int block_size, int Hkv, int D, void* stream) {
+  return append_host_common(K_new, V_new, nullptr, positions, slots, n, K_cache, V_cache, slot_pos, nullptr, false,
+                            num_blocks, block_size, Hkv, D, stream);
+}
+
+kvs_status_t kvs_paged_append_weighted_host(const void* K_new, const void* V_new, const float* W_new,
+                                            const int32_t* positions, const int32_t* slots, int n, void* K_cache,
+                                            void* V_cache, int32_t* slot_pos, float* slot_weight, int num_blocks,
+                                            int block_size, int Hkv, int D, void* stream) {
+  return append_host_common(K_new, V_new, W_new, positions, slots, n, K_cache, V_cache, slot_pos, slot_weight, true,
+                            num_blocks, block_size, Hkv, D, stream);
 }
 
 kvs_status_t kvs_paged_evict_host(const int32_t* slots, int n, int32_t* slot_pos, int num_blocks, int block_size,
@@ -666,6 +834,92 @@ kvs_status_t kvs_paged_decode(const void* Q, const void* K_cache, const void* V_
   p.stream = (hipStream_t)stream;
   hipError_t e = kvs::launch_paged_decode(p);
   return e == hipSuccess ? KVS_OK : hip_fail(e, "paged decode launch");
+}
+
+// ---------------------------------------------------------------- decode under a window and with weights
+// The sizes of such a call; workspace and launch sizes follow from them alone.
+static kvs::PagedDecode decode_ex_sizes(int S, int Hq, int Hkv, int D, int num_blocks, int max_blocks, int block_size,
+                                        int window, int sinks, bool weights) {
+  static float some;   // stands for the weights: only whether there are any counts here
+  kvs::PagedDecode p{};
+  p.S = S;
+  p.Hq = Hq;
+  p.Hkv = Hkv;
+  p.D = D;
+  p.num_blocks = num_blocks;
+  p.max_blocks = max_blocks;
+  p.block_size = block_size;
+  p.window = window;
+  p.sinks = window > 0 ? sinks : 0;
+  p.slot_weight = weights ? &some : nullptr;
+  return p;
+}
+
+size_t kvs_paged_decode_ex_workspace(int num_seqs, int Hq, int Hkv, int D, int num_blocks, int max_blocks,
+                                     int block_size, int window, int sinks, int weights) {
+  if (num_seqs < 1 || Hq < 1 || Hkv < 1 || num_blocks < 1 || max_blocks < 1 || block_size < 1 || window < 0 || sinks < 0)
+    return 0;
+  return kvs::paged_ex_ws_bytes(decode_ex_sizes(num_seqs, Hq, Hkv, D, num_blocks, max_blocks, block_size, window, sinks,
+                                                weights != 0));
+}
+
+kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
+                                 float* slot_weight, const int32_t* block_table, const int32_t* seq_blocks,
+                                 const int32_t* q_pos, void* O, float* LSE, int num_seqs, int Hq, int Hkv, int D,
+                                 int num_blocks, int block_size, int max_blocks, float softmax_scale, int window,
+                                 int sinks, void* workspace, size_t workspace_bytes, void* stream) {
+  t_err.clear();
+  if (kvs_status_t st = check_decode_dims(num_seqs, Hq, Hkv, D, num_blocks, block_size, max_blocks)) return st;
+  if (!(softmax_scale > 0.f) || softmax_scale != softmax_scale)
+    return fail(KVS_ERR_SHAPE, "softmax_scale must be positive and finite");
+  if (window < 0 || sinks < 0) return fail(KVS_ERR_SHAPE, "window and sinks must be >= 0 (got %d, %d)", window, sinks);
+  kvs::PagedDecode p = decode_ex_sizes(num_seqs, Hq, Hkv, D, num_blocks, max_blocks, block_size, window, sinks,
+                                       slot_weight != nullptr);
+  if (window > 0 && num_seqs > 65535) return fail(KVS_ERR_UNSUPPORTED, "more than 65535 sequences under a window");
+  if ((long long)Hkv * kvs::paged_ex_units(p) > 0x7fffffffll) return fail(KVS_ERR_UNSUPPORTED, "decode grid too large");
+  REQUIRE_PTR(Q, "Q");
+  REQUIRE_PTR(K_cache, "K_cache");
+  REQUIRE_PTR(V_cache, "V_cache");
+  REQUIRE_PTR(O, "O");
+  if (!slot_pos || !block_table || !seq_blocks || !LSE) return fail(KVS_ERR_NULL, "NULL table or output pointer");
+  if (window > 0 && !q_pos) return fail(KVS_ERR_NULL, "q_pos is NULL (a window needs the queries' positions)");
+  if (kvs_status_t st = check_ws(workspace, workspace_bytes, kvs::paged_ex_ws_bytes(p))) return st;
+  p.q = Q;
+  p.k_cache = K_cache;
+  p.v_cache = V_cache;
+  p.slot_pos = slot_pos;
+  p.slot_weight = slot_weight;
+  p.q_pos = q_pos;
+  p.block_table = block_table;
+  p.seq_blocks = seq_blocks;
+  p.o = O;
+  p.lse = LSE;
+  p.scale = softmax_scale;
+  p.ws = workspace;
+  p.ws_bytes = workspace_bytes;
+  p.stream = (hipStream_t)stream;
+  hipError_t e = kvs::launch_paged_decode_ex(p);
+  return e == hipSuccess ? KVS_OK : hip_fail(e, "paged decode launch");
+}
+
+kvs_status_t kvs_paged_evict_lowest(const float* slot_weight, int32_t* slot_pos, const int32_t* block_table,
+                                    const int32_t* seq_blocks, const int32_t* keep, int32_t* positions, int32_t* counts,
+                                    int num_seqs, int num_blocks, int block_size, int max_blocks, int sinks, int recent,
+                                    int max_out, void* stream) {
+  t_err.clear();
+  if (kvs_status_t st = check_cache_dims(num_blocks, block_size)) return st;
+  if (num_seqs < 1 || max_blocks < 1 || max_out < 1)
+    return fail(KVS_ERR_SHAPE, "num_seqs, max_blocks and max_out must be >= 1");
+  if (sinks < 0 || recent < 0) return fail(KVS_ERR_SHAPE, "sinks and recent must be >= 0 (got %d, %d)", sinks, recent);
+  if ((long long)max_blocks * block_size > 0x7fffffffll)
+    return fail(KVS_ERR_UNSUPPORTED, "max_blocks * block_size above INT32_MAX");
+  if (num_seqs > (1 << 21)) return fail(KVS_ERR_UNSUPPORTED, "more than 2097152 sequences");
+  if (!slot_weight || !slot_pos || !block_table || !seq_blocks || !keep || !positions || !counts)
+    return fail(KVS_ERR_NULL, "NULL argument");
+  const kvs::PagedEvictLowest p{slot_weight, slot_pos, block_table, seq_blocks, keep, positions, counts, num_seqs,
+                                num_blocks, block_size, max_blocks, sinks, recent, max_out, (hipStream_t)stream};
+  hipError_t e = kvs::launch_paged_evict_lowest(p);
+  return e == hipSuccess ? KVS_OK : hip_fail(e, "paged evict launch");
 }
 
 }  // extern "C"

@@ -47,6 +47,7 @@ struct RowArgs {
   int B, T, Hq, Hkv, G, HG, TC, nhg, nqt, ntok;
   int varlen;
   int flags;            // kFlagNoEmptySkip | kFlagFullAsPartial (consistency checks; 0 normally)
+  int window, sinks;    // of the windowed kernels, whose `evict` is the one the window makes of it (key_until)
   float scale_log2;     // softmax_scale * log2(e)
   float scale;
 };
@@ -113,25 +114,42 @@ __device__ __forceinline__ int2 key_tile_stats(const int* __restrict__ evict, co
   return make_int2(mn, mx);
 }
 
+// A sliding window with sinks (a window over the trace in which the first keys
+// stay visible): query i sees key j iff j <= i < evict_at[j] and (i - j <
+// window or j < sinks).  That is an eviction index again, min(evict_at[j], j +
+// window) for j >= sinks, so the attention kernels stay as they are; it is
+// made by the kernel that takes the tiles' statistics, which reads every
+// evict_at once anyway (4 bytes a token more to write, no launch of its own).
+struct KeyWindow {
+  int window, sinks;   // window 0: none
+  int* until;          // [ntok] out: the last query's index + 1 of every key; NULL: evict_at is that
+};
+__device__ __forceinline__ int key_until(const int* __restrict__ evict, const KeyWindow& kw, const Trace& tr, int j) {
+  const int e = evict ? min(evict[tr.tok0 + j], tr.L) : tr.L;
+  return kw.window > 0 && j >= kw.sinks ? min(e, j + kw.window) : e;   // j < 2^20, window at most 2^20
+}
+
 // Statistics of the 64-key tiles of all traces: one wave a tile, one lane a
 // key, four tiles a workgroup of 256 threads (group wg of tg per trace).  Bound
 // by one memory latency; one thread a tile walked its 64 keys in series, 6.0 us
 // for 512 tokens and 7.4 for 8,191, against 2.3 and 4.6 (a launch's own time).
 __device__ __forceinline__ void kstats_group(const int* __restrict__ evict, const int* __restrict__ cu, int T, int ntok,
-                                             int wg, int tg, int2* __restrict__ out) {
+                                             int wg, int tg, int2* __restrict__ out, const KeyWindow& kw) {
   const int b = wg / tg, kt = (wg - b * tg) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   const Trace tr = trace_of(cu, b, T, ntok);
   const int j0 = kt * kKeyTile;
   if (j0 >= tr.L) return;
-  const int e = min(evict[tr.tok0 + min(j0 + lane, tr.L - 1)], tr.L);   // lanes past the end repeat the last key
+  const int j = min(j0 + lane, tr.L - 1);   // lanes past the end repeat the last key
+  const int e = key_until(evict, kw, tr, j);
+  if (kw.until && j0 + lane < tr.L) kw.until[tr.tok0 + j] = e;
   const int mn = wave_min(e), mx = wave_max(e);
   if (lane == 0) out[kstat_index(b, tr.tok0, kt, kKeyTile)] = make_int2(mn, mx);
 }
 __host__ __device__ __forceinline__ int kstats_groups(int T) { return ((T + kKeyTile - 1) / kKeyTile + 3) / 4; }
 
 __global__ void __launch_bounds__(256) kstats_kernel(const int* __restrict__ evict, const int* __restrict__ cu, int T,
-                                                     int ntok, int2* __restrict__ out) {
-  kstats_group(evict, cu, T, ntok, blockIdx.x, kstats_groups(T), out);
+                                                     int ntok, int2* __restrict__ out, KeyWindow kw) {
+  kstats_group(evict, cu, T, ntok, blockIdx.x, kstats_groups(T), out, kw);
 }
 
 // ---------------------------------------------------------------- tile-class grid
@@ -187,18 +205,41 @@ __global__ void __launch_bounds__(256) check_kernel(const int* __restrict__ evic
 // evict_at statistics of its candidate tile, so the statistics of the tile
 // walker_next returns are read from a register (walker_stats) instead of from
 // memory, whose latency the wave would otherwise wait out on every tile.
+//
+// Under a window the tiles between the sinks and the window of the first query
+// hold nothing, however long the trace: the candidates are then counted
+// without them, so that the walk takes one look (64 candidates) instead of one
+// for every 4,096 keys in front of the window.
 struct TileWalker {
   int base, lim;
   unsigned long long live;
   int emin, emax;   // statistics of candidate tile base + lane
+  int sink, gap;    // windowed: tiles with sinks, and tiles behind them that are no candidates
 };
 
+template <bool WIN>
+__device__ __forceinline__ TileWalker walker_init(const RowArgs& a, int i0, int i1, int L) {
+  TileWalker w{0, (min(i1, L) + kKeyTile - 1) / kKeyTile, 0ull, 0, 0, 0, 0};
+  if (WIN) {
+    w.sink = min((a.sinks + kKeyTile - 1) / kKeyTile, w.lim);
+    w.gap = max(min(max(i0 - a.window + 1, 0) / kKeyTile, w.lim) - w.sink, 0);
+    w.lim -= w.gap;
+  }
+  return w;
+}
+// the tile of candidate c, the candidate of tile kt
+template <bool WIN>
+__device__ __forceinline__ int walker_tile(const TileWalker& w, int c) { return WIN && c >= w.sink ? c + w.gap : c; }
+template <bool WIN>
+__device__ __forceinline__ int walker_candidate(const TileWalker& w, int kt) { return WIN && kt >= w.sink ? kt - w.gap : kt; }
+
+template <bool WIN>
 __device__ __forceinline__ void walker_load(TileWalker& w, const int2* __restrict__ ks, int kidx0, int i0, int i1,
                                             int L, int flags) {
-  const int kt = w.base + (threadIdx.x & 63);
+  const int c = w.base + (threadIdx.x & 63), kt = walker_tile<WIN>(w, c);
   bool ne = false;
   int2 st = make_int2(0, 0);
-  if (kt < w.lim) {
+  if (c < w.lim) {
     st = ks[kidx0 + kt];
     ne = adjust_class(tile_class(i0, i1, kt * kKeyTile, kt * kKeyTile + kKeyTile, L, st.x, st.y), flags) != kEmpty;
   }
@@ -207,21 +248,23 @@ __device__ __forceinline__ void walker_load(TileWalker& w, const int2* __restric
   w.emax = st.y;
 }
 
+template <bool WIN>
 __device__ __forceinline__ int walker_next(TileWalker& w, const int2* __restrict__ ks, int kidx0, int i0, int i1,
                                            int L, int flags) {
   while (w.live == 0ull) {
     w.base += 64;
     if (w.base >= w.lim) return -1;
-    walker_load(w, ks, kidx0, i0, i1, L, flags);
+    walker_load<WIN>(w, ks, kidx0, i0, i1, L, flags);
   }
   const int bit = __builtin_ctzll(w.live);
   w.live &= w.live - 1ull;
-  return w.base + bit;
+  return walker_tile<WIN>(w, w.base + bit);
 }
 
 // evict_at minimum and maximum of tile kt, the tile the last walker_next call returned (kt >= 0)
+template <bool WIN>
 __device__ __forceinline__ int2 walker_stats(const TileWalker& w, int kt) {
-  const int l = kt - w.base;
+  const int l = walker_candidate<WIN>(w, kt) - w.base;
   return make_int2(__builtin_amdgcn_readlane(w.emin, l), __builtin_amdgcn_readlane(w.emax, l));
 }
 
@@ -336,7 +379,7 @@ constexpr int fwd_bn() { return D == 128 ? 32 : 64; }
 template <int D>
 using FwdStager = RowStager<D, fwd_bn<D>(), 4, true>;   // 4 waves
 
-template <int D>
+template <int D, bool WIN>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 3 : 4, D == 128 ? 3 : 4)))
 fwd_kernel(RowArgs a) {
   constexpr int KS = D / 16, DB = D / 32, BN = fwd_bn<D>(), NKB = BN / 32, NSUB = kKeyTile / BN;
@@ -393,10 +436,10 @@ fwd_kernel(RowArgs a) {
   const float inv_scale_log2 = 1.f / a.scale_log2;
 
   const int kidx0 = kstat_index(rt.b, tr.tok0, 0, kKeyTile);
-  TileWalker w{0, (min(rt.i1, tr.L) + kKeyTile - 1) / kKeyTile, 0ull, 0, 0};
-  walker_load(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags);
-  int kt = __builtin_amdgcn_readfirstlane(walker_next(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags));
-  int2 kst = kt >= 0 ? walker_stats(w, kt) : make_int2(0, 0);
+  TileWalker w = walker_init<WIN>(a, rt.i0, rt.i1, tr.L);
+  walker_load<WIN>(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags);
+  int kt = __builtin_amdgcn_readfirstlane(walker_next<WIN>(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags));
+  int2 kst = kt >= 0 ? walker_stats<WIN>(w, kt) : make_int2(0, 0);
 
   // The products and the softmax of the sub-tile of BN keys from j0 on.
   auto compute = [&](const uint16_t* cK, const uint16_t* cV, const int* cE, int j0) __attribute__((always_inline)) {
@@ -466,8 +509,8 @@ fwd_kernel(RowArgs a) {
   int nkt = -1;
   int2 nkst = make_int2(0, 0);
   auto walk = [&]() __attribute__((always_inline)) {
-    nkt = __builtin_amdgcn_readfirstlane(walker_next(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags));
-    if (nkt >= 0) nkst = walker_stats(w, nkt);
+    nkt = __builtin_amdgcn_readfirstlane(walker_next<WIN>(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags));
+    if (nkt >= 0) nkst = walker_stats<WIN>(w, nkt);
   };
   const int jend = min(rt.i1, tr.L);   // no row of the workgroup sees a key from here on
 
@@ -531,9 +574,9 @@ __global__ void __launch_bounds__(256) bwd_pre_kernel(const uint16_t* __restrict
                                                       const float* __restrict__ lse, float* __restrict__ delta,
                                                       float* __restrict__ lse2, int ntok, int Hq, int T, int varlen,
                                                       const int* __restrict__ evict, const int* __restrict__ cu,
-                                                      int nks, int2* __restrict__ kstats) {
+                                                      int nks, int2* __restrict__ kstats, KeyWindow kw) {
   if ((int)blockIdx.x < nks) {
-    kstats_group(evict, cu, T, ntok, blockIdx.x, kstats_groups(T), kstats);
+    kstats_group(evict, cu, T, ntok, blockIdx.x, kstats_groups(T), kstats, kw);
     return;
   }
   constexpr int PER = D / 16;  // elements per lane, 16 lanes per row
@@ -561,7 +604,7 @@ __global__ void __launch_bounds__(256) bwd_pre_kernel(const uint16_t* __restrict
 }
 
 // ---------------------------------------------------------------- backward: dQ (row kernel)
-template <int D>
+template <int D, bool WIN>
 __global__ void __launch_bounds__(512) dq_kernel(RowArgs a) {
   constexpr int KS = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(1024))) uint16_t sK0[kKeyTile * Lay<D, true>::PITCH];
@@ -615,18 +658,18 @@ __global__ void __launch_bounds__(512) dq_kernel(RowArgs a) {
   for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
 
   const int kidx0 = kstat_index(rt.b, tr.tok0, 0, kKeyTile);
-  TileWalker w{0, (min(rt.i1, tr.L) + kKeyTile - 1) / kKeyTile, 0ull, 0, 0};
-  walker_load(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags);
-  int kt = __builtin_amdgcn_readfirstlane(walker_next(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags));
-  int2 kst = kt >= 0 ? walker_stats(w, kt) : make_int2(0, 0);
+  TileWalker w = walker_init<WIN>(a, rt.i0, rt.i1, tr.L);
+  walker_load<WIN>(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags);
+  int kt = __builtin_amdgcn_readfirstlane(walker_next<WIN>(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags));
+  int2 kst = kt >= 0 ? walker_stats<WIN>(w, kt) : make_int2(0, 0);
 
   // The next tile and its statistics come from the walker's registers (no
   // memory access), one tile ahead and behind the current tile's products.
   int nkt = -1;
   int2 nkst = make_int2(0, 0);
   auto walk = [&]() __attribute__((always_inline)) {
-    nkt = __builtin_amdgcn_readfirstlane(walker_next(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags));
-    if (nkt >= 0) nkst = walker_stats(w, nkt);
+    nkt = __builtin_amdgcn_readfirstlane(walker_next<WIN>(w, a.kstats, kidx0, rt.i0, rt.i1, tr.L, a.flags));
+    if (nkt >= 0) nkst = walker_stats<WIN>(w, nkt);
   };
   auto body = [&](const uint16_t* cK, const uint16_t* cV, const int* cE, uint16_t* nK, uint16_t* nV, int* nE) {
     if (nkt >= 0) stage(nK, nV, nE, nkt * kKeyTile);
@@ -1210,10 +1253,14 @@ __global__ void __launch_bounds__(256) split_reduce_kernel(const PlanCtl* __rest
 }
 
 // Explicit instantiations: every kernel the launchers use is emitted, with its host stub.
-template __global__ void fwd_kernel<64>(RowArgs);
-template __global__ void fwd_kernel<128>(RowArgs);
-template __global__ void dq_kernel<64>(RowArgs);
-template __global__ void dq_kernel<128>(RowArgs);
+template __global__ void fwd_kernel<64, false>(RowArgs);
+template __global__ void fwd_kernel<128, false>(RowArgs);
+template __global__ void fwd_kernel<64, true>(RowArgs);
+template __global__ void fwd_kernel<128, true>(RowArgs);
+template __global__ void dq_kernel<64, false>(RowArgs);
+template __global__ void dq_kernel<128, false>(RowArgs);
+template __global__ void dq_kernel<64, true>(RowArgs);
+template __global__ void dq_kernel<128, true>(RowArgs);
 template __global__ void dkdv_kernel<64>(ColArgs);
 template __global__ void dkdv_kernel<128>(ColArgs);
 template __global__ void split_reduce_kernel<64>(const PlanCtl*, const int*, const int*, const float*, const int*, uint16_t*, uint16_t*,
@@ -1312,7 +1359,9 @@ static RowArgs row_args(const Problem& p, const int2* kstats) {
   a.q = (const uint16_t*)p.q;
   a.k = (const uint16_t*)p.k;
   a.v = (const uint16_t*)p.v;
-  a.evict = p.evict;
+  a.evict = p.until ? p.until : p.evict;
+  a.window = p.window;
+  a.sinks = p.sinks;
   a.cu = p.cu;
   a.kstats = kstats;
   a.o = (uint16_t*)p.o;
@@ -1339,11 +1388,13 @@ static RowArgs row_args(const Problem& p, const int2* kstats) {
 
 constexpr int kMaxTraces = 65535;   // keeps every grid and workgroup index within 31 bits
 
+static KeyWindow key_window(const Problem& p) { return {p.window, p.sinks, p.until}; }
+
 hipError_t launch_kstats(const Problem& p, int2* kstats) {
   if (p.B > kMaxTraces) return hipErrorInvalidConfiguration;
   prof_begin("classify", p.stream);
   hipLaunchKernelGGL(kstats_kernel, dim3((unsigned)((long long)kstats_groups(p.T) * p.B)), dim3(256), 0, p.stream,
-                     p.evict, p.cu, p.T, p.ntok, kstats);
+                     p.evict, p.cu, p.T, p.ntok, kstats, key_window(p));
   prof_end(p.stream);
   return hipGetLastError();
 }
@@ -1353,8 +1404,9 @@ hipError_t launch_fwd(const Problem& p, const int2* kstats) {
   const long long nblk = (long long)a.nqt * p.B * p.Hkv * p.nhg;
   dim3 grid((unsigned)nblk), block(64 * p.HG * p.TC);   // 4 waves
   prof_begin("fwd", p.stream);
-  if (p.D == 128) hipLaunchKernelGGL(fwd_kernel<128>, grid, block, 0, p.stream, a);
-  else hipLaunchKernelGGL(fwd_kernel<64>, grid, block, 0, p.stream, a);
+  const auto kernel = p.window > 0 ? (p.D == 128 ? fwd_kernel<128, true> : fwd_kernel<64, true>)
+                                   : (p.D == 128 ? fwd_kernel<128, false> : fwd_kernel<64, false>);
+  hipLaunchKernelGGL(kernel, grid, block, 0, p.stream, a);
   prof_end(p.stream);
   return hipGetLastError();
 }
@@ -1374,11 +1426,11 @@ hipError_t launch_bwd_pre(const Problem& p, int2* kstats, float* delta) {
   if (p.D == 128)
     hipLaunchKernelGGL(bwd_pre_kernel<128>, grid, block, 0, p.stream, (const uint16_t*)p.o_in,
                        (const uint16_t*)p.dout, p.lse_in, delta, lse2, p.ntok, p.Hq, p.T, (int)(p.cu != nullptr),
-                       p.evict, p.cu, nks, kstats);
+                       p.evict, p.cu, nks, kstats, key_window(p));
   else
     hipLaunchKernelGGL(bwd_pre_kernel<64>, grid, block, 0, p.stream, (const uint16_t*)p.o_in,
                        (const uint16_t*)p.dout, p.lse_in, delta, lse2, p.ntok, p.Hq, p.T, (int)(p.cu != nullptr),
-                       p.evict, p.cu, nks, kstats);
+                       p.evict, p.cu, nks, kstats, key_window(p));
   prof_end(p.stream);
   return hipGetLastError();
 }
@@ -1392,7 +1444,7 @@ hipError_t launch_bwd_dkdv(const Problem& p, const int2* kstats, const float* de
   a.dout = (const uint16_t*)p.dout;
   a.lse = (const float*)((const char*)delta + half_delta_bytes(p.Hq, p.ntok));   // LSE * log2(e)
   a.delta = delta;
-  a.evict = p.evict;
+  a.evict = p.until ? p.until : p.evict;
   a.cu = p.cu;
   a.dk = (uint16_t*)p.dk;
   a.dv = (uint16_t*)p.dv;
@@ -1450,8 +1502,9 @@ hipError_t launch_bwd_dq(const Problem& p, const int2* kstats, const float* delt
   const long long nblk = (long long)a.nqt * p.B * p.Hkv * p.nhg;
   dim3 grid((unsigned)nblk), block(64 * p.HG * p.TC);
   prof_begin("bwd_dq", p.stream);
-  if (p.D == 128) hipLaunchKernelGGL(dq_kernel<128>, grid, block, 0, p.stream, a);
-  else hipLaunchKernelGGL(dq_kernel<64>, grid, block, 0, p.stream, a);
+  const auto kernel = p.window > 0 ? (p.D == 128 ? dq_kernel<128, true> : dq_kernel<64, true>)
+                                   : (p.D == 128 ? dq_kernel<128, false> : dq_kernel<64, false>);
+  hipLaunchKernelGGL(kernel, grid, block, 0, p.stream, a);
   prof_end(p.stream);
   return hipGetLastError();
 }

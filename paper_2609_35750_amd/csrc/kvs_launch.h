@@ -15,7 +15,7 @@ struct Problem {
   const void* o_in;      // backward: forward output O
   const void* dout;      // backward: dO
   const float* lse_in;   // backward: forward LSE
-  const int32_t* evict;
+  const int32_t* evict;  // windowed calls: may be NULL (nothing is evicted)
   const int32_t* cu;     // NULL: fixed length
   void* o;               // forward output
   float* lse;            // forward output
@@ -29,6 +29,8 @@ struct Problem {
   int HG, TC, nhg;   // q-heads per workgroup, 32-token chunks per workgroup, head groups per KV head
   int flags;         // tile-classifier switches (kFlagNoEmptySkip, kFlagFullAsPartial); 0 normally
   float scale;
+  int window, sinks;   // 0: no window
+  int32_t* until;      // [ntok] workspace: the eviction indices under the window; NULL: `evict` has them
   void* ws;
   size_t ws_bytes;   // backward
   hipStream_t stream;
@@ -70,6 +72,12 @@ hipError_t launch_classify(const int32_t* evict, const int32_t* cu, int B, int T
 hipError_t launch_check(const int32_t* evict, const int32_t* cu, int B, int T, int ntok,
                         int64_t* first_bad, int* cu_bad, hipStream_t stream);
 
+// Attention weights of the keys (p.until, p.lse_in set; kstats taken under p's window): W [ntok] from `part`,
+// ws_weights_bytes of workspace.  last_rows: queries of each trace that count, at its end.
+size_t ws_weights_bytes(int B, int T, int ntok, int Hkv, int last_rows);
+long long weights_grid(int B, int T, int Hkv, int last_rows);   // workgroups of 256 threads
+hipError_t launch_key_weights(const Problem& p, const int2* kstats, int last_rows, float* part, float* w);
+
 // Paged decode over the streamed KV cache (after host-side validation).
 struct PagedDecode {
   const void* q;            // [S][Hq][D] bf16
@@ -80,6 +88,9 @@ struct PagedDecode {
   const int32_t* seq_blocks;    // [S]
   void* o;                  // [S][Hq][D] bf16
   float* lse;               // [S][Hq]
+  const int32_t* q_pos;     // [S] position of each query (window > 0)
+  float* slot_weight;       // [num_blocks * block_size]: added to; NULL: no weights
+  int window, sinks;        // window 0: none
   int S, Hq, Hkv, D, max_blocks, block_size, num_blocks;
   float scale;
   void* ws;
@@ -127,15 +138,40 @@ inline dim3 run_grid(const SlotRuns& runs, long long per_tok, RunList* list) {
   }
   return dim3(wg);
 }
+// Weights of the appended entries: to[slot] = from[token] (from NULL: 0); to NULL: the cache keeps none.
+struct SlotWeights {
+  const float* from;
+  float* to;
+};
 hipError_t launch_paged_append_runs(const void* kn, const void* vn, const SlotRuns& runs, void* kc, void* vc,
-                                    int* slot_pos, int num_slots, int BS, int Hkv, int D, hipStream_t stream);
+                                    int* slot_pos, int num_slots, int BS, int Hkv, int D, const SlotWeights& sw,
+                                    hipStream_t stream);
 hipError_t launch_paged_evict_runs(const SlotRuns& runs, int* slot_pos, int num_slots, hipStream_t stream);
 size_t paged_ws_bytes(int S, int Hq, int Hkv, int max_blocks, int BS, int D);   // that the decode can use
 size_t paged_ws_least(int S, int Hq, int Hkv, int max_blocks, int BS, int D);   // that it needs
 hipError_t launch_paged_append(const void* kn, const void* vn, const int* pos, const int* slots, int n, void* kc,
-                               void* vc, int* slot_pos, int num_slots, int BS, int Hkv, int D, hipStream_t stream);
+                               void* vc, int* slot_pos, int num_slots, int BS, int Hkv, int D, const SlotWeights& sw,
+                               hipStream_t stream);
 hipError_t launch_paged_evict(const int* slots, int n, int* slot_pos, int num_slots, hipStream_t stream);
 hipError_t launch_paged_decode(const PagedDecode& p);
+// The decode under a window and with weights (either, or neither): workspace, launches.
+size_t paged_ex_ws_bytes(const PagedDecode& p);
+long long paged_ex_units(const PagedDecode& p);   // of the decode grid, per KV head
+hipError_t launch_paged_decode_ex(const PagedDecode& p);
+
+// Eviction of the entries of lowest weight (after host-side validation).
+struct PagedEvictLowest {
+  const float* slot_weight;
+  int32_t* slot_pos;
+  const int32_t* block_table;
+  const int32_t* seq_blocks;
+  const int32_t* keep;   // [S]
+  int32_t* positions;    // [S][max_out]
+  int32_t* counts;       // [S]
+  int S, num_blocks, block_size, max_blocks, sinks, recent, max_out;
+  hipStream_t stream;
+};
+hipError_t launch_paged_evict_lowest(const PagedEvictLowest& p);
 
 // Per-kernel event bracketing (benchmark timing).
 void prof_begin(const char* name, hipStream_t s);

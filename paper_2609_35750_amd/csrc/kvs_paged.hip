@@ -36,7 +36,8 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const uint16_t* __res
                                                            const uint16_t* __restrict__ vn,
                                                            const int* __restrict__ pos, const int* __restrict__ slots,
                                                            int n, uint16_t* __restrict__ kc, uint16_t* __restrict__ vc,
-                                                           int* __restrict__ slot_pos, int num_slots, int Hkv, int BS) {
+                                                           int* __restrict__ slot_pos, int num_slots, int Hkv, int BS,
+                                                           SlotWeights sw) {
   const long long per_tok = (long long)Hkv * (D / 8);   // 16-byte chunks per token and tensor
   const long long chunks = (long long)n * per_tok;
   for (long long c = (long long)blockIdx.x * blockDim.x + threadIdx.x; c < chunks;
@@ -48,7 +49,10 @@ __global__ void __launch_bounds__(256) paged_append_kernel(const uint16_t* __res
     const long long dst = ((((long long)(slot / BS) * Hkv + h) * BS + slot % BS) * D) + 8 * d8;
     *reinterpret_cast<uint4*>(kc + dst) = *reinterpret_cast<const uint4*>(kn + c * 8);
     *reinterpret_cast<uint4*>(vc + dst) = *reinterpret_cast<const uint4*>(vn + c * 8);
-    if (r == 0) slot_pos[slot] = pos[t];
+    if (r == 0) {
+      slot_pos[slot] = pos[t];
+      if (sw.to) sw.to[slot] = sw.from ? sw.from[t] : 0.f;
+    }
   }
 }
 
@@ -92,7 +96,7 @@ __global__ void __launch_bounds__(256) paged_append_runs_kernel(const uint16_t* 
                                                                 const uint16_t* __restrict__ vn, SlotRuns runs,
                                                                 uint16_t* __restrict__ kc, uint16_t* __restrict__ vc,
                                                                 int* __restrict__ slot_pos, int num_slots, int Hkv,
-                                                                int BS, L list) {
+                                                                int BS, SlotWeights sw, L list) {
   long long begin, items;
   const SlotRun run = runs.r[run_of(runs, list, begin, items)];
   const long long per_tok = (long long)Hkv * (D / 8), chunks = (long long)(run.len < 0 ? -run.len : run.len) * per_tok;
@@ -105,7 +109,10 @@ __global__ void __launch_bounds__(256) paged_append_runs_kernel(const uint16_t* 
     const long long dst = (((slot / BS) * Hkv + h) * BS + slot % BS) * D + 8 * d8;
     *reinterpret_cast<uint4*>(kc + dst) = *reinterpret_cast<const uint4*>(kn + src * 8);
     *reinterpret_cast<uint4*>(vc + dst) = *reinterpret_cast<const uint4*>(vn + src * 8);
-    if (r == 0) slot_pos[slot] = (int)(run.pos + i);
+    if (r == 0) {
+      slot_pos[slot] = (int)(run.pos + i);
+      if (sw.to) sw.to[slot] = sw.from ? sw.from[run.tok + i] : 0.f;
+    }
   }
 }
 
@@ -139,6 +146,10 @@ struct DecodeArgs {
   uint16_t* o;            // [S][Hq][D]: written here for sequences of one unit, by the merge for the others
   float* lse;             // [S][Hq]
   int S, Hq, Hkv, G, max_blocks, BS, num_blocks, units;
+  int gran;               // slots a table entry stands for: BS, or 1 where the table lists the slots themselves
+  float* scores;          // [tiles][Hq][kDecTile]: raw scores, for the entries' weights (NULL: not kept)
+  const int* tile_base;   // [S + 1]: first tile of each sequence (more than kPlanSeqs sequences)
+  int tiles;              // rows of scores
   float scale_log2;       // softmax_scale * log2(e)
 };
 
@@ -214,7 +225,7 @@ __device__ __forceinline__ int quick_div(int x, int y) {
 }
 
 // slots of the blocks sequence s uses (clamped to the table width; some may be evicted)
-__device__ __forceinline__ int slots_of(const DecodeArgs& a, int s) { return min(max(a.nblk[s], 0), a.max_blocks) * a.BS; }
+__device__ __forceinline__ int slots_of(const DecodeArgs& a, int s) { return min(max(a.nblk[s], 0), a.max_blocks) * a.gran; }
 
 // The unit u of up to 64 REGS sequences: its sequence, that one's slots, first unit and units.  False past the last one.
 template <int REGS>
@@ -378,6 +389,24 @@ __device__ __forceinline__ void wait_vm_le() {
   __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 
+// First row of scores of sequence s: its tiles follow those of the sequences before it.
+__device__ __forceinline__ int tile_base(const DecodeArgs& a, int s, int lane) {
+  if (a.tile_base) return a.tile_base[s];
+  int base = 0;
+  for (int k = 0; k * kWave <= s; ++k) {
+    const int i = k * kWave + lane;
+    const int t = i < s ? plan_tiles(slots_of(a, i)) : 0;
+    base += wave_last(wave_scan(t));
+  }
+  return base;
+}
+
+// A store the compiler does not count (it would not know of the copies in flight either): 16 bytes of this lane.
+__device__ __forceinline__ void store_b128_uncounted(float* dst, float4 v) {
+  const f32x4 x = {v.x, v.y, v.z, v.w};
+  asm volatile("global_store_dwordx4 %0, %1, off" ::"v"(dst), "v"(x) : "memory");
+}
+
 // Every global read of the decode loop is an asynchronous copy to LDS, so all
 // of them complete in issue order under one counter and each wait is exact
 // (R = kDecRing):
@@ -387,16 +416,24 @@ __device__ __forceinline__ void wait_vm_le() {
 // copies of the R - 1 later steps are outstanding.  (A compiler-visible load
 // consumed while copies are in flight would make the compiler wait for all
 // of them, since it cannot see them.)
-template <int D>
+// LIST: the table lists the visible slots themselves (the decode under a
+// window), so every listed slot is live.  SCORES: the tile's raw scores are
+// stored (four stores a step, counted in the waits like the copies), 4 Hq bytes
+// a slot beside 4 Hkv D of K and V: 3% more at G = 4, D = 128, where reading K
+// once more for the weights when LSE is known would be 50%.
+template <int D, bool LIST, bool SCORES>
 __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
   constexpr int KS = D / 16, DB = D / 32, PITCH = Lay<D, true>::PITCH, TILE = kDecTile * PITCH, R = kDecRing;
   constexpr int OPS_KV = 2 * GatherStager<D>::NI;   // K and V copy instructions per tile
-  constexpr int OPS_STEP = OPS_KV + 2;             // plus the table and slot_pos copies
-  static_assert((R - 1) * OPS_STEP < 64, "outstanding copies must fit vmcnt");
+  constexpr int OPS_POS = LIST ? 0 : 1;            // slot_pos copies
+  constexpr int OPS_STEP = OPS_KV + 1 + OPS_POS;   // plus the table copy
+  constexpr int OPS_SCORES = SCORES ? 4 : 0;       // stores of a computed tile
+  static_assert(R == 2, "the waits count one tile ahead");
+  static_assert((R - 1) * OPS_STEP + OPS_SCORES < 64, "outstanding operations must fit vmcnt");
   __shared__ __attribute__((aligned(1024))) uint16_t sK[R * TILE];
   __shared__ __attribute__((aligned(1024))) uint16_t sV[R * TILE];
   __shared__ __attribute__((aligned(256))) int sTab[2][kWave];   // block-table entries of a tile's rows
-  __shared__ __attribute__((aligned(256))) int sPos[R][kWave];   // slot_pos of a tile's rows
+  __shared__ __attribute__((aligned(256))) int sPos[LIST ? 1 : R][kWave];   // slot_pos of a tile's rows
 
   const int lane = threadIdx.x, half = lane >> 5, col = lane & 31;
   int g;
@@ -444,8 +481,14 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
   // copy the block-table entries of tile t's rows (lanes 0..31) into sTab[t & 1]
   auto copy_table = [&](int t) __attribute__((always_inline)) {
     const int c = slot_index(t);
-    if (lane < 32) dma_b32_global(trow + c / a.BS, lds_addr(&sTab[t & 1][0]));
+    if (lane < 32) dma_b32_global(trow + (LIST ? c : c / a.BS), lds_addr(&sTab[t & 1][0]));
   };
+  float* score_row = nullptr;   // of this lane's q-head and tile row, in the first tile of all
+  int score_tile = 0;           // the unit's first tile
+  if (SCORES) {
+    score_tile = __builtin_amdgcn_readfirstlane(tile_base(a, s, lane) + c_begin / kDecTile);
+    score_row = a.scores + (size_t)(col_ok ? hcol : 0) * kDecTile + 4 * half;
+  }
 
   unsigned valid_q[R] = {};   // rows of tiles n .. n + R - 1 that hold a slot of the split (index 0 = tile n)
   if (ntile > 0) copy_table(0);
@@ -453,28 +496,34 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
   for (int n = -(R - 1); n < ntile; ++n) {
     const int tn = n + R - 1;   // tile whose copies this step issues
     if (tn < ntile) {
-      if (n > -(R - 1)) wait_vm_le<OPS_KV + 1>();   // table entries of tile tn have landed
+      // table entries of tile tn have landed: behind them only the copies of the step before, and its stores
+      if (SCORES && n > 0) wait_vm_le<OPS_KV + OPS_POS + OPS_SCORES>();
+      else if (n > -(R - 1)) wait_vm_le<OPS_KV + OPS_POS>();
       const int c = slot_index(tn);
-      const int blk = sTab[tn & 1][col];
+      const int entry = sTab[tn & 1][col], blk = LIST ? (int)((unsigned)entry / (unsigned)a.BS) : entry;
       // a table entry outside the cache reads slot 0 and is masked
       const bool bok = (unsigned)blk < (unsigned)a.num_blocks;
-      const int slot = bok ? blk * a.BS + c % a.BS : 0;
-      const long long roff = bok ? (long long)blk * blk_stride + (long long)(c % a.BS) * D : 0;
+      const int row = LIST ? (int)((unsigned)entry % (unsigned)a.BS) : c % a.BS;
+      const int slot = bok ? blk * a.BS + row : 0;
+      const long long roff = bok ? (long long)blk * blk_stride + (long long)row * D : 0;
       copy_table(min(tn + 1, ntile - 1));   // always one copy, so that every step issues the same count
       gst.issue(lds_addr(sK + (tn % R) * TILE), lds_addr(sV + (tn % R) * TILE), kbase, vbase, roff);
-      if (lane < 32) dma_b32_global(a.slot_pos + slot, lds_addr(&sPos[tn % R][0]));
+      if (!LIST && lane < 32) dma_b32_global(a.slot_pos + slot, lds_addr(&sPos[LIST ? 0 : tn % R][0]));
       valid_q[R - 1] = (unsigned)__ballot(lane < 32 && c_begin + tn * kDecTile + col < c_end && bok);
-      if (n >= 0) wait_vm_le<(R - 1) * OPS_STEP>();   // tile n has landed
+      // tile n has landed: behind it the copies of this step, and the stores of the last one
+      if (SCORES && n > 0) wait_vm_le<OPS_STEP + OPS_SCORES>();
+      else if (n >= 0) wait_vm_le<OPS_STEP>();
     } else if (n >= 0) {
       wait_vm_le<0>();
     }
     if (n >= 0) {
-      const unsigned live_cur = valid_q[0] & (unsigned)__ballot(lane < 32 && sPos[n % R][col] >= 0);
+      const unsigned live_cur =
+          LIST ? valid_q[0] : valid_q[0] & (unsigned)__ballot(lane < 32 && sPos[LIST ? 0 : n % R][col] >= 0);
       const uint16_t* cK = sK + (n % R) * TILE;
       const uint16_t* cV = sV + (n % R) * TILE;
+      f32x16 sc = f32x16{};
       if (live_cur != 0u) {
         // S^T block: keys on M (tile rows), q-heads on N
-        f32x16 sc = f32x16{};
         bf16x8 ka[KS];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) ka[ks] = lds_read_b128(cK + Lay<D, true>::row_at(rl, ks));
@@ -486,6 +535,18 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
           const int row = 8 * (r >> 2) + 4 * half + (r & 3);
           if (!((live_cur >> row) & 1u)) sc[r] = -INFINITY;
         }
+      }
+      if (SCORES && col_ok) {   // also of a tile without a live slot, where they are not read: the waits count them
+        float* dst = score_row + (size_t)min(score_tile + n, a.tiles - 1) * a.Hq * kDecTile;
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          store_b128_uncounted(dst + 8 * q4, make_float4(sc[4 * q4], sc[4 * q4 + 1], sc[4 * q4 + 2], sc[4 * q4 + 3]));
+      }
+      if (live_cur != 0u) {
+        // V rows of places without a live slot may hold anything (a slot never written, an evicted infinity): their
+        // product with P = 0 must not reach the sum.
+        for (unsigned dead = ~live_cur; dead != 0u; dead &= dead - 1u)
+          if (lane < D / 2) reinterpret_cast<uint32_t*>(sV + (n % R) * TILE + __builtin_ctz(dead) * PITCH)[lane] = 0u;
         float mx = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
@@ -659,20 +720,26 @@ __global__ void __launch_bounds__(64 * W) paged_combine_kernel(DecodeArgs a) {
 }
 
 template __global__ void paged_append_kernel<64>(const uint16_t*, const uint16_t*, const int*, const int*, int,
-                                                 uint16_t*, uint16_t*, int*, int, int, int);
+                                                 uint16_t*, uint16_t*, int*, int, int, int, SlotWeights);
 template __global__ void paged_append_kernel<128>(const uint16_t*, const uint16_t*, const int*, const int*, int,
-                                                  uint16_t*, uint16_t*, int*, int, int, int);
+                                                  uint16_t*, uint16_t*, int*, int, int, int, SlotWeights);
 #define KVS_RUNS(LL)                                                                                               \
   template __global__ void paged_append_runs_kernel<64, LL>(const uint16_t*, const uint16_t*, SlotRuns, uint16_t*, \
-                                                            uint16_t*, int*, int, int, int, LL);                   \
+                                                            uint16_t*, int*, int, int, int, SlotWeights, LL);      \
   template __global__ void paged_append_runs_kernel<128, LL>(const uint16_t*, const uint16_t*, SlotRuns, uint16_t*, \
-                                                             uint16_t*, int*, int, int, int, LL);                  \
+                                                             uint16_t*, int*, int, int, int, SlotWeights, LL);     \
   template __global__ void paged_evict_runs_kernel<LL>(SlotRuns, int*, int, LL)
 KVS_RUNS(NoRunList);
 KVS_RUNS(RunList);
 #undef KVS_RUNS
-template __global__ void paged_decode_kernel<64>(DecodeArgs);
-template __global__ void paged_decode_kernel<128>(DecodeArgs);
+#define KVS_DECODE(DD)                                                       \
+  template __global__ void paged_decode_kernel<DD, false, false>(DecodeArgs); \
+  template __global__ void paged_decode_kernel<DD, false, true>(DecodeArgs);  \
+  template __global__ void paged_decode_kernel<DD, true, false>(DecodeArgs);  \
+  template __global__ void paged_decode_kernel<DD, true, true>(DecodeArgs)
+KVS_DECODE(64);
+KVS_DECODE(128);
+#undef KVS_DECODE
 template __global__ void paged_combine_kernel<64, 1, false>(DecodeArgs);
 template __global__ void paged_combine_kernel<64, 4, false>(DecodeArgs);
 template __global__ void paged_combine_kernel<64, 16, false>(DecodeArgs);
@@ -685,17 +752,19 @@ template __global__ void paged_combine_kernel<128, 4, true>(DecodeArgs);
 // ---------------------------------------------------------------- launchers
 template <class L>
 static void launch_append_runs(dim3 grid, const void* kn, const void* vn, const SlotRuns& runs, void* kc, void* vc,
-                               int* slot_pos, int num_slots, int BS, int Hkv, int D, const L& list, hipStream_t stream) {
+                               int* slot_pos, int num_slots, int BS, int Hkv, int D, const SlotWeights& sw, const L& list,
+                               hipStream_t stream) {
   const auto kernel = D == 128 ? paged_append_runs_kernel<128, L> : paged_append_runs_kernel<64, L>;
   hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, (const uint16_t*)kn, (const uint16_t*)vn, runs, (uint16_t*)kc,
-                     (uint16_t*)vc, slot_pos, num_slots, Hkv, BS, list);
+                     (uint16_t*)vc, slot_pos, num_slots, Hkv, BS, sw, list);
 }
 hipError_t launch_paged_append_runs(const void* kn, const void* vn, const SlotRuns& runs, void* kc, void* vc,
-                                    int* slot_pos, int num_slots, int BS, int Hkv, int D, hipStream_t stream) {
+                                    int* slot_pos, int num_slots, int BS, int Hkv, int D, const SlotWeights& sw,
+                                    hipStream_t stream) {
   RunList list;
   const dim3 grid = run_grid(runs, (long long)Hkv * (D / 8), &list);
-  if (list.items) launch_append_runs(grid, kn, vn, runs, kc, vc, slot_pos, num_slots, BS, Hkv, D, list, stream);
-  else launch_append_runs(grid, kn, vn, runs, kc, vc, slot_pos, num_slots, BS, Hkv, D, NoRunList{}, stream);
+  if (list.items) launch_append_runs(grid, kn, vn, runs, kc, vc, slot_pos, num_slots, BS, Hkv, D, sw, list, stream);
+  else launch_append_runs(grid, kn, vn, runs, kc, vc, slot_pos, num_slots, BS, Hkv, D, sw, NoRunList{}, stream);
   return hipGetLastError();
 }
 
@@ -746,16 +815,19 @@ size_t paged_ws_least(int S, int Hq, int Hkv, int max_blocks, int BS, int D) {
 }
 
 hipError_t launch_paged_append(const void* kn, const void* vn, const int* pos, const int* slots, int n, void* kc,
-                               void* vc, int* slot_pos, int num_slots, int BS, int Hkv, int D, hipStream_t stream) {
+                               void* vc, int* slot_pos, int num_slots, int BS, int Hkv, int D, const SlotWeights& sw,
+                               hipStream_t stream) {
   if (n == 0) return hipSuccess;
   const long long chunks = (long long)n * Hkv * (D / 8);
   const int blocks = (int)std::min<long long>((chunks + 255) / 256, 65535);
   if (D == 128)
     hipLaunchKernelGGL(paged_append_kernel<128>, dim3(blocks), dim3(256), 0, stream, (const uint16_t*)kn,
-                       (const uint16_t*)vn, pos, slots, n, (uint16_t*)kc, (uint16_t*)vc, slot_pos, num_slots, Hkv, BS);
+                       (const uint16_t*)vn, pos, slots, n, (uint16_t*)kc, (uint16_t*)vc, slot_pos, num_slots, Hkv, BS,
+                       sw);
   else
     hipLaunchKernelGGL(paged_append_kernel<64>, dim3(blocks), dim3(256), 0, stream, (const uint16_t*)kn,
-                       (const uint16_t*)vn, pos, slots, n, (uint16_t*)kc, (uint16_t*)vc, slot_pos, num_slots, Hkv, BS);
+                       (const uint16_t*)vn, pos, slots, n, (uint16_t*)kc, (uint16_t*)vc, slot_pos, num_slots, Hkv, BS,
+                       sw);
   return hipGetLastError();
 }
 
@@ -794,43 +866,297 @@ static void launch_combine(int D, const DecodeArgs& a, hipStream_t stream) {
 // of 16,000 beside 299 of 200 749, 78.5, 72.0.
 constexpr int kPlanRounds = 3;
 
-hipError_t launch_paged_decode(const PagedDecode& p) {
+// Arguments of a decode over a table of `width` entries a sequence, each for gran slots; the units' workspace.
+static DecodeArgs decode_args(const PagedDecode& p, const int* table, const int* nblk, int width, int gran, void* ws,
+                              size_t ws_bytes) {
   DecodeArgs a{};
   a.q = (const uint16_t*)p.q;
   a.kc = (const uint16_t*)p.k_cache;
   a.vc = (const uint16_t*)p.v_cache;
   a.slot_pos = p.slot_pos;
-  a.table = p.block_table;
-  a.nblk = p.seq_blocks;
+  a.table = table;
+  a.nblk = nblk;
   a.S = p.S;
   a.Hq = p.Hq;
   a.Hkv = p.Hkv;
   a.G = p.Hq / p.Hkv;
-  a.max_blocks = p.max_blocks;
+  a.max_blocks = width;
   a.BS = p.block_size;
+  a.gran = gran;
   a.num_blocks = p.num_blocks;
-  a.units = fitting_units(p.S, p.Hq, p.D, paged_units(p.S, p.Hkv, p.max_blocks, p.block_size, p.D), p.ws_bytes);
+  a.units = fitting_units(p.S, p.Hq, p.D, paged_units(p.S, p.Hkv, width, gran, p.D), ws_bytes);
   a.o = (uint16_t*)p.o;
   a.lse = p.lse;
   const size_t rows = (size_t)partial_units(p.S, a.units) * p.Hq;
-  a.part = (float*)p.ws;
-  a.part_ml = (float2*)((char*)p.ws + round256(rows * p.D * sizeof(float)));
+  a.part = (float*)ws;
+  a.part_ml = (float2*)((char*)ws + round256(rows * p.D * sizeof(float)));
   a.seq_units = (int2*)((char*)a.part_ml + round256(rows * sizeof(float2)));
   a.cut = (int*)a.seq_units;   // their number and no more than S first units: at most S + 1 of 2 S words
   a.unit_seq = (int4*)((char*)a.seq_units + round256((size_t)p.S * sizeof(int2)));
   a.scale_log2 = p.scale * 1.4426950408889634f;
-  const dim3 grid((unsigned)((long long)a.units * p.Hkv));
   a.plan = a.units == p.S ? kOneUnit
            : p.S <= kPlanSeqs && (long long)a.units * p.Hkv <= kPlanRounds * decode_round(p.D) ? kByWave : kListed;
+  return a;
+}
+
+// Plan, decode, merge.
+template <bool LIST, bool SCORES>
+static hipError_t launch_decode(const PagedDecode& p, const DecodeArgs& a) {
+  const dim3 grid((unsigned)((long long)a.units * p.Hkv));
   if (a.plan == kListed) hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(1024), 0, p.stream, a);
   prof_begin("paged_decode", p.stream);
-  if (p.D == 128) hipLaunchKernelGGL(paged_decode_kernel<128>, grid, dim3(64), 0, p.stream, a);
-  else hipLaunchKernelGGL(paged_decode_kernel<64>, grid, dim3(64), 0, p.stream, a);
+  if (p.D == 128) hipLaunchKernelGGL((paged_decode_kernel<128, LIST, SCORES>), grid, dim3(64), 0, p.stream, a);
+  else hipLaunchKernelGGL((paged_decode_kernel<64, LIST, SCORES>), grid, dim3(64), 0, p.stream, a);
   prof_end(p.stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.plan == kOneUnit) return e;
   launch_combine(p.D, a, p.stream);
   return hipGetLastError();
+}
+
+hipError_t launch_paged_decode(const PagedDecode& p) {
+  return launch_decode<false, false>(p, decode_args(p, p.block_table, p.seq_blocks, p.max_blocks, p.block_size, p.ws,
+                                                    p.ws_bytes));
+}
+
+// ---------------------------------------------------------------- decode under a window, and with weights
+// Under a window a query sees the live entries at positions up to its own that
+// are less than `window` behind it or below `sinks`.  A long rollout's window
+// is a small part of its cache, and where it lies in the table follows from
+// the positions alone, so the visible slots are listed first (4 bytes read
+// for every slot of the table, beside 4 Hkv D for every visible one) and the
+// decode runs over the list: split evenly whatever the table holds, and no
+// slot is gathered that is not visible.
+struct WindowArgs {
+  const int* slot_pos;
+  const int* table;
+  const int* nblk;
+  const int* q_pos;
+  int* list;      // [S][cap]
+  int* counts;    // [S]
+  int max_blocks, BS, num_blocks, cap, window, sinks, chunk;
+};
+constexpr int kListThreads = 1024;
+
+// The list keeps the table's order: a workgroup takes a chunk of a sequence's
+// slots and counts the visible ones in front of it by itself (all those loads
+// are independent), so one launch does and nothing waits on another workgroup.
+__global__ void __launch_bounds__(kListThreads) paged_visible_kernel(WindowArgs a) {
+  constexpr int NW = kListThreads / kWave, STRIPS = 8;
+  __shared__ int wsum[NW], wbase[NW];
+  const int s = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = min(max(a.nblk[s], 0), a.max_blocks) * a.BS;   // slots of the sequence
+  const int c0 = (int)min((long long)blockIdx.x * a.chunk, (long long)n);
+  const int c1 = (int)min((long long)c0 + a.chunk, (long long)n);
+  if (c0 >= n && blockIdx.x > 0) return;
+  const int* trow = a.table + (size_t)s * a.max_blocks;
+  const int at = a.q_pos[s];
+  // whether the query sees place c of the table, and its slot
+  auto look = [&](int c, int& slot) __attribute__((always_inline)) {
+    const int blk = trow[c / a.BS];
+    const bool ok = (unsigned)blk < (unsigned)a.num_blocks;
+    slot = ok ? blk * a.BS + c % a.BS : 0;
+    const int pos = a.slot_pos[slot];
+    return ok && pos >= 0 && pos <= at && (at - pos < a.window || pos < a.sinks);
+  };
+  int before = 0;   // visible slots in front of the chunk
+#pragma unroll 8
+  for (int c = tid; c < c0; c += kListThreads) {
+    int slot;
+    before += look(c, slot);
+  }
+  before = wave_last(wave_scan(before));
+  if (lane == 0) wbase[wave] = before;
+  __syncthreads();
+  int base = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) base += wbase[w];
+  int* out = a.list + (size_t)s * a.cap;
+  // STRIPS strips of 64 slots a wave at a time
+  for (int r0 = c0; r0 < c1; r0 += STRIPS * kListThreads) {
+    const int first = r0 + wave * STRIPS * kWave;
+    unsigned long long hit[STRIPS];
+    int slot[STRIPS], cnt = 0;
+#pragma unroll
+    for (int k = 0; k < STRIPS; ++k) {
+      const int c = first + k * kWave + lane;
+      const bool see = look(min(c, c1 - 1), slot[k]);
+      hit[k] = __ballot(see && c < c1);
+      cnt += __builtin_popcountll(hit[k]);
+    }
+    if (lane == 0) wsum[wave] = cnt;
+    __syncthreads();
+    int o = base;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      o += w < wave ? wsum[w] : 0;
+      base += wsum[w];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < STRIPS; ++k) {
+      const int i = o + __builtin_popcountll(hit[k] & ((1ull << lane) - 1ull));
+      if (((hit[k] >> lane) & 1ull) && i < a.cap) out[i] = slot[k];   // more than cap only if positions repeat
+      o += __builtin_popcountll(hit[k]);
+    }
+  }
+  if (tid == 0 && c1 == n) a.counts[s] = min(base, a.cap);
+}
+
+// First rows of scores of all sequences, where there are too many for a wave to add them up.
+__global__ void __launch_bounds__(1024) paged_tile_base_kernel(DecodeArgs a, int* __restrict__ out) {
+  constexpr int NW = 1024 / kWave;
+  __shared__ int wsum[NW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int base = 0;
+  for (int s0 = 0; s0 < a.S; s0 += 1024) {
+    const int s = s0 + tid, t = s < a.S ? plan_tiles(slots_of(a, s)) : 0, incl = wave_scan(t);
+    if (lane == kWave - 1) wsum[wave] = incl;
+    __syncthreads();
+    int first = base + incl - t;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      first += w < wave ? wsum[w] : 0;
+      base += wsum[w];
+    }
+    if (s < a.S) out[s] = first;
+    __syncthreads();
+  }
+  if (tid == 0) out[a.S] = base;
+}
+
+// slot_weight[slot] += sum_h exp(s_h - LSE_h) over all q-heads, once LSE is
+// known.  One wave a tile of scores: 8 lanes read a head's 32 scores as float4,
+// the 64 lanes 8 heads at a time, and the heads are added in one order, so
+// the sums do not depend on how the decode was split.  Reads 4 Hq bytes a slot.
+template <bool LIST>
+__global__ void __launch_bounds__(256) paged_weight_kernel(DecodeArgs a, float* __restrict__ slot_weight) {
+  __shared__ int sBase[kPlanSeqs + 1];
+  __shared__ int wsum[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int* base = a.tile_base;
+  if (!base) {   // at most kPlanSeqs sequences, one a thread
+    const int t = (int)threadIdx.x < a.S ? plan_tiles(slots_of(a, threadIdx.x)) : 0, incl = wave_scan(t);
+    if (lane == kWave - 1) wsum[wave] = incl;
+    __syncthreads();
+    int end = incl;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) end += w < wave ? wsum[w] : 0;
+    sBase[threadIdx.x + 1] = end;
+    if (threadIdx.x == 0) sBase[0] = 0;
+    __syncthreads();
+    base = sBase;
+  }
+  const int total = min(base[a.S], a.tiles), waves = gridDim.x * 4, w = blockIdx.x * 4 + wave;
+  const int per = (total + waves - 1) / waves, t0 = min(w * per, total), t1 = min(t0 + per, total);
+  if (t0 >= t1) return;
+  int s = 0;   // the last sequence that begins at or before tile t0
+  for (int step = 1 << (31 - __builtin_clz(a.S)); step > 0; step >>= 1)
+    if (s + step < a.S && base[s + step] <= t0) s += step;
+  const int quad = lane & 7, h0 = lane >> 3;   // this lane's slots 4 quad .. + 3 of the tile, its first head
+  for (int t = t0; t < t1; ++t) {
+    while (s + 1 < a.S && base[s + 1] <= t) ++s;
+    const int ns = slots_of(a, s);
+    const float* row = a.scores + (size_t)t * a.Hq * kDecTile + 4 * quad;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int h = h0; h < a.Hq; h += 8) {
+      const float4 sc = *reinterpret_cast<const float4*>(row + (size_t)h * kDecTile);
+      const float l2 = a.lse[(size_t)s * a.Hq + h] * 1.4426950408889634f;
+      x[0] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc.x, a.scale_log2, -l2));
+      x[1] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc.y, a.scale_log2, -l2));
+      x[2] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc.z, a.scale_log2, -l2));
+      x[3] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc.w, a.scale_log2, -l2));
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int off = 8; off < kWave; off <<= 1) x[k] += __shfl_xor(x[k], off);
+    // lane l < 32 adds to place 4 (l % 8) + l / 8 of the tile
+    const int c = (t - base[s]) * kDecTile + 4 * quad + h0;
+    if (lane >= 32 || c >= ns) continue;
+    const float add = h0 == 0 ? x[0] : h0 == 1 ? x[1] : h0 == 2 ? x[2] : x[3];
+    const int entry = a.table[(size_t)s * a.max_blocks + (LIST ? c : c / a.BS)];
+    if (LIST) {
+      slot_weight[entry] += add;
+    } else if ((unsigned)entry < (unsigned)a.num_blocks) {
+      const int slot = entry * a.BS + c % a.BS;
+      if (a.slot_pos[slot] >= 0) slot_weight[slot] += add;
+    }
+  }
+}
+
+// Workspace of the decode under a window and with weights, in this order.
+struct ExSpace {
+  int cap;             // slots listed a sequence (window)
+  long long tiles;     // rows of scores (weights): every sequence's slots in tiles; no slot belongs to two sequences
+  size_t list, counts, base, scores, units;
+  size_t bytes() const { return list + counts + base + scores + units; }
+};
+static ExSpace ex_space(const PagedDecode& p) {
+  ExSpace x{};
+  const long long width = (long long)p.max_blocks * p.block_size;
+  long long each = width;
+  if (p.window > 0) {
+    x.cap = (int)std::min(width, (long long)p.window + p.sinks);
+    x.list = round256((size_t)p.S * x.cap * sizeof(int));
+    x.counts = round256((size_t)p.S * sizeof(int));
+    each = x.cap;
+  }
+  if (p.slot_weight) {
+    x.tiles = std::min(p.S * ((each + kDecTile - 1) / kDecTile),
+                       (long long)p.num_blocks * p.block_size / kDecTile + p.S);
+    x.base = p.S > kPlanSeqs ? round256((size_t)(p.S + 1) * sizeof(int)) : 0;
+    x.scores = round256((size_t)x.tiles * p.Hq * kDecTile * sizeof(float));
+  }
+  x.units = p.window > 0 ? paged_ws_bytes(p.S, p.Hq, p.Hkv, x.cap, 1, p.D)
+                         : paged_ws_bytes(p.S, p.Hq, p.Hkv, p.max_blocks, p.block_size, p.D);
+  return x;
+}
+size_t paged_ex_ws_bytes(const PagedDecode& p) { return ex_space(p).bytes(); }
+long long paged_ex_units(const PagedDecode& p) {
+  return p.window > 0 ? paged_units(p.S, p.Hkv, ex_space(p).cap, 1, p.D)
+                      : paged_units(p.S, p.Hkv, p.max_blocks, p.block_size, p.D);
+}
+
+// Slots of a sequence that one workgroup lists, at least; chunks of a sequence at most.
+constexpr int kListChunk = 8192, kListChunks = 16;
+
+template <bool LIST>
+static hipError_t launch_ex(const PagedDecode& p, const ExSpace& x, DecodeArgs a, int* base, float* scores) {
+  if (!p.slot_weight) return launch_decode<LIST, false>(p, a);
+  a.scores = scores;
+  a.tiles = (int)x.tiles;
+  if (p.S > kPlanSeqs) {
+    hipLaunchKernelGGL(paged_tile_base_kernel, dim3(1), dim3(1024), 0, p.stream, a, base);
+    a.tile_base = base;
+  }
+  hipError_t e = launch_decode<LIST, true>(p, a);
+  if (e != hipSuccess) return e;
+  const int grid = (int)std::min((x.tiles + 3) / 4, 2048ll);
+  hipLaunchKernelGGL(paged_weight_kernel<LIST>, dim3(grid), dim3(256), 0, p.stream, a, p.slot_weight);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_decode_ex(const PagedDecode& p) {
+  const ExSpace x = ex_space(p);
+  char* w = (char*)p.ws;
+  int* list = (int*)w;
+  int* counts = (int*)(w += x.list);
+  int* base = (int*)(w += x.counts);
+  float* scores = (float*)(w += x.base);
+  void* units = w += x.scores;
+  if (p.window == 0)
+    return launch_ex<false>(p, x, decode_args(p, p.block_table, p.seq_blocks, p.max_blocks, p.block_size, units, x.units),
+                            base, scores);
+  const long long width = (long long)p.max_blocks * p.block_size;
+  const int chunk = (int)std::max<long long>(kListChunk, (width + kListChunks - 1) / kListChunks);
+  const WindowArgs v{p.slot_pos, p.block_table, p.seq_blocks, p.q_pos, list, counts, p.max_blocks, p.block_size,
+                     p.num_blocks, x.cap, p.window, p.sinks, chunk};
+  const dim3 grid((unsigned)((width + chunk - 1) / chunk), (unsigned)p.S);
+  hipLaunchKernelGGL(paged_visible_kernel, grid, dim3(kListThreads), 0, p.stream, v);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_ex<true>(p, x, decode_args(p, list, counts, x.cap, 1, units, x.units), base, scores);
 }
 
 }  // namespace kvs

@@ -44,6 +44,13 @@ SIGNATURES = {
     "kvs_evict_attn_bwd_ex": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                                    _I, _I, _I, _I, _I, _I, _F, ctypes.c_uint, _P, _Z, _P]),
     "kvs_evict_attn_fwd_noalloc": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _F, _P]),
+    "kvs_window_attn_fwd_workspace": (_Z, [_I, _I, _I, _I, _I, _I]),
+    "kvs_window_attn_fwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _F, _I, _I, _P, _Z, _P]),
+    "kvs_window_attn_bwd_workspace": (_Z, [_I, _I, _I, _I, _I, _I]),
+    "kvs_window_attn_bwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                 _I, _I, _I, _I, _I, _I, _F, _I, _I, _P, _Z, _P]),
+    "kvs_key_weights_workspace": (_Z, [_I, _I, _I, _I, _I, _I, _I]),
+    "kvs_key_weights": (_I, [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _F, _I, _I, _I, _P, _Z, _P]),
     "kvs_classify_tiles": (_I, [_P, _P, _I, _I, _I, _I, _P, _P]),
     "kvs_classify_tiles_size": (_Z, [ctypes.POINTER(ctypes.c_int32), _I, _I, _I]),
     "kvs_check_evict_at": (_I, [_P, _P, _I, _I, ctypes.POINTER(_L), _P]),
@@ -63,6 +70,12 @@ SIGNATURES = {
     "kvs_paged_evict": (_I, [_P, _I, _P, _I, _I, _P]),
     "kvs_paged_append_host": (_I, [_P, _P, _P, _P, _I, _P, _P, _P, _I, _I, _I, _I, _P]),
     "kvs_paged_evict_host": (_I, [_P, _I, _P, _I, _I, _P]),
+    "kvs_paged_append_weighted": (_I, [_P, _P, _P, _P, _P, _I, _P, _P, _P, _P, _I, _I, _I, _I, _P]),
+    "kvs_paged_append_weighted_host": (_I, [_P, _P, _P, _P, _P, _I, _P, _P, _P, _P, _I, _I, _I, _I, _P]),
+    "kvs_paged_evict_lowest": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _P]),
+    "kvs_paged_decode_ex_workspace": (_Z, [_I, _I, _I, _I, _I, _I, _I, _I, _I, _I]),
+    "kvs_paged_decode_ex": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _F, _I, _I,
+                                 _P, _Z, _P]),
     "kvs_paged_decode_workspace": (_Z, [_I, _I, _I, _I, _I, _I]),
     "kvs_paged_decode": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _F, _P, _Z, _P]),
 }
@@ -237,6 +250,126 @@ def kvs_evict_attn_bwd(do, q, k, v, o, lse, evict_at, softmax_scale=None, cu_seq
     return dq, dk, dv
 
 
+def _i31(x) -> int:
+    """A count as a C int: values beyond its range count as the largest (or as negative)."""
+    return max(-1, min(int(x), 0x7FFFFFFF))
+
+
+def _window_args(tensors, bf16, fp32, q, k, evict_at, cu_seqlens, max_seqlen, softmax_scale, check_cu):
+    """Checks shared by the calls under a window; returns (B, Ntot, max_seqlen, Hq, Hkv, D, scale, LSE shape)."""
+    for t in tensors:
+        if t is not None and t.device != q.device:
+            raise ValueError("tensors must be on one device")
+    for t in bf16:
+        if t.dtype != torch.bfloat16:
+            raise ValueError("Q, K, V, O, dO and their gradients must be bfloat16")
+    for t in fp32:
+        if t.dtype != torch.float32:
+            raise ValueError("LSE and W must be float32")
+    for t in (evict_at, cu_seqlens):
+        if t is not None and t.dtype != torch.int32:
+            raise ValueError("evict_at and cu_seqlens must be int32")
+    B, T, ntok, Hq, Hkv, D = _dims(q, k, cu_seqlens)
+    if cu_seqlens is not None:
+        if max_seqlen is None:
+            raise ValueError("max_seqlen is required with cu_seqlens")
+        T = int(max_seqlen)
+    if k.shape[:-2] != q.shape[:-2] or k.shape[-1] != D:
+        raise ValueError(f"shape mismatch: q {tuple(q.shape)}, k {tuple(k.shape)}")
+    if evict_at is not None and evict_at.shape != q.shape[:-2]:
+        raise ValueError(f"evict_at has shape {tuple(evict_at.shape)}, expected {tuple(q.shape[:-2])}")
+    if cu_seqlens is not None and check_cu:
+        _check_shapes(q, k, k, q[..., 0, 0], cu_seqlens, T, True)
+    if not q.is_cuda:
+        raise ValueError("tensors must be on the GPU")
+    scale = 1.0 / math.sqrt(D) if softmax_scale is None else float(softmax_scale)
+    return B, ntok, T, Hq, Hkv, D, scale, (B, Hq, T) if cu_seqlens is None else (Hq, ntok)
+
+
+def _like(t, ref, name):
+    if t.shape != ref.shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(ref.shape)}")
+
+
+def kvs_window_attn_fwd(q, k, v, window: int, sinks: int = 0, evict_at=None, softmax_scale=None, cu_seqlens=None,
+                        max_seqlen=None, out=None, lse=None, check_cu=True) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Forward of attention under a sliding window with sinks; returns ``(O, LSE)``.
+
+    Query i sees key j iff ``j <= i``, ``i < evict_at[j]`` (if given) and ``i - j < window or j < sinks``.
+    Layouts as in ``kvs_evict_attn_fwd``; ``check_cu=False`` skips the host's look at ``cu_seqlens`` (a
+    synchronisation, which a stream that is being captured does not take).
+    """
+    out = torch.empty_like(q) if out is None else out
+    B, n, T, Hq, Hkv, D, scale, lse_shape = _window_args((k, v, evict_at, cu_seqlens, out, lse), (q, k, v, out), (), q, k,
+                                                         evict_at, cu_seqlens, max_seqlen, softmax_scale, check_cu)
+    if lse is None:
+        lse = torch.empty(lse_shape, dtype=torch.float32, device=q.device)
+    if tuple(lse.shape) != lse_shape or lse.dtype != torch.float32:
+        raise ValueError(f"LSE must be float32 {lse_shape}")
+    _like(v, k, "V")
+    _like(out, q, "O")
+    nws = lib.kvs_window_attn_fwd_workspace(B, n, T, Hq, Hkv, D)
+    ws = _workspace(nws, q.device)
+    with torch.cuda.device(q.device):
+        st = lib.kvs_window_attn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(evict_at), _ptr(cu_seqlens), _ptr(out), _ptr(lse),
+                                     B, n, T, Hq, Hkv, D, scale, _i31(window), _i31(sinks), _ptr(ws), nws, _stream(q))
+    _check("kvs_window_attn_fwd", st)
+    return out, lse
+
+
+def kvs_window_attn_bwd(do, q, k, v, o, lse, window: int, sinks: int = 0, evict_at=None, softmax_scale=None,
+                        cu_seqlens=None, max_seqlen=None, dq=None, dk=None, dv=None,
+                        check_cu=True) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Backward of ``kvs_window_attn_fwd``; returns ``(dQ, dK, dV)`` (bf16)."""
+    dq = torch.empty_like(q) if dq is None else dq
+    dk = torch.empty_like(k) if dk is None else dk
+    dv = torch.empty_like(v) if dv is None else dv
+    B, n, T, Hq, Hkv, D, scale, lse_shape = _window_args((do, k, v, o, lse, evict_at, cu_seqlens, dq, dk, dv),
+                                                         (do, q, k, v, o, dq, dk, dv), (lse,), q, k, evict_at,
+                                                         cu_seqlens, max_seqlen, softmax_scale, check_cu)
+    if tuple(lse.shape) != lse_shape:
+        raise ValueError(f"LSE must be float32 {lse_shape}")
+    for t, ref, name in ((do, q, "dO"), (o, q, "O"), (dq, q, "dQ"), (v, k, "V"), (dk, k, "dK"), (dv, k, "dV")):
+        _like(t, ref, name)
+    nws = lib.kvs_window_attn_bwd_workspace(B, n, T, Hq, Hkv, D)
+    ws = _workspace(nws, q.device)
+    with torch.cuda.device(q.device):
+        st = lib.kvs_window_attn_bwd(_ptr(do), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(evict_at),
+                                     _ptr(cu_seqlens), _ptr(dq), _ptr(dk), _ptr(dv), B, n, T, Hq, Hkv, D, scale,
+                                     _i31(window), _i31(sinks), _ptr(ws), nws, _stream(q))
+    _check("kvs_window_attn_bwd", st)
+    return dq, dk, dv
+
+
+def kvs_key_weights(q, k, lse, evict_at=None, softmax_scale=None, cu_seqlens=None, max_seqlen=None,
+                    window: Optional[int] = None, sinks: int = 0, last_rows: Optional[int] = None, out=None,
+                    check_cu=True) -> torch.Tensor:
+    """Attention weight of every key, ``W_j = sum over heads and over the queries i that see j of exp(s_ij - LSE_i)``.
+
+    ``lse`` is the forward's over the same mask (``window`` None: no window).  ``last_rows`` (None: all) counts the
+    last queries of each trace only.  Returns float32 [B, T] (varlen: [Ntot]).
+    """
+    if window is not None and window < 1:
+        raise ValueError("window must be >= 1 (None: no window)")
+    if last_rows is not None and last_rows < 1:
+        raise ValueError("last_rows must be >= 1 (None: all)")
+    w = torch.empty(q.shape[:-2], dtype=torch.float32, device=q.device) if out is None else out
+    B, n, T, Hq, Hkv, D, scale, lse_shape = _window_args((k, lse, evict_at, cu_seqlens, w), (q, k), (lse, w), q, k,
+                                                         evict_at, cu_seqlens, max_seqlen, softmax_scale, check_cu)
+    if tuple(lse.shape) != lse_shape:
+        raise ValueError(f"LSE must be float32 {lse_shape}")
+    if w.shape != q.shape[:-2]:
+        raise ValueError(f"W has shape {tuple(w.shape)}, expected {tuple(q.shape[:-2])}")
+    rows = 0 if last_rows is None else _i31(last_rows)
+    nws = lib.kvs_key_weights_workspace(B, n, T, Hq, Hkv, D, rows)
+    ws = _workspace(nws, q.device)
+    with torch.cuda.device(q.device):
+        st = lib.kvs_key_weights(_ptr(q), _ptr(k), _ptr(lse), _ptr(evict_at), _ptr(cu_seqlens), _ptr(w), B, n, T, Hq,
+                                 Hkv, D, scale, _i31(window or 0), _i31(sinks), rows, _ptr(ws), nws, _stream(q))
+    _check("kvs_key_weights", st)
+    return w
+
+
 def kvs_classify_tiles(evict_at, BM: int, BN: int, cu_seqlens=None) -> torch.Tensor:
     """Tile classes (uint8: 0 EMPTY, 1 PARTIAL, 2 FULL), per-trace grids concatenated.
 
@@ -309,3 +442,31 @@ def evict_attn(q, k, v, evict_at, softmax_scale=None, cu_seqlens=None, max_seqle
     """Differentiable eviction-masked attention: returns ``(O, LSE)``; LSE carries no gradient."""
     scale = 1.0 / math.sqrt(q.shape[-1]) if softmax_scale is None else float(softmax_scale)
     return _EvictAttn.apply(q, k, v, evict_at, scale, cu_seqlens, max_seqlen)
+
+
+class _WindowAttn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, window, sinks, evict_at, scale, cu_seqlens, max_seqlen, check_cu):
+        o, lse = kvs_window_attn_fwd(q, k, v, window, sinks, evict_at, scale, cu_seqlens, max_seqlen, check_cu=check_cu)
+        ctx.save_for_backward(q, k, v, o, lse, evict_at, cu_seqlens)
+        ctx.args = window, sinks, scale, max_seqlen
+        ctx.mark_non_differentiable(lse)
+        ctx.set_materialize_grads(False)   # LSE carries no gradient: no zeros filled for it
+        return o, lse
+
+    @staticmethod
+    def backward(ctx, do, _dlse):
+        q, k, v, o, lse, evict_at, cu_seqlens = ctx.saved_tensors
+        window, sinks, scale, max_seqlen = ctx.args
+        do = torch.zeros_like(o) if do is None else do
+        # cu_seqlens is the forward's, which has checked it
+        dq, dk, dv = kvs_window_attn_bwd(do.contiguous(), q, k, v, o, lse, window, sinks, evict_at, scale, cu_seqlens,
+                                         max_seqlen, check_cu=False)
+        return dq, dk, dv, None, None, None, None, None, None, None
+
+
+def window_attn(q, k, v, window: int, sinks: int = 0, evict_at=None, softmax_scale=None, cu_seqlens=None, max_seqlen=None,
+                check_cu=True):
+    """Differentiable attention under a sliding window with sinks: returns ``(O, LSE)``; LSE carries no gradient."""
+    scale = 1.0 / math.sqrt(q.shape[-1]) if softmax_scale is None else float(softmax_scale)
+    return _WindowAttn.apply(q, k, v, int(window), int(sinks), evict_at, scale, cu_seqlens, max_seqlen, check_cu)
