@@ -412,7 +412,8 @@ kvs_status_t kvs_paged_append_weighted_host(const void* K_new, const void* V_new
  * highest weight, equal weights leave in the table's order.  slot_pos of the
  * evicted slots becomes -1; their positions go to positions[s][0..counts[s])
  * (device int32 [num_seqs][max_out], in the table's order, the rest -1), for
- * kvs_bm_evict.  Tables are clamped as in the decode. */
+ * kvs_bm_evict.  Tables are clamped as in the decode; max_blocks * block_size
+ * is at most 2^30. */
 kvs_status_t kvs_paged_evict_lowest(const float* slot_weight, int32_t* slot_pos, const int32_t* block_table,
                                     const int32_t* seq_blocks, const int32_t* keep, int32_t* positions,
                                     int32_t* counts, int num_seqs, int num_blocks, int block_size, int max_blocks,
@@ -445,8 +446,9 @@ kvs_status_t kvs_paged_decode(const void* Q, const void* K_cache, const void* V_
  * window 0: every live entry, q_pos (may be NULL) and sinks without effect.
  * slot_weight not NULL: slot_weight[slot] += sum_h exp(s_h - LSE_h) over all
  * q-heads, for every entry the query sees.  Limits and layouts are those of
- * kvs_paged_decode (under a window at most 65535 sequences); the workspace is
- * the query's, `weights` nonzero for calls with slot_weight. */
+ * kvs_paged_decode (under a window at most 65535 sequences of at most 2^30
+ * slots, max_blocks * block_size); the workspace is the query's, `weights`
+ * nonzero for calls with slot_weight. */
 size_t kvs_paged_decode_ex_workspace(int num_seqs, int Hq, int Hkv, int D, int num_blocks, int max_blocks,
                                      int block_size, int window, int sinks, int weights);
 kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,

@@ -445,10 +445,10 @@ static int rows_counted(int last_rows, int max_seqlen) {
 }
 
 size_t kvs_key_weights_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D, int last_rows) {
-  if (B < 1 || Ntot < 0 || Hkv < 1 || max_seqlen < 1) return 0;
-  (void)Hq; (void)D;
+  if (B < 1 || Ntot < 0 || Hq < 1 || Hkv < 1 || max_seqlen < 1) return 0;
+  (void)D;
   return until_bytes(Ntot) + fwd_ws(B, Ntot) +
-         kvs::ws_weights_bytes(B, max_seqlen, Ntot, Hkv, rows_counted(last_rows, max_seqlen));
+         kvs::ws_weights_bytes(B, max_seqlen, Ntot, Hq, Hkv, rows_counted(last_rows, max_seqlen));
 }
 
 kvs_status_t kvs_key_weights(const void* Q, const void* K, const float* LSE, const int32_t* evict_at,
@@ -460,7 +460,7 @@ kvs_status_t kvs_key_weights(const void* Q, const void* K, const float* LSE, con
     return st;
   if (last_rows < 0) return fail(KVS_ERR_SHAPE, "last_rows must be >= 0 (got %d)", last_rows);
   const int rows = rows_counted(last_rows, max_seqlen);
-  if (kvs::weights_grid(B, max_seqlen, Hkv, rows) * 256 > 0xffffffffll)
+  if (kvs::weights_grid(B, max_seqlen, Hq, Hkv, rows) * 256 > 0xffffffffll)
     return fail(KVS_ERR_UNSUPPORTED, "key weights grid too large");
   if (Ntot == 0) return KVS_OK;
   REQUIRE_PTR(Q, "Q");
@@ -473,10 +473,7 @@ kvs_status_t kvs_key_weights(const void* Q, const void* K, const float* LSE, con
   kvs::Problem p = window_problem(Q, K, nullptr, evict_at, cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale,
                                   window, sinks, workspace, workspace_bytes, stream);
   p.lse_in = LSE;
-  int2* kstats = (int2*)p.ws;
-  hipError_t e = kvs::launch_kstats(p, kstats);
-  if (e != hipSuccess) return hip_fail(e, "key-tile statistics launch");
-  e = kvs::launch_key_weights(p, kstats, rows, (float*)((char*)p.ws + fwd_ws(B, Ntot)), W);
+  hipError_t e = kvs::launch_key_weights(p, (int2*)p.ws, rows, (char*)p.ws + fwd_ws(B, Ntot), W);
   return e == hipSuccess ? KVS_OK : hip_fail(e, "key weights launch");
 }
 
@@ -837,6 +834,8 @@ kvs_status_t kvs_paged_decode(const void* Q, const void* K_cache, const void* V_
 }
 
 // ---------------------------------------------------------------- decode under a window and with weights
+constexpr int kMaxPlaces = 1 << 30;   // slots of a sequence's table where kernels count places in strides of thousands
+
 // The sizes of such a call; workspace and launch sizes follow from them alone.
 static kvs::PagedDecode decode_ex_sizes(int S, int Hq, int Hkv, int D, int num_blocks, int max_blocks, int block_size,
                                         int window, int sinks, bool weights) {
@@ -873,6 +872,8 @@ kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void*
   if (!(softmax_scale > 0.f) || softmax_scale != softmax_scale)
     return fail(KVS_ERR_SHAPE, "softmax_scale must be positive and finite");
   if (window < 0 || sinks < 0) return fail(KVS_ERR_SHAPE, "window and sinks must be >= 0 (got %d, %d)", window, sinks);
+  if (window > 0 && (long long)max_blocks * block_size > kMaxPlaces)
+    return fail(KVS_ERR_UNSUPPORTED, "max_blocks * block_size above %d", kMaxPlaces);
   kvs::PagedDecode p = decode_ex_sizes(num_seqs, Hq, Hkv, D, num_blocks, max_blocks, block_size, window, sinks,
                                        slot_weight != nullptr);
   if (window > 0 && num_seqs > 65535) return fail(KVS_ERR_UNSUPPORTED, "more than 65535 sequences under a window");
@@ -911,8 +912,8 @@ kvs_status_t kvs_paged_evict_lowest(const float* slot_weight, int32_t* slot_pos,
   if (num_seqs < 1 || max_blocks < 1 || max_out < 1)
     return fail(KVS_ERR_SHAPE, "num_seqs, max_blocks and max_out must be >= 1");
   if (sinks < 0 || recent < 0) return fail(KVS_ERR_SHAPE, "sinks and recent must be >= 0 (got %d, %d)", sinks, recent);
-  if ((long long)max_blocks * block_size > 0x7fffffffll)
-    return fail(KVS_ERR_UNSUPPORTED, "max_blocks * block_size above INT32_MAX");
+  if ((long long)max_blocks * block_size > kMaxPlaces)
+    return fail(KVS_ERR_UNSUPPORTED, "max_blocks * block_size above %d", kMaxPlaces);
   if (num_seqs > (1 << 21)) return fail(KVS_ERR_UNSUPPORTED, "more than 2097152 sequences");
   if (!slot_weight || !slot_pos || !block_table || !seq_blocks || !keep || !positions || !counts)
     return fail(KVS_ERR_NULL, "NULL argument");

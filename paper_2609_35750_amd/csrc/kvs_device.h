@@ -217,6 +217,39 @@ __device__ __forceinline__ const T* uniform_ptr(const T* p) {
   return (const T*)(uintptr_t)(((uint64_t)hi << 32) | lo);
 }
 
+// A sliding window with sinks (a window over the trace in which the first keys
+// stay visible): query i sees key j iff j <= i < evict_at[j] and (i - j <
+// window or j < sinks).  That is an eviction index again, min(evict_at[j], j +
+// window) for j >= sinks, so the attention kernels stay as they are; it is
+// made by the kernel that takes the tiles' statistics, which reads every
+// evict_at once anyway (4 bytes a token more to write, no launch of its own).
+struct KeyWindow {
+  int window, sinks;   // window 0: none
+  int* until;          // [ntok] out: the last query's index + 1 of every key; NULL: evict_at is that
+};
+__device__ __forceinline__ int key_until(const int* __restrict__ evict, const KeyWindow& kw, const Trace& tr, int j) {
+  const int e = evict ? min(evict[tr.tok0 + j], tr.L) : tr.L;
+  return kw.window > 0 && j >= kw.sinks ? min(e, j + kw.window) : e;   // j < 2^20, window at most 2^20
+}
+
+// Statistics of the 64-key tiles of all traces: one wave a tile, one lane a
+// key, four tiles a workgroup of 256 threads (group wg of tg per trace).  Bound
+// by one memory latency; one thread a tile walked its 64 keys in series, 6.0 us
+// for 512 tokens and 7.4 for 8,191, against 2.3 and 4.6 (a launch's own time).
+__device__ __forceinline__ void kstats_group(const int* __restrict__ evict, const int* __restrict__ cu, int T, int ntok,
+                                             int wg, int tg, int2* __restrict__ out, const KeyWindow& kw) {
+  const int b = wg / tg, kt = (wg - b * tg) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const Trace tr = trace_of(cu, b, T, ntok);
+  const int j0 = kt * kKeyTile;
+  if (j0 >= tr.L) return;
+  const int j = min(j0 + lane, tr.L - 1);   // lanes past the end repeat the last key
+  const int e = key_until(evict, kw, tr, j);
+  if (kw.until && j0 + lane < tr.L) kw.until[tr.tok0 + j] = e;
+  const int mn = wave_min(e), mx = wave_max(e);
+  if (lane == 0) out[kstat_index(b, tr.tok0, kt, kKeyTile)] = make_int2(mn, mx);
+}
+__host__ __device__ __forceinline__ int kstats_groups(int T) { return ((T + kKeyTile - 1) / kKeyTile + 3) / 4; }
+
 // LDS tile of rows x D bf16 with padded rows and a per-row XOR on the
 // 16-byte chunk index ("swizzle").  The hardware serves a b128 read 16 lanes
 // at a time and a b64 read (the transposed operand reads) 32 lanes at a time,
@@ -350,5 +383,11 @@ __device__ __forceinline__ void stage_words_at(uint32_t lds, const void* base, i
 
 // Wait for this wave's outstanding global loads (including LDS-direct ones).
 __device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+// Wait until at most N vector memory operations of this wave are outstanding (N <= 63).
+template <int N>
+__device__ __forceinline__ void wait_vm_le() {
+  static_assert(N >= 0 && N < 64, "vmcnt is six bits");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
 
 }  // namespace kvs

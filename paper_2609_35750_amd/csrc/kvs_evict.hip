@@ -28,130 +28,153 @@ __device__ __forceinline__ unsigned weight_key(float w) {
   return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
 }
 
+// Places of the table a lane looks at, 64 apart: one division, then additions.
+struct Places {
+  int c, blk, row, BS, dblk, drow;
+  __device__ __forceinline__ Places(int first, int bs) : c(first), blk(first / bs), row(first % bs), BS(bs) {
+    dblk = kWave / bs;
+    drow = kWave % bs;
+  }
+  __device__ __forceinline__ void next() {
+    c += kWave;
+    blk += dblk;
+    row += drow;
+    if (row >= BS) {
+      row -= BS;
+      ++blk;
+    }
+  }
+};
+
 // Entries a thread keeps in registers: KEEP strips of 64 a wave; 0: read again for every count (longer tables).
 template <int KEEP>
 __global__ void __launch_bounds__(kEvictThreads) paged_evict_lowest_kernel(PagedEvictLowest a) {
+  constexpr int N = KEEP ? KEEP : 1;
   __shared__ int hist[kEvictBins];
-  __shared__ int red[4][kEvictWaves];
-  __shared__ int pick[2];   // bin of the n-th, entries below it
+  __shared__ int red[2][4][kEvictWaves];   // by turns, so that one barrier stands between two exchanges
+  __shared__ int pick[2][2];               // bin of the n-th, entries below it
   const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int BS = a.block_size;
-  const int n = min(max(a.seq_blocks[s], 0), a.max_blocks) * BS;   // slots of the sequence
+  const int n = min(max(a.seq_blocks[s], 0), a.max_blocks) * a.block_size;   // slots of the sequence
   const int* trow = a.block_table + (size_t)s * a.max_blocks;
   int32_t* out = a.positions + (size_t)s * a.max_out;
+  const int keep = max(a.keep[s], 0);
 
-  // wave w has the places [w per, (w + 1) per) of the table, in strips of 64
-  const int strips = KEEP ? KEEP : (n + kEvictThreads - 1) / kEvictThreads;
-  const int c0 = wave * strips * kWave;
-  auto slot_at = [&](int c) __attribute__((always_inline)) {   // -1: no slot
-    if (c >= n) return -1;
-    const int blk = trow[c / BS];
-    return (unsigned)blk < (unsigned)a.num_blocks ? blk * BS + c % BS : -1;
+  // wave w has the places [w strips 64, (w + 1) strips 64) of the table, in strips of 64
+  const int strips = (n + kEvictThreads - 1) / kEvictThreads, c0 = wave * strips * kWave + lane;
+  // an entry: its position (-1: none), the key of its weight, its slot
+  int pos_r[N], slot_r[N];
+  unsigned key_r[N];
+  auto slot_of = [&](int entry, const Places& p) __attribute__((always_inline)) {
+    return p.c < n && (unsigned)entry < (unsigned)a.num_blocks ? entry * a.block_size + p.row : -1;
   };
-  int pos_r[KEEP ? KEEP : 1];        // position of the entry; -1: none
-  unsigned key_r[KEEP ? KEEP : 1];
-  int slot_r[KEEP ? KEEP : 1];
-  int live = 0, last = -1;
+  if (KEEP) {
+    Places p(c0, a.block_size);
 #pragma unroll
-  for (int k = 0; k < (KEEP ? KEEP : 0); ++k) {
-    slot_r[k] = slot_at(c0 + k * kWave + lane);
-    pos_r[k] = slot_r[k] >= 0 ? a.slot_pos[slot_r[k]] : -1;
-    key_r[k] = slot_r[k] >= 0 ? weight_key(a.slot_weight[slot_r[k]]) : 0u;
+    for (int k = 0; k < N; ++k, p.next()) slot_r[k] = k < strips && p.c < n ? trow[p.blk] : -1;
+    p = Places(c0, a.block_size);
+#pragma unroll
+    for (int k = 0; k < N; ++k, p.next()) slot_r[k] = k < strips ? slot_of(slot_r[k], p) : -1;
+    float w[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      pos_r[k] = slot_r[k] >= 0 ? a.slot_pos[slot_r[k]] : -1;
+      w[k] = slot_r[k] >= 0 ? a.slot_weight[slot_r[k]] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) key_r[k] = weight_key(w[k]);
   }
-  // f(strip, position, key, slot) for every strip; position -1 where the lane has no entry
+  // f(position, key, slot) for every strip
   auto each = [&](auto f) __attribute__((always_inline)) {
     if (KEEP) {
 #pragma unroll
-      for (int k = 0; k < (KEEP ? KEEP : 1); ++k) f(pos_r[k], key_r[k], slot_r[k]);
+      for (int k = 0; k < N; ++k)
+        if (k < strips) f(pos_r[k], key_r[k], slot_r[k]);
     } else {
-#pragma unroll 4
-      for (int k = 0; k < strips; ++k) {
-        const int slot = slot_at(c0 + k * kWave + lane);
+      Places p(c0, a.block_size);
+#pragma unroll 8
+      for (int k = 0; k < strips; ++k, p.next()) {
+        const int slot = slot_of(p.c < n ? trow[p.blk] : -1, p);
         f(slot >= 0 ? a.slot_pos[slot] : -1, slot >= 0 ? weight_key(a.slot_weight[slot]) : 0u, slot);
       }
     }
   };
-  each([&](int pos, unsigned, int) __attribute__((always_inline)) {
-    live += __builtin_popcountll(__ballot(pos >= 0));
-    last = max(last, pos);
-  });
-  last = wave_max(last);
-  if (lane == 0) {
-    red[0][wave] = live;
-    red[1][wave] = last;
-  }
-  __syncthreads();
-  live = 0;
-#pragma unroll
-  for (int w = 0; w < kEvictWaves; ++w) {
-    live += red[0][w];
-    last = max(last, red[1][w]);
-  }
-  const int newest = last - a.recent;   // positions above it stay (last >= -1, recent >= 0)
-  auto is_free = [&](int pos) { return pos >= 0 && pos >= a.sinks && pos <= newest; };
-  // the entries that may leave: how many, and the range of their keys
-  int nfree = 0;
+
+  // live entries, the newest position, the range of the keys (of all but the sinks: the newest are not known yet)
+  int live = 0, last = -1;
   unsigned lo = 0xffffffffu, hi = 0u;
   each([&](int pos, unsigned key, int) __attribute__((always_inline)) {
-    const bool f = is_free(pos);
-    nfree += __builtin_popcountll(__ballot(f));
+    live += __builtin_popcountll(__ballot(pos >= 0));
+    last = max(last, pos);
+    const bool f = pos >= a.sinks && pos >= 0;
     lo = f ? min(lo, key) : lo;
     hi = f ? max(hi, key) : hi;
   });
+  last = wave_max(last);
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) {
     lo = min(lo, (unsigned)__shfl_xor((int)lo, off));
     hi = max(hi, (unsigned)__shfl_xor((int)hi, off));
   }
-  __syncthreads();   // red is read
   if (lane == 0) {
-    red[0][wave] = nfree;
-    red[1][wave] = (int)lo;
-    red[2][wave] = (int)hi;
+    red[0][0][wave] = live;
+    red[0][1][wave] = last;
+    red[0][2][wave] = (int)lo;
+    red[0][3][wave] = (int)hi;
   }
+  hist[tid] = 0;
   __syncthreads();
-  nfree = 0;
+  live = 0;
 #pragma unroll
   for (int w = 0; w < kEvictWaves; ++w) {
-    nfree += red[0][w];
-    lo = min(lo, (unsigned)red[1][w]);
-    hi = max(hi, (unsigned)red[2][w]);
+    live += red[0][0][w];
+    last = max(last, red[0][1][w]);
+    lo = min(lo, (unsigned)red[0][2][w]);
+    hi = max(hi, (unsigned)red[0][3][w]);
   }
-  const int go = min(min(max(live - max(a.keep[s], 0), 0), nfree), a.max_out);   // entries that leave
-  for (int i = go + tid; i < a.max_out; i += kEvictThreads) out[i] = -1;
-  if (tid == 0) a.counts[s] = go;
-  if (go == 0) return;
+  const int newest = last - a.recent;   // positions above it stay (last >= -1, recent >= 0)
+  auto is_free = [&](int pos) { return pos >= 0 && pos >= a.sinks && pos <= newest; };
 
-  // Narrow [lo, hi] to the key of the go-th lowest: `rank` of the entries in the range leave (1 <= rank <= entries in
-  // the range), and all below it.
-  int rank = go, inside = nfree;
-  while (rank < inside && lo < hi) {
-    const unsigned width = hi - lo;
-    const int shift = max(22 - (int)__builtin_clz(width), 0);   // width >> shift < 1,024
-    hist[tid] = 0;
-    __syncthreads();
+  // Narrow [lo, hi] to the key of the go-th lowest: `rank` of the free entries in the range leave (1 <= rank <= inside,
+  // how many those are), and all below it.  The first count also says how many free entries there are.
+  int go = min(max(live - keep, 0), a.max_out), rank = go, inside = INT_MAX;   // entries that leave
+  bool first = true;
+  int turn = 1;
+  while (rank > 0 && rank < inside && (first || lo < hi)) {
+    const unsigned width = hi >= lo ? hi - lo : 0u;
+    const int shift = max(22 - (width ? (int)__builtin_clz(width) : 32), 0);   // width >> shift < 1,024
     each([&](int pos, unsigned key, int) __attribute__((always_inline)) {
       if (is_free(pos) && key >= lo && key <= hi) atomicAdd(&hist[(key - lo) >> shift], 1);
     });
     __syncthreads();
     const int cnt = hist[tid], incl = wave_scan(cnt);
-    if (lane == kWave - 1) red[3][wave] = incl;
+    if (lane == kWave - 1) red[turn][0][wave] = incl;
     __syncthreads();
-    int below = incl - cnt;
+    int below = incl - cnt, all = 0;
 #pragma unroll
-    for (int w = 0; w < kEvictWaves; ++w) below += w < wave ? red[3][w] : 0;
-    if (below < rank && rank <= below + cnt) {   // one thread
-      pick[0] = tid;
-      pick[1] = below;
+    for (int w = 0; w < kEvictWaves; ++w) {
+      const int x = red[turn][0][w];
+      below += w < wave ? x : 0;
+      all += x;
     }
+    if (first) rank = go = min(go, all);
+    first = false;
+    if (below < rank && rank <= below + cnt) {   // one thread, if any entry leaves
+      pick[turn][0] = tid;
+      pick[turn][1] = below;
+    }
+    hist[tid] = 0;
+    if (below < rank && rank <= below + cnt) red[turn][1][0] = cnt;
     __syncthreads();
-    const int bin = pick[0];
-    rank -= pick[1];
-    inside = hist[bin];
-    lo += (unsigned)bin << shift;
+    if (rank == 0) break;
+    rank -= pick[turn][1];
+    inside = red[turn][1][0];
+    lo += (unsigned)pick[turn][0] << shift;
     hi = lo + min(hi - lo, (1u << shift) - 1u);
-    __syncthreads();   // hist and pick are read
+    turn ^= 1;
   }
+  for (int i = go + tid; i < a.max_out; i += kEvictThreads) out[i] = -1;
+  if (tid == 0) a.counts[s] = go;
+  if (go == 0) return;
 
   // All entries below lo leave, and of those in [lo, hi] the first `rank` in the table's order (all of them, or
   // all equal).
@@ -162,15 +185,15 @@ __global__ void __launch_bounds__(kEvictThreads) paged_evict_lowest_kernel(Paged
     nin += __builtin_popcountll(__ballot(f && key >= lo && key <= hi));
   });
   if (lane == 0) {
-    red[0][wave] = nbelow;
-    red[1][wave] = nin;
+    red[turn][2][wave] = nbelow;
+    red[turn][3][wave] = nin;
   }
   __syncthreads();
   int at = 0, in = 0;   // entries in front of this wave's that leave for certain, that lie in the range
 #pragma unroll
   for (int w = 0; w < kEvictWaves; ++w) {
-    at += w < wave ? red[0][w] : 0;
-    in += w < wave ? red[1][w] : 0;
+    at += w < wave ? red[turn][2][w] : 0;
+    in += w < wave ? red[turn][3][w] : 0;
   }
   at += min(in, rank);
   const unsigned long long before = (1ull << lane) - 1ull;

@@ -114,39 +114,6 @@ __device__ __forceinline__ int2 key_tile_stats(const int* __restrict__ evict, co
   return make_int2(mn, mx);
 }
 
-// A sliding window with sinks (a window over the trace in which the first keys
-// stay visible): query i sees key j iff j <= i < evict_at[j] and (i - j <
-// window or j < sinks).  That is an eviction index again, min(evict_at[j], j +
-// window) for j >= sinks, so the attention kernels stay as they are; it is
-// made by the kernel that takes the tiles' statistics, which reads every
-// evict_at once anyway (4 bytes a token more to write, no launch of its own).
-struct KeyWindow {
-  int window, sinks;   // window 0: none
-  int* until;          // [ntok] out: the last query's index + 1 of every key; NULL: evict_at is that
-};
-__device__ __forceinline__ int key_until(const int* __restrict__ evict, const KeyWindow& kw, const Trace& tr, int j) {
-  const int e = evict ? min(evict[tr.tok0 + j], tr.L) : tr.L;
-  return kw.window > 0 && j >= kw.sinks ? min(e, j + kw.window) : e;   // j < 2^20, window at most 2^20
-}
-
-// Statistics of the 64-key tiles of all traces: one wave a tile, one lane a
-// key, four tiles a workgroup of 256 threads (group wg of tg per trace).  Bound
-// by one memory latency; one thread a tile walked its 64 keys in series, 6.0 us
-// for 512 tokens and 7.4 for 8,191, against 2.3 and 4.6 (a launch's own time).
-__device__ __forceinline__ void kstats_group(const int* __restrict__ evict, const int* __restrict__ cu, int T, int ntok,
-                                             int wg, int tg, int2* __restrict__ out, const KeyWindow& kw) {
-  const int b = wg / tg, kt = (wg - b * tg) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const Trace tr = trace_of(cu, b, T, ntok);
-  const int j0 = kt * kKeyTile;
-  if (j0 >= tr.L) return;
-  const int j = min(j0 + lane, tr.L - 1);   // lanes past the end repeat the last key
-  const int e = key_until(evict, kw, tr, j);
-  if (kw.until && j0 + lane < tr.L) kw.until[tr.tok0 + j] = e;
-  const int mn = wave_min(e), mx = wave_max(e);
-  if (lane == 0) out[kstat_index(b, tr.tok0, kt, kKeyTile)] = make_int2(mn, mx);
-}
-__host__ __device__ __forceinline__ int kstats_groups(int T) { return ((T + kKeyTile - 1) / kKeyTile + 3) / 4; }
-
 __global__ void __launch_bounds__(256) kstats_kernel(const int* __restrict__ evict, const int* __restrict__ cu, int T,
                                                      int ntok, int2* __restrict__ out, KeyWindow kw) {
   kstats_group(evict, cu, T, ntok, blockIdx.x, kstats_groups(T), out, kw);

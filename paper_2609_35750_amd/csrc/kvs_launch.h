@@ -72,11 +72,11 @@ hipError_t launch_classify(const int32_t* evict, const int32_t* cu, int B, int T
 hipError_t launch_check(const int32_t* evict, const int32_t* cu, int B, int T, int ntok,
                         int64_t* first_bad, int* cu_bad, hipStream_t stream);
 
-// Attention weights of the keys (p.until, p.lse_in set; kstats taken under p's window): W [ntok] from `part`,
-// ws_weights_bytes of workspace.  last_rows: queries of each trace that count, at its end.
-size_t ws_weights_bytes(int B, int T, int ntok, int Hkv, int last_rows);
-long long weights_grid(int B, int T, int Hkv, int last_rows);   // workgroups of 256 threads
-hipError_t launch_key_weights(const Problem& p, const int2* kstats, int last_rows, float* part, float* w);
+// Attention weights of the keys (p.until, p.lse_in set), W [ntok]; kstats and ws_weights_bytes of workspace are written.
+// last_rows: queries of each trace that count, at its end.
+size_t ws_weights_bytes(int B, int T, int ntok, int Hq, int Hkv, int last_rows);
+long long weights_grid(int B, int T, int Hq, int Hkv, int last_rows);   // workgroups of 256 threads, of the largest launch
+hipError_t launch_key_weights(const Problem& p, int2* kstats, int last_rows, void* ws, float* w);
 
 // Paged decode over the streamed KV cache (after host-side validation).
 struct PagedDecode {

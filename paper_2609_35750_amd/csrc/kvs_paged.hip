@@ -147,7 +147,9 @@ struct DecodeArgs {
   float* lse;             // [S][Hq]
   int S, Hq, Hkv, G, max_blocks, BS, num_blocks, units;
   int gran;               // slots a table entry stands for: BS, or 1 where the table lists the slots themselves
-  float* scores;          // [tiles][Hq][kDecTile]: raw scores, for the entries' weights (NULL: not kept)
+  // raw scores, for the entries' weights (NULL: not kept): [tiles][Hkv][4][G][8], place 8 m + i of a tile at [m][.][i],
+  // so that a store instruction of a wave writes G x 32 bytes in a row
+  float* scores;
   const int* tile_base;   // [S + 1]: first tile of each sequence (more than kPlanSeqs sequences)
   int tiles;              // rows of scores
   float scale_log2;       // softmax_scale * log2(e)
@@ -382,13 +384,6 @@ __global__ void __launch_bounds__(1024) paged_plan_kernel(DecodeArgs a) {
 // measured 20% slower on the 64-rollout decode.
 constexpr int kDecRing = 2;
 
-// Wait until at most N vector memory operations of this wave are outstanding (N <= 63).
-template <int N>
-__device__ __forceinline__ void wait_vm_le() {
-  static_assert(N >= 0 && N < 64, "vmcnt is six bits");
-  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
-}
-
 // First row of scores of sequence s: its tiles follow those of the sequences before it.
 __device__ __forceinline__ int tile_base(const DecodeArgs& a, int s, int lane) {
   if (a.tile_base) return a.tile_base[s];
@@ -401,10 +396,12 @@ __device__ __forceinline__ int tile_base(const DecodeArgs& a, int s, int lane) {
   return base;
 }
 
-// A store the compiler does not count (it would not know of the copies in flight either): 16 bytes of this lane.
+// A store the compiler does not count (it would not know of the copies in flight either): 16 bytes of this lane.  The
+// wait states behind it are the ones the hardware asks for before a register of a store of more than 8 bytes is
+// written again; the compiler adds them behind its own stores only.
 __device__ __forceinline__ void store_b128_uncounted(float* dst, float4 v) {
   const f32x4 x = {v.x, v.y, v.z, v.w};
-  asm volatile("global_store_dwordx4 %0, %1, off" ::"v"(dst), "v"(x) : "memory");
+  asm volatile("global_store_dwordx4 %0, %1, off\n\ts_nop 1" ::"v"(dst), "v"(x) : "memory");
 }
 
 // Every global read of the decode loop is an asynchronous copy to LDS, so all
@@ -483,11 +480,11 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
     const int c = slot_index(t);
     if (lane < 32) dma_b32_global(trow + (LIST ? c : c / a.BS), lds_addr(&sTab[t & 1][0]));
   };
-  float* score_row = nullptr;   // of this lane's q-head and tile row, in the first tile of all
+  float* score_row = nullptr;   // of this lane's q-head and tile rows, in the first tile of all
   int score_tile = 0;           // the unit's first tile
   if (SCORES) {
     score_tile = __builtin_amdgcn_readfirstlane(tile_base(a, s, lane) + c_begin / kDecTile);
-    score_row = a.scores + (size_t)(col_ok ? hcol : 0) * kDecTile + 4 * half;
+    score_row = a.scores + (size_t)g * a.G * kDecTile + 8 * (col_ok ? col : 0) + 4 * half;
   }
 
   unsigned valid_q[R] = {};   // rows of tiles n .. n + R - 1 that hold a slot of the split (index 0 = tile n)
@@ -536,12 +533,7 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
           if (!((live_cur >> row) & 1u)) sc[r] = -INFINITY;
         }
       }
-      if (SCORES && col_ok) {   // also of a tile without a live slot, where they are not read: the waits count them
-        float* dst = score_row + (size_t)min(score_tile + n, a.tiles - 1) * a.Hq * kDecTile;
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4)
-          store_b128_uncounted(dst + 8 * q4, make_float4(sc[4 * q4], sc[4 * q4 + 1], sc[4 * q4 + 2], sc[4 * q4 + 3]));
-      }
+      const f32x16 raw = sc;
       if (live_cur != 0u) {
         // V rows of places without a live slot may hold anything (a slot never written, an evicted infinity): their
         // product with P = 0 must not reach the sum.
@@ -582,6 +574,13 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
         for (int d = 0; d < DB; ++d)
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[d][r] = __builtin_fmaf(ot[d][r], beta, acc[d][r]);
+      }
+      // also of a tile without a live slot, where they are not read: the waits count them
+      if (SCORES && col_ok) {
+        float* dst = score_row + (size_t)min(score_tile + n, a.tiles - 1) * a.Hq * kDecTile;
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          store_b128_uncounted(dst + 8 * q4 * a.G, make_float4(raw[4 * q4], raw[4 * q4 + 1], raw[4 * q4 + 2], raw[4 * q4 + 3]));
       }
     }
 #pragma unroll
@@ -939,65 +938,93 @@ struct WindowArgs {
 constexpr int kListThreads = 1024;
 
 // The list keeps the table's order: a workgroup takes a chunk of a sequence's
-// slots and counts the visible ones in front of it by itself (all those loads
-// are independent), so one launch does and nothing waits on another workgroup.
+// slots and counts the visible ones in front of it by itself (those loads are
+// independent of each other), so one launch does and nothing waits on another
+// workgroup.  A lane looks at four places in a row: V4, blocks of a multiple of
+// four slots, has one table entry and one 16-byte load for them.
+template <bool V4>
 __global__ void __launch_bounds__(kListThreads) paged_visible_kernel(WindowArgs a) {
-  constexpr int NW = kListThreads / kWave, STRIPS = 8;
+  constexpr int NW = kListThreads / kWave;
+  typedef int int4u __attribute__((ext_vector_type(4), aligned(4)));   // slot_pos need not be 16-byte aligned
   __shared__ int wsum[NW], wbase[NW];
-  const int s = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n = min(max(a.nblk[s], 0), a.max_blocks) * a.BS;   // slots of the sequence
+  const int s = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, BS = a.BS;
+  const int n = min(max(a.nblk[s], 0), a.max_blocks) * BS;   // slots of the sequence
   const int c0 = (int)min((long long)blockIdx.x * a.chunk, (long long)n);
   const int c1 = (int)min((long long)c0 + a.chunk, (long long)n);
   if (c0 >= n && blockIdx.x > 0) return;
   const int* trow = a.table + (size_t)s * a.max_blocks;
   const int at = a.q_pos[s];
-  // whether the query sees place c of the table, and its slot
-  auto look = [&](int c, int& slot) __attribute__((always_inline)) {
-    const int blk = trow[c / a.BS];
-    const bool ok = (unsigned)blk < (unsigned)a.num_blocks;
-    slot = ok ? blk * a.BS + c % a.BS : 0;
-    const int pos = a.slot_pos[slot];
-    return ok && pos >= 0 && pos <= at && (at - pos < a.window || pos < a.sinks);
+  auto sees = [&](int pos) __attribute__((always_inline)) {
+    return pos >= 0 && pos <= at && (at - pos < a.window || pos < a.sinks);
   };
-  int before = 0;   // visible slots in front of the chunk
+  // the visible ones of the places c .. c + 3 < n, as bits, and their slots; (blk, row): block and row of place c
+  auto look = [&](int c, int blk, int row, int* slot) __attribute__((always_inline)) {
+    unsigned bits = 0;
+    if (V4) {
+      const int entry = c < n ? trow[blk] : -1;
+      if ((unsigned)entry < (unsigned)a.num_blocks) {
+        const int first = entry * BS + row;
+        const int4u p = *reinterpret_cast<const int4u*>(a.slot_pos + first);
+        bits = sees(p.x) | sees(p.y) << 1 | sees(p.z) << 2 | sees(p.w) << 3;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) slot[k] = first + k;
+      }
+    } else {
+      int entry[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        entry[k] = c + k < n ? trow[blk] : -1;
+        slot[k] = (unsigned)entry[k] < (unsigned)a.num_blocks ? entry[k] * BS + row : -1;
+        if (++row == BS) {
+          row = 0;
+          ++blk;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) bits |= (slot[k] >= 0 && sees(a.slot_pos[slot[k]])) << k;
+    }
+    return bits;
+  };
+  constexpr int STEP = 4 * kListThreads;
+  const int dblk = STEP / BS, drow = STEP % BS;
+  auto advance = [&](int& blk, int& row) __attribute__((always_inline)) {
+    blk += dblk;
+    row += drow;
+    if (row >= BS) {
+      row -= BS;
+      ++blk;
+    }
+  };
+  int before = 0, blk = 4 * tid / BS, row = 4 * tid % BS, slot[4];   // visible slots in front of the chunk
 #pragma unroll 8
-  for (int c = tid; c < c0; c += kListThreads) {
-    int slot;
-    before += look(c, slot);
+  for (int c = 4 * tid; c < c0; c += STEP) {   // c0 is a multiple of STEP, or n
+    before += __builtin_popcount(look(c, blk, row, slot));
+    advance(blk, row);
   }
   before = wave_last(wave_scan(before));
   if (lane == 0) wbase[wave] = before;
-  __syncthreads();
   int base = 0;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) base += wbase[w];
   int* out = a.list + (size_t)s * a.cap;
-  // STRIPS strips of 64 slots a wave at a time
-  for (int r0 = c0; r0 < c1; r0 += STRIPS * kListThreads) {
-    const int first = r0 + wave * STRIPS * kWave;
-    unsigned long long hit[STRIPS];
-    int slot[STRIPS], cnt = 0;
-#pragma unroll
-    for (int k = 0; k < STRIPS; ++k) {
-      const int c = first + k * kWave + lane;
-      const bool see = look(min(c, c1 - 1), slot[k]);
-      hit[k] = __ballot(see && c < c1);
-      cnt += __builtin_popcountll(hit[k]);
-    }
-    if (lane == 0) wsum[wave] = cnt;
+  for (int r0 = c0; r0 < c1; r0 += STEP) {
+    const unsigned bits = look(r0 + 4 * tid, blk, row, slot);
+    advance(blk, row);
+    const int cnt = __builtin_popcount(bits), incl = wave_scan(cnt);
+    if (r0 != c0) __syncthreads();   // wsum is read
+    if (lane == kWave - 1) wsum[wave] = incl;
     __syncthreads();
-    int o = base;
+    if (r0 == c0)
+#pragma unroll
+      for (int w = 0; w < NW; ++w) base += wbase[w];
+    int o = base + incl - cnt;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       o += w < wave ? wsum[w] : 0;
       base += wsum[w];
     }
-    __syncthreads();
 #pragma unroll
-    for (int k = 0; k < STRIPS; ++k) {
-      const int i = o + __builtin_popcountll(hit[k] & ((1ull << lane) - 1ull));
-      if (((hit[k] >> lane) & 1ull) && i < a.cap) out[i] = slot[k];   // more than cap only if positions repeat
-      o += __builtin_popcountll(hit[k]);
+    for (int k = 0; k < 4; ++k) {
+      if (((bits >> k) & 1u) && o < a.cap) out[o] = slot[k];   // more than cap only if positions repeat
+      o += (bits >> k) & 1u;
     }
   }
   if (tid == 0 && c1 == n) a.counts[s] = min(base, a.cap);
@@ -1057,10 +1084,12 @@ __global__ void __launch_bounds__(256) paged_weight_kernel(DecodeArgs a, float* 
   for (int t = t0; t < t1; ++t) {
     while (s + 1 < a.S && base[s + 1] <= t) ++s;
     const int ns = slots_of(a, s);
-    const float* row = a.scores + (size_t)t * a.Hq * kDecTile + 4 * quad;
+    // place 4 quad of q-head h: [h / G][quad / 2][h % G][4 (quad % 2)]
+    const float* row = a.scores + (size_t)t * a.Hq * kDecTile + 4 * (quad & 1);
     float x[4] = {0.f, 0.f, 0.f, 0.f};
     for (int h = h0; h < a.Hq; h += 8) {
-      const float4 sc = *reinterpret_cast<const float4*>(row + (size_t)h * kDecTile);
+      const int hg = quick_div(h, a.G);
+      const float4 sc = *reinterpret_cast<const float4*>(row + 8 * (a.G * (4 * hg + (quad >> 1)) + h - hg * a.G));
       const float l2 = a.lse[(size_t)s * a.Hq + h] * 1.4426950408889634f;
       x[0] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc.x, a.scale_log2, -l2));
       x[1] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc.y, a.scale_log2, -l2));
@@ -1118,8 +1147,8 @@ long long paged_ex_units(const PagedDecode& p) {
                       : paged_units(p.S, p.Hkv, p.max_blocks, p.block_size, p.D);
 }
 
-// Slots of a sequence that one workgroup lists, at least; chunks of a sequence at most.
-constexpr int kListChunk = 8192, kListChunks = 16;
+// Slots of a sequence that one workgroup lists, at least (what its threads look at together); chunks at most.
+constexpr int kListChunk = 4 * kListThreads, kListChunks = 16;
 
 template <bool LIST>
 static hipError_t launch_ex(const PagedDecode& p, const ExSpace& x, DecodeArgs a, int* base, float* scores) {
@@ -1149,11 +1178,13 @@ hipError_t launch_paged_decode_ex(const PagedDecode& p) {
     return launch_ex<false>(p, x, decode_args(p, p.block_table, p.seq_blocks, p.max_blocks, p.block_size, units, x.units),
                             base, scores);
   const long long width = (long long)p.max_blocks * p.block_size;
-  const int chunk = (int)std::max<long long>(kListChunk, (width + kListChunks - 1) / kListChunks);
+  const long long rounds = (width + (long long)kListChunk * kListChunks - 1) / ((long long)kListChunk * kListChunks);
+  const int chunk = (int)std::min(rounds * kListChunk, (long long)INT_MAX / kListChunk * kListChunk);
   const WindowArgs v{p.slot_pos, p.block_table, p.seq_blocks, p.q_pos, list, counts, p.max_blocks, p.block_size,
                      p.num_blocks, x.cap, p.window, p.sinks, chunk};
   const dim3 grid((unsigned)((width + chunk - 1) / chunk), (unsigned)p.S);
-  hipLaunchKernelGGL(paged_visible_kernel, grid, dim3(kListThreads), 0, p.stream, v);
+  hipLaunchKernelGGL(p.block_size % 4 == 0 ? paged_visible_kernel<true> : paged_visible_kernel<false>, grid,
+                     dim3(kListThreads), 0, p.stream, v);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   return launch_ex<true>(p, x, decode_args(p, list, counts, x.cap, 1, units, x.units), base, scores);
