@@ -412,12 +412,15 @@ kvs_status_t kvs_paged_append_weighted_host(const void* K_new, const void* V_new
  * highest weight, equal weights leave in the table's order.  slot_pos of the
  * evicted slots becomes -1; their positions go to positions[s][0..counts[s])
  * (device int32 [num_seqs][max_out], in the table's order, the rest -1), for
- * kvs_bm_evict.  Tables are clamped as in the decode; max_blocks * block_size
- * is at most 2^30. */
+ * kvs_bm_evict.  Tables are clamped as in the decode; num_seqs is at most 65535,
+ * max_blocks * block_size at most 2^30, and the product of all three below 2^32.
+ * The workspace query may give 0 (workspace NULL then). */
+size_t kvs_paged_evict_lowest_workspace(int num_seqs, int max_blocks, int block_size);
 kvs_status_t kvs_paged_evict_lowest(const float* slot_weight, int32_t* slot_pos, const int32_t* block_table,
                                     const int32_t* seq_blocks, const int32_t* keep, int32_t* positions,
                                     int32_t* counts, int num_seqs, int num_blocks, int block_size, int max_blocks,
-                                    int sinks, int recent, int max_out, void* stream);
+                                    int sinks, int recent, int max_out, void* workspace, size_t workspace_bytes,
+                                    void* stream);
 
 /* ---- decode attention over the live cache
  * One query token per sequence: Q, O bf16 [num_seqs][Hq][D], LSE fp32

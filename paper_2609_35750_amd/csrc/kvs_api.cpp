@@ -903,10 +903,15 @@ kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void*
   return e == hipSuccess ? KVS_OK : hip_fail(e, "paged decode launch");
 }
 
+size_t kvs_paged_evict_lowest_workspace(int num_seqs, int max_blocks, int block_size) {
+  if (num_seqs < 1 || max_blocks < 1 || block_size < 1) return 0;
+  return kvs::paged_evict_ws_bytes(num_seqs, max_blocks, block_size);
+}
+
 kvs_status_t kvs_paged_evict_lowest(const float* slot_weight, int32_t* slot_pos, const int32_t* block_table,
                                     const int32_t* seq_blocks, const int32_t* keep, int32_t* positions, int32_t* counts,
                                     int num_seqs, int num_blocks, int block_size, int max_blocks, int sinks, int recent,
-                                    int max_out, void* stream) {
+                                    int max_out, void* workspace, size_t workspace_bytes, void* stream) {
   t_err.clear();
   if (kvs_status_t st = check_cache_dims(num_blocks, block_size)) return st;
   if (num_seqs < 1 || max_blocks < 1 || max_out < 1)
@@ -914,11 +919,17 @@ kvs_status_t kvs_paged_evict_lowest(const float* slot_weight, int32_t* slot_pos,
   if (sinks < 0 || recent < 0) return fail(KVS_ERR_SHAPE, "sinks and recent must be >= 0 (got %d, %d)", sinks, recent);
   if ((long long)max_blocks * block_size > kMaxPlaces)
     return fail(KVS_ERR_UNSUPPORTED, "max_blocks * block_size above %d", kMaxPlaces);
-  if (num_seqs > (1 << 21)) return fail(KVS_ERR_UNSUPPORTED, "more than 2097152 sequences");
+  if (num_seqs > 65535) return fail(KVS_ERR_UNSUPPORTED, "more than 65535 sequences");
+  if (((long long)max_blocks * block_size + 255) * num_seqs > 0xffffffffll)
+    return fail(KVS_ERR_UNSUPPORTED, "num_seqs * max_blocks * block_size above 2^32");
   if (!slot_weight || !slot_pos || !block_table || !seq_blocks || !keep || !positions || !counts)
     return fail(KVS_ERR_NULL, "NULL argument");
+  if (kvs_status_t st = check_ws(workspace, workspace_bytes,
+                                 kvs_paged_evict_lowest_workspace(num_seqs, max_blocks, block_size)))
+    return st;
   const kvs::PagedEvictLowest p{slot_weight, slot_pos, block_table, seq_blocks, keep, positions, counts, num_seqs,
-                                num_blocks, block_size, max_blocks, sinks, recent, max_out, (hipStream_t)stream};
+                                num_blocks, block_size, max_blocks, sinks, recent, max_out, (int2*)workspace,
+                                (hipStream_t)stream};
   hipError_t e = kvs::launch_paged_evict_lowest(p);
   return e == hipSuccess ? KVS_OK : hip_fail(e, "paged evict launch");
 }

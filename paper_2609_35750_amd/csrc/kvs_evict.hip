@@ -11,6 +11,12 @@
 // integers are equal steps of a weight's exponent and leading bits, so weights
 // that span many powers of two spread over the bins, and the counts (atomics on
 // integers in LDS) rarely meet.  Bound by latency: 8 bytes a slot are read.
+//
+// One CU asks for one line of memory a clock or two, so where a table's slots
+// lie apart (blocks of fewer than four), reading them is what costs: 64
+// sequences of 2,000 to 16,000 single slots 54 us.  There, and where a
+// sequence's places do not fit the workgroup's registers, a kernel on all CUs
+// first brings positions and weights into the table's order (KWGATHER).
 #include "kvs_device.h"
 #include "kvs_launch.h"
 
@@ -21,12 +27,13 @@ namespace kvs {
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave, kEvictBins = 1024;
 
-// Integers that order like the floats; -0 like +0, and NaN above everything.
+// Integers that order like the floats; -0 like +0, and NaN above everything but kStays.
 __device__ __forceinline__ unsigned weight_key(float w) {
-  if (w != w) return 0xffffffffu;
+  if (w != w) return 0xfffffffeu;
   const unsigned b = w == 0.f ? 0u : __float_as_uint(w);
   return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
 }
+constexpr unsigned kStays = 0xffffffffu;   // no entry, or one that is not taken: outside every range of keys
 
 // Places of the table a lane looks at, 64 apart: one division, then additions.
 struct Places {
@@ -46,13 +53,29 @@ struct Places {
   }
 };
 
+// Position and weight's key of every place of the tables, in their order: (-1, 0) where there is no slot.
+constexpr int kGatherThreads = 256;
+__global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(PagedEvictLowest a) {
+  const int s = blockIdx.y, c = blockIdx.x * kGatherThreads + threadIdx.x;
+  const int n = min(max(a.seq_blocks[s], 0), a.max_blocks) * a.block_size;
+  if (c >= n) return;
+  const int entry = a.block_table[(size_t)s * a.max_blocks + c / a.block_size];
+  int2 v = make_int2(-1, 0);
+  if ((unsigned)entry < (unsigned)a.num_blocks) {
+    const int slot = entry * a.block_size + c % a.block_size;
+    v = make_int2(a.slot_pos[slot], (int)weight_key(a.slot_weight[slot]));
+  }
+  a.gathered[(size_t)s * a.max_blocks * a.block_size + c] = v;
+}
+
 // Entries a thread keeps in registers: KEEP strips of 64 a wave; 0: read again for every count (longer tables).
-template <int KEEP>
+// GATHERED: from what paged_gather_kernel wrote.
+template <int KEEP, bool GATHERED>
 __global__ void __launch_bounds__(kEvictThreads) paged_evict_lowest_kernel(PagedEvictLowest a) {
   constexpr int N = KEEP ? KEEP : 1;
   __shared__ int hist[kEvictBins];
   __shared__ int red[2][4][kEvictWaves];   // by turns, so that one barrier stands between two exchanges
-  __shared__ int pick[2][2];               // bin of the n-th, entries below it
+  __shared__ int pick[2][3];               // bin of the n-th, entries below it, in it
   const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = min(max(a.seq_blocks[s], 0), a.max_blocks) * a.block_size;   // slots of the sequence
   const int* trow = a.block_table + (size_t)s * a.max_blocks;
@@ -61,13 +84,26 @@ __global__ void __launch_bounds__(kEvictThreads) paged_evict_lowest_kernel(Paged
 
   // wave w has the places [w strips 64, (w + 1) strips 64) of the table, in strips of 64
   const int strips = (n + kEvictThreads - 1) / kEvictThreads, c0 = wave * strips * kWave + lane;
-  // an entry: its position (-1: none), the key of its weight, its slot
+  const int2* gathered = GATHERED ? a.gathered + (size_t)s * a.max_blocks * a.block_size : nullptr;
+  // an entry: its position (-1: none), the key of its weight, its slot (GATHERED: its place)
   int pos_r[N], slot_r[N];
   unsigned key_r[N];
   auto slot_of = [&](int entry, const Places& p) __attribute__((always_inline)) {
     return p.c < n && (unsigned)entry < (unsigned)a.num_blocks ? entry * a.block_size + p.row : -1;
   };
-  if (KEEP) {
+  if (KEEP && GATHERED) {
+    int2 v[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      slot_r[k] = c0 + k * kWave;
+      v[k] = k < strips && slot_r[k] < n ? gathered[slot_r[k]] : make_int2(-1, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      pos_r[k] = v[k].x;
+      key_r[k] = (unsigned)v[k].y;
+    }
+  } else if (KEEP) {
     Places p(c0, a.block_size);
 #pragma unroll
     for (int k = 0; k < N; ++k, p.next()) slot_r[k] = k < strips && p.c < n ? trow[p.blk] : -1;
@@ -90,36 +126,25 @@ __global__ void __launch_bounds__(kEvictThreads) paged_evict_lowest_kernel(Paged
       for (int k = 0; k < N; ++k)
         if (k < strips) f(pos_r[k], key_r[k], slot_r[k]);
     } else {
-      Places p(c0, a.block_size);
 #pragma unroll 8
-      for (int k = 0; k < strips; ++k, p.next()) {
-        const int slot = slot_of(p.c < n ? trow[p.blk] : -1, p);
-        f(slot >= 0 ? a.slot_pos[slot] : -1, slot >= 0 ? weight_key(a.slot_weight[slot]) : 0u, slot);
+      for (int k = 0; k < strips; ++k) {
+        const int c = c0 + k * kWave;
+        const int2 v = c < n ? gathered[c] : make_int2(-1, 0);
+        f(v.x, (unsigned)v.y, c);
       }
     }
   };
 
-  // live entries, the newest position, the range of the keys (of all but the sinks: the newest are not known yet)
+  // live entries, the newest position
   int live = 0, last = -1;
-  unsigned lo = 0xffffffffu, hi = 0u;
-  each([&](int pos, unsigned key, int) __attribute__((always_inline)) {
+  each([&](int pos, unsigned, int) __attribute__((always_inline)) {
     live += __builtin_popcountll(__ballot(pos >= 0));
     last = max(last, pos);
-    const bool f = pos >= a.sinks && pos >= 0;
-    lo = f ? min(lo, key) : lo;
-    hi = f ? max(hi, key) : hi;
   });
   last = wave_max(last);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    lo = min(lo, (unsigned)__shfl_xor((int)lo, off));
-    hi = max(hi, (unsigned)__shfl_xor((int)hi, off));
-  }
   if (lane == 0) {
     red[0][0][wave] = live;
     red[0][1][wave] = last;
-    red[0][2][wave] = (int)lo;
-    red[0][3][wave] = (int)hi;
   }
   hist[tid] = 0;
   __syncthreads();
@@ -128,46 +153,78 @@ __global__ void __launch_bounds__(kEvictThreads) paged_evict_lowest_kernel(Paged
   for (int w = 0; w < kEvictWaves; ++w) {
     live += red[0][0][w];
     last = max(last, red[0][1][w]);
-    lo = min(lo, (unsigned)red[0][2][w]);
-    hi = max(hi, (unsigned)red[0][3][w]);
   }
-  const int newest = last - a.recent;   // positions above it stay (last >= -1, recent >= 0)
-  auto is_free = [&](int pos) { return pos >= 0 && pos >= a.sinks && pos <= newest; };
+  // positions in [sinks, newest] may leave (last >= -1, recent >= 0; none do if newest < sinks)
+  const int newest = last - a.recent;
+  const unsigned span = newest >= a.sinks ? (unsigned)(newest - a.sinks) : 0u;
+  const bool none = newest < a.sinks;
+  auto key_of = [&](int pos, unsigned key) __attribute__((always_inline)) {
+    return pos >= 0 && (unsigned)(pos - a.sinks) <= span && !none ? key : kStays;
+  };
+  if (KEEP) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) key_r[k] = key_of(pos_r[k], key_r[k]);
+  }
+  // f(position, key or kStays, slot)
+  auto each_key = [&](auto f) __attribute__((always_inline)) {
+    each([&](int pos, unsigned key, int slot) __attribute__((always_inline)) { f(pos, KEEP ? key : key_of(pos, key), slot); });
+  };
 
-  // Narrow [lo, hi] to the key of the go-th lowest: `rank` of the free entries in the range leave (1 <= rank <= inside,
-  // how many those are), and all below it.  The first count also says how many free entries there are.
-  int go = min(max(live - keep, 0), a.max_out), rank = go, inside = INT_MAX;   // entries that leave
-  bool first = true;
-  int turn = 1;
-  while (rank > 0 && rank < inside && (first || lo < hi)) {
-    const unsigned width = hi >= lo ? hi - lo : 0u;
-    const int shift = max(22 - (width ? (int)__builtin_clz(width) : 32), 0);   // width >> shift < 1,024
-    each([&](int pos, unsigned key, int) __attribute__((always_inline)) {
-      if (is_free(pos) && key >= lo && key <= hi) atomicAdd(&hist[(key - lo) >> shift], 1);
+  // Narrow [lo, hi] to the key of the go-th lowest: `rank` of the entries in the range leave (1 <= rank <= inside, how
+  // many those are), and all below it.  Every turn first finds the range of the keys that are there (one value,
+  // however many entries, ends the search); the first one also says how many entries may leave.
+  int go = min(max(live - keep, 0), a.max_out), rank = go, inside = INT_MAX, turn = 1;   // go: entries that leave
+  unsigned lo = 0u, hi = 0xfffffffeu;
+  while (rank > 0 && rank < inside) {
+    unsigned mn = kStays, mx = 0u;
+    int cnt = 0;
+    each_key([&](int, unsigned key, int) __attribute__((always_inline)) {
+      const bool f = key - lo <= hi - lo;
+      mn = f ? min(mn, key) : mn;
+      mx = f ? max(mx, key) : mx;
+      if (inside == INT_MAX) cnt += __builtin_popcountll(__ballot(f));
     });
+    mn = (unsigned)wave_min((int)(mn ^ 0x80000000u)) ^ 0x80000000u;
+    mx = (unsigned)wave_max((int)(mx ^ 0x80000000u)) ^ 0x80000000u;
+    if (lane == 0) {
+      red[turn][1][wave] = cnt;
+      red[turn][2][wave] = (int)mn;
+      red[turn][3][wave] = (int)mx;
+    }
     __syncthreads();
-    const int cnt = hist[tid], incl = wave_scan(cnt);
-    if (lane == kWave - 1) red[turn][0][wave] = incl;
-    __syncthreads();
-    int below = incl - cnt, all = 0;
+    cnt = 0;
 #pragma unroll
     for (int w = 0; w < kEvictWaves; ++w) {
-      const int x = red[turn][0][w];
-      below += w < wave ? x : 0;
-      all += x;
+      cnt += red[turn][1][w];
+      mn = min(mn, (unsigned)red[turn][2][w]);
+      mx = max(mx, (unsigned)red[turn][3][w]);
     }
-    if (first) rank = go = min(go, all);
-    first = false;
-    if (below < rank && rank <= below + cnt) {   // one thread, if any entry leaves
+    if (inside == INT_MAX) rank = go = min(go, inside = cnt);
+    lo = mn;
+    hi = mx;
+    if (rank == 0 || rank == inside || lo == hi) break;
+    const unsigned width = hi - lo;
+    const int shift = max(22 - (int)__builtin_clz(width), 0);   // width >> shift < 1,024
+    each_key([&](int, unsigned key, int) __attribute__((always_inline)) {
+      const unsigned d = key - lo;
+      if (d <= width) atomicAdd(&hist[d >> shift], 1);
+    });
+    __syncthreads();
+    const int n_bin = hist[tid], incl = wave_scan(n_bin);
+    if (lane == kWave - 1) red[turn][0][wave] = incl;
+    hist[tid] = 0;
+    __syncthreads();
+    int below = incl - n_bin;
+#pragma unroll
+    for (int w = 0; w < kEvictWaves; ++w) below += w < wave ? red[turn][0][w] : 0;
+    if (below < rank && rank <= below + n_bin) {   // one thread
       pick[turn][0] = tid;
       pick[turn][1] = below;
+      pick[turn][2] = n_bin;
     }
-    hist[tid] = 0;
-    if (below < rank && rank <= below + cnt) red[turn][1][0] = cnt;
     __syncthreads();
-    if (rank == 0) break;
     rank -= pick[turn][1];
-    inside = red[turn][1][0];
+    inside = pick[turn][2];
     lo += (unsigned)pick[turn][0] << shift;
     hi = lo + min(hi - lo, (1u << shift) - 1u);
     turn ^= 1;
@@ -179,11 +236,12 @@ __global__ void __launch_bounds__(kEvictThreads) paged_evict_lowest_kernel(Paged
   // All entries below lo leave, and of those in [lo, hi] the first `rank` in the table's order (all of them, or
   // all equal).
   int nbelow = 0, nin = 0;
-  each([&](int pos, unsigned key, int) __attribute__((always_inline)) {
-    const bool f = is_free(pos);
-    nbelow += __builtin_popcountll(__ballot(f && key < lo));
-    nin += __builtin_popcountll(__ballot(f && key >= lo && key <= hi));
+  const unsigned width = hi - lo;
+  each_key([&](int, unsigned key, int) __attribute__((always_inline)) {
+    nbelow += __builtin_popcountll(__ballot(key < lo));
+    nin += __builtin_popcountll(__ballot(key - lo <= width));
   });
+  turn ^= 1;   // of red: the other one's values may still be read
   if (lane == 0) {
     red[turn][2][wave] = nbelow;
     red[turn][3][wave] = nin;
@@ -197,31 +255,59 @@ __global__ void __launch_bounds__(kEvictThreads) paged_evict_lowest_kernel(Paged
   }
   at += min(in, rank);
   const unsigned long long before = (1ull << lane) - 1ull;
-  each([&](int pos, unsigned key, int slot) __attribute__((always_inline)) {
-    const bool f = is_free(pos), in_range = f && key >= lo && key <= hi;
+  unsigned gone_r = 0;   // strips whose entry leaves
+  int k_at = 0;
+  each_key([&](int pos, unsigned key, int slot) __attribute__((always_inline)) {
+    const bool in_range = key - lo <= width;
     const unsigned long long range = __ballot(in_range);
-    const bool gone = (f && key < lo) || (in_range && in + __builtin_popcountll(range & before) < rank);
+    const bool gone = key < lo || (in_range && in + __builtin_popcountll(range & before) < rank);
     const unsigned long long leave = __ballot(gone);
     if (gone) {
       out[at + __builtin_popcountll(leave & before)] = pos;
-      a.slot_pos[slot] = -1;
+      if (!KEEP) a.slot_pos[trow[slot / a.block_size] * a.block_size + slot % a.block_size] = -1;
     }
+    if (KEEP) gone_r |= (unsigned)gone << k_at++;
     in += __builtin_popcountll(range);
     at += __builtin_popcountll(leave);
   });
+  if (KEEP && GATHERED) {   // all table entries at once: one latency, not one a strip
+    int blk[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) blk[k] = (gone_r >> k) & 1u ? trow[slot_r[k] / a.block_size] : 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) slot_r[k] = blk[k] * a.block_size + slot_r[k] % a.block_size;
+  }
+  if (KEEP) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if ((gone_r >> k) & 1u) a.slot_pos[slot_r[k]] = -1;
+  }
 }
 
-template __global__ void paged_evict_lowest_kernel<4>(PagedEvictLowest);
-template __global__ void paged_evict_lowest_kernel<16>(PagedEvictLowest);
-template __global__ void paged_evict_lowest_kernel<0>(PagedEvictLowest);
+template __global__ void paged_evict_lowest_kernel<4, false>(PagedEvictLowest);
+template __global__ void paged_evict_lowest_kernel<16, false>(PagedEvictLowest);
+template __global__ void paged_evict_lowest_kernel<16, true>(PagedEvictLowest);
+template __global__ void paged_evict_lowest_kernel<0, true>(PagedEvictLowest);
+
+static bool gathers(long long width, int block_size) { return width > 16 * kEvictThreads || (block_size < 4 && width > kEvictThreads); }
+
+size_t paged_evict_ws_bytes(int S, int max_blocks, int block_size) {
+  const long long width = (long long)max_blocks * block_size;
+  return gathers(width, block_size) ? ((size_t)S * width * sizeof(int2) + 255) & ~(size_t)255 : 0;
+}
 
 hipError_t launch_paged_evict_lowest(const PagedEvictLowest& p) {
   const long long width = (long long)p.max_blocks * p.block_size;
-  const auto kernel = width <= 4 * kEvictThreads    ? paged_evict_lowest_kernel<4>
-                      : width <= 16 * kEvictThreads ? paged_evict_lowest_kernel<16>
-                                                    : paged_evict_lowest_kernel<0>;
   prof_begin("paged_evict_lowest", p.stream);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)p.S), dim3(kEvictThreads), 0, p.stream, p);
+  if (gathers(width, p.block_size)) {
+    const dim3 grid((unsigned)((width + kGatherThreads - 1) / kGatherThreads), (unsigned)p.S);
+    hipLaunchKernelGGL(paged_gather_kernel, grid, dim3(kGatherThreads), 0, p.stream, p);
+    hipLaunchKernelGGL((width <= 16 * kEvictThreads ? paged_evict_lowest_kernel<16, true> : paged_evict_lowest_kernel<0, true>),
+                       dim3((unsigned)p.S), dim3(kEvictThreads), 0, p.stream, p);
+  } else {
+    hipLaunchKernelGGL((width <= 4 * kEvictThreads ? paged_evict_lowest_kernel<4, false> : paged_evict_lowest_kernel<16, false>),
+                       dim3((unsigned)p.S), dim3(kEvictThreads), 0, p.stream, p);
+  }
   prof_end(p.stream);
   return hipGetLastError();
 }

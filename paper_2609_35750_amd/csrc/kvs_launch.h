@@ -169,8 +169,10 @@ struct PagedEvictLowest {
   int32_t* positions;    // [S][max_out]
   int32_t* counts;       // [S]
   int S, num_blocks, block_size, max_blocks, sinks, recent, max_out;
+  int2* gathered;        // workspace, where paged_evict_ws_bytes asks for some
   hipStream_t stream;
 };
+size_t paged_evict_ws_bytes(int S, int max_blocks, int block_size);
 hipError_t launch_paged_evict_lowest(const PagedEvictLowest& p);
 
 // Per-kernel event bracketing (benchmark timing).

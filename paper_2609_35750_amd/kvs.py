@@ -10,6 +10,7 @@ Importing this module fails if ``libkvs.so`` has not been built.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -72,7 +73,8 @@ SIGNATURES = {
     "kvs_paged_evict_host": (_I, [_P, _I, _P, _I, _I, _P]),
     "kvs_paged_append_weighted": (_I, [_P, _P, _P, _P, _P, _I, _P, _P, _P, _P, _I, _I, _I, _I, _P]),
     "kvs_paged_append_weighted_host": (_I, [_P, _P, _P, _P, _P, _I, _P, _P, _P, _P, _I, _I, _I, _I, _P]),
-    "kvs_paged_evict_lowest": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _P]),
+    "kvs_paged_evict_lowest_workspace": (_Z, [_I, _I, _I]),
+    "kvs_paged_evict_lowest": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _P, _Z, _P]),
     "kvs_paged_decode_ex_workspace": (_Z, [_I, _I, _I, _I, _I, _I, _I, _I, _I, _I]),
     "kvs_paged_decode_ex": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _F, _I, _I,
                                  _P, _Z, _P]),
@@ -250,6 +252,14 @@ def kvs_evict_attn_bwd(do, q, k, v, o, lse, evict_at, softmax_scale=None, cu_seq
     return dq, dk, dv
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _on(t: torch.Tensor):
+    """Context in which t's device is the current one (nothing to do, the usual case, if it is)."""
+    return _HERE if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
 def _i31(x) -> int:
     """A count as a C int: values beyond its range count as the largest (or as negative)."""
     return max(-1, min(int(x), 0x7FFFFFFF))
@@ -310,7 +320,7 @@ def kvs_window_attn_fwd(q, k, v, window: int, sinks: int = 0, evict_at=None, sof
     _like(out, q, "O")
     nws = lib.kvs_window_attn_fwd_workspace(B, n, T, Hq, Hkv, D)
     ws = _workspace(nws, q.device)
-    with torch.cuda.device(q.device):
+    with _on(q):
         st = lib.kvs_window_attn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(evict_at), _ptr(cu_seqlens), _ptr(out), _ptr(lse),
                                      B, n, T, Hq, Hkv, D, scale, _i31(window), _i31(sinks), _ptr(ws), nws, _stream(q))
     _check("kvs_window_attn_fwd", st)
@@ -333,7 +343,7 @@ def kvs_window_attn_bwd(do, q, k, v, o, lse, window: int, sinks: int = 0, evict_
         _like(t, ref, name)
     nws = lib.kvs_window_attn_bwd_workspace(B, n, T, Hq, Hkv, D)
     ws = _workspace(nws, q.device)
-    with torch.cuda.device(q.device):
+    with _on(q):
         st = lib.kvs_window_attn_bwd(_ptr(do), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(evict_at),
                                      _ptr(cu_seqlens), _ptr(dq), _ptr(dk), _ptr(dv), B, n, T, Hq, Hkv, D, scale,
                                      _i31(window), _i31(sinks), _ptr(ws), nws, _stream(q))
@@ -363,7 +373,7 @@ def kvs_key_weights(q, k, lse, evict_at=None, softmax_scale=None, cu_seqlens=Non
     rows = 0 if last_rows is None else _i31(last_rows)
     nws = lib.kvs_key_weights_workspace(B, n, T, Hq, Hkv, D, rows)
     ws = _workspace(nws, q.device)
-    with torch.cuda.device(q.device):
+    with _on(q):
         st = lib.kvs_key_weights(_ptr(q), _ptr(k), _ptr(lse), _ptr(evict_at), _ptr(cu_seqlens), _ptr(w), B, n, T, Hq,
                                  Hkv, D, scale, _i31(window or 0), _i31(sinks), rows, _ptr(ws), nws, _stream(q))
     _check("kvs_key_weights", st)

@@ -17,7 +17,7 @@ from typing import Optional, Sequence, Tuple
 import numpy as np
 import torch
 
-from .kvs import KVS_ERR_UNSUPPORTED, KvsError, _check, _i31, _ptr, _stream, _workspace, lib
+from .kvs import KVS_ERR_UNSUPPORTED, KvsError, _check, _i31, _on, _ptr, _stream, _workspace, lib
 
 
 def _i32(a) -> np.ndarray:
@@ -143,7 +143,7 @@ def kvs_paged_append_weighted(k_new, v_new, w_new, positions, slots, k_cache, v_
         raise ValueError("w_new must be float32 [n]")
     _int32(positions, slots, slot_pos)
     _same_device(k_cache, k_new, v_new, w_new, positions, slots, v_cache, slot_pos, slot_weight)
-    with torch.cuda.device(k_cache.device):
+    with _on(k_cache):
         _check("kvs_paged_append_weighted", lib.kvs_paged_append_weighted(
             _ptr(k_new), _ptr(v_new), _ptr(w_new), _ptr(positions), _ptr(slots), n, _ptr(k_cache), _ptr(v_cache),
             _ptr(slot_pos), _ptr(slot_weight), nb, block_size, Hkv, D, _stream(k_cache)))
@@ -193,7 +193,7 @@ def kvs_paged_decode_ex(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, 
     win, sinks = _i31(window or 0), _i31(sinks)
     need = lib.kvs_paged_decode_ex_workspace(S, Hq, Hkv, D, nb, max_blocks, bs, win, sinks, slot_weight is not None)
     ws = _workspace(need, q.device)
-    with torch.cuda.device(q.device):
+    with _on(q):
         _check("kvs_paged_decode_ex", lib.kvs_paged_decode_ex(
             _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(slot_pos), _ptr(slot_weight), _ptr(block_table),
             _ptr(seq_blocks), _ptr(q_pos), _ptr(o), _ptr(lse), S, Hq, Hkv, D, nb, bs, max_blocks, scale, win, sinks,
@@ -221,10 +221,12 @@ def kvs_paged_evict_lowest(slot_weight, slot_pos, block_table, seq_blocks, keep,
     most = max_blocks * block_size if max_out is None else int(max_out)
     pos = torch.empty((S, max(most, 0)), dtype=torch.int32, device=slot_pos.device)
     counts = torch.empty(S, dtype=torch.int32, device=slot_pos.device)
-    with torch.cuda.device(slot_pos.device):
+    need = lib.kvs_paged_evict_lowest_workspace(S, max_blocks, block_size)
+    ws = _workspace(need, slot_pos.device) if need else None
+    with _on(slot_pos):
         _check("kvs_paged_evict_lowest", lib.kvs_paged_evict_lowest(
             _ptr(slot_weight), _ptr(slot_pos), _ptr(block_table), _ptr(seq_blocks), _ptr(keep), _ptr(pos), _ptr(counts),
-            S, slot_pos.numel() // block_size, block_size, max_blocks, _i31(sinks), _i31(recent), most,
+            S, slot_pos.numel() // block_size, block_size, max_blocks, _i31(sinks), _i31(recent), most, _ptr(ws), need,
             _stream(slot_pos)))
     return pos, counts
 
