@@ -329,6 +329,12 @@ __device__ __forceinline__ void store_rows(const f32x16* acc, float sc, uint16_t
   }
 }
 
+// Whether the n keys from j0 on have all left the window of the queries from i0 on (a finer look than the 64-key tiles'
+// statistics allow: a window's edge costs a row block half a tile less).
+__device__ __forceinline__ bool behind_window(const RowArgs& a, int i0, int j0, int n) {
+  return j0 >= a.sinks && j0 + n - 1 + a.window <= i0;
+}
+
 // ---------------------------------------------------------------- forward
 // K/V are staged in sub-tiles of BN keys (D = 128: 32, so that a workgroup
 // needs 37 KB of LDS and three workgroups, three waves per SIMD, share a CU;
@@ -411,7 +417,7 @@ fwd_kernel(RowArgs a) {
   // The products and the softmax of the sub-tile of BN keys from j0 on.
   auto compute = [&](const uint16_t* cK, const uint16_t* cV, const int* cE, int j0) __attribute__((always_inline)) {
     const int cls = adjust_class(tile_class(rt.i0w, rt.i0w + 32, j0, j0 + BN, tr.L, kst.x, kst.y), a.flags);
-    if (cls != kEmpty) {
+    if (cls != kEmpty && !(WIN && behind_window(a, rt.i0w, j0, BN))) {
       f32x16 s[NKB];
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb) {
@@ -645,6 +651,7 @@ __global__ void __launch_bounds__(512) dq_kernel(RowArgs a) {
     if (cls != kEmpty) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
+        if (WIN && (j0 + 32 * kb > rt.i0w + 31 || behind_window(a, rt.i0w, j0 + 32 * kb, 32))) continue;
         f32x16 s = scores_t<D, true>(cK, 32 * kb, qreg, rl);
         if (cls == kPartial) mask_t(s, cE, kb, j0, i, tr.L, half);
         // dP - Delta: the product starts at -Delta
