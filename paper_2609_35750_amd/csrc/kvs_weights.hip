@@ -263,7 +263,7 @@ static size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // How the rows are cut: about kWeightItems items (half of them above the diagonal, empty), of whole steps; where those
 // of one chunk do not start a workgroup on every CU, by q-heads too (24 traces of 100 to 1,500 tokens, the last 64
-// queries, 16/2 heads: KWNHP).  16k trace: 8,192 items 567 us in all, 16,384 575, 32,768 603.
+// queries, 16/2 heads: 26.0 us whole groups, 18.5 two heads a part, 22.1 one).  16k trace: 8,192 items 567 us in all, 16,384 575, 32,768 603.
 struct WeightCut {
   int nkb, nchunk, chunk_rows, nhp, part_heads;
 };
