@@ -839,7 +839,6 @@ constexpr int kMaxPlaces = 1 << 30;   // slots of a sequence's table where kerne
 // The sizes of such a call; workspace and launch sizes follow from them alone.
 static kvs::PagedDecode decode_ex_sizes(int S, int Hq, int Hkv, int D, int num_blocks, int max_blocks, int block_size,
                                         int window, int sinks, bool weights) {
-  static float some;   // stands for the weights: only whether there are any counts here
   kvs::PagedDecode p{};
   p.S = S;
   p.Hq = Hq;
@@ -850,7 +849,7 @@ static kvs::PagedDecode decode_ex_sizes(int S, int Hq, int Hkv, int D, int num_b
   p.block_size = block_size;
   p.window = window;
   p.sinks = window > 0 ? sinks : 0;
-  p.slot_weight = weights ? &some : nullptr;
+  p.weights = weights;
   return p;
 }
 

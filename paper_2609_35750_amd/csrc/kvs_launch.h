@@ -89,7 +89,8 @@ struct PagedDecode {
   void* o;                  // [S][Hq][D] bf16
   float* lse;               // [S][Hq]
   const int32_t* q_pos;     // [S] position of each query (window > 0)
-  float* slot_weight;       // [num_blocks * block_size]: added to; NULL: no weights
+  bool weights;             // whether slot_weight [num_blocks * block_size] is added to
+  float* slot_weight;
   int window, sinks;        // window 0: none
   int S, Hq, Hkv, D, max_blocks, block_size, num_blocks;
   float scale;

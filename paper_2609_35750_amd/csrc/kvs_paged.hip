@@ -1137,7 +1137,7 @@ static ExSpace ex_space(const PagedDecode& p) {
     x.counts = round256((size_t)p.S * sizeof(int));
     each = x.cap;
   }
-  if (p.slot_weight) {
+  if (p.weights) {
     x.tiles = std::min(p.S * ((each + kDecTile - 1) / kDecTile),
                        (long long)p.num_blocks * p.block_size / kDecTile + p.S);
     x.base = p.S > kPlanSeqs ? round256((size_t)(p.S + 1) * sizeof(int)) : 0;
@@ -1158,7 +1158,7 @@ constexpr int kListChunk = 4 * kListThreads, kListChunks = 16;
 
 template <bool LIST>
 static hipError_t launch_ex(const PagedDecode& p, const ExSpace& x, DecodeArgs a, int* base, float* scores) {
-  if (!p.slot_weight) return launch_decode<LIST, false>(p, a);
+  if (!p.weights) return launch_decode<LIST, false>(p, a);
   a.scores = scores;
   a.tiles = (int)x.tiles;
   if (p.S > kPlanSeqs) {
