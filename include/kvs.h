@@ -213,6 +213,9 @@ kvs_status_t kvs_evict_attn_fwd_noalloc(const void* Q, const void* K, const void
  * flags: cu_seqlens NULL means B fixed-length traces of max_seqlen tokens.
  * Workspaces come from the queries below; the backward's may be smaller in
  * the way kvs_evict_attn_bwd's may.  Every query sees itself, so no row is empty.
+ * Hidden places take part in the products of a tile as factors 0: an infinity
+ * or NaN in V (in the backward, in any input) may reach outputs of the same
+ * tile that do not see it.
  */
 size_t kvs_window_attn_fwd_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D);
 kvs_status_t kvs_window_attn_fwd(const void* Q, const void* K, const void* V,
@@ -241,7 +244,11 @@ kvs_status_t kvs_window_attn_bwd(const void* dO, const void* Q, const void* K, c
  * (sinks is then without effect); evict_at NULL: nothing is evicted.  A key no
  * counted query sees gets 0; tokens behind the last trace keep what W held.
  * These are the weights a cache starts from (kvs_paged_append_weighted) when
- * the trace's keys enter it.
+ * the trace's keys enter it.  Whatever Q, K or LSE hold where a query does not
+ * see a key, or does not count, has no effect.  B traces of max_seqlen tokens
+ * may be up to 2^24 pieces of work (every 256 keys of a KV head one, cut by
+ * rows up to 8,192 in all; every 256 counted rows of a q-head one): more is
+ * KVS_ERR_UNSUPPORTED.
  */
 size_t kvs_key_weights_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D, int last_rows);
 kvs_status_t kvs_key_weights(const void* Q, const void* K, const float* LSE,

@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -360,7 +361,7 @@ static kvs_status_t window_dims(const int32_t* cu, int B, int Ntot, int max_seql
                                 int window, int least, int sinks) {
   if (kvs_status_t st = ex_dims(cu, B, Ntot, max_seqlen)) return st;
   if (kvs_status_t st = check_dims(B, max_seqlen, Ntot, Hq, Hkv, D)) return st;
-  if (!(scale > 0.f) || scale != scale) return fail(KVS_ERR_SHAPE, "softmax_scale must be positive and finite");
+  if (!(scale > 0.f) || std::isinf(scale)) return fail(KVS_ERR_SHAPE, "softmax_scale must be positive and finite");
   if (window < least) return fail(KVS_ERR_SHAPE, "window must be >= %d (got %d)", least, window);
   if (sinks < 0) return fail(KVS_ERR_SHAPE, "sinks must be >= 0 (got %d)", sinks);
   return KVS_OK;
@@ -868,7 +869,7 @@ kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void*
                                  int sinks, void* workspace, size_t workspace_bytes, void* stream) {
   t_err.clear();
   if (kvs_status_t st = check_decode_dims(num_seqs, Hq, Hkv, D, num_blocks, block_size, max_blocks)) return st;
-  if (!(softmax_scale > 0.f) || softmax_scale != softmax_scale)
+  if (!(softmax_scale > 0.f) || std::isinf(softmax_scale))
     return fail(KVS_ERR_SHAPE, "softmax_scale must be positive and finite");
   if (window < 0 || sinks < 0) return fail(KVS_ERR_SHAPE, "window and sinks must be >= 0 (got %d, %d)", window, sinks);
   if (window > 0 && (long long)max_blocks * block_size > kMaxPlaces)

@@ -454,6 +454,25 @@ def evict_attn(q, k, v, evict_at, softmax_scale=None, cu_seqlens=None, max_seqle
     return _EvictAttn.apply(q, k, v, evict_at, scale, cu_seqlens, max_seqlen)
 
 
+# Gradients of a leaf are added up by one autograd node, which stays on the stream where the leaf was first used for as
+# long as any graph of it lives.  If that is the default stream, a backward pass that is being captured would pull it
+# into the capture, which ends the process; graphs of window_attn leave a mark on the node so that this can be refused.
+_EAGER_MARK = "kvs: used on the default stream"
+
+
+def _mark_eager(o: torch.Tensor) -> None:
+    for node, _ in o.grad_fn.next_functions:
+        if node is not None and not node.next_functions:   # a leaf's
+            node.metadata[_EAGER_MARK] = True
+
+
+def _refuse_captured(nodes) -> None:
+    for node, _ in nodes:
+        if node is not None and not node.next_functions and _EAGER_MARK in node.metadata:
+            raise RuntimeError("window_attn: this backward is being captured, but an autograd graph made on the default "
+                               "stream still uses the same leaves; let go of it before the capture")
+
+
 class _WindowAttn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, window, sinks, evict_at, scale, cu_seqlens, max_seqlen, check_cu):
@@ -468,6 +487,8 @@ class _WindowAttn(torch.autograd.Function):
     def backward(ctx, do, _dlse):
         q, k, v, o, lse, evict_at, cu_seqlens = ctx.saved_tensors
         window, sinks, scale, max_seqlen = ctx.args
+        if torch.cuda.is_current_stream_capturing():
+            _refuse_captured(ctx.next_functions)
         do = torch.zeros_like(o) if do is None else do
         # cu_seqlens is the forward's, which has checked it
         dq, dk, dv = kvs_window_attn_bwd(do.contiguous(), q, k, v, o, lse, window, sinks, evict_at, scale, cu_seqlens,
@@ -479,4 +500,7 @@ def window_attn(q, k, v, window: int, sinks: int = 0, evict_at=None, softmax_sca
                 check_cu=True):
     """Differentiable attention under a sliding window with sinks: returns ``(O, LSE)``; LSE carries no gradient."""
     scale = 1.0 / math.sqrt(q.shape[-1]) if softmax_scale is None else float(softmax_scale)
-    return _WindowAttn.apply(q, k, v, int(window), int(sinks), evict_at, scale, cu_seqlens, max_seqlen, check_cu)
+    o, lse = _WindowAttn.apply(q, k, v, int(window), int(sinks), evict_at, scale, cu_seqlens, max_seqlen, check_cu)
+    if o.requires_grad and torch.cuda.current_stream(q.device).cuda_stream == 0:
+        _mark_eager(o)
+    return o, lse

@@ -1,5 +1,6 @@
 """Attention under a sliding window with sinks on the GPU (MI355X): against the 64-bit oracle under the mask's eviction
 indices, its gradients against differences of a plain 64-bit loss, and bit for bit against the eviction-masked kernels."""
+import gc
 import math
 
 import numpy as np
@@ -178,3 +179,32 @@ def test_captured_and_replayed_on_another_stream(kvs):
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_captured_backward_beside_an_eager_graph_of_the_same_leaves(kvs):
+    """Refused while the eager graph lives, by the host; the same capture works once it is gone."""
+    announce("window attention: captured backward, refused and not")
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    leaf = lambda h: torch.randn(1, 70, h, 64, generator=gen, device=DEV).bfloat16().requires_grad_()  # noqa: E731
+    q, k, v = leaf(4), leaf(2), leaf(2)
+    do = torch.randn(1, 70, 4, 64, generator=gen, device=DEV).bfloat16()
+    o, _ = kvs.window_attn(q, k, v, 16, 2)
+    want = torch.autograd.grad(o, (q, k, v), do, retain_graph=True)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        o2, _ = kvs.window_attn(q, k, v, 16, 2)
+        with pytest.raises(RuntimeError, match="captured"):
+            torch.autograd.grad(o2, (q, k, v), do)
+    del o, o2, g
+    gc.collect()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        o, _ = kvs.window_attn(q, k, v, 16, 2)
+        got = torch.autograd.grad(o, (q, k, v), do)
+    for _ in range(3):
+        for x in got:
+            x.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

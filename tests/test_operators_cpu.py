@@ -209,3 +209,23 @@ def test_cache_without_weights_refuses(paged):
     assert [g.size for g in cache.evict_lowest(0)] == [0, 0]      # nothing is cached: nothing to do
     with pytest.raises(ValueError):
         cache.evict_lowest(0, sinks=-1)
+
+
+# ---------------------------------------------------------------- captured backward
+def test_backward_under_capture_refuses_leaves_of_an_eager_graph(kvs):
+    """The leaf's node is marked while a graph made on the default stream lives, through other nodes it is not looked
+    for, and the mark goes with the graph."""
+    x, w = torch.ones(3, requires_grad=True), torch.ones(3, requires_grad=True)
+    eager = x * w
+    kvs._mark_eager(eager)
+    with pytest.raises(RuntimeError, match="captured"):
+        kvs._refuse_captured((x * 2.0).grad_fn.next_functions)
+    kvs._refuse_captured(((x * 2.0) * 3.0).grad_fn.next_functions)
+    kvs._refuse_captured(torch.ones(2, requires_grad=True).exp().grad_fn.next_functions)
+    del eager
+    kvs._refuse_captured((x * 2.0).grad_fn.next_functions)
+
+
+def test_scales_that_are_not_finite(kvs):
+    for scale in (float("inf"), float("-inf"), float("nan"), 0.0, -1.0):
+        assert _wfwd(kvs, scale=scale) == SHAPE, scale
