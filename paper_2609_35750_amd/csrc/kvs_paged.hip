@@ -153,10 +153,19 @@ struct DecodeArgs {
   const int* tile_base;   // [S + 1]: first tile of each sequence (more than kPlanSeqs sequences)
   int tiles;              // rows of scores
   float scale_log2;       // softmax_scale * log2(e)
+  // window (kPicks)
+  const int* q_pos;       // [S]
+  int window, sinks;
+  int* picked;            // scores: [tiles][32], the slots whose scores a row holds (-1: none)
 };
 
 __device__ __forceinline__ int partial_row(const DecodeArgs& a, int s, int first) {
   return partial_row(a.S, a.units, s, first);
+}
+
+// Of a window's query at position `at`, the live entries it sees.
+__device__ __forceinline__ bool window_sees(int pos, int at, int window, int sinks) {
+  return pos >= 0 && pos <= at && (at - pos < window || pos < sinks);
 }
 
 // One unit a sequence; each wave plans by itself; looked up in unit_seq, which the plan kernel wrote.
@@ -413,26 +422,33 @@ __device__ __forceinline__ void store_b128_uncounted(float* dst, float4 v) {
 // copies of the R - 1 later steps are outstanding.  (A compiler-visible load
 // consumed while copies are in flight would make the compiler wait for all
 // of them, since it cannot see them.)
-// LIST: the table lists the visible slots themselves (the decode under a
-// window), so every listed slot is live.  SCORES: the tile's raw scores are
-// stored (four stores a step, counted in the waits like the copies), 4 Hq bytes
+// kList: the table lists the visible slots themselves (the decode under a
+// window), so every listed slot is live.  kPicks: a wave picks the visible
+// slots of its unit's tiles by itself, kPickTiles at a time, from the table
+// and slot_pos; the unit has every n-th tile of the sequence then, so that a
+// window, a run of the table more often than not, falls on all units alike (see
+// picks()).  SCORES: the tile's raw scores are stored (four stores a step, counted in the waits like the copies), 4 Hq bytes
 // a slot beside 4 Hkv D of K and V: 3% more at G = 4, D = 128, where reading K
 // once more for the weights when LSE is known would be 50%.  64 rollouts of 4,096
 // entries (32/8 heads): 174 -> 215 us.  It is the writes' way to memory: stores
 // to the same few lines cost 4 us, a quarter of them 20, and issuing them a step
 // later, behind the next copies, changes nothing.
-template <int D, bool LIST, bool SCORES>
+enum DecodeMode : int { kTable = 0, kList = 1, kPicks = 2 };
+constexpr int kPickTiles = 16;
+template <int D, int MODE, bool SCORES>
 __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
+  constexpr bool LIST = MODE != kTable, PICKS = MODE == kPicks;
   constexpr int KS = D / 16, DB = D / 32, PITCH = Lay<D, true>::PITCH, TILE = kDecTile * PITCH, R = kDecRing;
   constexpr int OPS_KV = 2 * GatherStager<D>::NI;   // K and V copy instructions per tile
   constexpr int OPS_POS = LIST ? 0 : 1;            // slot_pos copies
-  constexpr int OPS_STEP = OPS_KV + 1 + OPS_POS;   // plus the table copy
+  constexpr int OPS_STEP = OPS_KV + (PICKS ? 0 : 1) + OPS_POS;   // plus the table copy
   constexpr int OPS_SCORES = SCORES ? 4 : 0;       // stores of a computed tile
   static_assert(R == 2, "the waits count one tile ahead");
   static_assert((R - 1) * OPS_STEP + OPS_SCORES < 64, "outstanding operations must fit vmcnt");
   __shared__ __attribute__((aligned(1024))) uint16_t sK[R * TILE];
   __shared__ __attribute__((aligned(1024))) uint16_t sV[R * TILE];
-  __shared__ __attribute__((aligned(256))) int sTab[2][kWave];   // block-table entries of a tile's rows
+  __shared__ __attribute__((aligned(256))) int sTab[2][PICKS ? kPickTiles * kDecTile / 2 : kWave];   // block-table entries
+                                                                 // of a tile's rows; the slots picked
   __shared__ __attribute__((aligned(256))) int sPos[LIST ? 1 : R][kWave];   // slot_pos of a tile's rows
 
   const int lane = threadIdx.x, half = lane >> 5, col = lane & 31;
@@ -447,9 +463,9 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
   // the sequence's tiles in du.n equal runs
   const int tiles = (int)(((unsigned)nslots + kDecTile - 1) / kDecTile);
   const long long per = (long long)__builtin_amdgcn_readfirstlane(quick_div(tiles + du.n - 1, du.n)) * kDecTile;
-  const int c_begin = (int)min(du.chunk * per, (long long)nslots);
-  const int c_end = (int)min(c_begin + per, (long long)nslots);
-  const int ntile = c_end > c_begin ? (int)(((unsigned)(c_end - c_begin) + kDecTile - 1) / kDecTile) : 0;
+  const int c_begin = PICKS ? 0 : (int)min(du.chunk * per, (long long)nslots);
+  int c_end = PICKS ? 0 : (int)min(c_begin + per, (long long)nslots);
+  int ntile = c_end > c_begin ? (int)(((unsigned)(c_end - c_begin) + kDecTile - 1) / kDecTile) : 0;
 
   // Q^T operand: column n = q-head g * G + n of the group (zero for n >= G)
   const int hcol = g * a.G + col;
@@ -486,27 +502,62 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
   float* score_row = nullptr;   // of this lane's q-head and tile rows, in the first tile of all
   int score_tile = 0;           // the unit's first tile
   if (SCORES) {
-    score_tile = __builtin_amdgcn_readfirstlane(tile_base(a, s, lane) + c_begin / kDecTile);
+    score_tile = __builtin_amdgcn_readfirstlane(tile_base(a, s, lane) + (PICKS ? du.chunk : c_begin / kDecTile));
     score_row = a.scores + (size_t)g * a.G * kDecTile + 8 * (col_ok ? col : 0) + 4 * half;
   }
 
+  // PICKS: the visible slots of the unit's tiles t0, t0 + du.n, ... to the front of sTab, in the table's order.  All
+  // table entries are asked for first, then all positions: two memory latencies.
+  auto pick = [&](int t0, int at) __attribute__((always_inline)) {
+    constexpr int N = kPickTiles / 2;   // two tiles a time
+    int slot[N], pos[N], cnt = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int c = (t0 + (2 * k + half) * du.n) * kDecTile + col, blk = quick_div(c, a.BS);
+      const int entry = c < nslots ? trow[blk] : -1;
+      slot[k] = (unsigned)entry < (unsigned)a.num_blocks ? entry * a.BS + (c - blk * a.BS) : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) pos[k] = slot[k] >= 0 ? a.slot_pos[slot[k]] : -1;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const bool vis = window_sees(pos[k], at, a.window, a.sinks);
+      const unsigned long long m = __ballot(vis);
+      if (vis) (&sTab[0][0])[cnt + __builtin_popcountll(m & ((1ull << lane) - 1ull))] = slot[k];
+      cnt += __builtin_popcountll(m);
+    }
+    c_end = __builtin_amdgcn_readfirstlane(cnt);
+    ntile = (c_end + kDecTile - 1) / kDecTile;
+    if (SCORES && g == 0) {   // for the weights; a tile has its row whether or not there is something to put there
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int t = 2 * k + half, i = t * kDecTile + col, row = min(score_tile + t * du.n, a.tiles - 1);
+        if (t0 + t * du.n < tiles) a.picked[(size_t)row * kDecTile + col] = i < cnt ? (&sTab[0][0])[i] : -1;
+      }
+    }
+  };
+  const int at = PICKS ? a.q_pos[s] : 0;
+
+  int t0 = du.chunk;
+  do {   // once, but for PICKS
+  if (PICKS) pick(t0, at);
   unsigned valid_q[R] = {};   // rows of tiles n .. n + R - 1 that hold a slot of the split (index 0 = tile n)
-  if (ntile > 0) copy_table(0);
+  if (!PICKS && ntile > 0) copy_table(0);
   wait_vm_le<0>();   // Q and the first table entries are in (no compiler-visible load stays pending in the loop)
   for (int n = -(R - 1); n < ntile; ++n) {
     const int tn = n + R - 1;   // tile whose copies this step issues
     if (tn < ntile) {
       // table entries of tile tn have landed: behind them only the copies of the step before, and its stores
       if (SCORES && n > 0) wait_vm_le<OPS_KV + OPS_POS + OPS_SCORES>();
-      else if (n > -(R - 1)) wait_vm_le<OPS_KV + OPS_POS>();
+      else if (!PICKS && n > -(R - 1)) wait_vm_le<OPS_KV + OPS_POS>();
       const int c = slot_index(tn);
-      const int entry = sTab[tn & 1][col], blk = LIST ? (int)((unsigned)entry / (unsigned)a.BS) : entry;
+      const int entry = PICKS ? (&sTab[0][0])[c] : sTab[tn & 1][col], blk = LIST ? (int)((unsigned)entry / (unsigned)a.BS) : entry;
       // a table entry outside the cache reads slot 0 and is masked
       const bool bok = (unsigned)blk < (unsigned)a.num_blocks;
       const int row = LIST ? (int)((unsigned)entry % (unsigned)a.BS) : c % a.BS;
       const int slot = bok ? blk * a.BS + row : 0;
       const long long roff = bok ? (long long)blk * blk_stride + (long long)row * D : 0;
-      copy_table(min(tn + 1, ntile - 1));   // always one copy, so that every step issues the same count
+      if (!PICKS) copy_table(min(tn + 1, ntile - 1));   // always one copy, so that every step issues the same count
       gst.issue(lds_addr(sK + (tn % R) * TILE), lds_addr(sV + (tn % R) * TILE), kbase, vbase, roff);
       if (!LIST && lane < 32) dma_b32_global(a.slot_pos + slot, lds_addr(&sPos[LIST ? 0 : tn % R][0]));
       valid_q[R - 1] = (unsigned)__ballot(lane < 32 && c_begin + tn * kDecTile + col < c_end && bok);
@@ -580,7 +631,7 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
       }
       // also of a tile without a live slot, where they are not read: the waits count them
       if (SCORES && col_ok) {
-        float* dst = score_row + (size_t)min(score_tile + n, a.tiles - 1) * a.Hq * kDecTile;
+        float* dst = score_row + (size_t)min(score_tile + (PICKS ? n * du.n : n), a.tiles - 1) * a.Hq * kDecTile;
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4)
           store_b128_uncounted(dst + 8 * q4 * a.G, make_float4(raw[4 * q4], raw[4 * q4 + 1], raw[4 * q4 + 2], raw[4 * q4 + 3]));
@@ -590,6 +641,9 @@ __global__ void __launch_bounds__(64) paged_decode_kernel(DecodeArgs a) {
     for (int i = 0; i < R - 1; ++i) valid_q[i] = valid_q[i + 1];
     valid_q[R - 1] = 0u;
   }
+  t0 += kPickTiles * du.n;
+  score_tile += kPickTiles * du.n;
+  } while (PICKS && t0 < tiles);
 
   if (a.plan == kByWave && lane == 0 && g == 0 && du.chunk == 0) a.seq_units[s] = make_int2(partial_row(a, s, du.first), du.n);
   const float l_tot = halves_sum(l_run);
@@ -734,11 +788,13 @@ template __global__ void paged_append_kernel<128>(const uint16_t*, const uint16_
 KVS_RUNS(NoRunList);
 KVS_RUNS(RunList);
 #undef KVS_RUNS
-#define KVS_DECODE(DD)                                                       \
-  template __global__ void paged_decode_kernel<DD, false, false>(DecodeArgs); \
-  template __global__ void paged_decode_kernel<DD, false, true>(DecodeArgs);  \
-  template __global__ void paged_decode_kernel<DD, true, false>(DecodeArgs);  \
-  template __global__ void paged_decode_kernel<DD, true, true>(DecodeArgs)
+#define KVS_DECODE(DD)                                                        \
+  template __global__ void paged_decode_kernel<DD, kTable, false>(DecodeArgs); \
+  template __global__ void paged_decode_kernel<DD, kTable, true>(DecodeArgs);  \
+  template __global__ void paged_decode_kernel<DD, kList, false>(DecodeArgs);  \
+  template __global__ void paged_decode_kernel<DD, kList, true>(DecodeArgs);   \
+  template __global__ void paged_decode_kernel<DD, kPicks, false>(DecodeArgs); \
+  template __global__ void paged_decode_kernel<DD, kPicks, true>(DecodeArgs)
 KVS_DECODE(64);
 KVS_DECODE(128);
 #undef KVS_DECODE
@@ -902,13 +958,13 @@ static DecodeArgs decode_args(const PagedDecode& p, const int* table, const int*
 }
 
 // Plan, decode, merge.
-template <bool LIST, bool SCORES>
+template <int MODE, bool SCORES>
 static hipError_t launch_decode(const PagedDecode& p, const DecodeArgs& a) {
   const dim3 grid((unsigned)((long long)a.units * p.Hkv));
   if (a.plan == kListed) hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(1024), 0, p.stream, a);
   prof_begin("paged_decode", p.stream);
-  if (p.D == 128) hipLaunchKernelGGL((paged_decode_kernel<128, LIST, SCORES>), grid, dim3(64), 0, p.stream, a);
-  else hipLaunchKernelGGL((paged_decode_kernel<64, LIST, SCORES>), grid, dim3(64), 0, p.stream, a);
+  if (p.D == 128) hipLaunchKernelGGL((paged_decode_kernel<128, MODE, SCORES>), grid, dim3(64), 0, p.stream, a);
+  else hipLaunchKernelGGL((paged_decode_kernel<64, MODE, SCORES>), grid, dim3(64), 0, p.stream, a);
   prof_end(p.stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.plan == kOneUnit) return e;
@@ -917,7 +973,7 @@ static hipError_t launch_decode(const PagedDecode& p, const DecodeArgs& a) {
 }
 
 hipError_t launch_paged_decode(const PagedDecode& p) {
-  return launch_decode<false, false>(p, decode_args(p, p.block_table, p.seq_blocks, p.max_blocks, p.block_size, p.ws,
+  return launch_decode<kTable, false>(p, decode_args(p, p.block_table, p.seq_blocks, p.max_blocks, p.block_size, p.ws,
                                                     p.ws_bytes));
 }
 
@@ -925,10 +981,11 @@ hipError_t launch_paged_decode(const PagedDecode& p) {
 // Under a window a query sees the live entries at positions up to its own that
 // are less than `window` behind it or below `sinks`.  A long rollout's window
 // is a small part of its cache, and where it lies in the table follows from
-// the positions alone, so the visible slots are listed first (4 bytes read
-// for every slot of the table, beside 4 Hkv D for every visible one) and the
-// decode runs over the list: split evenly whatever the table holds, and no
-// slot is gathered that is not visible.
+// the positions alone, so the visible slots are found first (4 bytes read
+// for every slot of the table, beside 4 Hkv D for every visible one) and no
+// slot is gathered that is not visible.  Small batches find them in the decode
+// itself (picks()); for larger ones a kernel lists them and the decode runs
+// over the list, split evenly whatever the table holds.
 struct WindowArgs {
   const int* slot_pos;
   const int* table;
@@ -960,7 +1017,7 @@ __global__ void __launch_bounds__(kListThreads) paged_visible_kernel(WindowArgs 
   const int* trow = a.table + (size_t)s * a.max_blocks;
   const int at = a.q_pos[s];
   auto sees = [&](int pos) __attribute__((always_inline)) {
-    return pos >= 0 && pos <= at && (at - pos < a.window || pos < a.sinks);
+    return window_sees(pos, at, a.window, a.sinks);
   };
   // the visible ones of the places c .. c + 3 < n, as bits, and their slots; (blk, row): block and row of place c
   auto look = [&](int c, int blk, int row, int* slot) __attribute__((always_inline)) {
@@ -1062,7 +1119,7 @@ __global__ void __launch_bounds__(1024) paged_tile_base_kernel(DecodeArgs a, int
 // the 64 lanes 8 heads at a time, and the heads are added in one order, so
 // the sums do not depend on how the decode was split.  Bound by reading 4 Hq
 // bytes a slot: 64 rollouts of 4,096 entries, 32 heads, 11.5 us (2.9 TB/s).
-template <bool LIST>
+template <int MODE>
 __global__ void __launch_bounds__(256) paged_weight_kernel(DecodeArgs a, float* __restrict__ slot_weight) {
   __shared__ int sBase[kPlanSeqs + 1];
   __shared__ int wsum[4];
@@ -1089,7 +1146,8 @@ __global__ void __launch_bounds__(256) paged_weight_kernel(DecodeArgs a, float* 
   const int quad = lane & 7, h0 = lane >> 3;   // this lane's slots 4 quad .. + 3 of the tile, its first head
   for (int t = t0; t < t1; ++t) {
     while (s + 1 < a.S && base[s + 1] <= t) ++s;
-    const int ns = slots_of(a, s);
+    const int ns = slots_of(a, s), picked = MODE == kPicks ? a.picked[(size_t)t * kDecTile + 4 * quad + (h0 & 3)] : 0;
+    if (MODE == kPicks && __ballot(picked >= 0) == 0ull) continue;
     // place 4 quad of q-head h: [h / G][quad / 2][h % G][4 (quad % 2)]
     const float* row = a.scores + (size_t)t * a.Hq * kDecTile + 4 * (quad & 1);
     float x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -1108,10 +1166,15 @@ __global__ void __launch_bounds__(256) paged_weight_kernel(DecodeArgs a, float* 
       for (int off = 8; off < kWave; off <<= 1) x[k] += __shfl_xor(x[k], off);
     // lane l < 32 adds to place 4 (l % 8) + l / 8 of the tile
     const int c = (t - base[s]) * kDecTile + 4 * quad + h0;
-    if (lane >= 32 || c >= ns) continue;
+    if (lane >= 32) continue;
     const float add = h0 == 0 ? x[0] : h0 == 1 ? x[1] : h0 == 2 ? x[2] : x[3];
-    const int entry = a.table[(size_t)s * a.max_blocks + (LIST ? c : c / a.BS)];
-    if (LIST) {
+    if (MODE == kPicks) {
+      if (picked >= 0) slot_weight[picked] += add;
+      continue;
+    }
+    if (c >= ns) continue;
+    const int entry = a.table[(size_t)s * a.max_blocks + (MODE == kList ? c : c / a.BS)];
+    if (MODE == kList) {
       slot_weight[entry] += add;
     } else if ((unsigned)entry < (unsigned)a.num_blocks) {
       const int slot = entry * a.BS + c % a.BS;
@@ -1124,14 +1187,25 @@ __global__ void __launch_bounds__(256) paged_weight_kernel(DecodeArgs a, float* 
 struct ExSpace {
   int cap;             // slots listed a sequence (window)
   long long tiles;     // rows of scores (weights): every sequence's slots in tiles; no slot belongs to two sequences
-  size_t list, counts, base, scores, units;
+  size_t list, counts, base, scores, units;   // list: of all tiles of scores, if the decode's waves pick
   size_t bytes() const { return list + counts + base + scores + units; }
 };
+// Whether the decode's waves pick the visible slots by themselves: where the tables' tiles are no more than all units
+// look at in one go, every KV head's on its own.  That saves a launch and its latencies, and leaves the units unequal
+// where the window is.  Listed against picked (32/8 heads, D = 128, blocks of 16): one sequence of 32,000, window 4,096,
+// 18.3 and 14.1 us, 512 16.2 and 11.8; in blocks of one 30.2 and 14.6; two 21.6 and 17.2; 8 of 8,000, all seen, 55.0
+// and 51.4; 64 of 1,000, window 512 (the line), 33.5 and 33.1.
+static bool picks(const PagedDecode& p) {
+  const long long tiles = ((long long)p.max_blocks * p.block_size + kDecTile - 1) / kDecTile;
+  return p.window > 0 &&
+         p.S * tiles <= (long long)kPickTiles * paged_units(p.S, p.Hkv, p.max_blocks, p.block_size, p.D);
+}
 static ExSpace ex_space(const PagedDecode& p) {
   ExSpace x{};
   const long long width = (long long)p.max_blocks * p.block_size;
   long long each = width;
-  if (p.window > 0) {
+  const bool lists = p.window > 0 && !picks(p);
+  if (lists) {
     x.cap = (int)std::min(width, (long long)p.window + p.sinks);
     x.list = round256((size_t)p.S * x.cap * sizeof(int));
     x.counts = round256((size_t)p.S * sizeof(int));
@@ -1142,33 +1216,34 @@ static ExSpace ex_space(const PagedDecode& p) {
                        (long long)p.num_blocks * p.block_size / kDecTile + p.S);
     x.base = p.S > kPlanSeqs ? round256((size_t)(p.S + 1) * sizeof(int)) : 0;
     x.scores = round256((size_t)x.tiles * p.Hq * kDecTile * sizeof(float));
+    if (picks(p)) x.list = round256((size_t)x.tiles * kDecTile * sizeof(int));
   }
-  x.units = p.window > 0 ? paged_ws_bytes(p.S, p.Hq, p.Hkv, x.cap, 1, p.D)
+  x.units = lists ? paged_ws_bytes(p.S, p.Hq, p.Hkv, x.cap, 1, p.D)
                          : paged_ws_bytes(p.S, p.Hq, p.Hkv, p.max_blocks, p.block_size, p.D);
   return x;
 }
 size_t paged_ex_ws_bytes(const PagedDecode& p) { return ex_space(p).bytes(); }
 long long paged_ex_units(const PagedDecode& p) {
-  return p.window > 0 ? paged_units(p.S, p.Hkv, ex_space(p).cap, 1, p.D)
-                      : paged_units(p.S, p.Hkv, p.max_blocks, p.block_size, p.D);
+  return p.window > 0 && !picks(p) ? paged_units(p.S, p.Hkv, ex_space(p).cap, 1, p.D)
+                                   : paged_units(p.S, p.Hkv, p.max_blocks, p.block_size, p.D);
 }
 
 // Slots of a sequence that one workgroup lists, at least (what its threads look at together); chunks at most.
 constexpr int kListChunk = 4 * kListThreads, kListChunks = 16;
 
-template <bool LIST>
+template <int MODE>
 static hipError_t launch_ex(const PagedDecode& p, const ExSpace& x, DecodeArgs a, int* base, float* scores) {
-  if (!p.weights) return launch_decode<LIST, false>(p, a);
+  if (!p.weights) return launch_decode<MODE, false>(p, a);
   a.scores = scores;
   a.tiles = (int)x.tiles;
   if (p.S > kPlanSeqs) {
     hipLaunchKernelGGL(paged_tile_base_kernel, dim3(1), dim3(1024), 0, p.stream, a, base);
     a.tile_base = base;
   }
-  hipError_t e = launch_decode<LIST, true>(p, a);
+  hipError_t e = launch_decode<MODE, true>(p, a);
   if (e != hipSuccess) return e;
   const int grid = (int)std::min((x.tiles + 3) / 4, 2048ll);
-  hipLaunchKernelGGL(paged_weight_kernel<LIST>, dim3(grid), dim3(256), 0, p.stream, a, p.slot_weight);
+  hipLaunchKernelGGL(paged_weight_kernel<MODE>, dim3(grid), dim3(256), 0, p.stream, a, p.slot_weight);
   return hipGetLastError();
 }
 
@@ -1180,8 +1255,16 @@ hipError_t launch_paged_decode_ex(const PagedDecode& p) {
   int* base = (int*)(w += x.counts);
   float* scores = (float*)(w += x.base);
   void* units = w += x.scores;
+  if (picks(p)) {
+    DecodeArgs a = decode_args(p, p.block_table, p.seq_blocks, p.max_blocks, p.block_size, units, x.units);
+    a.q_pos = p.q_pos;
+    a.window = p.window;
+    a.sinks = p.sinks;
+    a.picked = list;
+    return launch_ex<kPicks>(p, x, a, base, scores);
+  }
   if (p.window == 0)
-    return launch_ex<false>(p, x, decode_args(p, p.block_table, p.seq_blocks, p.max_blocks, p.block_size, units, x.units),
+    return launch_ex<kTable>(p, x, decode_args(p, p.block_table, p.seq_blocks, p.max_blocks, p.block_size, units, x.units),
                             base, scores);
   const long long width = (long long)p.max_blocks * p.block_size;
   const long long rounds = (width + (long long)kListChunk * kListChunks - 1) / ((long long)kListChunk * kListChunks);
@@ -1193,7 +1276,7 @@ hipError_t launch_paged_decode_ex(const PagedDecode& p) {
                      dim3(kListThreads), 0, p.stream, v);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return launch_ex<true>(p, x, decode_args(p, list, counts, x.cap, 1, units, x.units), base, scores);
+  return launch_ex<kList>(p, x, decode_args(p, list, counts, x.cap, 1, units, x.units), base, scores);
 }
 
 }  // namespace kvs
