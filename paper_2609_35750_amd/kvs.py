@@ -486,15 +486,23 @@ class _WindowAttn(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, do, _dlse):
-        q, k, v, o, lse, evict_at, cu_seqlens = ctx.saved_tensors
-        window, sinks, scale, max_seqlen = ctx.args
-        if torch.cuda.is_current_stream_capturing():
-            _refuse_captured(ctx.next_functions)
-        do = torch.zeros_like(o) if do is None else do
-        # cu_seqlens is the forward's, which has checked it
-        dq, dk, dv = kvs_window_attn_bwd(do.contiguous(), q, k, v, o, lse, window, sinks, evict_at, scale, cu_seqlens,
-                                         max_seqlen, check_cu=False)
-        return dq, dk, dv, None, None, None, None, None, None, None
+        # under create_graph a second derivative is refused, not zero (that wrapper takes 4 us)
+        return (_window_grads_once if torch.is_grad_enabled() else _window_grads)(ctx, do)
+
+
+def _window_grads(ctx, do):
+    q, k, v, o, lse, evict_at, cu_seqlens = ctx.saved_tensors
+    window, sinks, scale, max_seqlen = ctx.args
+    if torch.cuda.is_current_stream_capturing():
+        _refuse_captured(ctx.next_functions)
+    do = torch.zeros_like(o) if do is None else do
+    # cu_seqlens is the forward's, which has checked it
+    dq, dk, dv = kvs_window_attn_bwd(do.contiguous(), q, k, v, o, lse, window, sinks, evict_at, scale, cu_seqlens,
+                                     max_seqlen, check_cu=False)
+    return dq, dk, dv, None, None, None, None, None, None, None
+
+
+_window_grads_once = torch.autograd.function.once_differentiable(_window_grads)
 
 
 def window_attn(q, k, v, window: int, sinks: int = 0, evict_at=None, softmax_scale=None, cu_seqlens=None, max_seqlen=None,

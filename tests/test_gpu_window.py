@@ -208,3 +208,31 @@ def test_captured_backward_beside_an_eager_graph_of_the_same_leaves(kvs):
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_second_derivatives_are_refused(kvs):
+    announce("window attention: double backward")
+    q, k, v = (torch.randn(1, 40, h, 64, device=DEV).bfloat16().requires_grad_() for h in (4, 2, 2))
+    o, _ = kvs.window_attn(q, k, v, 8)
+    dq, = torch.autograd.grad(o.float().square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        dq.float().sum().backward()
+
+
+def test_keys_and_values_that_are_one_tensor(kvs):
+    """Its gradient is the sum of both, and one leaf in all three places gets all three."""
+    announce("window attention: shared inputs")
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    x, do = (torch.randn(1, 90, 2, 64, generator=gen, device=DEV).bfloat16() for _ in range(2))
+    a, b, c = (x.clone().requires_grad_() for _ in range(3))
+    o, _ = kvs.window_attn(a, b, c, 20, 3)
+    parts = torch.autograd.grad(o, (a, b, c), do)
+    y = x.clone().requires_grad_()
+    o2, _ = kvs.window_attn(y, y, y, 20, 3)
+    got, = torch.autograd.grad(o2, y, do)
+    torch.cuda.synchronize()
+    assert torch.equal(o, o2)
+    want = sum(p.double() for p in parts)
+    # two additions in bf16, each half a step of a partial sum
+    bound = 2.0 * 2.0 ** -8 * sum(p.double().abs() for p in parts)
+    assert ((got.double() - want).abs() <= bound).all()
