@@ -112,10 +112,8 @@ kvs_status_t run_bwd(kvs::Problem& p) {
   hipError_t e = kvs::launch_bwd_pre(p, kstats, delta);
   if (e != hipSuccess) return hip_fail(e, "backward preprocess launch");
   void* split_ws = (char*)delta + kvs::ws_delta_bytes(p.Hq, p.ntok);
-  e = kvs::launch_bwd_dkdv(p, kstats, delta, split_ws, p.ws_bytes - bwd_ws_fixed(p.B, p.ntok, p.Hq));
-  if (e != hipSuccess) return hip_fail(e, "dK/dV launch");
-  e = kvs::launch_bwd_dq(p, kstats, delta);
-  if (e != hipSuccess) return hip_fail(e, "dQ launch");
+  e = kvs::launch_bwd_main(p, kstats, delta, split_ws, p.ws_bytes - bwd_ws_fixed(p.B, p.ntok, p.Hq));
+  if (e != hipSuccess) return hip_fail(e, "backward launch");
   return KVS_OK;
 }
 

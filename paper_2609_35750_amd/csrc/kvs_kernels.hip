@@ -576,9 +576,73 @@ __global__ void __launch_bounds__(256) bwd_pre_kernel(const uint16_t* __restrict
   }
 }
 
+// Sum of the parts' partials of split key blocks, in part order; dK scaled.
+// The split blocks are listed by the plan, and the last kReduceGrid workgroups
+// of the dQ kernel, which fill its tail, walk the 32-key groups of dV and dK of
+// all of them.  Bound by reading the partials, so every thread keeps several
+// parts' loads in flight; the sums are turned in LDS and stored as whole rows.
+constexpr int kReduceGrid = 512;
+struct ReduceArgs {
+  const PlanCtl* ctl;     // NULL: nothing is split
+  const int* plan;
+  const int* split;
+  const float* part;
+  uint16_t* dk;
+  uint16_t* dv;
+  int nkt, first;         // first of the workgroups
+};
+// buf: 32 (D + 8) elements of LDS
+template <int D>
+__device__ __forceinline__ void split_reduce(const ReduceArgs& ra, const int* __restrict__ cu, int T, int ntok, int Hkv, float scale,
+                                             uint16_t* buf) {
+  constexpr int P = D + 8, NF = D / 32;              // LDS row pitch; float4s of a thread: fragments of 256
+  constexpr size_t kSlot = (size_t)2 * kColKeys * D;    // floats of one slot
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
+  const int tasks = ra.ctl->nsplit * Hkv * 8;
+  for (int t = (int)blockIdx.x - ra.first; t < tasks; t += kReduceGrid) {
+    const int grp = t & 7, bg = t >> 3, g = bg % Hkv, blk = ra.split[bg / Hkv];   // group: dV 0..3, dK 4..7
+    const int nc = ra.plan[2 * blk], s0 = ra.plan[2 * blk + 1];
+    const int b = blk / ra.nkt, kt = blk % ra.nkt;
+    const float* src = ra.part + ((size_t)s0 * Hkv + g) * kSlot + (size_t)grp * 32 * D + 4 * tid;
+    float4 sum[NF];
+#pragma unroll
+    for (int n = 0; n < NF; ++n) sum[n] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (int c = 0; c < nc; ++c) {
+      float4 v[NF];
+#pragma unroll
+      for (int n = 0; n < NF; ++n) v[n] = *reinterpret_cast<const float4*>(src + (size_t)c * Hkv * kSlot + n * 1024);
+#pragma unroll
+      for (int n = 0; n < NF; ++n) {
+        sum[n].x += v[n].x;
+        sum[n].y += v[n].y;
+        sum[n].z += v[n].z;
+        sum[n].w += v[n].w;
+      }
+    }
+    const float sc = grp >= 4 ? scale : 1.f;
+    // float4 n of wave w is fragment 4 n + w: columns 32 n + 8 w + 4 half of key `col`
+#pragma unroll
+    for (int n = 0; n < NF; ++n)
+      *reinterpret_cast<uint2*>(buf + col * P + 32 * n + 8 * (tid >> 6) + 4 * half) =
+          pack4_bf16(sum[n].x * sc, sum[n].y * sc, sum[n].z * sc, sum[n].w * sc);
+    asm volatile("" ::: "memory");   // the same bytes are read back as another type
+    __syncthreads();
+    const Trace tr = trace_of(cu, b, T, ntok);
+    constexpr int LPR = D / 8;
+#pragma unroll
+    for (int n = 0; n < 32 * LPR / 256; ++n) {
+      const int r = (n * 256 + tid) / LPR, c = 8 * (tid % LPR), j = kt * kColKeys + 32 * (grp & 3) + r;
+      const uint4 v = *reinterpret_cast<const uint4*>(buf + r * P + c);
+      if (j < tr.L) *reinterpret_cast<uint4*>((grp >= 4 ? ra.dk : ra.dv) + ((size_t)(tr.tok0 + j) * Hkv + g) * D + c) = v;
+    }
+    __syncthreads();
+  }
+}
+
 // ---------------------------------------------------------------- backward: dQ (row kernel)
 template <int D, bool WIN>
-__global__ void __launch_bounds__(512) dq_kernel(RowArgs a) {
+__global__ void __launch_bounds__(512) dq_kernel(RowArgs a, ReduceArgs ra) {
   constexpr int KS = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(1024))) uint16_t sK0[kKeyTile * Lay<D, true>::PITCH];
   __shared__ __attribute__((aligned(1024))) uint16_t sK1[kKeyTile * Lay<D, true>::PITCH];
@@ -587,6 +651,10 @@ __global__ void __launch_bounds__(512) dq_kernel(RowArgs a) {
   __shared__ __attribute__((aligned(256))) int sE0[kKeyTile];
   __shared__ __attribute__((aligned(256))) int sE1[kKeyTile];
 
+  if (ra.ctl && (int)blockIdx.x >= ra.first) {
+    split_reduce<D>(ra, a.cu, a.T, a.ntok, a.Hkv, a.scale, sK0);
+    return;
+  }
   RowTile rt;
   if (!row_tile(a, rt)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
@@ -1009,7 +1077,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (nchunk > 1) {
     // fp32 partial sums of this part: [slot][dV, dK][32-key group], each group
     // as the accumulators lie, [d][q4][lane][4], so that a store instruction
-    // writes 1 KB in a row (split_reduce_kernel turns the sums)
+    // writes 1 KB in a row (split_reduce turns the sums)
     float* dst = a.part + ((((size_t)(slot0 + chunk) * a.Hkv + g) * 2 + (role_dk ? 1 : 0)) * 4 + kw) * 32 * D + 4 * lane;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -1168,80 +1236,17 @@ __global__ void __launch_bounds__(1024) split_plan_kernel(const int2* __restrict
   }
 }
 
-// Sum of the parts' partials of split key blocks, in part order; dK scaled.
-// The split blocks are listed by the plan, and a fixed grid walks the 32-key
-// groups of dV and dK of all of them.  Bound by reading the partials, so every
-// thread keeps several parts' loads in flight; the sums are turned in LDS and
-// stored as whole rows.
-constexpr int kReduceGrid = 2048;
-template <int D>
-__global__ void __launch_bounds__(256) split_reduce_kernel(const PlanCtl* __restrict__ ctl,
-                                                           const int* __restrict__ plan, const int* __restrict__ split,
-                                                           const float* __restrict__ part, const int* __restrict__ cu,
-                                                           uint16_t* __restrict__ dk, uint16_t* __restrict__ dv, int B,
-                                                           int T, int ntok, int nkt, int Hkv, float scale) {
-  constexpr int P = D + 8, NF = D / 32;              // LDS row pitch; float4s of a thread: fragments of 256
-  constexpr size_t kSlot = (size_t)2 * kColKeys * D;    // floats of one slot
-  __shared__ __attribute__((aligned(16))) uint16_t buf[32 * P];
-  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
-  const int tasks = ctl->nsplit * Hkv * 8;
-  for (int t = blockIdx.x; t < tasks; t += gridDim.x) {
-    const int grp = t & 7, bg = t >> 3, g = bg % Hkv, blk = split[bg / Hkv];   // group: dV 0..3, dK 4..7
-    const int nc = plan[2 * blk], s0 = plan[2 * blk + 1];
-    const int b = blk / nkt, kt = blk % nkt;
-    const float* src = part + ((size_t)s0 * Hkv + g) * kSlot + (size_t)grp * 32 * D + 4 * tid;
-    float4 sum[NF];
-#pragma unroll
-    for (int n = 0; n < NF; ++n) sum[n] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-    for (int c = 0; c < nc; ++c) {
-      float4 v[NF];
-#pragma unroll
-      for (int n = 0; n < NF; ++n) v[n] = *reinterpret_cast<const float4*>(src + (size_t)c * Hkv * kSlot + n * 1024);
-#pragma unroll
-      for (int n = 0; n < NF; ++n) {
-        sum[n].x += v[n].x;
-        sum[n].y += v[n].y;
-        sum[n].z += v[n].z;
-        sum[n].w += v[n].w;
-      }
-    }
-    const float sc = grp >= 4 ? scale : 1.f;
-    // float4 n of wave w is fragment 4 n + w: columns 32 n + 8 w + 4 half of key `col`
-#pragma unroll
-    for (int n = 0; n < NF; ++n)
-      *reinterpret_cast<uint2*>(buf + col * P + 32 * n + 8 * (tid >> 6) + 4 * half) =
-          pack4_bf16(sum[n].x * sc, sum[n].y * sc, sum[n].z * sc, sum[n].w * sc);
-    asm volatile("" ::: "memory");   // the same bytes are read back as another type
-    __syncthreads();
-    const Trace tr = trace_of(cu, b, T, ntok);
-    constexpr int LPR = D / 8;
-#pragma unroll
-    for (int n = 0; n < 32 * LPR / 256; ++n) {
-      const int r = (n * 256 + tid) / LPR, c = 8 * (tid % LPR), j = kt * kColKeys + 32 * (grp & 3) + r;
-      const uint4 v = *reinterpret_cast<const uint4*>(buf + r * P + c);
-      if (j < tr.L) *reinterpret_cast<uint4*>((grp >= 4 ? dk : dv) + ((size_t)(tr.tok0 + j) * Hkv + g) * D + c) = v;
-    }
-    __syncthreads();
-  }
-}
-
 // Explicit instantiations: every kernel the launchers use is emitted, with its host stub.
 template __global__ void fwd_kernel<64, false>(RowArgs);
 template __global__ void fwd_kernel<128, false>(RowArgs);
 template __global__ void fwd_kernel<64, true>(RowArgs);
 template __global__ void fwd_kernel<128, true>(RowArgs);
-template __global__ void dq_kernel<64, false>(RowArgs);
-template __global__ void dq_kernel<128, false>(RowArgs);
-template __global__ void dq_kernel<64, true>(RowArgs);
-template __global__ void dq_kernel<128, true>(RowArgs);
+template __global__ void dq_kernel<64, false>(RowArgs, ReduceArgs);
+template __global__ void dq_kernel<128, false>(RowArgs, ReduceArgs);
+template __global__ void dq_kernel<64, true>(RowArgs, ReduceArgs);
+template __global__ void dq_kernel<128, true>(RowArgs, ReduceArgs);
 template __global__ void dkdv_kernel<64>(ColArgs);
 template __global__ void dkdv_kernel<128>(ColArgs);
-template __global__ void split_reduce_kernel<64>(const PlanCtl*, const int*, const int*, const float*, const int*, uint16_t*, uint16_t*,
-                                                  int, int, int, int, int, float);
-template __global__ void split_reduce_kernel<128>(const PlanCtl*, const int*, const int*, const float*, const int*, uint16_t*, uint16_t*,
-                                                  int, int, int, int, int, float);
-
 // ---------------------------------------------------------------- library-owned scratch (allocation-free forward)
 // Per-key-tile statistics of kvs_evict_attn_fwd_noalloc.  In host code the
 // name `scratch` is only a host-side stand-in: its device address (one per
@@ -1409,8 +1414,8 @@ hipError_t launch_bwd_pre(const Problem& p, int2* kstats, float* delta) {
   return hipGetLastError();
 }
 
-hipError_t launch_bwd_dkdv(const Problem& p, const int2* kstats, const float* delta, void* split_ws,
-                           size_t split_bytes) {
+// dK and dV, and dQ, whose last workgroups add up what the first has split.
+hipError_t launch_bwd_main(const Problem& p, const int2* kstats, const float* delta, void* split_ws, size_t split_bytes) {
   ColArgs a{};
   a.q = (const uint16_t*)p.q;
   a.k = (const uint16_t*)p.k;
@@ -1459,26 +1464,16 @@ hipError_t launch_bwd_dkdv(const Problem& p, const int2* kstats, const float* de
   else hipLaunchKernelGGL(dkdv_kernel<64>, dim3(grid), dim3(512), 0, p.stream, a);
   prof_end(p.stream);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || cap == 0) return e;
-  if (p.D == 128)
-    hipLaunchKernelGGL(split_reduce_kernel<128>, dim3(kReduceGrid), dim3(256), 0, p.stream, ctl, a.plan, split, a.part, p.cu,
-                       (uint16_t*)p.dk, (uint16_t*)p.dv, p.B, p.T, p.ntok, a.nkt, p.Hkv, p.scale);
-  else
-    hipLaunchKernelGGL(split_reduce_kernel<64>, dim3(kReduceGrid), dim3(256), 0, p.stream, ctl, a.plan, split, a.part, p.cu,
-                       (uint16_t*)p.dk, (uint16_t*)p.dv, p.B, p.T, p.ntok, a.nkt, p.Hkv, p.scale);
-  return hipGetLastError();
-}
-
-hipError_t launch_bwd_dq(const Problem& p, const int2* kstats, const float* delta) {
-  RowArgs a = row_args(p, kstats);
-  a.delta = delta;
-  a.lse_in = (const float*)((const char*)delta + half_delta_bytes(p.Hq, p.ntok));   // LSE * log2(e)
-  const long long nblk = (long long)a.nqt * p.B * p.Hkv * p.nhg;
-  dim3 grid((unsigned)nblk), block(64 * p.HG * p.TC);
+  if (e != hipSuccess) return e;
+  RowArgs r = row_args(p, kstats);
+  r.delta = delta;
+  r.lse_in = a.lse;
+  const int nblk = (int)((long long)r.nqt * p.B * p.Hkv * p.nhg);
+  const ReduceArgs ra{cap ? ctl : nullptr, plan, split, a.part, a.dk, a.dv, a.nkt, nblk};
   prof_begin("bwd_dq", p.stream);
   const auto kernel = p.window > 0 ? (p.D == 128 ? dq_kernel<128, true> : dq_kernel<64, true>)
                                    : (p.D == 128 ? dq_kernel<128, false> : dq_kernel<64, false>);
-  hipLaunchKernelGGL(kernel, grid, block, 0, p.stream, a);
+  hipLaunchKernelGGL(kernel, dim3(nblk + (cap ? kReduceGrid : 0)), dim3(64 * p.HG * p.TC), 0, p.stream, r, ra);
   prof_end(p.stream);
   return hipGetLastError();
 }

@@ -64,9 +64,7 @@ inline PreGrid bwd_pre_grid(long long rows, long long kstats_blocks) {
 hipError_t launch_kstats(const Problem& p, int2* kstats);
 hipError_t launch_fwd(const Problem& p, const int2* kstats);
 hipError_t launch_bwd_pre(const Problem& p, int2* kstats, float* delta);   // and the key-tile statistics
-hipError_t launch_bwd_dkdv(const Problem& p, const int2* kstats, const float* delta, void* split_ws,
-                           size_t split_bytes);
-hipError_t launch_bwd_dq(const Problem& p, const int2* kstats, const float* delta);
+hipError_t launch_bwd_main(const Problem& p, const int2* kstats, const float* delta, void* split_ws, size_t split_bytes);
 hipError_t launch_classify(const int32_t* evict, const int32_t* cu, int B, int T, int BM, int BN,
                            uint8_t* out, hipStream_t stream);
 hipError_t launch_check(const int32_t* evict, const int32_t* cu, int B, int T, int ntok,
