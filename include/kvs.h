@@ -452,7 +452,7 @@ kvs_status_t kvs_paged_decode(const void* Q, const void* K_cache, const void* V_
  * [num_seqs]), sees of the live entries those at positions p <= q_pos[s] with
  * q_pos[s] - p < window or p < sinks: row q_pos[s] of kvs_window_attn_fwd.
  * Positions within a sequence are distinct (as a block manager has them); of
- * one with repeated positions at most window + sinks entries are seen.
+ * one with more visible entries than window + sinks some may be left out.
  * window 0: every live entry, q_pos (may be NULL) and sinks without effect.
  * slot_weight not NULL: slot_weight[slot] += sum_h exp(s_h - LSE_h) over all
  * q-heads, for every entry the query sees.  Limits and layouts are those of
