@@ -232,6 +232,23 @@ kvs_status_t kvs_window_attn_bwd(const void* dO, const void* Q, const void* K, c
                                  int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D,
                                  float softmax_scale, int window, int sinks,
                                  void* workspace, size_t workspace_bytes, void* stream);
+/* The same with O_rem (device int8, in O's layout; NULL: as above): what the
+ * rounding to bf16 takes from O, the eight bits below it.  The backward then
+ * forms Delta = rowsum(dO O) from the unrounded O; gradients of short rows are
+ * about a tenth closer to the exact ones, for a byte a value written and read. */
+kvs_status_t kvs_window_attn_fwd_rem(const void* Q, const void* K, const void* V,
+                                     const int32_t* evict_at, const int32_t* cu_seqlens,
+                                     void* O, int8_t* O_rem, float* LSE,
+                                     int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D,
+                                     float softmax_scale, int window, int sinks,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+kvs_status_t kvs_window_attn_bwd_rem(const void* dO, const void* Q, const void* K, const void* V,
+                                     const void* O, const int8_t* O_rem, const float* LSE,
+                                     const int32_t* evict_at, const int32_t* cu_seqlens,
+                                     void* dQ, void* dK, void* dV,
+                                     int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D,
+                                     float softmax_scale, int window, int sinks,
+                                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------- attention weights of the keys
  * What every key of a trace has received from the softmax, over all q-heads:

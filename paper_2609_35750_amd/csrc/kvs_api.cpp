@@ -391,6 +391,14 @@ kvs_status_t kvs_window_attn_fwd(const void* Q, const void* K, const void* V, co
                                  const int32_t* cu_seqlens, void* O, float* LSE, int B, int Ntot, int max_seqlen,
                                  int Hq, int Hkv, int D, float softmax_scale, int window, int sinks, void* workspace,
                                  size_t workspace_bytes, void* stream) {
+  return kvs_window_attn_fwd_rem(Q, K, V, evict_at, cu_seqlens, O, nullptr, LSE, B, Ntot, max_seqlen, Hq, Hkv, D,
+                                 softmax_scale, window, sinks, workspace, workspace_bytes, stream);
+}
+
+kvs_status_t kvs_window_attn_fwd_rem(const void* Q, const void* K, const void* V, const int32_t* evict_at,
+                                     const int32_t* cu_seqlens, void* O, int8_t* O_rem, float* LSE, int B, int Ntot,
+                                     int max_seqlen, int Hq, int Hkv, int D, float softmax_scale, int window, int sinks,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
   t_err.clear();
   if (kvs_status_t st = window_dims(cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale, window, 1, sinks))
     return st;
@@ -400,10 +408,11 @@ kvs_status_t kvs_window_attn_fwd(const void* Q, const void* K, const void* V, co
   REQUIRE_PTR(V, "V");
   REQUIRE_PTR(O, "O");
   REQUIRE_PTR(LSE, "LSE");
+  if (!aligned16(O_rem)) return fail(KVS_ERR_ALIGN, "O_rem is not 16-byte aligned");
   if (kvs_status_t st = check_ws(workspace, workspace_bytes, until_bytes(Ntot) + fwd_ws(B, Ntot))) return st;
   kvs::Problem p = window_problem(Q, K, V, evict_at, cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale, window,
                                   sinks, workspace, workspace_bytes, stream);
-  p.o = O; p.lse = LSE;
+  p.o = O; p.lse = LSE; p.o_rem = O_rem;
   return run_fwd(p);
 }
 
@@ -417,6 +426,15 @@ kvs_status_t kvs_window_attn_bwd(const void* dO, const void* Q, const void* K, c
                                  void* dK, void* dV, int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D,
                                  float softmax_scale, int window, int sinks, void* workspace, size_t workspace_bytes,
                                  void* stream) {
+  return kvs_window_attn_bwd_rem(dO, Q, K, V, O, nullptr, LSE, evict_at, cu_seqlens, dQ, dK, dV, B, Ntot, max_seqlen, Hq,
+                                 Hkv, D, softmax_scale, window, sinks, workspace, workspace_bytes, stream);
+}
+
+kvs_status_t kvs_window_attn_bwd_rem(const void* dO, const void* Q, const void* K, const void* V, const void* O,
+                                     const int8_t* O_rem, const float* LSE, const int32_t* evict_at,
+                                     const int32_t* cu_seqlens, void* dQ, void* dK, void* dV, int B, int Ntot,
+                                     int max_seqlen, int Hq, int Hkv, int D, float softmax_scale, int window, int sinks,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
   t_err.clear();
   if (kvs_status_t st = window_dims(cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale, window, 1, sinks))
     return st;
@@ -427,6 +445,7 @@ kvs_status_t kvs_window_attn_bwd(const void* dO, const void* Q, const void* K, c
   REQUIRE_PTR(V, "V");
   REQUIRE_PTR(O, "O");
   REQUIRE_PTR(LSE, "LSE");
+  if (!aligned16(O_rem)) return fail(KVS_ERR_ALIGN, "O_rem is not 16-byte aligned");
   REQUIRE_PTR(dQ, "dQ");
   REQUIRE_PTR(dK, "dK");
   REQUIRE_PTR(dV, "dV");
@@ -435,7 +454,7 @@ kvs_status_t kvs_window_attn_bwd(const void* dO, const void* Q, const void* K, c
     return st;
   kvs::Problem p = window_problem(Q, K, V, evict_at, cu_seqlens, B, Ntot, max_seqlen, Hq, Hkv, D, softmax_scale, window,
                                   sinks, workspace, workspace_bytes, stream);
-  p.o_in = O; p.dout = dO; p.lse_in = LSE; p.dq = dQ; p.dk = dK; p.dv = dV;
+  p.o_in = O; p.dout = dO; p.lse_in = LSE; p.dq = dQ; p.dk = dK; p.dv = dV; p.o_rem_in = O_rem;
   return run_bwd(p);
 }
 

@@ -48,6 +48,7 @@ struct RowArgs {
   int varlen;
   int flags;            // kFlagNoEmptySkip | kFlagFullAsPartial (consistency checks; 0 normally)
   int window, sinks;    // of the windowed kernels, whose `evict` is the one the window makes of it (key_until)
+  int8_t* o_rem;        // windowed forward: what O's rounding takes (store_remainders); NULL: not kept
   float scale_log2;     // softmax_scale * log2(e)
   float scale;
 };
@@ -329,6 +330,45 @@ __device__ __forceinline__ void store_rows(const f32x16* acc, float sc, uint16_t
   }
 }
 
+// What rounding takes from O, for a backward whose Delta = rowsum(dO O) shall be
+// that of the unrounded O: a byte a value, the eight bits of the fp32 value
+// below its bf16 (the difference of the two as integers, shifted, in -128 ..
+// 127).  With the rounded O, dQ and dK of short rows are 1.5 to 1.7 times as
+// far from the exact ones as those, rounded, are; with this 1.4 to 1.5, what
+// dS in bf16 leaves.  Rows as in store_rows, behind it.
+template <int D>
+__device__ __forceinline__ void store_remainders(const f32x16* acc, float sc, uint16_t* buf, int8_t* __restrict__ dst,
+                                                 long long row_stride, int nrows, int lane) {
+  constexpr int P = D + 16;   // row pitch in bytes
+  int8_t* bytes = reinterpret_cast<int8_t*>(buf);
+  const int half = lane >> 5, col = lane & 31;
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = acc[d][4 * q4 + e] * sc;
+      const uint2 y = pack4_bf16(x[0], x[1], x[2], x[3]);
+      const uint32_t yb[4] = {y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u};
+      uint32_t w = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        w |= (((uint32_t)min((int)(__float_as_uint(x[e]) - yb[e]), 0x7fff) >> 8) & 0xffu) << 8 * e;
+      *reinterpret_cast<uint32_t*>(bytes + col * P + 32 * d + 8 * q4 + 4 * half) = w;
+    }
+  asm volatile("" ::: "memory");
+  constexpr int LPR = D / 16, RPI = kWave / LPR;   // lanes per row, rows per store
+  const int r0 = lane / LPR, c = 16 * (lane % LPR);
+#pragma unroll
+  for (int it = 0; it < 32 / RPI; ++it) {
+    const int r = it * RPI + r0;
+    const uint4 v = *reinterpret_cast<const uint4*>(bytes + r * P + c);
+    if (r < nrows) *reinterpret_cast<uint4*>(dst + r * row_stride + c) = v;
+  }
+}
+
 // Whether the n keys from j0 on have all left the window of the queries from i0 on (a finer look than the 64-key tiles'
 // statistics allow: a window's edge costs a row block half a tile less).
 __device__ __forceinline__ bool behind_window(const RowArgs& a, int i0, int j0, int n) {
@@ -531,8 +571,10 @@ fwd_kernel(RowArgs a) {
   const float l_tot = l_run + wave_xor32(l_run);
   const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
   __syncthreads();   // the tile buffers are free
-  store_rows<D>(acc, inv, wave < 2 ? (wave ? sK1 : sK0) : (wave == 2 ? sV0 : sV1),
-                a.o + ((size_t)(tr.tok0 + rt.i0w) * a.Hq + rt.h) * D, (long long)a.Hq * D, tr.L - rt.i0w, lane);
+  uint16_t* buf = wave < 2 ? (wave ? sK1 : sK0) : (wave == 2 ? sV0 : sV1);
+  const size_t row0 = ((size_t)(tr.tok0 + rt.i0w) * a.Hq + rt.h) * D;
+  store_rows<D>(acc, inv, buf, a.o + row0, (long long)a.Hq * D, tr.L - rt.i0w, lane);
+  if (WIN && a.o_rem) store_remainders<D>(acc, inv, buf, a.o_rem + row0, (long long)a.Hq * D, tr.L - rt.i0w, lane);
   if (row_ok && half == 0)
     a.lse[lse_index(a.varlen, a.ntok, a.Hq, a.T, rt.b, rt.h, tr.tok0, i)] =
         (m_run + __log2f(l_tot)) * 0.6931471805599453f;
@@ -540,10 +582,11 @@ fwd_kernel(RowArgs a) {
 
 // ---------------------------------------------------------------- backward: Delta = rowsum(dO * O), stored as -Delta
 // Also writes LSE * log2(e), the form in which the backward kernels use it.
-// The first nks workgroups take the key-tile statistics instead (a launch less
+// REM: of the O that o and the remainders of its rounding make.  The first nks workgroups take the key-tile statistics instead (a launch less
 // ahead of the backward's main kernels).
-template <int D>
-__global__ void __launch_bounds__(256) bwd_pre_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict__ dout,
+template <int D, bool REM>
+__global__ void __launch_bounds__(256) bwd_pre_kernel(const uint16_t* __restrict__ o, const int8_t* __restrict__ o_rem,
+                                                      const uint16_t* __restrict__ dout,
                                                       const float* __restrict__ lse, float* __restrict__ delta,
                                                       float* __restrict__ lse2, int ntok, int Hq, int T, int varlen,
                                                       const int* __restrict__ evict, const int* __restrict__ cu,
@@ -561,7 +604,7 @@ __global__ void __launch_bounds__(256) bwd_pre_kernel(const uint16_t* __restrict
     const size_t off = (size_t)row * D + sub * PER;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-      const float x = (float)__builtin_bit_cast(__bf16, o[off + e]);
+      const float x = __uint_as_float(((uint32_t)o[off + e] << 16) + (REM ? (uint32_t)(int)o_rem[off + e] << 8 : 0u));
       const float y = (float)__builtin_bit_cast(__bf16, dout[off + e]);
       s += x * y;
     }
@@ -1344,6 +1387,7 @@ static RowArgs row_args(const Problem& p, const int2* kstats) {
   a.cu = p.cu;
   a.kstats = kstats;
   a.o = (uint16_t*)p.o;
+  a.o_rem = p.o_rem;
   a.lse = p.lse;
   a.dout = (const uint16_t*)p.dout;
   a.lse_in = p.lse_in;
@@ -1402,14 +1446,11 @@ hipError_t launch_bwd_pre(const Problem& p, int2* kstats, float* delta) {
   const int nks = pg.with_kstats ? kstats_groups(p.T) * p.B : 0;
   dim3 grid(pg.blocks), block(256);
   prof_begin("bwd_pre", p.stream);
-  if (p.D == 128)
-    hipLaunchKernelGGL(bwd_pre_kernel<128>, grid, block, 0, p.stream, (const uint16_t*)p.o_in,
-                       (const uint16_t*)p.dout, p.lse_in, delta, lse2, p.ntok, p.Hq, p.T, (int)(p.cu != nullptr),
-                       p.evict, p.cu, nks, kstats, key_window(p));
-  else
-    hipLaunchKernelGGL(bwd_pre_kernel<64>, grid, block, 0, p.stream, (const uint16_t*)p.o_in,
-                       (const uint16_t*)p.dout, p.lse_in, delta, lse2, p.ntok, p.Hq, p.T, (int)(p.cu != nullptr),
-                       p.evict, p.cu, nks, kstats, key_window(p));
+  const auto kernel = p.o_rem_in ? (p.D == 128 ? bwd_pre_kernel<128, true> : bwd_pre_kernel<64, true>)
+                                 : (p.D == 128 ? bwd_pre_kernel<128, false> : bwd_pre_kernel<64, false>);
+  hipLaunchKernelGGL(kernel, grid, block, 0, p.stream, (const uint16_t*)p.o_in, p.o_rem_in, (const uint16_t*)p.dout,
+                     p.lse_in, delta, lse2, p.ntok, p.Hq, p.T, (int)(p.cu != nullptr), p.evict, p.cu, nks, kstats,
+                     key_window(p));
   prof_end(p.stream);
   return hipGetLastError();
 }

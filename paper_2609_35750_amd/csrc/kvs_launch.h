@@ -19,6 +19,8 @@ struct Problem {
   const int32_t* cu;     // NULL: fixed length
   void* o;               // forward output
   float* lse;            // forward output
+  int8_t* o_rem;         // forward output of windowed calls: what O's rounding takes; NULL: not kept
+  const int8_t* o_rem_in;   // the backward's; NULL: Delta of the rounded O
   void* dq;
   void* dk;
   void* dv;

@@ -50,6 +50,9 @@ SIGNATURES = {
     "kvs_window_attn_bwd_workspace": (_Z, [_I, _I, _I, _I, _I, _I]),
     "kvs_window_attn_bwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                                  _I, _I, _I, _I, _I, _I, _F, _I, _I, _P, _Z, _P]),
+    "kvs_window_attn_fwd_rem": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _F, _I, _I, _P, _Z, _P]),
+    "kvs_window_attn_bwd_rem": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                     _I, _I, _I, _I, _I, _I, _F, _I, _I, _P, _Z, _P]),
     "kvs_key_weights_workspace": (_Z, [_I, _I, _I, _I, _I, _I, _I]),
     "kvs_key_weights": (_I, [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _F, _I, _I, _I, _P, _Z, _P]),
     "kvs_classify_tiles": (_I, [_P, _P, _I, _I, _I, _I, _P, _P]),
@@ -302,52 +305,64 @@ def _like(t, ref, name):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(ref.shape)}")
 
 
+def _rem_like(rem, q):
+    if rem is not None:
+        if rem.dtype != torch.int8:
+            raise ValueError("the remainders of O must be int8")
+        _like(rem, q, "the remainders of O")
+
+
 def kvs_window_attn_fwd(q, k, v, window: int, sinks: int = 0, evict_at=None, softmax_scale=None, cu_seqlens=None,
-                        max_seqlen=None, out=None, lse=None, check_cu=True) -> Tuple[torch.Tensor, torch.Tensor]:
+                        max_seqlen=None, out=None, lse=None, check_cu=True,
+                        rem=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Forward of attention under a sliding window with sinks; returns ``(O, LSE)``.
 
     Query i sees key j iff ``j <= i``, ``i < evict_at[j]`` (if given) and ``i - j < window or j < sinks``.
     Layouts as in ``kvs_evict_attn_fwd``; ``check_cu=False`` skips the host's look at ``cu_seqlens`` (a
-    synchronisation, which a stream that is being captured does not take).
+    synchronisation, which a stream that is being captured does not take).  ``rem`` (int8, O's shape) receives what
+    O's rounding takes, for a backward whose Delta is that of the unrounded O.
     """
     out = torch.empty_like(q) if out is None else out
-    B, n, T, Hq, Hkv, D, scale, lse_shape = _window_args((k, v, evict_at, cu_seqlens, out, lse), (q, k, v, out), (), q, k,
-                                                         evict_at, cu_seqlens, max_seqlen, softmax_scale, check_cu)
+    B, n, T, Hq, Hkv, D, scale, lse_shape = _window_args((k, v, evict_at, cu_seqlens, out, lse, rem), (q, k, v, out), (), q,
+                                                         k, evict_at, cu_seqlens, max_seqlen, softmax_scale, check_cu)
     if lse is None:
         lse = torch.empty(lse_shape, dtype=torch.float32, device=q.device)
     if tuple(lse.shape) != lse_shape or lse.dtype != torch.float32:
         raise ValueError(f"LSE must be float32 {lse_shape}")
     _like(v, k, "V")
     _like(out, q, "O")
+    _rem_like(rem, q)
     nws = lib.kvs_window_attn_fwd_workspace(B, n, T, Hq, Hkv, D)
     ws = _workspace(nws, q.device)
     with _on(q):
-        st = lib.kvs_window_attn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(evict_at), _ptr(cu_seqlens), _ptr(out), _ptr(lse),
-                                     B, n, T, Hq, Hkv, D, scale, _i31(window), _i31(sinks), _ptr(ws), nws, _stream(q))
+        st = lib.kvs_window_attn_fwd_rem(_ptr(q), _ptr(k), _ptr(v), _ptr(evict_at), _ptr(cu_seqlens), _ptr(out), _ptr(rem),
+                                         _ptr(lse), B, n, T, Hq, Hkv, D, scale, _i31(window), _i31(sinks), _ptr(ws), nws,
+                                         _stream(q))
     _check("kvs_window_attn_fwd", st)
     return out, lse
 
 
 def kvs_window_attn_bwd(do, q, k, v, o, lse, window: int, sinks: int = 0, evict_at=None, softmax_scale=None,
-                        cu_seqlens=None, max_seqlen=None, dq=None, dk=None, dv=None,
-                        check_cu=True) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
-    """Backward of ``kvs_window_attn_fwd``; returns ``(dQ, dK, dV)`` (bf16)."""
+                        cu_seqlens=None, max_seqlen=None, dq=None, dk=None, dv=None, check_cu=True,
+                        rem=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Backward of ``kvs_window_attn_fwd``; returns ``(dQ, dK, dV)`` (bf16).  ``rem``: the forward's."""
     dq = torch.empty_like(q) if dq is None else dq
     dk = torch.empty_like(k) if dk is None else dk
     dv = torch.empty_like(v) if dv is None else dv
-    B, n, T, Hq, Hkv, D, scale, lse_shape = _window_args((do, k, v, o, lse, evict_at, cu_seqlens, dq, dk, dv),
+    B, n, T, Hq, Hkv, D, scale, lse_shape = _window_args((do, k, v, o, lse, evict_at, cu_seqlens, dq, dk, dv, rem),
                                                          (do, q, k, v, o, dq, dk, dv), (lse,), q, k, evict_at,
                                                          cu_seqlens, max_seqlen, softmax_scale, check_cu)
     if tuple(lse.shape) != lse_shape:
         raise ValueError(f"LSE must be float32 {lse_shape}")
     for t, ref, name in ((do, q, "dO"), (o, q, "O"), (dq, q, "dQ"), (v, k, "V"), (dk, k, "dK"), (dv, k, "dV")):
         _like(t, ref, name)
+    _rem_like(rem, q)
     nws = lib.kvs_window_attn_bwd_workspace(B, n, T, Hq, Hkv, D)
     ws = _workspace(nws, q.device)
     with _on(q):
-        st = lib.kvs_window_attn_bwd(_ptr(do), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(evict_at),
-                                     _ptr(cu_seqlens), _ptr(dq), _ptr(dk), _ptr(dv), B, n, T, Hq, Hkv, D, scale,
-                                     _i31(window), _i31(sinks), _ptr(ws), nws, _stream(q))
+        st = lib.kvs_window_attn_bwd_rem(_ptr(do), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(rem), _ptr(lse),
+                                         _ptr(evict_at), _ptr(cu_seqlens), _ptr(dq), _ptr(dk), _ptr(dv), B, n, T, Hq, Hkv,
+                                         D, scale, _i31(window), _i31(sinks), _ptr(ws), nws, _stream(q))
     _check("kvs_window_attn_bwd", st)
     return dq, dk, dv
 
@@ -477,8 +492,10 @@ def _refuse_captured(nodes) -> None:
 class _WindowAttn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, window, sinks, evict_at, scale, cu_seqlens, max_seqlen, check_cu):
-        o, lse = kvs_window_attn_fwd(q, k, v, window, sinks, evict_at, scale, cu_seqlens, max_seqlen, check_cu=check_cu)
-        ctx.save_for_backward(q, k, v, o, lse, evict_at, cu_seqlens)
+        rem = torch.empty_like(q, dtype=torch.int8) if any(ctx.needs_input_grad[:3]) else None
+        o, lse = kvs_window_attn_fwd(q, k, v, window, sinks, evict_at, scale, cu_seqlens, max_seqlen, check_cu=check_cu,
+                                     rem=rem)
+        ctx.save_for_backward(q, k, v, o, rem, lse, evict_at, cu_seqlens)
         ctx.args = window, sinks, scale, max_seqlen
         ctx.mark_non_differentiable(lse)
         ctx.set_materialize_grads(False)   # LSE carries no gradient: no zeros filled for it
@@ -491,14 +508,14 @@ class _WindowAttn(torch.autograd.Function):
 
 
 def _window_grads(ctx, do):
-    q, k, v, o, lse, evict_at, cu_seqlens = ctx.saved_tensors
+    q, k, v, o, rem, lse, evict_at, cu_seqlens = ctx.saved_tensors
     window, sinks, scale, max_seqlen = ctx.args
     if torch.cuda.is_current_stream_capturing():
         _refuse_captured(ctx.next_functions)
     do = torch.zeros_like(o) if do is None else do
     # cu_seqlens is the forward's, which has checked it
     dq, dk, dv = kvs_window_attn_bwd(do.contiguous(), q, k, v, o, lse, window, sinks, evict_at, scale, cu_seqlens,
-                                     max_seqlen, check_cu=False)
+                                     max_seqlen, check_cu=False, rem=rem)
     return dq, dk, dv, None, None, None, None, None, None, None
 
 

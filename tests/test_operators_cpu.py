@@ -229,3 +229,16 @@ def test_backward_under_capture_refuses_leaves_of_an_eager_graph(kvs):
 def test_scales_that_are_not_finite(kvs):
     for scale in (float("inf"), float("-inf"), float("nan"), 0.0, -1.0):
         assert _wfwd(kvs, scale=scale) == SHAPE, scale
+
+
+def test_remainders_are_checked(kvs):
+    L, need = kvs.lib, kvs.lib.kvs_window_attn_bwd_workspace(2, 120, 60, 4, 2, 64)
+    assert L.kvs_window_attn_fwd_rem(FAKE, FAKE, FAKE, None, None, FAKE, FAKE + 8, FAKE, 2, 120, 60, 4, 2, 64, 0.1, 8, 2,
+                                     FAKE, need, None) == ALIGN
+    assert L.kvs_window_attn_bwd_rem(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE + 4, FAKE, None, None, FAKE, FAKE, FAKE, 2, 120, 60,
+                                     4, 2, 64, 0.1, 8, 2, FAKE, need, None) == ALIGN
+    q = torch.zeros(1, 8, 4, 64).bfloat16()
+    with pytest.raises(ValueError, match="int8"):
+        kvs._rem_like(torch.zeros(1, 8, 4, 64), q)
+    with pytest.raises(ValueError, match="shape"):
+        kvs._rem_like(torch.zeros(1, 8, 2, 64, dtype=torch.int8), q)
