@@ -151,7 +151,8 @@ struct DecodeArgs {
   // so that a store instruction of a wave writes G x 32 bytes in a row
   float* scores;
   const int* tile_base;   // [S + 1]: first tile of each sequence (more than kPlanSeqs sequences)
-  int tiles;              // rows of scores
+  int tiles;              // rows of scores; where the tables list more tiles, the last one takes all that have no row
+  int D;
   float scale_log2;       // softmax_scale * log2(e)
   // window (kPicks)
   const int* q_pos;       // [S]
@@ -938,6 +939,7 @@ static DecodeArgs decode_args(const PagedDecode& p, const int* table, const int*
   a.Hq = p.Hq;
   a.Hkv = p.Hkv;
   a.G = p.Hq / p.Hkv;
+  a.D = p.D;
   a.max_blocks = width;
   a.BS = p.block_size;
   a.gran = gran;
@@ -1114,6 +1116,30 @@ __global__ void __launch_bounds__(1024) paged_tile_base_kernel(DecodeArgs a, int
   if (tid == 0) out[a.S] = base;
 }
 
+// slot_weight[slot] += sum_h exp(s_h - LSE_h) for the slots of the sequence's tile at c0, the scores taken from K again:
+// of a tile that found no row.  Slots that exist have rows for all of them, so this is met only under tables that list
+// many entries outside the cache, and is not made fast: a slot at a time, a lane a q-head.
+__device__ void add_weights_from_k(const DecodeArgs& a, int s, int c0, int ns, int lane, float* __restrict__ slot_weight) {
+  for (int r = 0; r < kDecTile && r < ns - c0; ++r) {
+    const int c = c0 + r, entry = a.table[(size_t)s * a.max_blocks + c / a.BS], row = c % a.BS;
+    if ((unsigned)entry >= (unsigned)a.num_blocks) continue;
+    const int slot = entry * a.BS + row;
+    if (a.slot_pos[slot] < 0) continue;
+    float x = 0.f;
+    for (int h = lane; h < a.Hq; h += kWave) {
+      const uint16_t* q = a.q + ((size_t)s * a.Hq + h) * a.D;
+      const uint16_t* k = a.kc + (((size_t)entry * a.Hkv + h / a.G) * a.BS + row) * a.D;
+      float dot = 0.f;
+      for (int d = 0; d < a.D; ++d)
+        dot = __builtin_fmaf(__uint_as_float((uint32_t)q[d] << 16), __uint_as_float((uint32_t)k[d] << 16), dot);
+      x += __builtin_amdgcn_exp2f(__builtin_fmaf(dot, a.scale_log2, -a.lse[(size_t)s * a.Hq + h] * 1.4426950408889634f));
+    }
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) x += __shfl_xor(x, off);
+    if (lane == 0) slot_weight[slot] += x;
+  }
+}
+
 // slot_weight[slot] += sum_h exp(s_h - LSE_h) over all q-heads, once LSE is
 // known.  One wave a tile of scores: 8 lanes read a head's 32 scores as float4,
 // the 64 lanes 8 heads at a time, and the heads are added in one order, so
@@ -1137,8 +1163,10 @@ __global__ void __launch_bounds__(256) paged_weight_kernel(DecodeArgs a, float* 
     __syncthreads();
     base = sBase;
   }
-  const int total = min(base[a.S], a.tiles), waves = gridDim.x * 4, w = blockIdx.x * 4 + wave;
-  const int per = (total + waves - 1) / waves, t0 = min(w * per, total), t1 = min(t0 + per, total);
+  const int listed = base[a.S], rows = listed <= a.tiles ? listed : a.tiles - 1;   // tiles with a row of their own
+  const int total = MODE == kTable ? listed : rows, waves = gridDim.x * 4, w = blockIdx.x * 4 + wave;
+  const int per = total / waves + (total % waves > 0);
+  const int t0 = (int)min((long long)w * per, (long long)total), t1 = (int)min((long long)t0 + per, (long long)total);
   if (t0 >= t1) return;
   int s = 0;   // the last sequence that begins at or before tile t0
   for (int step = 1 << (31 - __builtin_clz(a.S)); step > 0; step >>= 1)
@@ -1146,6 +1174,10 @@ __global__ void __launch_bounds__(256) paged_weight_kernel(DecodeArgs a, float* 
   const int quad = lane & 7, h0 = lane >> 3;   // this lane's slots 4 quad .. + 3 of the tile, its first head
   for (int t = t0; t < t1; ++t) {
     while (s + 1 < a.S && base[s + 1] <= t) ++s;
+    if (MODE == kTable && t >= rows) {
+      add_weights_from_k(a, s, (t - base[s]) * kDecTile, slots_of(a, s), lane, slot_weight);
+      continue;
+    }
     const int ns = slots_of(a, s), picked = MODE == kPicks ? a.picked[(size_t)t * kDecTile + 4 * quad + (h0 & 3)] : 0;
     if (MODE == kPicks && __ballot(picked >= 0) == 0ull) continue;
     // place 4 quad of q-head h: [h / G][quad / 2][h % G][4 (quad % 2)]
@@ -1186,7 +1218,7 @@ __global__ void __launch_bounds__(256) paged_weight_kernel(DecodeArgs a, float* 
 // Workspace of the decode under a window and with weights, in this order.
 struct ExSpace {
   int cap;             // slots listed a sequence (window)
-  long long tiles;     // rows of scores (weights): every sequence's slots in tiles; no slot belongs to two sequences
+  long long tiles;     // rows of scores (weights)
   size_t list, counts, base, scores, units;   // list: of all tiles of scores, if the decode's waves pick
   size_t bytes() const { return list + counts + base + scores + units; }
 };
@@ -1200,20 +1232,28 @@ static bool picks(const PagedDecode& p) {
   return p.window > 0 &&
          p.S * tiles <= (long long)kPickTiles * paged_units(p.S, p.Hkv, p.max_blocks, p.block_size, p.D);
 }
+// Tiles that all tables, or lists, could hold.
+static long long paged_ex_tiles(const PagedDecode& p) {
+  const long long width = (long long)p.max_blocks * p.block_size;
+  const long long each = p.window > 0 && !picks(p) ? std::min(width, (long long)p.window + p.sinks) : width;
+  return p.S * ((each + kDecTile - 1) / kDecTile);
+}
 static ExSpace ex_space(const PagedDecode& p) {
   ExSpace x{};
   const long long width = (long long)p.max_blocks * p.block_size;
-  long long each = width;
   const bool lists = p.window > 0 && !picks(p);
   if (lists) {
     x.cap = (int)std::min(width, (long long)p.window + p.sinks);
     x.list = round256((size_t)p.S * x.cap * sizeof(int));
     x.counts = round256((size_t)p.S * sizeof(int));
-    each = x.cap;
   }
   if (p.weights) {
-    x.tiles = std::min(p.S * ((each + kDecTile - 1) / kDecTile),
-                       (long long)p.num_blocks * p.block_size / kDecTile + p.S);
+    // Every sequence's slots in tiles; no slot belongs to two sequences, so of slots that exist there are no more than
+    // the cache has.  A table may list entries outside it as well: all their tiles have rows too where the waves pick
+    // (16 tiles a unit at most), lists hold none, and else one row more takes the scores that find none of their own
+    // (the tables' whole width may be many times the cache).
+    const long long cached = (long long)p.num_blocks * p.block_size / kDecTile + p.S, listed = paged_ex_tiles(p);
+    x.tiles = picks(p) ? listed : std::min(listed, lists ? cached : cached + 1);
     x.base = p.S > kPlanSeqs ? round256((size_t)(p.S + 1) * sizeof(int)) : 0;
     x.scores = round256((size_t)x.tiles * p.Hq * kDecTile * sizeof(float));
     if (picks(p)) x.list = round256((size_t)x.tiles * kDecTile * sizeof(int));

@@ -1,0 +1,36 @@
+"""Workspaces of the weighted decode under tables that list entries outside the cache (no GPU)."""
+import os
+
+import pytest
+
+LIB = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_35750_amd", "libkvs.so")
+pytestmark = pytest.mark.skipif(not os.path.exists(LIB), reason="libkvs.so not built (run __graft_entry__.build())")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2609_35750_amd import kvs
+
+    return kvs.lib
+
+
+def _scores(lib, S, Hq, Hkv, D, nb, mb, bs, window):
+    """Bytes the weights add to a call's workspace."""
+    return (lib.kvs_paged_decode_ex_workspace(S, Hq, Hkv, D, nb, mb, bs, window, 0, 1) -
+            lib.kvs_paged_decode_ex_workspace(S, Hq, Hkv, D, nb, mb, bs, window, 0, 0))
+
+
+@pytest.mark.parametrize("S,mb", [(1, 12), (4, 60), (20, 8)])
+def test_picked_slots_have_rows_for_all_listed_tiles(lib, S, mb):
+    """Four blocks of 16 slots, tables of many more entries: every tile a wave may pick from has its scores and slots."""
+    tiles = S * -(-mb * 16 // 32)
+    assert tiles > 4 * 16 // 32 + S
+    assert _scores(lib, S, 4, 2, 128, 4, mb, 16, 8) >= tiles * 32 * 4 * (4 + 1)
+
+
+def test_without_a_window_one_row_more_than_the_cache_fills(lib):
+    """A row takes the scores of all tiles beyond those the cache's slots make; wide tables cost nothing more."""
+    row = 4 * 32 * 4
+    rows = 4 * 16 // 32 + 1
+    assert (rows + 1) * row <= _scores(lib, 1, 4, 2, 128, 4, 12, 16, 0) < (rows + 2) * row + 256
+    assert _scores(lib, 1, 4, 2, 128, 4, 12, 16, 0) == _scores(lib, 1, 4, 2, 128, 4, 1 << 16, 16, 0)
