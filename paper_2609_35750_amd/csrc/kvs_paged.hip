@@ -394,13 +394,19 @@ __global__ void __launch_bounds__(1024) paged_plan_kernel(DecodeArgs a) {
 // measured 20% slower on the 64-rollout decode.
 constexpr int kDecRing = 2;
 
+// Tiles of a sequence as rows of scores are numbered: those of all its slots, also beyond kTileCap, where the plan's
+// count ends.
+__device__ __forceinline__ int score_tiles(const DecodeArgs& a, int s) {
+  return (int)(((unsigned)slots_of(a, s) + kDecTile - 1) / kDecTile);
+}
+
 // First row of scores of sequence s: its tiles follow those of the sequences before it.
 __device__ __forceinline__ int tile_base(const DecodeArgs& a, int s, int lane) {
   if (a.tile_base) return a.tile_base[s];
   int base = 0;
   for (int k = 0; k * kWave <= s; ++k) {
     const int i = k * kWave + lane;
-    const int t = i < s ? plan_tiles(slots_of(a, i)) : 0;
+    const int t = i < s ? score_tiles(a, i) : 0;
     base += wave_last(wave_scan(t));
   }
   return base;
@@ -1101,7 +1107,7 @@ __global__ void __launch_bounds__(1024) paged_tile_base_kernel(DecodeArgs a, int
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int base = 0;
   for (int s0 = 0; s0 < a.S; s0 += 1024) {
-    const int s = s0 + tid, t = s < a.S ? plan_tiles(slots_of(a, s)) : 0, incl = wave_scan(t);
+    const int s = s0 + tid, t = s < a.S ? score_tiles(a, s) : 0, incl = wave_scan(t);
     if (lane == kWave - 1) wsum[wave] = incl;
     __syncthreads();
     int first = base + incl - t;
@@ -1152,7 +1158,7 @@ __global__ void __launch_bounds__(256) paged_weight_kernel(DecodeArgs a, float* 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int* base = a.tile_base;
   if (!base) {   // at most kPlanSeqs sequences, one a thread
-    const int t = (int)threadIdx.x < a.S ? plan_tiles(slots_of(a, threadIdx.x)) : 0, incl = wave_scan(t);
+    const int t = (int)threadIdx.x < a.S ? score_tiles(a, threadIdx.x) : 0, incl = wave_scan(t);
     if (lane == kWave - 1) wsum[wave] = incl;
     __syncthreads();
     int end = incl;
