@@ -474,7 +474,9 @@ kvs_status_t kvs_paged_decode(const void* Q, const void* K_cache, const void* V_
  * slot_weight not NULL: slot_weight[slot] += sum_h exp(s_h - LSE_h) over all
  * q-heads, for every entry the query sees.  Limits and layouts are those of
  * kvs_paged_decode (under a window at most 65535 sequences of at most 2^30
- * slots, max_blocks * block_size); the workspace is the query's, `weights`
+ * slots, max_blocks * block_size; with slot_weight fewer than 2^31 tiles of 32
+ * slots in all tables, num_seqs * ceil(max_blocks * block_size / 32), or under a
+ * window in all lists of at most window + sinks slots); the workspace is the query's, `weights`
  * nonzero for calls with slot_weight. */
 size_t kvs_paged_decode_ex_workspace(int num_seqs, int Hq, int Hkv, int D, int num_blocks, int max_blocks,
                                      int block_size, int window, int sinks, int weights);

@@ -895,6 +895,8 @@ kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void*
                                        slot_weight != nullptr);
   if (window > 0 && num_seqs > 65535) return fail(KVS_ERR_UNSUPPORTED, "more than 65535 sequences under a window");
   if ((long long)Hkv * kvs::paged_ex_units(p) > 0x7fffffffll) return fail(KVS_ERR_UNSUPPORTED, "decode grid too large");
+  if (p.weights && kvs::paged_ex_tiles(p) > 0x7fffffffll)
+    return fail(KVS_ERR_UNSUPPORTED, "weights of tables of 2^31 tiles of 32 slots or more");
   REQUIRE_PTR(Q, "Q");
   REQUIRE_PTR(K_cache, "K_cache");
   REQUIRE_PTR(V_cache, "V_cache");

@@ -158,6 +158,7 @@ hipError_t launch_paged_decode(const PagedDecode& p);
 // The decode under a window and with weights (either, or neither): workspace, launches.
 size_t paged_ex_ws_bytes(const PagedDecode& p);
 long long paged_ex_units(const PagedDecode& p);   // of the decode grid, per KV head
+long long paged_ex_tiles(const PagedDecode& p);   // 32-slot tiles that all tables, or lists, could hold
 hipError_t launch_paged_decode_ex(const PagedDecode& p);
 
 // Eviction of the entries of lowest weight (after host-side validation).

@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(1024) paged_plan_kernel(DecodeArgs a) {
 constexpr int kDecRing = 2;
 
 // Tiles of a sequence as rows of scores are numbered: those of all its slots, also beyond kTileCap, where the plan's
-// count ends.
+// count ends.  All sequences' together fit 31 bits (the call refuses more).
 __device__ __forceinline__ int score_tiles(const DecodeArgs& a, int s) {
   return (int)(((unsigned)slots_of(a, s) + kDecTile - 1) / kDecTile);
 }
@@ -1239,7 +1239,7 @@ static bool picks(const PagedDecode& p) {
          p.S * tiles <= (long long)kPickTiles * paged_units(p.S, p.Hkv, p.max_blocks, p.block_size, p.D);
 }
 // Tiles that all tables, or lists, could hold.
-static long long paged_ex_tiles(const PagedDecode& p) {
+long long paged_ex_tiles(const PagedDecode& p) {
   const long long width = (long long)p.max_blocks * p.block_size;
   const long long each = p.window > 0 && !picks(p) ? std::min(width, (long long)p.window + p.sinks) : width;
   return p.S * ((each + kDecTile - 1) / kDecTile);

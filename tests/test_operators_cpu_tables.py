@@ -34,3 +34,19 @@ def test_without_a_window_one_row_more_than_the_cache_fills(lib):
     rows = 4 * 16 // 32 + 1
     assert (rows + 1) * row <= _scores(lib, 1, 4, 2, 128, 4, 12, 16, 0) < (rows + 2) * row + 256
     assert _scores(lib, 1, 4, 2, 128, 4, 12, 16, 0) == _scores(lib, 1, 4, 2, 128, 4, 1 << 16, 16, 0)
+
+
+def test_more_tiles_than_31_bits_number_are_refused(lib):
+    """Tables as wide as 65,536 sequences of 2^20 slots: their tiles' numbers would leave 32-bit integers."""
+    fake = 1 << 20
+
+    def dec(S, mb, weight, window=0):
+        need = lib.kvs_paged_decode_ex_workspace(S, 4, 1, 64, 64, mb, 64, window, 0, weight is not None)
+        return lib.kvs_paged_decode_ex(fake, fake, fake, fake, weight, fake, fake, fake if window else None, None, fake, S, 4,
+                                       1, 64, 64, 64, mb, 0.1, window, 0, fake, need, None)
+    null, unsupported = 1, 7      # with everything else in order the missing O is what is found
+    assert dec(65536, 1 << 14, fake) == unsupported and b"tiles" in lib.kvs_last_error()
+    assert dec(65535, 1 << 14, fake) == null
+    assert dec(65536, 1 << 14, None) == null            # without weights no tile is numbered
+    assert dec(64, 1 << 24, fake, 1 << 30) == unsupported
+    assert dec(64, 1 << 24, fake, 4096) == null         # the window bounds what is listed
