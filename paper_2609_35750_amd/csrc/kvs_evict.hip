@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kEvictThreads) paged_evict_lowest_kernel(Paged
     hi = lo + min(hi - lo, (1u << shift) - 1u);
     turn ^= 1;
   }
-  for (int i = go + tid; i < a.max_out; i += kEvictThreads) out[i] = -1;
+  for (long long i = (long long)go + tid; i < a.max_out; i += kEvictThreads) out[i] = -1;   // max_out: up to INT32_MAX
   if (tid == 0) a.counts[s] = go;
   if (go == 0) return;
 
