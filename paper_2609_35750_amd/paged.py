@@ -212,6 +212,8 @@ def kvs_paged_evict_lowest(slot_weight, slot_pos, block_table, seq_blocks, keep,
     if block_table.dim() != 2 or seq_blocks.shape != (block_table.shape[0],) or keep.shape != seq_blocks.shape:
         raise ValueError("block_table must be [S, max_blocks], seq_blocks and keep [S]")
     _int32(slot_pos, block_table, seq_blocks, keep)
+    if max_out is not None and max_out > 0x7FFFFFFF:
+        raise ValueError("max_out must fit 32 bits")
     if block_size < 1 or slot_pos.numel() % block_size:
         raise ValueError("slot_pos must hold num_blocks * block_size entries")
     if slot_weight.dtype != torch.float32 or slot_weight.numel() != slot_pos.numel():

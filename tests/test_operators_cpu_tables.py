@@ -50,3 +50,15 @@ def test_more_tiles_than_31_bits_number_are_refused(lib):
     assert dec(65536, 1 << 14, None) == null            # without weights no tile is numbered
     assert dec(64, 1 << 24, fake, 1 << 30) == unsupported
     assert dec(64, 1 << 24, fake, 4096) == null         # the window bounds what is listed
+
+
+def test_counts_beyond_32_bits_are_refused_not_cut():
+    """A list of 2^32 + 5 positions would be taken for one of 5, its rows for rows of 5."""
+    import torch
+
+    from paper_2609_35750_amd import paged
+
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    for most in (1 << 31, (1 << 32) + 5):
+        with pytest.raises(ValueError, match="max_out"):
+            paged.kvs_paged_evict_lowest(torch.zeros(48), i32(48), i32(1, 2), i32(1), i32(1), 16, max_out=most)
