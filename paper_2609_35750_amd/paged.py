@@ -137,6 +137,10 @@ def kvs_paged_append_weighted(k_new, v_new, w_new, positions, slots, k_cache, v_
     nb = k_cache.shape[0]
     if v_new.shape != k_new.shape or positions.shape != (n,) or slots.shape != (n,):
         raise ValueError("k_new, v_new, positions and slots do not match")
+    if k_cache.shape != (nb, Hkv, block_size, D) or v_cache.shape != k_cache.shape or slot_pos.numel() != nb * block_size:
+        raise ValueError("the caches must be [num_blocks, Hkv, block_size, D] with k_new's Hkv and D, slot_pos one entry a slot")
+    if any(t.dtype != torch.bfloat16 for t in (k_new, v_new, k_cache, v_cache)):
+        raise ValueError("k_new, v_new and the caches must be bfloat16")
     if slot_weight.dtype != torch.float32 or slot_weight.numel() != nb * block_size:
         raise ValueError("slot_weight must be float32 with num_blocks * block_size entries")
     if w_new is not None and (w_new.dtype != torch.float32 or w_new.shape != (n,)):
@@ -263,6 +267,8 @@ class PagedKVCache:
         pos = _i32(positions)
         if k_new.shape != (pos.size, self.Hkv, self.D) or v_new.shape != k_new.shape:
             raise ValueError("k_new/v_new must be [n, Hkv, D]")
+        if k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16:
+            raise ValueError("k_new/v_new must be bfloat16")
         if weights is not None:
             if self.slot_weight is None:
                 raise ValueError("the cache keeps no weights (weights=True)")

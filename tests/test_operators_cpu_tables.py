@@ -62,3 +62,28 @@ def test_counts_beyond_32_bits_are_refused_not_cut():
     for most in (1 << 31, (1 << 32) + 5):
         with pytest.raises(ValueError, match="max_out"):
             paged.kvs_paged_evict_lowest(torch.zeros(48), i32(48), i32(1, 2), i32(1), i32(1), 16, max_out=most)
+
+
+def test_weighted_append_checks_the_caches():
+    """Entries of other sizes or types than the cache's would be read and written out of range."""
+    import torch
+
+    from paper_2609_35750_amd import paged
+
+    b16 = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    good = dict(k_new=b16(3, 2, 64), v_new=b16(3, 2, 64), k_cache=b16(4, 2, 16, 64), v_cache=b16(4, 2, 16, 64),
+                slot_pos=i32(64), block_size=16)
+    for bad, match in ((dict(k_new=b16(3, 4, 64), v_new=b16(3, 4, 64)), "Hkv"), (dict(v_cache=b16(4, 1, 16, 64)), "Hkv"),
+                       (dict(k_new=b16(3, 2, 128), v_new=b16(3, 2, 128)), "Hkv"), (dict(slot_pos=i32(63)), "slot_pos"),
+                       (dict(k_new=torch.zeros(3, 2, 64, dtype=torch.int8)), "bfloat16"),
+                       (dict(v_cache=torch.zeros(4, 2, 16, 64)), "bfloat16"), ({}, "GPU")):
+        a = {**good, **bad}
+        with pytest.raises(ValueError, match=match):
+            paged.kvs_paged_append_weighted(a["k_new"], a["v_new"], None, i32(3), i32(3), a["k_cache"], a["v_cache"],
+                                            a["slot_pos"], torch.zeros(64), a["block_size"])
+    for weights in (False, True):
+        cache = paged.PagedKVCache(4, 16, 1, 2, 2, 64, device="cpu", weights=weights)
+        with pytest.raises(ValueError, match="bfloat16"):
+            cache.append(0, [0, 1, 2], b16(3, 2, 64), torch.zeros(3, 2, 64, dtype=torch.int8))
+        assert cache.bm.live(0) == 0
