@@ -275,7 +275,8 @@ class PagedKVCache:
             if weights.shape != (pos.size,) or weights.dtype != torch.float32:
                 raise ValueError("weights must be float32 [n]")
             weights = weights.contiguous()
-            _ptr(weights)
+        if pos.size:   # before the manager reserves the slots
+            _same_device(self.k, k_new, v_new, weights)
         slots = self.bm.append(seq, pos)
         if pos.size:
             k_new, v_new = k_new.contiguous(), v_new.contiguous()

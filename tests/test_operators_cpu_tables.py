@@ -87,3 +87,21 @@ def test_weighted_append_checks_the_caches():
         with pytest.raises(ValueError, match="bfloat16"):
             cache.append(0, [0, 1, 2], b16(3, 2, 64), torch.zeros(3, 2, 64, dtype=torch.int8))
         assert cache.bm.live(0) == 0
+
+
+def test_refused_append_leaves_the_manager_as_it_was():
+    """Tensors that are not where the cache is are refused before slots are reserved for them."""
+    import torch
+
+    from paper_2609_35750_amd import paged
+
+    cache = paged.PagedKVCache(4, 16, 1, 2, 2, 64, device="cpu", weights=True)
+    k = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    for w in (None, torch.zeros(3)):
+        with pytest.raises(ValueError, match="GPU"):
+            cache.append(0, [0, 1, 2], k, k, weights=w)
+        assert cache.bm.live(0) == 0 and cache.bm.free_blocks() == 4
+    cache.k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16, device="meta")
+    with pytest.raises(ValueError, match="one device"):
+        cache.append(0, [0, 1, 2], k, k)
+    assert cache.bm.live(0) == 0
