@@ -254,8 +254,8 @@ class PagedKVCache:
         self.bm = BlockManager(num_blocks, block_size, num_seqs, max_blocks)
         self.num_blocks, self.block_size, self.num_seqs, self.max_blocks = num_blocks, block_size, num_seqs, max_blocks
         self.Hkv, self.D = Hkv, D
-        self.device = torch.device(device)
-        self.k = torch.zeros((num_blocks, Hkv, block_size, D), dtype=torch.bfloat16, device=self.device)
+        self.k = torch.zeros((num_blocks, Hkv, block_size, D), dtype=torch.bfloat16, device=device)
+        self.device = self.k.device   # with its index: another one may be the current one later
         self.v = torch.zeros_like(self.k)
         self.slot_pos = torch.full((num_blocks * block_size,), -1, dtype=torch.int32, device=self.device)
         self.slot_weight = torch.zeros(num_blocks * block_size, dtype=torch.float32, device=self.device) if weights else None
@@ -280,36 +280,38 @@ class PagedKVCache:
         slots = self.bm.append(seq, pos)
         if pos.size:
             k_new, v_new = k_new.contiguous(), v_new.contiguous()
-            if self.slot_weight is None:
-                name = "kvs_paged_append_host"
-                st = lib.kvs_paged_append_host(_ptr(k_new), _ptr(v_new), _np_ptr(pos), _np_ptr(slots), pos.size,
-                                               _ptr(self.k), _ptr(self.v), _ptr(self.slot_pos), self.num_blocks,
-                                               self.block_size, self.Hkv, self.D, _stream(self.k))
-            else:
-                name = "kvs_paged_append_weighted_host"
-                st = lib.kvs_paged_append_weighted_host(
-                    _ptr(k_new), _ptr(v_new), _ptr(weights), _np_ptr(pos), _np_ptr(slots), pos.size, _ptr(self.k),
-                    _ptr(self.v), _ptr(self.slot_pos), _ptr(self.slot_weight), self.num_blocks, self.block_size,
-                    self.Hkv, self.D, _stream(self.k))
-            if st == KVS_ERR_UNSUPPORTED:   # too many runs of slots for the launch's arguments, or under capture
-                dev_pos, dev_slots = torch.from_numpy(pos).to(self.device), torch.from_numpy(slots).to(self.device)
+            with _on(self.k):
                 if self.slot_weight is None:
-                    kvs_paged_append(k_new, v_new, dev_pos, dev_slots, self.k, self.v, self.slot_pos, self.block_size)
+                    name = "kvs_paged_append_host"
+                    st = lib.kvs_paged_append_host(_ptr(k_new), _ptr(v_new), _np_ptr(pos), _np_ptr(slots), pos.size,
+                                                   _ptr(self.k), _ptr(self.v), _ptr(self.slot_pos), self.num_blocks,
+                                                   self.block_size, self.Hkv, self.D, _stream(self.k))
                 else:
-                    kvs_paged_append_weighted(k_new, v_new, weights, dev_pos, dev_slots, self.k, self.v, self.slot_pos,
-                                              self.slot_weight, self.block_size)
-            else:
-                _check(name, st)
+                    name = "kvs_paged_append_weighted_host"
+                    st = lib.kvs_paged_append_weighted_host(
+                        _ptr(k_new), _ptr(v_new), _ptr(weights), _np_ptr(pos), _np_ptr(slots), pos.size, _ptr(self.k),
+                        _ptr(self.v), _ptr(self.slot_pos), _ptr(self.slot_weight), self.num_blocks, self.block_size,
+                        self.Hkv, self.D, _stream(self.k))
+                if st == KVS_ERR_UNSUPPORTED:   # too many runs of slots for the launch's arguments, or under capture
+                    dev_pos, dev_slots = torch.from_numpy(pos).to(self.device), torch.from_numpy(slots).to(self.device)
+                    if self.slot_weight is None:
+                        kvs_paged_append(k_new, v_new, dev_pos, dev_slots, self.k, self.v, self.slot_pos, self.block_size)
+                    else:
+                        kvs_paged_append_weighted(k_new, v_new, weights, dev_pos, dev_slots, self.k, self.v, self.slot_pos,
+                                                  self.slot_weight, self.block_size)
+                else:
+                    _check(name, st)
         self._tables = None
         return slots
 
     def _mark_evicted(self, slots: np.ndarray) -> None:
-        st = lib.kvs_paged_evict_host(_np_ptr(slots), slots.size, _ptr(self.slot_pos), self.num_blocks,
-                                      self.block_size, _stream(self.slot_pos))
-        if st == KVS_ERR_UNSUPPORTED:
-            kvs_paged_evict(torch.from_numpy(slots).to(self.device), self.slot_pos, self.num_blocks, self.block_size)
-        else:
-            _check("kvs_paged_evict_host", st)
+        with _on(self.slot_pos):
+            st = lib.kvs_paged_evict_host(_np_ptr(slots), slots.size, _ptr(self.slot_pos), self.num_blocks,
+                                          self.block_size, _stream(self.slot_pos))
+            if st == KVS_ERR_UNSUPPORTED:
+                kvs_paged_evict(torch.from_numpy(slots).to(self.device), self.slot_pos, self.num_blocks, self.block_size)
+            else:
+                _check("kvs_paged_evict_host", st)
 
     def evict(self, seq: int, positions) -> np.ndarray:
         slots = self.bm.evict(seq, _i32(positions))
@@ -346,7 +348,8 @@ class PagedKVCache:
         """
         table, nblk = self.device_tables()
         if window is None and not accumulate:
-            return kvs_paged_decode(q, self.k, self.v, self.slot_pos, table, nblk, softmax_scale, out, lse)
+            with _on(self.k):
+                return kvs_paged_decode(q, self.k, self.v, self.slot_pos, table, nblk, softmax_scale, out, lse)
         if accumulate and self.slot_weight is None:
             raise ValueError("the cache keeps no weights (weights=True)")
         if positions is not None and not torch.is_tensor(positions):

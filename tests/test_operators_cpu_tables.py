@@ -105,3 +105,58 @@ def test_refused_append_leaves_the_manager_as_it_was():
     with pytest.raises(ValueError, match="one device"):
         cache.append(0, [0, 1, 2], k, k)
     assert cache.bm.live(0) == 0
+
+
+def test_cache_calls_run_with_its_device_current(monkeypatch):
+    """Every call of a cache into the library is made with the cache's device as the current one."""
+    import contextlib
+
+    import numpy as np
+    import torch
+
+    from paper_2609_35750_amd import paged
+
+    inside, calls = [0], []
+
+    @contextlib.contextmanager
+    def on(t):
+        inside[0] += 1
+        yield
+        inside[0] -= 1
+
+    class Lib:
+        """The library's host side; its calls for the GPU are recorded. Host lists are declined, so that the
+        calls behind them are seen too."""
+        def __getattr__(self, name):
+            real = getattr(paged_lib, name)
+            if name.startswith("kvs_bm_") or name.endswith("_workspace"):
+                return real
+
+            def call(*a):
+                calls.append((name, inside[0]))
+                return paged.KVS_ERR_UNSUPPORTED if name.endswith("_host") else 0
+            return call
+    paged_lib = paged.lib
+    cache = paged.PagedKVCache(8, 16, 1, 8, 2, 64, device="cpu", weights=True)
+    plain = paged.PagedKVCache(8, 16, 1, 8, 2, 64, device="cpu")
+    for name, to in (("lib", Lib()), ("_on", on), ("_ptr", lambda t: 1 << 20), ("_stream", lambda t: 0),
+                     ("_same_device", lambda *t: None)):
+        monkeypatch.setattr(paged, name, to)
+    k, q = torch.zeros(30, 2, 64, dtype=torch.bfloat16), torch.zeros(1, 4, 64, dtype=torch.bfloat16)
+    for c in (cache, plain):
+        c.append(0, np.arange(30), k, k)
+        c.evict(0, [3, 5])
+        c.decode(q)
+        c.decode(q, positions=[30], window=8)
+    cache.decode(q, accumulate=True)
+    pos, counts = torch.tensor([[1, 2]], dtype=torch.int32), torch.tensor([2], dtype=torch.int32)
+    made = paged.kvs_paged_evict_lowest
+    monkeypatch.setattr(paged, "kvs_paged_evict_lowest", lambda *a: (made(*a), (pos, counts))[1])
+    assert [g.tolist() for g in cache.evict_lowest(26)] == [[1, 2]]
+    for c in (cache, plain):
+        c.release(0)
+    names = {n for n, _ in calls}
+    assert names >= {"kvs_paged_append_host", "kvs_paged_append", "kvs_paged_append_weighted_host",
+                     "kvs_paged_append_weighted", "kvs_paged_evict_host", "kvs_paged_evict", "kvs_paged_decode",
+                     "kvs_paged_decode_ex", "kvs_paged_evict_lowest"}
+    assert all(depth >= 1 for _, depth in calls), [n for n, depth in calls if depth < 1]
