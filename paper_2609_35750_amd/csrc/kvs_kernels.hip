@@ -626,7 +626,6 @@ __global__ void __launch_bounds__(256) bwd_pre_kernel(const uint16_t* __restrict
 // of the dQ kernel, which fill its tail, walk the 32-key groups of dV and dK of
 // all of them.  Bound by reading the partials, so every thread keeps several
 // parts' loads in flight; the sums are turned in LDS and stored as whole rows.
-constexpr int kReduceGrid = 512;
 struct ReduceArgs {
   const PlanCtl* ctl;     // NULL: nothing is split
   const int* plan;
@@ -1512,12 +1511,18 @@ hipError_t launch_bwd_main(const Problem& p, const int2* kstats, const float* de
   r.delta = delta;
   r.lse_in = a.lse;
   const int nblk = (int)((long long)r.nqt * p.B * p.Hkv * p.nhg);
-  const ReduceArgs ra{cap ? ctl : nullptr, plan, split, a.part, a.dk, a.dv, a.nkt, nblk};
+  const bool tail = cap > 0 && sums_fit_dq(nblk);
+  ReduceArgs ra{tail ? ctl : nullptr, plan, split, a.part, a.dk, a.dv, a.nkt, nblk};
   prof_begin("bwd_dq", p.stream);
   const auto kernel = p.window > 0 ? (p.D == 128 ? dq_kernel<128, true> : dq_kernel<64, true>)
                                    : (p.D == 128 ? dq_kernel<128, false> : dq_kernel<64, false>);
-  hipLaunchKernelGGL(kernel, dim3(nblk + (cap ? kReduceGrid : 0)), dim3(64 * p.HG * p.TC), 0, p.stream, r, ra);
+  hipLaunchKernelGGL(kernel, dim3(nblk + (tail ? kReduceGrid : 0)), dim3(64 * p.HG * p.TC), 0, p.stream, r, ra);
   prof_end(p.stream);
+  e = hipGetLastError();
+  if (e != hipSuccess || cap == 0 || tail) return e;
+  ra.ctl = ctl;
+  ra.first = 0;   // all workgroups add up
+  hipLaunchKernelGGL(kernel, dim3(kReduceGrid), dim3(64 * p.HG * p.TC), 0, p.stream, r, ra);
   return hipGetLastError();
 }
 

@@ -62,6 +62,11 @@ inline PreGrid bwd_pre_grid(long long rows, long long kstats_blocks) {
   return {(unsigned)(both ? blocks + kstats_blocks : blocks), both};
 }
 
+// Grid of the dQ kernel: its row workgroups of 256 threads and, where a launch of at most 2^32 - 1 threads holds both, those
+// that add up the split key blocks behind them.  Else the sums have a launch of their own.
+constexpr int kReduceGrid = 512;
+inline bool sums_fit_dq(long long row_blocks) { return (row_blocks + kReduceGrid) * 256 <= 0xffffffffll; }
+
 // Launchers.  Each returns the hipError_t of its launch(es).
 hipError_t launch_kstats(const Problem& p, int2* kstats);
 hipError_t launch_fwd(const Problem& p, const int2* kstats);
