@@ -1412,6 +1412,8 @@ static RowArgs row_args(const Problem& p, const int2* kstats) {
 
 constexpr int kMaxTraces = 65535;   // keeps every grid and workgroup index within 31 bits
 
+static long long row_blocks(const Problem& p, const RowArgs& a) { return (long long)a.nqt * p.B * p.Hkv * p.nhg; }
+
 static KeyWindow key_window(const Problem& p) { return {p.window, p.sinks, p.until}; }
 
 hipError_t launch_kstats(const Problem& p, int2* kstats) {
@@ -1425,7 +1427,8 @@ hipError_t launch_kstats(const Problem& p, int2* kstats) {
 
 hipError_t launch_fwd(const Problem& p, const int2* kstats) {
   RowArgs a = row_args(p, kstats);
-  const long long nblk = (long long)a.nqt * p.B * p.Hkv * p.nhg;
+  const long long nblk = row_blocks(p, a);
+  if (!row_blocks_fit(nblk)) return hipErrorInvalidConfiguration;
   dim3 grid((unsigned)nblk), block(64 * p.HG * p.TC);   // 4 waves
   prof_begin("fwd", p.stream);
   const auto kernel = p.window > 0 ? (p.D == 128 ? fwd_kernel<128, true> : fwd_kernel<64, true>)
@@ -1458,12 +1461,17 @@ hipError_t launch_bwd_pre(const Problem& p, int2* kstats, float* delta) {
 
 // dK and dV, and dQ, whose last workgroups add up what the first has split.
 hipError_t launch_bwd_main(const Problem& p, const int2* kstats, const float* delta, void* split_ws, size_t split_bytes) {
+  RowArgs r = row_args(p, kstats);
+  const long long rows = row_blocks(p, r);
+  if (!row_blocks_fit(rows)) return hipErrorInvalidConfiguration;
+  r.delta = delta;
+  r.lse_in = (const float*)((const char*)delta + half_delta_bytes(p.Hq, p.ntok));   // LSE * log2(e)
   ColArgs a{};
   a.q = (const uint16_t*)p.q;
   a.k = (const uint16_t*)p.k;
   a.v = (const uint16_t*)p.v;
   a.dout = (const uint16_t*)p.dout;
-  a.lse = (const float*)((const char*)delta + half_delta_bytes(p.Hq, p.ntok));   // LSE * log2(e)
+  a.lse = r.lse_in;
   a.delta = delta;
   a.evict = p.until ? p.until : p.evict;
   a.cu = p.cu;
@@ -1507,10 +1515,7 @@ hipError_t launch_bwd_main(const Problem& p, const int2* kstats, const float* de
   prof_end(p.stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  RowArgs r = row_args(p, kstats);
-  r.delta = delta;
-  r.lse_in = a.lse;
-  const int nblk = (int)((long long)r.nqt * p.B * p.Hkv * p.nhg);
+  const int nblk = (int)rows;
   const bool tail = cap > 0 && sums_fit_dq(nblk);
   ReduceArgs ra{tail ? ctl : nullptr, plan, split, a.part, a.dk, a.dv, a.nkt, nblk};
   prof_begin("bwd_dq", p.stream);

@@ -65,6 +65,7 @@ inline PreGrid bwd_pre_grid(long long rows, long long kstats_blocks) {
 // Grid of the dQ kernel: its row workgroups of 256 threads and, where a launch of at most 2^32 - 1 threads holds both, those
 // that add up the split key blocks behind them.  Else the sums have a launch of their own.
 constexpr int kReduceGrid = 512;
+inline bool row_blocks_fit(long long row_blocks) { return row_blocks * 256 <= 0xffffffffll; }
 inline bool sums_fit_dq(long long row_blocks) { return (row_blocks + kReduceGrid) * 256 <= 0xffffffffll; }
 
 // Launchers.  Each returns the hipError_t of its launch(es).

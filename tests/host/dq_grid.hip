@@ -7,7 +7,8 @@
 int main() {
   const long long most = 0xffffffffll / 256;   // workgroups of a launch
   for (long long rows = most - 2 * kvs::kReduceGrid; rows <= most; ++rows)
-    if (kvs::sums_fit_dq(rows) != (rows + kvs::kReduceGrid <= most)) {
+    if (!kvs::row_blocks_fit(rows) || kvs::row_blocks_fit(rows + 2 * kvs::kReduceGrid + 1) ||
+        kvs::sums_fit_dq(rows) != (rows + kvs::kReduceGrid <= most)) {
       std::printf("%lld row workgroups\n", rows);
       return 1;
     }
