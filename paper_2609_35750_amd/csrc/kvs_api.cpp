@@ -417,7 +417,7 @@ kvs_status_t kvs_window_attn_fwd_rem(const void* Q, const void* K, const void* V
 }
 
 size_t kvs_window_attn_bwd_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D) {
-  if (B < 1 || Ntot < 0 || Hq < 1 || Hkv < 1 || max_seqlen < 1) return 0;
+  if (B < 1 || Ntot < 0 || Hq < 1 || Hkv < 1 || max_seqlen < 1 || max_seqlen > kMaxSeq) return 0;
   return until_bytes(Ntot) + bwd_ws(B, max_seqlen, Ntot, Hq, Hkv, D);
 }
 
@@ -463,7 +463,7 @@ static int rows_counted(int last_rows, int max_seqlen) {
 }
 
 size_t kvs_key_weights_workspace(int B, int Ntot, int max_seqlen, int Hq, int Hkv, int D, int last_rows) {
-  if (B < 1 || Ntot < 0 || Hq < 1 || Hkv < 1 || max_seqlen < 1) return 0;
+  if (B < 1 || Ntot < 0 || Hq < 1 || Hkv < 1 || max_seqlen < 1 || max_seqlen > kMaxSeq) return 0;
   (void)D;
   return until_bytes(Ntot) + fwd_ws(B, Ntot) +
          kvs::ws_weights_bytes(B, max_seqlen, Ntot, Hq, Hkv, rows_counted(last_rows, max_seqlen));

@@ -287,7 +287,7 @@ def _window_args(tensors, bf16, fp32, q, k, evict_at, cu_seqlens, max_seqlen, so
     if cu_seqlens is not None:
         if max_seqlen is None:
             raise ValueError("max_seqlen is required with cu_seqlens")
-        T = int(max_seqlen)
+        T = _i31(max_seqlen)
     if k.shape[:-2] != q.shape[:-2] or k.shape[-1] != D:
         raise ValueError(f"shape mismatch: q {tuple(q.shape)}, k {tuple(k.shape)}")
     if evict_at is not None and evict_at.shape != q.shape[:-2]:

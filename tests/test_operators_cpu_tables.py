@@ -160,3 +160,25 @@ def test_cache_calls_run_with_its_device_current(monkeypatch):
                      "kvs_paged_append_weighted", "kvs_paged_evict_host", "kvs_paged_evict", "kvs_paged_decode",
                      "kvs_paged_decode_ex", "kvs_paged_evict_lowest"}
     assert all(depth >= 1 for _, depth in calls), [n for n, depth in calls if depth < 1]
+
+
+def test_lengths_beyond_32_bits_are_not_cut(monkeypatch):
+    """A bound of 2^32 + 4 tokens would be taken for one of 4, and every trace cut to it."""
+    import torch
+
+    from paper_2609_35750_amd import kvs
+
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True)
+    q, k = torch.zeros(8, 4, 64, dtype=torch.bfloat16), torch.zeros(8, 2, 64, dtype=torch.bfloat16)
+    cu = torch.tensor([0, 8], dtype=torch.int32)
+    for mx, T in ((8, 8), ((1 << 32) + 4, 2 ** 31 - 1), (1 << 31, 2 ** 31 - 1)):
+        got = kvs._window_args((), (), (), q, k, None, cu, mx, None, True)
+        assert got[2] == T
+    # the calls refuse such a bound, and the queries do not compute with it
+    assert kvs.lib.kvs_window_attn_bwd_workspace(1, 8, 2 ** 31 - 1, 4, 2, 64) == 0
+    assert kvs.lib.kvs_key_weights_workspace(1, 8, 2 ** 31 - 1, 4, 2, 64, 0) == 0
+    fake = 1 << 20
+    assert kvs.lib.kvs_window_attn_bwd(fake, fake, fake, fake, fake, fake, None, fake, fake, fake, fake, 1, 8, 2 ** 31 - 1, 4,
+                                       2, 64, 0.1, 8, 0, fake, 0, None) == 7
+    assert kvs.lib.kvs_key_weights(fake, fake, fake, None, fake, fake, 1, 8, 2 ** 31 - 1, 4, 2, 64, 0.1, 0, 0, 0, fake, 0,
+                                   None) == 7
