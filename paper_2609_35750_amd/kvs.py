@@ -118,9 +118,13 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr()
 
 
+# The current stream's handle alone; no public name gives it, so a torch without this one makes the Stream object
+# (2 us on every call's way to the GPU).
+_RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(t: torch.Tensor):
-    # current_stream() makes a Stream object, 2 us on every call's way to the GPU
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+    return torch.cuda.current_stream(t.device).cuda_stream if _RAW_STREAM is None else _RAW_STREAM(t.device.index)
 
 
 def _workspace(nbytes: int, device) -> torch.Tensor:

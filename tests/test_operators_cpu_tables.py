@@ -182,3 +182,19 @@ def test_lengths_beyond_32_bits_are_not_cut(monkeypatch):
                                        2, 64, 0.1, 8, 0, fake, 0, None) == 7
     assert kvs.lib.kvs_key_weights(fake, fake, fake, None, fake, fake, 1, 8, 2 ** 31 - 1, 4, 2, 64, 0.1, 0, 0, 0, fake, 0,
                                    None) == 7
+
+
+def test_stream_handle_without_the_private_name(monkeypatch):
+    """A torch that lacks the name for the raw handle gives the same stream through its public calls."""
+    import types
+
+    import torch
+
+    from paper_2609_35750_amd import kvs
+
+    t = types.SimpleNamespace(device=types.SimpleNamespace(index=3))
+    monkeypatch.setattr(kvs, "_RAW_STREAM", lambda i: 100 + i)
+    assert kvs._stream(t) == 103
+    monkeypatch.setattr(kvs, "_RAW_STREAM", None)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d: types.SimpleNamespace(cuda_stream=200 + d.index))
+    assert kvs._stream(t) == 203
