@@ -416,7 +416,11 @@ kvs_status_t kvs_paged_evict_host(const int32_t* slots, int n, int32_t* slot_pos
  * meaning.  Caches of several layers that share one block manager may share
  * one slot_weight (each layer's decode then adds to the sum), on one stream.
  * Calls that take it expect every block in the table of at most one sequence,
- * once; otherwise the weights are unspecified (nothing else is). */
+ * once.  Otherwise the weights are unspecified, and with them what
+ * kvs_paged_evict_lowest evicts: under shared blocks one sequence's evictions may
+ * also change the live entries that another one's are counted from.  Nothing
+ * outside the tables' blocks and the outputs is written even then, and a
+ * decode's O and LSE do not depend on weights. */
 
 /* kvs_paged_append and kvs_paged_append_host for such a cache: also
  * slot_weight[slots[t]] = W_new[t] (device fp32 [n], e.g. from kvs_key_weights), or 0 if W_new is NULL. */
@@ -437,7 +441,8 @@ kvs_status_t kvs_paged_append_weighted_host(const void* K_new, const void* V_new
  * evicted slots becomes -1; their positions go to positions[s][0..counts[s])
  * (device int32 [num_seqs][max_out], in the table's order, the rest -1), for
  * kvs_bm_evict.  Tables are clamped as in the decode; num_seqs is at most 65535,
- * max_blocks * block_size at most 2^30, and the product of all three below 2^32.
+ * max_blocks * block_size at most 2^30, and num_seqs * (max_blocks * block_size +
+ * 255) below 2^32.
  * The workspace query may give 0 (workspace NULL then). */
 size_t kvs_paged_evict_lowest_workspace(int num_seqs, int max_blocks, int block_size);
 kvs_status_t kvs_paged_evict_lowest(const float* slot_weight, int32_t* slot_pos, const int32_t* block_table,

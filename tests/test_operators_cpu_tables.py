@@ -198,3 +198,15 @@ def test_stream_handle_without_the_private_name(monkeypatch):
     monkeypatch.setattr(kvs, "_RAW_STREAM", None)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda d: types.SimpleNamespace(cuda_stream=200 + d.index))
     assert kvs._stream(t) == 203
+
+
+def test_eviction_limits_are_the_documented_ones(lib):
+    """num_seqs * (max_blocks * block_size + 255) below 2^32, at the line."""
+    fake = 1 << 20
+
+    def ev(S, mb):
+        return lib.kvs_paged_evict_lowest(fake, fake, fake, fake, None, fake, fake, S, 64, 1, mb, 0, 0, 4, None, 0, None)
+    null, unsupported = 1, 7      # keep is missing: what is found when the sizes are in order
+    for S in (1, 5, 65535):
+        mb = min((2 ** 32 - 1) // S - 255, 1 << 30)
+        assert ev(S, mb) == null and ev(S, mb + 1) == unsupported
