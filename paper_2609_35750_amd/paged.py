@@ -343,8 +343,9 @@ class PagedKVCache:
         """One query a sequence, q [num_seqs, Hq, D]; returns (O, LSE).
 
         ``window`` (with ``positions``, the queries' trace positions: a list or an int32 tensor on the GPU) shows each
-        query the entries less than ``window`` behind it and the first ``sinks``; ``accumulate`` adds the entries'
-        attention weights to ``slot_weight``.
+        query the entries less than ``window`` behind it and the first ``sinks``; without a window every live entry is
+        seen, and ``positions`` and ``sinks`` have no effect (layers of both kinds take the same call).  ``accumulate``
+        adds the entries' attention weights to ``slot_weight``.
         """
         table, nblk = self.device_tables()
         if window is None and not accumulate:
