@@ -623,7 +623,8 @@ __global__ void __launch_bounds__(256) bwd_pre_kernel(const uint16_t* __restrict
 
 // Sum of the parts' partials of split key blocks, in part order; dK scaled.
 // The split blocks are listed by the plan, and the last kReduceGrid workgroups
-// of the dQ kernel, which fill its tail, walk the 32-key groups of dV and dK of
+// of the dQ kernel, which fill its tail (a launch of their own where the row
+// workgroups leave no room, sums_fit_dq), walk the 32-key groups of dV and dK of
 // all of them.  Bound by reading the partials, so every thread keeps several
 // parts' loads in flight; the sums are turned in LDS and stored as whole rows.
 struct ReduceArgs {
