@@ -336,7 +336,7 @@ __device__ __forceinline__ void store_rows(const f32x16* acc, float sc, uint16_t
 // 127).  With the rounded O, dQ and dK of short rows are 1.5 to 1.7 times as
 // far from the exact ones as those, rounded, are; with this 1.4 to 1.5, what
 // dS in bf16 leaves.  Bound by the byte a value more to write and read: 24 short
-// traces 331 -> 346 us a step, one of 16k 2,082 -> 2,098.  Rows as in
+// traces 313 -> 328 us a step, one of 16k 2,060 -> 2,079.  Rows as in
 // store_rows, behind it.
 template <int D>
 __device__ __forceinline__ void store_remainders(const f32x16* acc, float sc, uint16_t* buf, int8_t* __restrict__ dst,

@@ -437,7 +437,7 @@ __device__ __forceinline__ void store_b128_uncounted(float* dst, float4 v) {
 // picks()).  SCORES: the tile's raw scores are stored (four stores a step, counted in the waits like the copies), 4 Hq bytes
 // a slot beside 4 Hkv D of K and V: 3% more at G = 4, D = 128, where reading K
 // once more for the weights when LSE is known would be 50%.  64 rollouts of 4,096
-// entries (32/8 heads): 174 -> 215 us.  It is the writes' way to memory: stores
+// entries (32/8 heads): 171 -> 216 us.  It is the writes' way to memory: stores
 // to the same few lines cost 4 us, a quarter of them 20, and issuing them a step
 // later, behind the next copies, changes nothing.
 enum DecodeMode : int { kTable = 0, kList = 1, kPicks = 2 };

@@ -16,16 +16,21 @@
 // two products (with one, the four SIMDs would ask for all of the LDS
 // bandwidth), and the products of the two are the two chains that keep the
 // matrix core fed.  Chunks cut long columns into items of about equal length
-// without a plan; their sums are added, heads and chunks in order, by a second
-// kernel, so the result does not depend on the order in which the workgroups run.
+// without a plan (by the trace's length: under a window the block with the
+// sinks, which all rows see, has far longer items than the others); their sums
+// are added, heads and chunks in order, by a second kernel, so the result does
+// not depend on the order in which the workgroups run.
 //
-// Bound by what matrix core and vector unit can do at once: 16 products and 96
-// vector operations of a wave for every 32 rows x 64 keys.  16k trace with
-// evicted segments (32/8 heads, D = 128): 544 us, 885 TFLOP/s, where a large
-// matrix product reaches 1,336; without the exponentials 526, without the
-// copies 514 (kernels of 128 keys x 128 rows).  Two waves a SIMD that hold two
-// pairs of accumulators, the exponentials of one between the products of the
-// other, are no faster (559) than these three that take turns; 128 keys a
+// 16 products and 96 vector operations of a wave for every 32 rows x 64 keys. 
+// 16k trace with evicted segments (32/8 heads, D = 128): 498 us of a call of
+// 506, 966 TFLOP/s, where a large matrix product reaches 1,336.  The matrix
+// core is busy for 44% of the time and the vector unit for 56%, at 2.0 GHz, as
+// if the two took turns; which of their instructions or waits keeps them apart
+// is not known: an earlier form, of 128 keys x 128 rows, took 544 us, 526
+// without the exponentials and 514 without the copies.  Other forms, each
+// measured beside the one of its time (the last of those 542): two waves a
+// SIMD that hold two pairs of accumulators, the exponentials of one between
+// the products of the other, 559, no faster than these three; 128 keys a
 // workgroup, twice the copies, 590; class and addresses found for every step
 // and LSE scaled on the way to LDS 757.
 #include "kvs_device.h"
