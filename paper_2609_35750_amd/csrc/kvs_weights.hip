@@ -21,17 +21,17 @@
 // are added, heads and chunks in order, by a second kernel, so the result does
 // not depend on the order in which the workgroups run.
 //
-// 16 products and 96 vector operations of a wave for every 32 rows x 64 keys. 
+// 16 products and 96 vector operations of a wave for every 32 rows x 64 keys.
 // 16k trace with evicted segments (32/8 heads, D = 128): 498 us of a call of
-// 506, 966 TFLOP/s, where a large matrix product reaches 1,336.  The matrix
-// core is busy for 44% of the time and the vector unit for 56%, at 2.0 GHz, as
-// if the two took turns; which of their instructions or waits keeps them apart
-// is not known: an earlier form, of 128 keys x 128 rows, took 544 us, 526
-// without the exponentials and 514 without the copies.  Other forms, each
-// measured beside the one of its time (the last of those 542): two waves a
-// SIMD that hold two pairs of accumulators, the exponentials of one between
-// the products of the other, 559, no faster than these three; 128 keys a
-// workgroup, twice the copies, 590; class and addresses found for every step
+// 506, 966 TFLOP/s, where a large matrix product reaches 1,336. Bound by the
+// sum of its parts, which do not hide each other: the matrix core is busy for
+// 44% of the time and the vector unit for 56%, at 2.0 GHz, and of 528 us
+// (passes without pause) the call loses 73 without the exponentials, 45
+// without the copies and 181 without seven in eight of the products. Other
+// forms, each measured beside the one of its time (the last of those 542): two
+// waves a SIMD that hold two pairs of accumulators, the exponentials of one
+// between the products of the other, 559, no faster than these three; 128 keys
+// a workgroup, twice the copies, 590; class and addresses found for every step
 // and LSE scaled on the way to LDS 757.
 #include "kvs_device.h"
 #include "kvs_launch.h"
