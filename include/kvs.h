@@ -307,7 +307,7 @@ kvs_status_t kvs_check_evict_at(const int32_t* evict_at, const int32_t* cu_seqle
  * Per-kernel timing for benchmarks.  While enabled, each call brackets every
  * kernel it launches with HIP events on the call's stream.  kvs_prof_read
  * waits for the recorded events and returns, for the kernel named `name`
- * ("classify", "fwd", "bwd_pre", "bwd_dkdv", "bwd_dq", "key_weights", "paged_decode", "paged_evict_lowest"), the
+ * ("classify", "fwd", "bwd_pre", "bwd_dkdv", "bwd_dq", "key_weights", "paged_decode", "paged_decode_shared", "paged_extend", "paged_evict_lowest"), the
  * number of launches and their total duration in milliseconds.  The records
  * are process-wide (every thread's launches land in one list, guarded by a
  * lock), so enable timing only while the calls to be timed are the only
@@ -366,11 +366,15 @@ kvs_status_t kvs_bm_append(kvs_block_manager* bm, int seq, const int32_t* pos, i
 /* Evict the entries of sequence seq at trace positions pos[0..n); slots[i]
  * receives the slot that held pos[i] (pass them to kvs_paged_evict).  Blocks
  * left without a live entry return to the free list and leave the sequence's
- * table.  All-or-nothing; KVS_ERR_STATE if a position is not cached or repeated. */
+ * table.  All-or-nothing; KVS_ERR_STATE if a position is not cached or repeated,
+ * or if it lies in a block that other sequences hold too (kvs_bm_fork) and that
+ * seq keeps other entries of: see kvs_bm_evict_shared.  slots[i] is -1 where a
+ * shared block leaves seq's table as a whole (kvs_paged_evict skips it). */
 kvs_status_t kvs_bm_evict(kvs_block_manager* bm, int seq, const int32_t* pos, int n, int32_t* slots);
 
 /* Drop sequence seq entirely: writes its live slots (sorted; `slots` must hold
- * kvs_bm_live(bm, seq) entries) and their count, and frees all its blocks. */
+ * kvs_bm_live(bm, seq) entries) and their count, and frees all its blocks.  Blocks
+ * that other sequences hold too stay theirs, and their slots are not among them. */
 kvs_status_t kvs_bm_release(kvs_block_manager* bm, int seq, int32_t* slots, int* n_slots);
 
 /* Host copies of block_table [num_seqs][max_blocks] (unused entries 0) and seq_blocks [num_seqs]. */
@@ -379,6 +383,52 @@ kvs_status_t kvs_bm_tables(const kvs_block_manager* bm, int32_t* block_table, in
 /* Free blocks; live entries of sequence seq (-1 for a bad index or NULL manager). */
 int kvs_bm_free_blocks(const kvs_block_manager* bm);
 int kvs_bm_live(const kvs_block_manager* bm, int seq);
+
+/* ---- sequences that share blocks
+ * Rollouts of one prompt, or branches of one rollout, hold the same entries up
+ * to where they part.  A slot has one position and one live mark, so all
+ * sequences that hold a block see the same entries of it: a shared block is
+ * appended to by none of them, and what one of them evicts there leaves its own
+ * table alone.  Caches that keep weights of the entries (below) have them for one
+ * sequence each: use kvs_bm_copy there, not kvs_bm_fork.
+ *
+ * The empty sequence dst gets the table and the entries of src; nothing is
+ * copied.  Later appends of either open a new block.  KVS_ERR_STATE if dst holds
+ * blocks. */
+kvs_status_t kvs_bm_fork(kvs_block_manager* bm, int src, int dst);
+
+/* kvs_bm_evict for sequences with shared blocks.  Such a block leaves seq's table
+ * if seq evicts all its entries; if some stay, a fresh block takes its place in
+ * the table, for copies of those: slot from[i] goes to slot to[i], i < *n_copies
+ * (kvs_paged_copy; from, to: kvs_bm_live(bm, seq) entries each).  slots[i] is the
+ * slot that held pos[i] as in kvs_bm_evict, and -1 for an entry in a shared block,
+ * which the others keep.  All-or-nothing; KVS_ERR_CAPACITY if there is no free
+ * block for the copies. */
+kvs_status_t kvs_bm_evict_shared(kvs_block_manager* bm, int seq, const int32_t* pos, int n, int32_t* slots,
+                                 int32_t* from, int32_t* to, int* n_copies);
+
+/* The empty sequence dst gets copies of the entries of src, in order of their
+ * positions, in as few fresh blocks as hold them: slot from[i] goes to slot
+ * to[i], i < *n (kvs_paged_copy; from, to: kvs_bm_live(bm, src) entries each). */
+kvs_status_t kvs_bm_copy(kvs_block_manager* bm, int src, int dst, int32_t* from, int32_t* to, int* n);
+
+/* Entries of seq move together: of the blocks that it holds alone (but for a last
+ * one with room for appends) the fullest stay, as many as hold the entries of all
+ * of them, and the others' entries move to free rows there; the blocks left empty
+ * return to the free list.  Slot from[i] goes to slot to[i], i < *n (kvs_paged_copy
+ * with move; no slot is both; from, to: kvs_bm_live(bm, seq) entries each).  *n is
+ * 0 where no block would be saved. */
+kvs_status_t kvs_bm_compact(kvs_block_manager* bm, int seq, int32_t* from, int32_t* to, int* n);
+
+/* Groups for kvs_paged_decode_shared: prefix_group [num_seqs] and prefix_blocks
+ * (at most num_seqs entries; host arrays), and their number.  All sequences whose
+ * tables begin alike are one group, or those among them that are alike for longer,
+ * whichever saves more reads of blocks. */
+kvs_status_t kvs_bm_groups(const kvs_block_manager* bm, int32_t* prefix_group, int32_t* prefix_blocks,
+                           int* num_groups);
+
+/* Blocks of sequence seq that other sequences hold too (-1 for a bad index or NULL manager). */
+int kvs_bm_shared(const kvs_block_manager* bm, int seq);
 
 /* ---- device updates (enqueued on `stream`) */
 
@@ -407,6 +457,16 @@ kvs_status_t kvs_paged_append_host(const void* K_new, const void* V_new, const i
                                    int num_blocks, int block_size, int Hkv, int D, void* stream);
 kvs_status_t kvs_paged_evict_host(const int32_t* slots, int n, int32_t* slot_pos, int num_blocks, int block_size,
                                   void* stream);
+
+/* Copy n entries: slot dst[i] takes the K and V rows of slot src[i] and, where
+ * slot_pos and slot_weight are not NULL, its position and its weight; with move
+ * nonzero slot_pos[src[i]] becomes -1.  src, dst: device int32 [n].  No slot may be
+ * twice in dst, or in both (the contents of such slots are unspecified then).  A
+ * pair with a slot outside the cache is skipped.  Caches of several layers that
+ * share slot_pos: pass it with the last layer's only. */
+kvs_status_t kvs_paged_copy(const int32_t* src, const int32_t* dst, int n, void* K_cache, void* V_cache,
+                            int32_t* slot_pos, float* slot_weight, int move, int num_blocks, int block_size, int Hkv,
+                            int D, void* stream);
 
 /* ---- weights of the entries
  * A cache may keep a weight for every entry, fp32 slot_weight [num_blocks *
@@ -490,6 +550,46 @@ kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void*
                                  const int32_t* q_pos, void* O, float* LSE, int num_seqs, int Hq, int Hkv, int D,
                                  int num_blocks, int block_size, int max_blocks, float softmax_scale, int window,
                                  int sinks, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The decode of sequences that share the beginning of their tables (rollouts of
+ * one prompt), whose common entries are read once for all of them.  Q, O, LSE, the
+ * caches and the tables are those of kvs_paged_decode, and so are the results.
+ * prefix_group (device int32 [num_seqs]): the group of each sequence, in [0,
+ * num_groups) (anything else: none); prefix_blocks (device int32 [num_groups]): how
+ * many leading table entries the members of each group have in common
+ * (kvs_bm_groups gives both).  The library takes them as they are: only the first
+ * member's table is read there, up to its seq_blocks, and results are unspecified
+ * where another member's begins differently.
+ * Supported: D in {64, 128}; Hq / Hkv <= 64; block_size in [1, 64]; max_blocks *
+ * block_size <= 2^30; num_blocks * block_size * Hkv <= 2^32 (num_blocks *
+ * block_size <= INT32_MAX); num_seqs * Hq < 2^26.  Workspace from the query. */
+size_t kvs_paged_decode_shared_workspace(int num_seqs, int num_groups, int Hq, int Hkv, int D);
+kvs_status_t kvs_paged_decode_shared(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
+                                     const int32_t* block_table, const int32_t* seq_blocks,
+                                     const int32_t* prefix_group, const int32_t* prefix_blocks, void* O, float* LSE,
+                                     int num_seqs, int num_groups, int Hq, int Hkv, int D, int num_blocks,
+                                     int block_size, int max_blocks, float softmax_scale, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* Attention of several new tokens a sequence over the cache, to which their own
+ * entries have been appended (a tool observation, drafted tokens): Q, O bf16
+ * [Ntot][Hq][D], LSE fp32 [Ntot][Hq]; sequence s has the tokens [cu_seqlens[s],
+ * cu_seqlens[s + 1]) (device int32 [num_seqs + 1], non-decreasing; clamped to [0,
+ * Ntot], and tokens of no sequence keep what O and LSE held).  The token at trace
+ * position q_pos[t] (device int32 [Ntot]) sees of its sequence's live entries
+ * those at p <= q_pos[t], and under a window (window > 0) of these those with
+ * q_pos[t] - p < window or p < sinks: one token a sequence is kvs_paged_decode_ex,
+ * and all tokens of a trace at once, nothing evicted, are kvs_window_attn_fwd.
+ * A token that sees nothing gets O = 0, LSE = -inf.  Entries that are live but not
+ * visible to a token are factors 0 in its products: an infinity or NaN in their V
+ * may reach it.  Slots without a live entry may hold anything.  Limits as in
+ * kvs_paged_decode_shared (Ntot * Hq < 2^26); Ntot = 0 is valid. */
+size_t kvs_paged_extend_workspace(int num_seqs, int Ntot, int Hq, int Hkv, int D);
+kvs_status_t kvs_paged_extend(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
+                              const int32_t* block_table, const int32_t* seq_blocks, const int32_t* q_pos,
+                              const int32_t* cu_seqlens, void* O, float* LSE, int num_seqs, int Ntot, int Hq, int Hkv,
+                              int D, int num_blocks, int block_size, int max_blocks, float softmax_scale, int window,
+                              int sinks, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -624,6 +624,49 @@ kvs_status_t kvs_bm_release(kvs_block_manager* bm, int seq, int32_t* slots, int*
   return bm_status(bm->impl.release(seq, slots, n_slots, &msg), msg);
 }
 
+kvs_status_t kvs_bm_fork(kvs_block_manager* bm, int src, int dst) {
+  t_err.clear();
+  if (!bm) return fail(KVS_ERR_NULL, "block manager is NULL");
+  std::string msg;
+  return bm_status(bm->impl.fork(src, dst, &msg), msg);
+}
+
+kvs_status_t kvs_bm_evict_shared(kvs_block_manager* bm, int seq, const int32_t* pos, int n, int32_t* slots,
+                                 int32_t* from, int32_t* to, int* n_copies) {
+  t_err.clear();
+  if (!bm || !n_copies) return fail(KVS_ERR_NULL, "block manager or n_copies is NULL");
+  *n_copies = 0;
+  if (n < 0) return fail(KVS_ERR_SHAPE, "n must be >= 0");
+  if (n > 0 && (!pos || !slots || !from || !to)) return fail(KVS_ERR_NULL, "pos, slots, from or to is NULL");
+  std::string msg;
+  return bm_status(bm->impl.evict_shared(seq, pos, n, slots, from, to, n_copies, &msg), msg);
+}
+
+kvs_status_t kvs_bm_copy(kvs_block_manager* bm, int src, int dst, int32_t* from, int32_t* to, int* n) {
+  t_err.clear();
+  if (!bm || !n) return fail(KVS_ERR_NULL, "block manager or n is NULL");
+  *n = 0;
+  if (bm->impl.live(src) > 0 && (!from || !to)) return fail(KVS_ERR_NULL, "from or to is NULL");
+  std::string msg;
+  return bm_status(bm->impl.copy(src, dst, from, to, n, &msg), msg);
+}
+
+kvs_status_t kvs_bm_compact(kvs_block_manager* bm, int seq, int32_t* from, int32_t* to, int* n) {
+  t_err.clear();
+  if (!bm || !n) return fail(KVS_ERR_NULL, "block manager or n is NULL");
+  *n = 0;
+  if (bm->impl.live(seq) > 0 && (!from || !to)) return fail(KVS_ERR_NULL, "from or to is NULL");
+  std::string msg;
+  return bm_status(bm->impl.compact(seq, from, to, n, &msg), msg);
+}
+
+kvs_status_t kvs_bm_groups(const kvs_block_manager* bm, int32_t* prefix_group, int32_t* prefix_blocks, int* num_groups) {
+  t_err.clear();
+  if (!bm || !prefix_group || !prefix_blocks || !num_groups) return fail(KVS_ERR_NULL, "NULL argument");
+  std::string msg;
+  return bm_status(bm->impl.groups(prefix_group, prefix_blocks, num_groups, &msg), msg);
+}
+
 kvs_status_t kvs_bm_tables(const kvs_block_manager* bm, int32_t* block_table, int32_t* seq_blocks) {
   t_err.clear();
   if (!bm || !block_table || !seq_blocks) return fail(KVS_ERR_NULL, "NULL argument");
@@ -633,6 +676,7 @@ kvs_status_t kvs_bm_tables(const kvs_block_manager* bm, int32_t* block_table, in
 
 int kvs_bm_free_blocks(const kvs_block_manager* bm) { return bm ? bm->impl.free_blocks() : -1; }
 int kvs_bm_live(const kvs_block_manager* bm, int seq) { return bm ? bm->impl.live(seq) : -1; }
+int kvs_bm_shared(const kvs_block_manager* bm, int seq) { return bm ? bm->impl.shared(seq) : -1; }
 
 static kvs_status_t check_cache_dims(int num_blocks, int block_size) {
   if (num_blocks < 1 || block_size < 1 || block_size > 64)
@@ -951,6 +995,132 @@ kvs_status_t kvs_paged_evict_lowest(const float* slot_weight, int32_t* slot_pos,
                                 (hipStream_t)stream};
   hipError_t e = kvs::launch_paged_evict_lowest(p);
   return e == hipSuccess ? KVS_OK : hip_fail(e, "paged evict launch");
+}
+
+// ---------------------------------------------------------------- copies of slots
+kvs_status_t kvs_paged_copy(const int32_t* src, const int32_t* dst, int n, void* K_cache, void* V_cache,
+                            int32_t* slot_pos, float* slot_weight, int move, int num_blocks, int block_size, int Hkv,
+                            int D, void* stream) {
+  t_err.clear();
+  if (kvs_status_t st = check_cache_dims(num_blocks, block_size)) return st;
+  if (n < 0 || Hkv < 1) return fail(KVS_ERR_SHAPE, "n must be >= 0 and Hkv >= 1");
+  if (D != 64 && D != 128) return fail(KVS_ERR_SHAPE, "head dim D must be 64 or 128 (got %d)", D);
+  REQUIRE_PTR(K_cache, "K_cache");
+  REQUIRE_PTR(V_cache, "V_cache");
+  if (move && !slot_pos) return fail(KVS_ERR_NULL, "slot_pos is NULL (a move clears the sources' positions)");
+  if (n == 0) return KVS_OK;
+  if (!src || !dst) return fail(KVS_ERR_NULL, "src or dst is NULL");
+  const kvs::PagedCopy p{src, dst, K_cache, V_cache, slot_pos, slot_weight, n, num_blocks, block_size, Hkv, D,
+                         move != 0, (hipStream_t)stream};
+  hipError_t e = kvs::launch_paged_copy(p);
+  return e == hipSuccess ? KVS_OK : hip_fail(e, "paged copy launch");
+}
+
+// ---------------------------------------------------------------- many query rows over the cache
+// Sizes of a call; workspace and launch sizes follow from them alone.
+static kvs::PagedRows rows_sizes(bool shared, int S, int groups, int ntok, int Hq, int Hkv, int D) {
+  kvs::PagedRows p{};
+  p.shared = shared;
+  p.S = S;
+  p.groups = groups;
+  p.ntok = ntok;
+  p.Hq = Hq;
+  p.Hkv = Hkv;
+  p.D = D;
+  return p;
+}
+
+static kvs_status_t check_rows_dims(const kvs::PagedRows& p, int num_blocks, int block_size, int max_blocks,
+                                    float softmax_scale) {
+  if (p.S < 1 || p.Hq < 1 || p.Hkv < 1 || max_blocks < 1)
+    return fail(KVS_ERR_SHAPE, "num_seqs, Hq, Hkv, max_blocks must be >= 1");
+  if (p.Hq % p.Hkv != 0) return fail(KVS_ERR_SHAPE, "Hq (%d) must be a multiple of Hkv (%d)", p.Hq, p.Hkv);
+  if (p.D != 64 && p.D != 128) return fail(KVS_ERR_SHAPE, "head dim D must be 64 or 128 (got %d)", p.D);
+  if (kvs_status_t st = check_cache_dims(num_blocks, block_size)) return st;
+  if (p.Hq / p.Hkv > 64) return fail(KVS_ERR_UNSUPPORTED, "GQA groups of at most 64 (got %d)", p.Hq / p.Hkv);
+  if ((long long)num_blocks * block_size * p.Hkv > 0xffffffffll)
+    return fail(KVS_ERR_UNSUPPORTED, "num_blocks * block_size * Hkv above 2^32");
+  if ((long long)max_blocks * block_size > kMaxPlaces)
+    return fail(KVS_ERR_UNSUPPORTED, "max_blocks * block_size above %d", kMaxPlaces);
+  if (!kvs::paged_rows_fit(p)) return fail(KVS_ERR_UNSUPPORTED, "too many query rows");
+  if (!(softmax_scale > 0.f) || std::isinf(softmax_scale))
+    return fail(KVS_ERR_SHAPE, "softmax_scale must be positive and finite");
+  return KVS_OK;
+}
+
+static kvs_status_t rows_call(kvs::PagedRows& p, const void* Q, const void* K_cache, const void* V_cache,
+                              const int32_t* slot_pos, const int32_t* block_table, const int32_t* seq_blocks, void* O,
+                              float* LSE, int num_blocks, int block_size, int max_blocks, float softmax_scale,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  REQUIRE_PTR(Q, "Q");
+  REQUIRE_PTR(K_cache, "K_cache");
+  REQUIRE_PTR(V_cache, "V_cache");
+  REQUIRE_PTR(O, "O");
+  if (!slot_pos || !block_table || !seq_blocks || !LSE) return fail(KVS_ERR_NULL, "NULL table or output pointer");
+  if (kvs_status_t st = check_ws(workspace, workspace_bytes, kvs::paged_rows_ws_bytes(p))) return st;
+  p.q = Q;
+  p.k_cache = K_cache;
+  p.v_cache = V_cache;
+  p.slot_pos = slot_pos;
+  p.block_table = block_table;
+  p.seq_blocks = seq_blocks;
+  p.o = O;
+  p.lse = LSE;
+  p.max_blocks = max_blocks;
+  p.block_size = block_size;
+  p.num_blocks = num_blocks;
+  p.scale = softmax_scale;
+  p.ws = workspace;
+  p.stream = (hipStream_t)stream;
+  hipError_t e = kvs::launch_paged_rows(p);
+  return e == hipSuccess ? KVS_OK : hip_fail(e, "paged attention launch");
+}
+
+size_t kvs_paged_decode_shared_workspace(int num_seqs, int num_groups, int Hq, int Hkv, int D) {
+  if (num_seqs < 1 || num_groups < 1 || Hkv < 1 || Hq < Hkv || D < 1) return 0;
+  return kvs::paged_rows_ws_bytes(rows_sizes(true, num_seqs, num_groups, 0, Hq, Hkv, D));
+}
+
+kvs_status_t kvs_paged_decode_shared(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
+                                     const int32_t* block_table, const int32_t* seq_blocks,
+                                     const int32_t* prefix_group, const int32_t* prefix_blocks, void* O, float* LSE,
+                                     int num_seqs, int num_groups, int Hq, int Hkv, int D, int num_blocks,
+                                     int block_size, int max_blocks, float softmax_scale, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  t_err.clear();
+  kvs::PagedRows p = rows_sizes(true, num_seqs, num_groups, 0, Hq, Hkv, D);
+  if (num_groups < 1) return fail(KVS_ERR_SHAPE, "num_groups must be >= 1 (got %d)", num_groups);
+  if (kvs_status_t st = check_rows_dims(p, num_blocks, block_size, max_blocks, softmax_scale)) return st;
+  if (!prefix_group || !prefix_blocks) return fail(KVS_ERR_NULL, "prefix_group or prefix_blocks is NULL");
+  p.prefix_group = prefix_group;
+  p.prefix_blocks = prefix_blocks;
+  return rows_call(p, Q, K_cache, V_cache, slot_pos, block_table, seq_blocks, O, LSE, num_blocks, block_size, max_blocks,
+                   softmax_scale, workspace, workspace_bytes, stream);
+}
+
+size_t kvs_paged_extend_workspace(int num_seqs, int Ntot, int Hq, int Hkv, int D) {
+  if (num_seqs < 1 || Ntot < 1 || Hkv < 1 || Hq < Hkv || D < 1) return 0;
+  return kvs::paged_rows_ws_bytes(rows_sizes(false, num_seqs, 0, Ntot, Hq, Hkv, D));
+}
+
+kvs_status_t kvs_paged_extend(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
+                              const int32_t* block_table, const int32_t* seq_blocks, const int32_t* q_pos,
+                              const int32_t* cu_seqlens, void* O, float* LSE, int num_seqs, int Ntot, int Hq, int Hkv,
+                              int D, int num_blocks, int block_size, int max_blocks, float softmax_scale, int window,
+                              int sinks, void* workspace, size_t workspace_bytes, void* stream) {
+  t_err.clear();
+  kvs::PagedRows p = rows_sizes(false, num_seqs, 0, Ntot, Hq, Hkv, D);
+  if (Ntot < 0) return fail(KVS_ERR_SHAPE, "Ntot must be >= 0 (got %d)", Ntot);
+  if (kvs_status_t st = check_rows_dims(p, num_blocks, block_size, max_blocks, softmax_scale)) return st;
+  if (window < 0 || sinks < 0) return fail(KVS_ERR_SHAPE, "window and sinks must be >= 0 (got %d, %d)", window, sinks);
+  if (Ntot == 0) return KVS_OK;
+  if (!q_pos || !cu_seqlens) return fail(KVS_ERR_NULL, "q_pos or cu_seqlens is NULL");
+  p.q_pos = q_pos;
+  p.cu = cu_seqlens;
+  p.window = window;
+  p.sinks = sinks;
+  return rows_call(p, Q, K_cache, V_cache, slot_pos, block_table, seq_blocks, O, LSE, num_blocks, block_size, max_blocks,
+                   softmax_scale, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

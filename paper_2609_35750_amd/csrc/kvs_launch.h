@@ -183,6 +183,45 @@ struct PagedEvictLowest {
 size_t paged_evict_ws_bytes(int S, int max_blocks, int block_size);
 hipError_t launch_paged_evict_lowest(const PagedEvictLowest& p);
 
+// Copies of cache slots (after host-side validation).
+struct PagedCopy {
+  const int32_t* src;      // [n]
+  const int32_t* dst;      // [n]
+  void* k_cache;
+  void* v_cache;
+  int32_t* slot_pos;       // NULL: left alone
+  float* slot_weight;      // NULL: left alone
+  int n, num_blocks, block_size, Hkv, D;
+  bool move;               // the sources are empty then
+  hipStream_t stream;
+};
+hipError_t launch_paged_copy(const PagedCopy& p);
+
+// Attention of many query rows over the cache (after host-side validation): one token of each of S sequences, groups of
+// which share the first blocks of their tables, or ntok new tokens of S sequences.
+struct PagedRows {
+  const void* q;               // [S or ntok][Hq][D] bf16
+  const void* k_cache;
+  const void* v_cache;
+  const int32_t* slot_pos;
+  const int32_t* block_table;
+  const int32_t* seq_blocks;
+  bool shared;
+  const int32_t* prefix_group;    // shared: [S]
+  const int32_t* prefix_blocks;   // [groups]
+  const int32_t* q_pos;           // else: [ntok]
+  const int32_t* cu;              // [S + 1]
+  void* o;
+  float* lse;                  // [S or ntok][Hq]
+  int S, groups, ntok, Hq, Hkv, D, max_blocks, block_size, num_blocks, window, sinks;
+  float scale;
+  void* ws;
+  hipStream_t stream;
+};
+size_t paged_rows_ws_bytes(const PagedRows& p);
+bool paged_rows_fit(const PagedRows& p);   // whether the launches hold its units and rows
+hipError_t launch_paged_rows(const PagedRows& p);
+
 // Per-kernel event bracketing (benchmark timing).
 void prof_begin(const char* name, hipStream_t s);
 void prof_end(hipStream_t s);

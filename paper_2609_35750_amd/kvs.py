@@ -70,6 +70,12 @@ SIGNATURES = {
     "kvs_bm_tables": (_I, [_P, _P, _P]),
     "kvs_bm_free_blocks": (_I, [_P]),
     "kvs_bm_live": (_I, [_P, _I]),
+    "kvs_bm_fork": (_I, [_P, _I, _I]),
+    "kvs_bm_evict_shared": (_I, [_P, _I, _P, _I, _P, _P, _P, ctypes.POINTER(_I)]),
+    "kvs_bm_copy": (_I, [_P, _I, _I, _P, _P, ctypes.POINTER(_I)]),
+    "kvs_bm_compact": (_I, [_P, _I, _P, _P, ctypes.POINTER(_I)]),
+    "kvs_bm_groups": (_I, [_P, _P, _P, ctypes.POINTER(_I)]),
+    "kvs_bm_shared": (_I, [_P, _I]),
     "kvs_paged_append": (_I, [_P, _P, _P, _P, _I, _P, _P, _P, _I, _I, _I, _I, _P]),
     "kvs_paged_evict": (_I, [_P, _I, _P, _I, _I, _P]),
     "kvs_paged_append_host": (_I, [_P, _P, _P, _P, _I, _P, _P, _P, _I, _I, _I, _I, _P]),
@@ -81,6 +87,13 @@ SIGNATURES = {
     "kvs_paged_decode_ex_workspace": (_Z, [_I, _I, _I, _I, _I, _I, _I, _I, _I, _I]),
     "kvs_paged_decode_ex": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _F, _I, _I,
                                  _P, _Z, _P]),
+    "kvs_paged_copy": (_I, [_P, _P, _I, _P, _P, _P, _P, _I, _I, _I, _I, _I, _P]),
+    "kvs_paged_decode_shared_workspace": (_Z, [_I, _I, _I, _I, _I]),
+    "kvs_paged_decode_shared": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _F, _P, _Z,
+                                     _P]),
+    "kvs_paged_extend_workspace": (_Z, [_I, _I, _I, _I, _I]),
+    "kvs_paged_extend": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _F, _I, _I, _P, _Z,
+                              _P]),
     "kvs_paged_decode_workspace": (_Z, [_I, _I, _I, _I, _I, _I]),
     "kvs_paged_decode": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _F, _P, _Z, _P]),
 }

@@ -61,6 +61,44 @@ class BlockManager:
         _check("kvs_bm_release", lib.kvs_bm_release(self._h, seq, _np_ptr(slots), ctypes.byref(n)))
         return slots[: n.value]
 
+    def fork(self, src: int, dst: int) -> None:
+        _check("kvs_bm_fork", lib.kvs_bm_fork(self._h, src, dst))
+
+    def _pairs(self, seq: int):
+        """Room for (source, destination) slots of a sequence's entries, and their number."""
+        return np.empty((2, max(self.live(seq), 1)), dtype=np.int32), ctypes.c_int()
+
+    def evict_shared(self, seq: int, positions: Sequence[int]) -> Tuple[np.ndarray, np.ndarray]:
+        """(slots as ``evict`` gives them, -1 for entries in shared blocks; [2, n] slots to copy from and to)."""
+        pos = _i32(positions)
+        slots = np.empty_like(pos)
+        pairs, n = self._pairs(seq)
+        _check("kvs_bm_evict_shared", lib.kvs_bm_evict_shared(
+            self._h, seq, _np_ptr(pos), pos.size, _np_ptr(slots), _np_ptr(pairs), _np_ptr(pairs[1]), ctypes.byref(n)))
+        return slots, pairs[:, : n.value]
+
+    def copy(self, src: int, dst: int) -> np.ndarray:
+        """[2, n] slots to copy from and to."""
+        pairs, n = self._pairs(src)
+        _check("kvs_bm_copy", lib.kvs_bm_copy(self._h, src, dst, _np_ptr(pairs), _np_ptr(pairs[1]), ctypes.byref(n)))
+        return pairs[:, : n.value]
+
+    def compact(self, seq: int) -> np.ndarray:
+        """[2, n] slots to move from and to."""
+        pairs, n = self._pairs(seq)
+        _check("kvs_bm_compact", lib.kvs_bm_compact(self._h, seq, _np_ptr(pairs), _np_ptr(pairs[1]), ctypes.byref(n)))
+        return pairs[:, : n.value]
+
+    def groups(self) -> Tuple[np.ndarray, np.ndarray]:
+        """Group of every sequence (-1: none), leading blocks each group has in common."""
+        group, blocks = np.empty((2, self.num_seqs), dtype=np.int32)
+        n = ctypes.c_int()
+        _check("kvs_bm_groups", lib.kvs_bm_groups(self._h, _np_ptr(group), _np_ptr(blocks), ctypes.byref(n)))
+        return group, blocks[: n.value]
+
+    def shared(self, seq: int) -> int:
+        return lib.kvs_bm_shared(self._h, seq)
+
     def tables(self) -> Tuple[np.ndarray, np.ndarray]:
         table = np.empty((self.num_seqs, self.max_blocks), dtype=np.int32)
         nblk = np.empty(self.num_seqs, dtype=np.int32)
@@ -237,6 +275,108 @@ def kvs_paged_evict_lowest(slot_weight, slot_pos, block_table, seq_blocks, keep,
     return pos, counts
 
 
+def _check_caches(k_cache, v_cache, slot_pos) -> None:
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+        raise ValueError("the caches must be [num_blocks, Hkv, block_size, D]")
+    if k_cache.dtype != torch.bfloat16 or v_cache.dtype != torch.bfloat16:
+        raise ValueError("the caches must be bfloat16")
+    if slot_pos is not None and (slot_pos.dtype != torch.int32 or slot_pos.numel() != k_cache.shape[0] * k_cache.shape[2]):
+        raise ValueError("slot_pos must be int32 with num_blocks * block_size entries")
+
+
+def kvs_paged_copy(src, dst, k_cache, v_cache, slot_pos=None, slot_weight=None, move: bool = False) -> None:
+    """``kvs_paged_copy``: slot ``dst[i]`` takes the entry of slot ``src[i]`` (int32 [n]); ``move`` empties the sources.
+
+    With its position where ``slot_pos`` is given, and its weight where ``slot_weight`` is.
+    """
+    _check_caches(k_cache, v_cache, slot_pos)
+    nb, Hkv, bs, D = k_cache.shape
+    _int32(src, dst)
+    if src.dim() != 1 or dst.shape != src.shape:
+        raise ValueError("src and dst must be [n]")
+    if slot_weight is not None and (slot_weight.dtype != torch.float32 or slot_weight.numel() != nb * bs):
+        raise ValueError("slot_weight must be float32 with num_blocks * block_size entries")
+    _same_device(k_cache, v_cache, src, dst, slot_pos, slot_weight)
+    with _on(k_cache):
+        _check("kvs_paged_copy", lib.kvs_paged_copy(
+            _ptr(src), _ptr(dst), src.numel(), _ptr(k_cache), _ptr(v_cache), _ptr(slot_pos), _ptr(slot_weight), int(move),
+            nb, bs, Hkv, D, _stream(k_cache)))
+
+
+def _rows_args(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, softmax_scale, out, lse, *more):
+    """Checks shared by the calls with many query rows; returns (O, LSE, scale)."""
+    _check_caches(k_cache, v_cache, slot_pos)
+    if q.dim() != 3 or q.dtype != torch.bfloat16:
+        raise ValueError("q must be bfloat16 [n, Hq, D]")
+    if q.shape[2] != k_cache.shape[3]:
+        raise ValueError("cache shapes do not match q")
+    _int32(block_table, seq_blocks, *more)
+    if block_table.dim() != 2 or seq_blocks.shape != (block_table.shape[0],):
+        raise ValueError("block_table must be [S, max_blocks] and seq_blocks [S]")
+    if out is not None and (out.shape != q.shape or out.dtype != torch.bfloat16):
+        raise ValueError("O must have q's shape and type")
+    if lse is not None and (lse.shape != q.shape[:2] or lse.dtype != torch.float32):
+        raise ValueError("LSE must be float32 [n, Hq]")
+    _same_device(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, out, lse, *more)
+    scale = 1.0 / math.sqrt(q.shape[2]) if softmax_scale is None else float(softmax_scale)
+    o = torch.empty_like(q) if out is None else out
+    return o, torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse, scale
+
+
+def kvs_paged_decode_shared(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, prefix_group, prefix_blocks,
+                            softmax_scale=None, out=None, lse=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """``kvs_paged_decode_shared``: ``kvs_paged_decode`` of sequences whose tables begin alike; returns (O, LSE).
+
+    ``prefix_group`` int32 [S]: the group of each sequence (-1: none); ``prefix_blocks`` int32 [groups]: the leading
+    table entries its members have in common, which are read once for all of them.
+    """
+    o, lse, scale = _rows_args(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, softmax_scale, out, lse,
+                               prefix_group, prefix_blocks)
+    S, Hq, D = q.shape
+    nb, Hkv, bs, _ = k_cache.shape
+    if block_table.shape[0] != S or prefix_group.shape != (S,):
+        raise ValueError("q, block_table and prefix_group must have one row a sequence")
+    if prefix_blocks.dim() != 1 or prefix_blocks.numel() < 1:
+        raise ValueError("prefix_blocks must be [groups], one group at least")
+    groups = prefix_blocks.numel()
+    need = lib.kvs_paged_decode_shared_workspace(S, groups, Hq, Hkv, D)
+    ws = _workspace(need, q.device)
+    with _on(q):
+        _check("kvs_paged_decode_shared", lib.kvs_paged_decode_shared(
+            _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(slot_pos), _ptr(block_table), _ptr(seq_blocks), _ptr(prefix_group),
+            _ptr(prefix_blocks), _ptr(o), _ptr(lse), S, groups, Hq, Hkv, D, nb, bs, block_table.shape[1], scale, _ptr(ws),
+            need, _stream(q)))
+    return o, lse
+
+
+def kvs_paged_extend(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, q_pos, cu_seqlens, softmax_scale=None,
+                     window: Optional[int] = None, sinks: int = 0, out=None,
+                     lse=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """``kvs_paged_extend``: new tokens q [Ntot, Hq, D] of S sequences over the cache that holds them; returns (O, LSE).
+
+    Sequence s has the tokens ``cu_seqlens[s]`` to ``cu_seqlens[s + 1]`` (int32 [S + 1]), at trace positions ``q_pos``
+    int32 [Ntot]; each sees the live entries at p <= its own position, under a ``window`` (None: none) those less than
+    ``window`` behind it and the first ``sinks``.  LSE is float32 [Ntot, Hq].
+    """
+    o, lse, scale = _rows_args(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, softmax_scale, out, lse, q_pos,
+                               cu_seqlens)
+    n, Hq, D = q.shape
+    nb, Hkv, bs, _ = k_cache.shape
+    S = block_table.shape[0]
+    if q_pos.shape != (n,) or cu_seqlens.shape != (S + 1,):
+        raise ValueError("q_pos must be [Ntot] and cu_seqlens [S + 1]")
+    if window is not None and window < 1:
+        raise ValueError("window must be >= 1 (None: no window)")
+    need = lib.kvs_paged_extend_workspace(S, n, Hq, Hkv, D)
+    ws = _workspace(need, q.device)
+    with _on(q):
+        _check("kvs_paged_extend", lib.kvs_paged_extend(
+            _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(slot_pos), _ptr(block_table), _ptr(seq_blocks), _ptr(q_pos),
+            _ptr(cu_seqlens), _ptr(o), _ptr(lse), S, n, Hq, Hkv, D, nb, bs, block_table.shape[1], scale,
+            _i31(window or 0), _i31(sinks), _ptr(ws), need, _stream(q)))
+    return o, lse
+
+
 class PagedKVCache:
     """Device pools of a streamed paged KV cache plus its native block manager.
 
@@ -247,6 +387,11 @@ class PagedKVCache:
     attention weight (``slot_weight``): entries start with the weights
     ``append`` is given, ``decode(q, accumulate=True)`` adds to them and
     ``evict_lowest(keep)`` evicts the lowest.
+
+    ``fork(src, dst)`` lets an empty sequence share the entries of another one,
+    whose common part ``decode`` then reads once for all; ``extend`` attends
+    several new tokens a sequence.  ``copy(src, dst)`` gives a sequence entries
+    of its own, ``compact()`` brings what evictions have left into fewer blocks.
     """
 
     def __init__(self, num_blocks: int, block_size: int, num_seqs: int, max_blocks: int, Hkv: int, D: int,
@@ -260,6 +405,7 @@ class PagedKVCache:
         self.slot_pos = torch.full((num_blocks * block_size,), -1, dtype=torch.int32, device=self.device)
         self.slot_weight = torch.zeros(num_blocks * block_size, dtype=torch.float32, device=self.device) if weights else None
         self._tables = None
+        self._shares = None   # groups of sequences that share a prefix, on the device; None: not known, (): none
 
     def append(self, seq: int, positions, k_new: torch.Tensor, v_new: torch.Tensor,
                weights: Optional[torch.Tensor] = None) -> np.ndarray:
@@ -314,18 +460,57 @@ class PagedKVCache:
                 _check("kvs_paged_evict_host", st)
 
     def evict(self, seq: int, positions) -> np.ndarray:
-        slots = self.bm.evict(seq, _i32(positions))
-        if slots.size:
-            self._mark_evicted(slots)
+        """Entries of a sequence leave; returns their slots, -1 for those in blocks that other sequences hold too."""
+        if not self.bm.shared(seq) > 0:
+            slots = self.bm.evict(seq, _i32(positions))
+            if slots.size:
+                self._mark_evicted(slots)
+        else:   # what stays of a shared block goes to one of the sequence's own
+            slots, pairs = self.bm.evict_shared(seq, positions)
+            mine = slots[slots >= 0]
+            if mine.size:
+                self._mark_evicted(mine)
+            self._copy(pairs)
+            self._shares = None
         self._tables = None
         return slots
 
     def release(self, seq: int) -> np.ndarray:
+        if self.bm.shared(seq) > 0:
+            self._shares = None
         slots = self.bm.release(seq)
         if slots.size:
             self._mark_evicted(slots)
         self._tables = None
         return slots
+
+    def _copy(self, pairs: np.ndarray, move: bool = False) -> None:
+        if pairs.shape[1]:
+            src, dst = torch.from_numpy(np.ascontiguousarray(pairs)).to(self.device)
+            kvs_paged_copy(src, dst, self.k, self.v, self.slot_pos, self.slot_weight, move)
+
+    def fork(self, src: int, dst: int) -> None:
+        """The empty sequence ``dst`` shares the entries of ``src``; what either appends or evicts then is its own."""
+        if self.slot_weight is not None:
+            raise ValueError("entries' weights are one sequence's: a cache that keeps them takes copy()")
+        self.bm.fork(src, dst)
+        self._tables = self._shares = None
+
+    def copy(self, src: int, dst: int) -> None:
+        """The empty sequence ``dst`` gets copies of the entries of ``src``, with their weights, in fresh blocks."""
+        self._copy(self.bm.copy(src, dst))
+        self._tables = None
+
+    def compact(self, seq: Optional[int] = None) -> int:
+        """Entries of a sequence (None: of every one) move into as few blocks as hold them; returns the blocks freed.
+
+        Blocks it shares, and a last one with room for appends, stay as they are.
+        """
+        before = self.bm.free_blocks()
+        todo = [self.bm.compact(s) for s in (range(self.num_seqs) if seq is None else [seq])]
+        self._copy(np.concatenate(todo, axis=1), move=True)
+        self._tables = None
+        return self.bm.free_blocks() - before
 
     def device_tables(self) -> Tuple[torch.Tensor, torch.Tensor]:
         if self._tables is None:
@@ -338,6 +523,31 @@ class PagedKVCache:
             self._tables = (dev[:n].view(self.num_seqs, self.max_blocks), dev[n:])
         return self._tables
 
+    def device_groups(self) -> Tuple[torch.Tensor, ...]:
+        """(group of every sequence, leading blocks each group has in common); empty if no sequences share their first."""
+        if self._shares is None:
+            group, blocks = self.bm.groups()
+            self._shares = ()
+            if blocks.size:
+                both = torch.from_numpy(np.concatenate([group, blocks])).to(self.device)
+                self._shares = both[: group.size], both[group.size:]
+        return self._shares
+
+    def extend(self, q: torch.Tensor, positions, lengths, softmax_scale=None, out=None, lse=None,
+               window: Optional[int] = None, sinks: int = 0):
+        """New tokens q [Ntot, Hq, D], ``lengths[s]`` of sequence s, at trace ``positions`` (a list, or an int32 tensor on
+        the GPU), whose entries the cache holds; each sees the live entries up to its own, under a ``window`` those less
+        than ``window`` behind it and the first ``sinks``.  Returns (O, LSE [Ntot, Hq])."""
+        lengths = np.asarray(lengths, dtype=np.int64)
+        if lengths.shape != (self.num_seqs,) or (lengths < 0).any() or lengths.sum() != q.shape[0]:
+            raise ValueError("lengths must be one number a sequence, q's rows in all")
+        table, nblk = self.device_tables()
+        cu = torch.from_numpy(_i32(np.concatenate([[0], np.cumsum(lengths)]))).to(self.device)
+        if not torch.is_tensor(positions):
+            positions = torch.from_numpy(_i32(positions)).to(self.device)
+        return kvs_paged_extend(q, self.k, self.v, self.slot_pos, table, nblk, positions, cu, softmax_scale, window, sinks,
+                                out, lse)
+
     def decode(self, q: torch.Tensor, softmax_scale=None, out=None, lse=None, positions=None,
                window: Optional[int] = None, sinks: int = 0, accumulate: bool = False):
         """One query a sequence, q [num_seqs, Hq, D]; returns (O, LSE).
@@ -349,6 +559,9 @@ class PagedKVCache:
         """
         table, nblk = self.device_tables()
         if window is None and not accumulate:
+            shares = self.device_groups()
+            if shares:
+                return kvs_paged_decode_shared(q, self.k, self.v, self.slot_pos, table, nblk, *shares, softmax_scale, out, lse)
             with _on(self.k):
                 return kvs_paged_decode(q, self.k, self.v, self.slot_pos, table, nblk, softmax_scale, out, lse)
         if accumulate and self.slot_weight is None:
