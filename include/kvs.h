@@ -563,7 +563,8 @@ kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void*
  * Supported: D in {64, 128}; Hq / Hkv <= 64; block_size in [1, 64]; max_blocks *
  * block_size <= 2^30; num_blocks * block_size * Hkv <= 2^32 (num_blocks *
  * block_size <= INT32_MAX); num_seqs * Hq < 2^26.  Workspace from the query. */
-size_t kvs_paged_decode_shared_workspace(int num_seqs, int num_groups, int Hq, int Hkv, int D);
+size_t kvs_paged_decode_shared_workspace(int num_seqs, int num_groups, int Hq, int Hkv, int D, int max_blocks,
+                                         int block_size);
 kvs_status_t kvs_paged_decode_shared(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
                                      const int32_t* block_table, const int32_t* seq_blocks,
                                      const int32_t* prefix_group, const int32_t* prefix_blocks, void* O, float* LSE,
@@ -584,7 +585,7 @@ kvs_status_t kvs_paged_decode_shared(const void* Q, const void* K_cache, const v
  * visible to a token are factors 0 in its products: an infinity or NaN in their V
  * may reach it.  Slots without a live entry may hold anything.  Limits as in
  * kvs_paged_decode_shared (Ntot * Hq < 2^26); Ntot = 0 is valid. */
-size_t kvs_paged_extend_workspace(int num_seqs, int Ntot, int Hq, int Hkv, int D);
+size_t kvs_paged_extend_workspace(int num_seqs, int Ntot, int Hq, int Hkv, int D, int max_blocks, int block_size);
 kvs_status_t kvs_paged_extend(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
                               const int32_t* block_table, const int32_t* seq_blocks, const int32_t* q_pos,
                               const int32_t* cu_seqlens, void* O, float* LSE, int num_seqs, int Ntot, int Hq, int Hkv,

@@ -1018,7 +1018,8 @@ kvs_status_t kvs_paged_copy(const int32_t* src, const int32_t* dst, int n, void*
 
 // ---------------------------------------------------------------- many query rows over the cache
 // Sizes of a call; workspace and launch sizes follow from them alone.
-static kvs::PagedRows rows_sizes(bool shared, int S, int groups, int ntok, int Hq, int Hkv, int D) {
+static kvs::PagedRows rows_sizes(bool shared, int S, int groups, int ntok, int Hq, int Hkv, int D, int max_blocks,
+                                 int block_size) {
   kvs::PagedRows p{};
   p.shared = shared;
   p.S = S;
@@ -1027,11 +1028,13 @@ static kvs::PagedRows rows_sizes(bool shared, int S, int groups, int ntok, int H
   p.Hq = Hq;
   p.Hkv = Hkv;
   p.D = D;
+  p.max_blocks = max_blocks;
+  p.block_size = block_size;
   return p;
 }
 
-static kvs_status_t check_rows_dims(const kvs::PagedRows& p, int num_blocks, int block_size, int max_blocks,
-                                    float softmax_scale) {
+static kvs_status_t check_rows_dims(const kvs::PagedRows& p, int num_blocks, float softmax_scale) {
+  const int block_size = p.block_size, max_blocks = p.max_blocks;
   if (p.S < 1 || p.Hq < 1 || p.Hkv < 1 || max_blocks < 1)
     return fail(KVS_ERR_SHAPE, "num_seqs, Hq, Hkv, max_blocks must be >= 1");
   if (p.Hq % p.Hkv != 0) return fail(KVS_ERR_SHAPE, "Hq (%d) must be a multiple of Hkv (%d)", p.Hq, p.Hkv);
@@ -1050,8 +1053,8 @@ static kvs_status_t check_rows_dims(const kvs::PagedRows& p, int num_blocks, int
 
 static kvs_status_t rows_call(kvs::PagedRows& p, const void* Q, const void* K_cache, const void* V_cache,
                               const int32_t* slot_pos, const int32_t* block_table, const int32_t* seq_blocks, void* O,
-                              float* LSE, int num_blocks, int block_size, int max_blocks, float softmax_scale,
-                              void* workspace, size_t workspace_bytes, void* stream) {
+                              float* LSE, int num_blocks, float softmax_scale, void* workspace, size_t workspace_bytes,
+                              void* stream) {
   REQUIRE_PTR(Q, "Q");
   REQUIRE_PTR(K_cache, "K_cache");
   REQUIRE_PTR(V_cache, "V_cache");
@@ -1066,8 +1069,6 @@ static kvs_status_t rows_call(kvs::PagedRows& p, const void* Q, const void* K_ca
   p.seq_blocks = seq_blocks;
   p.o = O;
   p.lse = LSE;
-  p.max_blocks = max_blocks;
-  p.block_size = block_size;
   p.num_blocks = num_blocks;
   p.scale = softmax_scale;
   p.ws = workspace;
@@ -1076,9 +1077,10 @@ static kvs_status_t rows_call(kvs::PagedRows& p, const void* Q, const void* K_ca
   return e == hipSuccess ? KVS_OK : hip_fail(e, "paged attention launch");
 }
 
-size_t kvs_paged_decode_shared_workspace(int num_seqs, int num_groups, int Hq, int Hkv, int D) {
-  if (num_seqs < 1 || num_groups < 1 || Hkv < 1 || Hq < Hkv || D < 1) return 0;
-  return kvs::paged_rows_ws_bytes(rows_sizes(true, num_seqs, num_groups, 0, Hq, Hkv, D));
+size_t kvs_paged_decode_shared_workspace(int num_seqs, int num_groups, int Hq, int Hkv, int D, int max_blocks,
+                                         int block_size) {
+  if (num_seqs < 1 || num_groups < 1 || Hkv < 1 || Hq < Hkv || D < 1 || max_blocks < 1 || block_size < 1) return 0;
+  return kvs::paged_rows_ws_bytes(rows_sizes(true, num_seqs, num_groups, 0, Hq, Hkv, D, max_blocks, block_size));
 }
 
 kvs_status_t kvs_paged_decode_shared(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
@@ -1088,19 +1090,19 @@ kvs_status_t kvs_paged_decode_shared(const void* Q, const void* K_cache, const v
                                      int block_size, int max_blocks, float softmax_scale, void* workspace,
                                      size_t workspace_bytes, void* stream) {
   t_err.clear();
-  kvs::PagedRows p = rows_sizes(true, num_seqs, num_groups, 0, Hq, Hkv, D);
+  kvs::PagedRows p = rows_sizes(true, num_seqs, num_groups, 0, Hq, Hkv, D, max_blocks, block_size);
   if (num_groups < 1) return fail(KVS_ERR_SHAPE, "num_groups must be >= 1 (got %d)", num_groups);
-  if (kvs_status_t st = check_rows_dims(p, num_blocks, block_size, max_blocks, softmax_scale)) return st;
+  if (kvs_status_t st = check_rows_dims(p, num_blocks, softmax_scale)) return st;
   if (!prefix_group || !prefix_blocks) return fail(KVS_ERR_NULL, "prefix_group or prefix_blocks is NULL");
   p.prefix_group = prefix_group;
   p.prefix_blocks = prefix_blocks;
-  return rows_call(p, Q, K_cache, V_cache, slot_pos, block_table, seq_blocks, O, LSE, num_blocks, block_size, max_blocks,
-                   softmax_scale, workspace, workspace_bytes, stream);
+  return rows_call(p, Q, K_cache, V_cache, slot_pos, block_table, seq_blocks, O, LSE, num_blocks, softmax_scale,
+                   workspace, workspace_bytes, stream);
 }
 
-size_t kvs_paged_extend_workspace(int num_seqs, int Ntot, int Hq, int Hkv, int D) {
-  if (num_seqs < 1 || Ntot < 1 || Hkv < 1 || Hq < Hkv || D < 1) return 0;
-  return kvs::paged_rows_ws_bytes(rows_sizes(false, num_seqs, 0, Ntot, Hq, Hkv, D));
+size_t kvs_paged_extend_workspace(int num_seqs, int Ntot, int Hq, int Hkv, int D, int max_blocks, int block_size) {
+  if (num_seqs < 1 || Ntot < 1 || Hkv < 1 || Hq < Hkv || D < 1 || max_blocks < 1 || block_size < 1) return 0;
+  return kvs::paged_rows_ws_bytes(rows_sizes(false, num_seqs, 0, Ntot, Hq, Hkv, D, max_blocks, block_size));
 }
 
 kvs_status_t kvs_paged_extend(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
@@ -1109,9 +1111,9 @@ kvs_status_t kvs_paged_extend(const void* Q, const void* K_cache, const void* V_
                               int D, int num_blocks, int block_size, int max_blocks, float softmax_scale, int window,
                               int sinks, void* workspace, size_t workspace_bytes, void* stream) {
   t_err.clear();
-  kvs::PagedRows p = rows_sizes(false, num_seqs, 0, Ntot, Hq, Hkv, D);
+  kvs::PagedRows p = rows_sizes(false, num_seqs, 0, Ntot, Hq, Hkv, D, max_blocks, block_size);
   if (Ntot < 0) return fail(KVS_ERR_SHAPE, "Ntot must be >= 0 (got %d)", Ntot);
-  if (kvs_status_t st = check_rows_dims(p, num_blocks, block_size, max_blocks, softmax_scale)) return st;
+  if (kvs_status_t st = check_rows_dims(p, num_blocks, softmax_scale)) return st;
   if (window < 0 || sinks < 0) return fail(KVS_ERR_SHAPE, "window and sinks must be >= 0 (got %d, %d)", window, sinks);
   if (Ntot == 0) return KVS_OK;
   if (!q_pos || !cu_seqlens) return fail(KVS_ERR_NULL, "q_pos or cu_seqlens is NULL");
@@ -1119,8 +1121,8 @@ kvs_status_t kvs_paged_extend(const void* Q, const void* K_cache, const void* V_
   p.cu = cu_seqlens;
   p.window = window;
   p.sinks = sinks;
-  return rows_call(p, Q, K_cache, V_cache, slot_pos, block_table, seq_blocks, O, LSE, num_blocks, block_size, max_blocks,
-                   softmax_scale, workspace, workspace_bytes, stream);
+  return rows_call(p, Q, K_cache, V_cache, slot_pos, block_table, seq_blocks, O, LSE, num_blocks, softmax_scale,
+                   workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

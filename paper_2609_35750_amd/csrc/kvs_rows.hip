@@ -15,6 +15,7 @@
 // each).  A unit leaves for each row the largest score m, l = sum exp(s - m) and
 // o = sum exp(s - m) V; the merge joins what belongs to a row: m = max m_i, l =
 // sum l_i exp(m_i - m), o likewise, O = o / l, LSE = m + ln l.
+#include "kvs_decode_plan.h"
 #include "kvs_device.h"
 #include "kvs_launch.h"
 
@@ -63,11 +64,13 @@ hipError_t launch_paged_copy(const PagedCopy& p) {
 }
 
 // ---------------------------------------------------------------- the plan
-constexpr int kRowBlock = 128;   // rows of a unit: 32 a wave
+// Jobs of more than 32 rows have units of 128 rows, four waves that share a tile of keys and values; smaller ones
+// units of one wave.  The two kinds run one after the other, each cut so that it fills the chip.
+constexpr int kWideRows = 128, kNarrowRows = 32;
 template <int D>
-constexpr int rows_bn() { return D == 128 ? 32 : 64; }   // keys of a tile
-constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / kWave;
-constexpr int kLeastTiles = 4;   // of a unit, in 32-key tiles
+constexpr int rows_bn() { return D == 128 ? 32 : 64; }   // keys of a tile of wide units
+constexpr int kLeastTiles = 4;    // of a unit, in 32-key tiles
+constexpr int kPlanSmall = 256;   // sequences, and groups, that one wave plans, in LDS
 
 // What a unit is, as its workgroups read it.
 struct Unit {
@@ -100,248 +103,374 @@ struct RowsArgs {
   uint16_t* o;
   float* lse;
   int S, groups, ntok, Hq, Hkv, G, max_blocks, BS, num_blocks, window, sinks;
+  int shift;                  // BS = 1 << shift; -1: BS is no power of two
   float scale_log2;
   // workspace
   int* rank;        // [S] SHARED: of a sequence among its group's members
-  int* count;       // [groups] members
-  int* base;        // [groups] first member in `list`
   int* list;        // [S] members, group by group
-  int* first;       // [jobs + 1] first unit of each job
+  int* count;       // [groups] members, and
+  int* base;        // [groups] the first of them in `list` (more than kPlanSmall sequences or groups)
+  int* jobs;        // [4][jobs + 1] tiles, rows, first wide and narrow unit (the same)
   Parts* own;       // [S] of each sequence
-  Parts* prefix;    // [S] of its group
-  Unit* units;      // [max_units]
+  Parts* prefix;    // [groups] of each group
+  Unit* units;      // [max_units[0] + max_units[1]]: wide, narrow
   float* part;      // [max_part][D]
   float2* part_ml;  // [max_part]: m (log2 units), l
-  int max_units;
+  int* parts;       // number of partial rows
   long long max_part;
-  int want;         // units per KV head that fill the chip
+  int max_units[2];
+  int want[2];      // units per KV head that fill the chip
 };
 
 struct Job {
   int s, c0, c1, rows, tok, listed;
 };
-
-// Job j: the groups first, then the sequences.
+__device__ __forceinline__ int block_of(const RowsArgs& a, int place) { return a.shift >= 0 ? place >> a.shift : place / a.BS; }
+__device__ __forceinline__ bool is_wide(int rows) { return rows > kNarrowRows; }
+__device__ __forceinline__ int row_blocks(int rows) { return is_wide(rows) ? (rows + kWideRows - 1) / kWideRows : rows > 0; }
+// Splits of a job of `tiles` (at most kTileCap) under runs of c tiles.  New tokens that see nothing still have rows to write.
 template <bool SHARED>
-__device__ __forceinline__ int prefix_of(const RowsArgs& a, int g) {   // blocks of group g's prefix
-  const int m = a.count[g];
-  if (m < 2) return 0;
-  const int s = a.list[a.base[g]];
-  return max(0, min(min(a.prefix_blocks[g], a.nblk[s]), a.max_blocks));
-}
-template <bool SHARED>
-__device__ __forceinline__ Job job_of(const RowsArgs& a, int j) {
-  if (SHARED && j < a.groups) {
-    const int n = a.count[j], b = prefix_of<SHARED>(a, j);
-    if (b == 0) return {0, 0, 0, 0, 0, 1};
-    return {a.list[a.base[j]], 0, b * a.BS, n * a.G, a.base[j], 1};
-  }
-  const int s = SHARED ? j - a.groups : j;
-  const int blocks = min(max(a.nblk[s], 0), a.max_blocks);
-  if (SHARED) {
-    const int g = a.prefix_group[s], b = (unsigned)g < (unsigned)a.groups ? min(prefix_of<SHARED>(a, g), blocks) : 0;
-    return {s, b * a.BS, blocks * a.BS, a.G, s, 0};
-  }
-  const int t0 = min(max(a.cu[s], 0), a.ntok), t1 = min(max(a.cu[s + 1], t0), a.ntok);
-  return {s, 0, blocks * a.BS, (t1 - t0) * a.G, t0, 0};
-}
-__device__ __forceinline__ int job_tiles(const Job& j) { return (int)(((unsigned)(j.c1 - j.c0) + 31) / 32); }
-__device__ __forceinline__ int job_blocks(const Job& j) { return (j.rows + kRowBlock - 1) / kRowBlock; }
-// Splits of a job under runs of c tiles.  New tokens that see nothing still have rows to write.
-template <bool SHARED>
-__device__ __forceinline__ int job_splits(const Job& j, int c) {
-  if (j.rows == 0) return 0;
-  const int n = (job_tiles(j) + c - 1) / c;
-  return SHARED ? n : max(n, 1);
+__device__ __forceinline__ int job_splits(int tiles, int rows, int c, float rc) {
+  return rows == 0 || (SHARED && tiles == 0) ? 0 : unit_count(tiles, c, rc);
 }
 
-// One workgroup.  The size of the runs, the same for all jobs, is the smallest for which units and partial results fit.
-template <bool SHARED>
-__global__ void __launch_bounds__(kPlanThreads) rows_plan_kernel(RowsArgs a) {
-  __shared__ long long su[kPlanWaves], sp[kPlanWaves];
-  __shared__ int st[kPlanWaves], pick[2];
+// Prefix sums over the workgroup's NT threads, without the own value, on top of `from`, which moves on by their total.
+template <int NT>
+__device__ __forceinline__ long long block_scan(int x, long long& from, int* buf) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, incl = wave_scan(x);
+  long long before = from + incl - x;
+  if (NT == kWave) {
+    from += wave_last(incl);
+    return before;
+  }
+  __syncthreads();   // buf is read
+  if (lane == kWave - 1) buf[wave] = incl;
+  __syncthreads();
+  for (int w = 0; w < NT / kWave; ++w) {
+    before += w < wave ? buf[w] : 0;
+    from += buf[w];
+  }
+  return before;
+}
+
+// One workgroup; one wave for up to 256 sequences and groups, with what it knows of them in LDS.  All jobs of a kind are
+// cut into runs of the same size, about the smallest for which the units are as many as fill the chip (and half as many
+// on top of the row blocks, where these do).  Bound by latency.
+template <bool SHARED, int NT>
+__global__ void __launch_bounds__(NT) rows_plan_kernel(RowsArgs a) {
+  constexpr bool SMALL = NT == kWave;
+  constexpr int CAP = SMALL ? kPlanSmall : 1, JOBS = SHARED ? 2 * CAP : CAP;
+  __shared__ int sJobs[4 * JOBS + 2], sGroup[SHARED ? 6 * CAP : 1];
+  __shared__ Job sJob[JOBS];
+  __shared__ int sPart[JOBS];
+  __shared__ int buf[NT / kWave], sTop[2][NT / kWave];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, J = SHARED ? a.groups + a.S : a.S;
+  int* tiles = SMALL ? sJobs : a.jobs;
+  int* rows = SMALL ? sJobs + JOBS : a.jobs + J;
+  // units of the jobs in front of each, wide and narrow ones counted apart
+  int* first[2] = {SMALL ? sJobs + 2 * JOBS : a.jobs + 2 * J, SMALL ? sJobs + 3 * JOBS + 1 : a.jobs + 3 * J + 1};
+  int* count = SMALL ? sGroup : a.count;
+  int* base = SMALL ? sGroup + CAP : a.base;
+  int* rank = SMALL ? sGroup + 2 * CAP : a.rank;
+  int* list = SMALL ? sGroup + 3 * CAP : a.list;
+  // a sequence's blocks and group, SMALL: read once
+  int* sBlocks = sGroup + 4 * CAP;
+  int* sOf = sGroup + 5 * CAP;
+  auto blocks_of = [&](int s) { return SMALL && SHARED ? sBlocks[s] : min(max(a.nblk[s], 0), a.max_blocks); };
+  auto group_of = [&](int s) { return SMALL ? sOf[s] : a.prefix_group[s]; };
   if (SHARED) {
-    for (int g = tid; g < a.groups; g += kPlanThreads) a.count[g] = 0;
+    for (int g = tid; g < a.groups; g += NT) count[g] = 0;
+    if (SMALL) {
+      constexpr int N = SMALL ? CAP / NT : 1;
+      int nb[N], gr[N];   // all reads at once
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        nb[k] = k * NT + tid < a.S ? a.nblk[k * NT + tid] : 0;
+        gr[k] = k * NT + tid < a.S ? a.prefix_group[k * NT + tid] : -1;
+      }
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        sBlocks[k * NT + tid] = min(max(nb[k], 0), a.max_blocks);
+        sOf[k * NT + tid] = gr[k];
+      }
+    }
     __syncthreads();
     if (wave == 0)   // ranks in the sequences' order: 64 of them at a time, group by group of those among them
       for (int s0 = 0; s0 < a.S; s0 += kWave) {
-        const int s = s0 + lane, g = s < a.S ? a.prefix_group[s] : -1;
+        const int s = s0 + lane, g = s < a.S ? group_of(s) : -1;
         unsigned long long todo = __ballot((unsigned)g < (unsigned)a.groups);
         while (todo) {
           const int g1 = __builtin_amdgcn_readlane(g, __builtin_ctzll(todo));
           const unsigned long long same = __ballot(g == g1);
-          const int before = a.count[g1];
-          if (g == g1) a.rank[s] = before + __builtin_popcountll(same & ((1ull << lane) - 1ull));
-          if (lane == 0) a.count[g1] = before + __builtin_popcountll(same);
+          const int before = count[g1];
+          if (g == g1) rank[s] = before + __builtin_popcountll(same & ((1ull << lane) - 1ull));
+          if (lane == 0) count[g1] = before + __builtin_popcountll(same);
           __threadfence_block();
           todo &= ~same;
         }
       }
     __syncthreads();
-    int from = 0;
-    for (int g0 = 0; g0 < a.groups; g0 += kPlanThreads) {
-      const int g = g0 + tid, n = g < a.groups ? a.count[g] : 0, incl = wave_scan(n);
-      if (lane == kWave - 1) st[wave] = incl;
-      __syncthreads();
-      int x = from + incl - n;
-      for (int w = 0; w < kPlanWaves; ++w) {
-        x += w < wave ? st[w] : 0;
-        from += st[w];
-      }
-      if (g < a.groups) a.base[g] = x;
-      __syncthreads();
+    long long from = 0;
+    for (int g0 = 0; g0 < a.groups; g0 += NT) {
+      const int g = g0 + tid;
+      const int x = (int)block_scan<NT>(g < a.groups ? count[g] : 0, from, buf);
+      if (g < a.groups) base[g] = x;
     }
-    for (int s = tid; s < a.S; s += kPlanThreads) {
-      const int g = a.prefix_group[s];
-      if ((unsigned)g < (unsigned)a.groups) a.list[a.base[g] + a.rank[s]] = s;
+    __syncthreads();
+    for (int s = tid; s < a.S; s += NT) {
+      const int g = group_of(s);
+      if ((unsigned)g < (unsigned)a.groups) {
+        const int r = rank[s], i = base[g] + r;
+        list[i] = s;
+        if (SMALL) {
+          a.list[i] = s;
+          a.rank[s] = r;
+        }
+      }
     }
     __syncthreads();
   }
-  // units and partial rows for runs of c tiles, by one wave
-  auto need = [&](int c, long long& units, long long& rows) {
-    units = rows = 0;
-    for (int j = lane; j < J; j += kWave) {
-      const Job x = job_of<SHARED>(a, j);
-      const int n = job_splits<SHARED>(x, c);
-      units += (long long)n * job_blocks(x);
-      if (SHARED || n > 1) rows += (long long)n * x.rows * a.Hkv;
+  // blocks of group g's prefix
+  auto prefix_of = [&](int g) { return count[g] < 2 ? 0 : min(max(a.prefix_blocks[g], 0), blocks_of(list[base[g]])); };
+  // job j: the groups first, then the sequences
+  auto job_of = [&](int j) {
+    if (SHARED && j < a.groups) {
+      const int b = prefix_of(j);
+      if (b == 0) return Job{0, 0, 0, 0, 0, 1};
+      return Job{list[base[j]], 0, b * a.BS, count[j] * a.G, base[j], 1};
     }
-    for (int off = 32; off > 0; off >>= 1) {
-      units += __shfl_xor(units, off);
-      rows += __shfl_xor(rows, off);
+    const int s = SHARED ? j - a.groups : j, blocks = blocks_of(s);
+    if (SHARED) {
+      const int g = group_of(s), b = (unsigned)g < (unsigned)a.groups ? min(prefix_of(g), blocks) : 0;
+      return Job{s, b * a.BS, blocks * a.BS, a.G, s, 0};
     }
+    const int t0 = min(max(a.cu[s], 0), a.ntok), t1 = min(max(a.cu[s + 1], t0), a.ntok);
+    return Job{s, 0, blocks * a.BS, (t1 - t0) * a.G, t0, 0};
   };
-  int top = 1;
-  long long least = 0;
-  for (int j = tid; j < J; j += kPlanThreads) {
-    const Job x = job_of<SHARED>(a, j);
-    top = max(top, job_tiles(x));
-    least += job_blocks(x);
-  }
-  for (int off = 32; off > 0; off >>= 1) least += __shfl_xor(least, off);
-  top = wave_max(top);
-  if (lane == 0) {
-    st[wave] = top;
-    su[wave] = least;
-  }
-  __syncthreads();
-  least = 0;
-  for (int w = 0; w < kPlanWaves; ++w) {
-    top = max(top, st[w]);
-    least += su[w];
-  }
-  // as many units as fill the chip, and half as many on top where the row blocks alone do
-  const long long most = min((long long)a.max_units, max((long long)a.want, least + a.want / 2));
-  __syncthreads();
-  // 16 sizes at a time: first in equal ratios from the least to the whole of the longest job, then between two of these
-  int lo = min(kLeastTiles, top), hi = top;
-  for (int turn = 0; turn < 2; ++turn) {
-    int c = lo + (int)((long long)(hi - lo) * (wave + 1) / kPlanWaves);
-    if (turn == 0) c = min(hi, max(lo, (int)(lo * __builtin_amdgcn_exp2f(__log2f((float)hi / (float)lo) * ((float)wave / (kPlanWaves - 1))))));
-    if (turn == 0 && wave == kPlanWaves - 1) c = hi;
-    long long units, rows;
-    need(c, units, rows);
-    if (lane == 0) {
-      su[wave] = units <= most && rows <= a.max_part;
-      st[wave] = c;
-    }
-    __syncthreads();
-    if (tid == 0) {
-      int w = 0;
-      while (w < kPlanWaves - 1 && !su[w]) ++w;
-      pick[0] = w > 0 ? st[w - 1] : lo;
-      pick[1] = st[w];
-    }
-    __syncthreads();
-    lo = pick[0];
-    hi = pick[1];
-    if (turn == 0 && lo == hi) break;
-  }
-  const int C = hi;
-  // first units and first partial rows
-  long long unit0 = 0, part0 = 0;
-  for (int j0 = 0; j0 < J; j0 += kPlanThreads) {
+  int top[2] = {1, 1};
+  long long least[2] = {0, 0};
+  for (int j0 = 0; j0 < J; j0 += NT) {
     const int j = j0 + tid;
-    const Job x = j < J ? job_of<SHARED>(a, j) : Job{0, 0, 0, 0, 0, 0};
-    const int n = job_splits<SHARED>(x, C);
-    const long long mu = (long long)n * job_blocks(x), mp = SHARED || n > 1 ? (long long)n * x.rows * a.Hkv : 0;
-    long long u = mu, p = mp;
-    for (int off = 1; off < kWave; off <<= 1) {
-      const long long du = __shfl_up(u, off), dp = __shfl_up(p, off);
-      if (lane >= off) {
-        u += du;
-        p += dp;
-      }
-    }
-    if (lane == kWave - 1) {
-      su[wave] = u;
-      sp[wave] = p;
-    }
-    __syncthreads();
-    u += unit0 - mu;
-    p += part0 - mp;
-    for (int w = 0; w < kPlanWaves; ++w) {
-      if (w < wave) {
-        u += su[w];
-        p += sp[w];
-      }
-      unit0 += su[w];
-      part0 += sp[w];
-    }
+    const Job x = j < J ? job_of(j) : Job{0, 0, 0, 0, 0, 0};
+    const int t = plan_tiles(x.c1 - x.c0), k = is_wide(x.rows) ? 0 : 1;
     if (j < J) {
-      a.first[j] = (int)min(u, (long long)a.max_units);
-      const Parts parts = {(int)p, x.rows, mp ? n : 0};
+      tiles[j] = t;
+      rows[j] = x.rows;
+      if (SMALL) sJob[j] = x;
+    }
+    top[0] = max(top[0], k == 0 ? t : 0);
+    top[1] = max(top[1], k == 1 ? t : 0);
+    block_scan<NT>(k == 0 ? row_blocks(x.rows) : 0, least[0], buf);
+    block_scan<NT>(k == 1 ? row_blocks(x.rows) : 0, least[1], buf);
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    top[k] = wave_max(top[k]);
+    if (lane == 0) sTop[k][wave] = top[k];
+  }
+  __syncthreads();
+  int C[2];
+  float rC[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    for (int w = 0; w < NT / kWave; ++w) top[k] = max(top[k], sTop[k][w]);
+    // bisection to within an eighth; every wave the same.  The whole of the longest job always fits.
+    const long long most = min((long long)a.max_units[k], max((long long)a.want[k], least[k] + a.want[k] / 2));
+    auto fits = [&](int c) {
+      const float rc = __builtin_amdgcn_rcpf((float)c);
+      long long units = 0;
+      for (int j0 = 0; j0 < J; j0 += kWave) {
+        const int j = j0 + lane, r = j < J ? rows[j] : 0;
+        const long long u = j < J && is_wide(r) == (k == 0) ? (long long)job_splits<SHARED>(tiles[j], r, c, rc) * row_blocks(r) : 0;
+        units += wave_last(wave_scan((int)min(u, 1ll << 24)));   // more than `most` at any rate
+      }
+      return units <= most;
+    };
+    int lo = min(kLeastTiles, top[k]), hi = top[k];
+    if (fits(lo)) hi = lo;
+    while (hi - lo > 1 + (hi >> 3)) {
+      const int c = lo + (hi - lo) / 2;
+      if (fits(c)) hi = c;
+      else lo = c;
+    }
+    C[k] = hi;
+    rC[k] = __builtin_amdgcn_rcpf((float)hi);
+  }
+  // first units of the jobs, wide and narrow ones counted apart, their first partial rows, and the units themselves
+  long long units0[2] = {0, 0}, part0 = 0;
+  for (int j0 = 0; j0 < J; j0 += NT) {
+    const int j = j0 + tid, r = j < J ? rows[j] : 0, k = is_wide(r) ? 0 : 1;
+    const int n = job_splits<SHARED>(j < J ? tiles[j] : 0, r, C[k], rC[k]), u = n * row_blocks(r);
+    const long long uw = block_scan<NT>(k == 0 ? u : 0, units0[0], buf);
+    const long long un = block_scan<NT>(k == 1 ? u : 0, units0[1], buf);
+    const long long pn = block_scan<NT>(SHARED || n > 1 ? n * r : 0, part0, buf);
+    if (j < J) {
+      first[0][j] = (int)min(uw, (long long)INT_MAX);
+      first[1][j] = (int)min(un, (long long)INT_MAX);
+      const Parts parts = {(int)(pn * a.Hkv), r, SHARED || n > 1 ? n : 0};
+      if (SMALL) sPart[j] = parts.part;
       if (SHARED && j < a.groups) a.prefix[j] = parts;
       else a.own[SHARED ? j - a.groups : j] = parts;
     }
-    __syncthreads();
   }
   // offsets that overlap (only where cu_seqlens decreases) may ask for more than there is: nothing is computed then
-  const bool fits = unit0 <= a.max_units && part0 <= a.max_part;
-  const int total = fits ? (int)unit0 : 0;
-  if (!fits)
-    for (int s = tid; s < a.S; s += kPlanThreads) a.own[s].n = 0;
-  for (int u = tid; u < a.max_units; u += kPlanThreads) {
-    Unit x{};
-    x.s = -1;
-    if (u < total) {
-      int j = 0;   // the last job that begins at or before u
+  const bool fit = units0[0] <= a.max_units[0] && units0[1] <= a.max_units[1] && part0 * a.Hkv <= a.max_part;
+  if (tid == 0) a.parts[0] = fit && part0 > 0;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    for (int u = tid; u < (fit ? (int)units0[k] : 0); u += NT) {
+      int j = 0;   // the last job that begins at or before u: those without a unit of this kind begin where the next one does
       for (int step = 1 << (31 - __builtin_clz(J)); step > 0; step >>= 1)
-        if (j + step < J && a.first[j + step] <= u) j += step;
-      const Job b = job_of<SHARED>(a, j);
-      const Parts parts = SHARED ? (j < a.groups ? a.prefix[j] : a.own[j - a.groups]) : a.own[j];
-      const int nb = job_blocks(b), tiles = job_tiles(b), n = max(job_splits<SHARED>(b, C), 1);
-      const int k = (u - a.first[j]) / nb, rb = nb - 1 - (u - a.first[j] - k * nb);   // the last rows see most: first
-      const int per = (tiles + n - 1) / n;
-      x = {b.s,   (int)min((long long)b.c0 + 32ll * per * k, (long long)b.c1),
-           (int)min((long long)b.c0 + 32ll * per * (k + 1), (long long)b.c1),
-           b.rows, b.tok, rb * kRowBlock, parts.n ? parts.part + k * a.Hkv * b.rows : -1, b.listed};
+        if (j + step < J && first[k][j + step] <= u) j += step;
+      const Job b = SMALL ? sJob[j] : job_of(j);
+      const int nb = row_blocks(b.rows), n = job_splits<SHARED>(tiles[j], b.rows, C[k], rC[k]), i = u - first[k][j];
+      const int sp = nb == 1 ? i : i / nb, rb = nb - 1 - (i - sp * nb);   // the last rows see most: first
+      const int part = SMALL ? sPart[j] : SHARED && j < a.groups ? a.prefix[j].part : a.own[SHARED ? j - a.groups : j].part;
+      const long long per = (((long long)b.c1 - b.c0 + 31) / 32 + n - 1) / n * 32;
+      a.units[(k == 0 ? 0 : a.max_units[0]) + u] = {
+          b.s, (int)min(b.c0 + per * sp, (long long)b.c1), (int)min(b.c0 + per * (sp + 1), (long long)b.c1), b.rows, b.tok,
+          rb * kWideRows, SHARED || n > 1 ? part + sp * a.Hkv * b.rows : -1, b.listed};
     }
-    a.units[u] = x;
-  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    for (int u = (fit ? (int)units0[k] : 0) + tid; u < a.max_units[k]; u += NT) a.units[(k ? a.max_units[0] : 0) + u].s = -1;
 }
 
 // ---------------------------------------------------------------- the units
-constexpr int kRowsPick = 1024;   // places of the table that are looked at together
+// A row of a unit (lane % 32 of a wave) and what it sees: the entry at position p iff p <= at and (at - p < window or
+// p < sinks); SHARED: every live entry.
+struct RowLane {
+  int tok, h, at;
+  bool ok;
+};
+template <bool SHARED>
+__device__ __forceinline__ RowLane row_of(const RowsArgs& a, const Unit& un, int g, int row) {
+  const int r = min(row, un.rows - 1), i = r / a.G;   // lanes past the last row repeat it
+  RowLane x;
+  x.tok = un.listed ? a.list[un.tok + i] : un.tok + i;
+  x.h = g * a.G + r - i * a.G;
+  x.at = SHARED ? INT_MAX - 1 : max(a.q_pos[x.tok], -1);
+  x.ok = row < un.rows;
+  return x;
+}
+template <bool SHARED>
+__device__ __forceinline__ bool seen(const RowsArgs& a, int p, int at) {
+  return p <= at && (SHARED || a.window == 0 || at - p < a.window || p < a.sinks);
+}
+// Whether some row at a position in [lo, hi] may see the entry at p (-1: there is none).
+template <bool SHARED>
+__device__ __forceinline__ bool seen_by_some(const RowsArgs& a, int p, int lo, int hi) {
+  return p >= 0 && (SHARED || (p <= hi && (a.window == 0 || lo - p < a.window || p < a.sinks)));
+}
 
-// A unit walks its run of the table 1,024 places at a time: the slots that some
+// The running softmax of 32 rows (a lane's column) and their sums of V.
+template <int D>
+struct RowState {
+  static constexpr int DB = D / 32;
+  f32x16 acc[DB];
+  float m, l;   // maximum (log2 units), sum
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
+    m = -INFINITY;
+    l = 0.f;
+  }
+  // NKB blocks of 32 keys: masked scores, V in LDS.  The maximum moves only when a score exceeds it by more than 8 (log2
+  // units): probabilities are at most 2^8 then, and bf16 keeps their relative precision.
+  template <int NKB>
+  __device__ __forceinline__ void add(f32x16 (&s)[NKB], const uint16_t* cV, int tl, int th, float scale_log2) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+    if (__ballot(mx * scale_log2 > m + 8.f)) {
+      const float m_new = fmaxf(m, fmaxf(mx, wave_xor32(mx)) * scale_log2);
+      const float alpha = m_new == m ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[d][r] *= alpha;
+      m = m_new;
+    }
+    const float use = m == -INFINITY ? 0.f : m;   // 0 until the row has seen an entry
+    float ls = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][r], scale_log2, -use));
+        s[kb][r] = e;
+        ls += e;
+      }
+    l += ls;
+    __builtin_amdgcn_s_setprio(3);
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16x8 pb = pack8(s[kb], 8 * t);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) acc[d] = mfma32(tr_operand<D, true>(cV, 32 * kb + 16 * t, 32 * d, tl, th), pb, acc[d]);
+      }
+    __builtin_amdgcn_s_setprio(0);
+  }
+  // O and LSE, or the partial results, of row `row`.
+  __device__ __forceinline__ void finish(const RowsArgs& a, const Unit& un, const RowLane& rw, int g, int row, int half) {
+    const float sum = halves_sum(l);
+    if (!rw.ok) return;
+    if (un.part < 0) {
+      const float inv = sum <= 0.f ? 0.f : 1.f / sum;
+      uint16_t* orow = a.o + ((size_t)rw.tok * a.Hq + rw.h) * D;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *reinterpret_cast<uint2*>(orow + 32 * d + 8 * q4 + 4 * half) = pack4_bf16(
+              acc[d][4 * q4] * inv, acc[d][4 * q4 + 1] * inv, acc[d][4 * q4 + 2] * inv, acc[d][4 * q4 + 3] * inv);
+      if (half == 0)
+        a.lse[(size_t)rw.tok * a.Hq + rw.h] = sum <= 0.f ? -INFINITY : (m + __log2f(sum)) * 0.6931471805599453f;
+      return;
+    }
+    const size_t pidx = (size_t)un.part + (size_t)g * un.rows + row;
+    float* dst = a.part + pidx * D;
+    if (!(sum <= 0.f)) {   // else O is left unwritten (the merge skips it)
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *reinterpret_cast<float4*>(dst + 32 * d + 8 * q4 + 4 * half) =
+              make_float4(acc[d][4 * q4], acc[d][4 * q4 + 1], acc[d][4 * q4 + 2], acc[d][4 * q4 + 3]);
+    }
+    if (half == 0) a.part_ml[pidx] = make_float2(m, sum);
+  }
+};
+
+// Places of the table that a wide unit looks at together (more of them and new tokens' loop spills registers).
+template <bool SHARED>
+constexpr int rows_look() { return SHARED ? 1024 : 512; }
+
+// A wide unit walks its run of the table 512 or 1,024 places at a time: the slots that some
 // row of it sees go to a list in LDS (two dependent reads, for all places at
 // once), and the keys and values of the listed slots are gathered tile by tile,
 // double-buffered, each tile read by the four waves.  Scores are S^T = K Q^T
 // (keys on M, rows on N), so that a lane holds 16 scores of one row; softmax and
 // the products with V as in the forward of the eviction mask.
 template <int D, bool SHARED>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) rows_kernel(RowsArgs a) {
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) rows_wide_kernel(RowsArgs a) {
   using LY = Lay<D, true>;
-  constexpr int KS = D / 16, DB = D / 32, BN = rows_bn<D>(), NKB = BN / 32, PITCH = LY::PITCH, TILE = BN * PITCH;
-  constexpr int PIECES = BN * LY::CPRP / kWave, PW = (PIECES + 3) / 4, LOOK = kRowsPick / 256;
+  constexpr int KS = D / 16, BN = rows_bn<D>(), NKB = BN / 32, PITCH = LY::PITCH, TILE = BN * PITCH;
+  constexpr int PIECES = BN * LY::CPRP / kWave, PW = (PIECES + 3) / 4, PICK = rows_look<SHARED>(), LOOK = PICK / 256;
   static_assert(BN * LY::CPRP % kWave == 0, "tile must fill whole 64-slot pieces");
-  __shared__ __attribute__((aligned(1024))) uint16_t sK[2][TILE];
-  __shared__ __attribute__((aligned(1024))) uint16_t sV[2][TILE];
-  __shared__ __attribute__((aligned(16))) uint32_t sRow[kRowsPick];   // rows [block][KV head][row] of the listed slots
-  __shared__ __attribute__((aligned(16))) int sPos[kRowsPick];        // and their positions; INT_MAX: nothing there
-  __shared__ int sCnt[LOOK * 4], sMin[4], sMax[4];
+  __shared__ __attribute__((aligned(1024))) uint16_t sK0[TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t sK1[TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t sV0[TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t sV1[TILE];
+  __shared__ __attribute__((aligned(16))) uint32_t sRow[PICK];   // rows [block][KV head][row] of the listed slots
+  __shared__ __attribute__((aligned(16))) int sPos[PICK];        // and their positions; INT_MAX: nothing there
+  __shared__ int sCnt[LOOK * 4], sAll[4], sMin[4], sMax[4];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
   const int uidx = blockIdx.x / a.Hkv, g = blockIdx.x - uidx * a.Hkv;
@@ -349,19 +478,18 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
   if (un.s < 0) return;
   const auto rl = LY::row_lane(lane);
   const int tl = LY::tr_lo(lane), th = LY::tr_hi(lane);
-
-  // this lane's row: its token and q-head
-  const int row = un.row0 + 32 * wave + col, rr = min(row, un.rows - 1);
-  const bool row_ok = row < un.rows, wave_ok = un.row0 + 32 * wave < un.rows;
-  const int ti = rr / a.G, tok = un.listed ? a.list[un.tok + ti] : un.tok + ti, h = g * a.G + rr - ti * a.G;
+  const int row = un.row0 + 32 * wave + col;
+  const bool wave_ok = un.row0 + 32 * wave < un.rows;
+  int at;   // this lane's row sees entries up to there
   bf16x8 qreg[KS];
   {
-    const uint16_t* qrow = a.q + ((size_t)tok * a.Hq + h) * D + 8 * half;
+    const RowLane rw = row_of<SHARED>(a, un, g, row);
+    at = rw.at;
+    const uint16_t* qrow = a.q + ((size_t)rw.tok * a.Hq + rw.h) * D + 8 * half;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qreg[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qrow + 16 * ks));
   }
-  const int at = SHARED ? INT_MAX - 1 : max(a.q_pos[tok], -1);
-  const int wlo = wave_min(at), whi = wave_max(at);   // lanes past the last row repeat it
+  const int wlo = SHARED ? at : wave_min(at), whi = SHARED ? at : wave_max(at);
   int lo = wlo, hi = whi;
   if (!SHARED) {
     if (lane == 0) {
@@ -375,45 +503,36 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
         lo = min(lo, sMin[w]);
         hi = max(hi, sMax[w]);
       }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
   }
-  // p is seen by the row at position i iff p <= i and (i - p < window or p < sinks)
-  auto seen = [&](int p, int i) __attribute__((always_inline)) {
-    return p <= i && (SHARED || a.window == 0 || i - p < a.window || p < a.sinks);
-  };
+  RowState<D> st;
+  st.init();
+  const int* trow = uniform_ptr(a.table + (size_t)un.s * a.max_blocks);
 
-  f32x16 acc[DB];
-#pragma unroll
-  for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
-  // running maximum (log2 units), the offset of the exponentials (0 until the row has seen an entry), and the raw score
-  // above which the maximum moves
-  float m_run = -INFINITY, l_run = 0.f, m_use = 0.f, thr = -INFINITY;
-  const float inv_scale_log2 = 1.f / a.scale_log2;
-  const int* trow = a.table + (size_t)un.s * a.max_blocks;
-
-  // this lane's 16-byte slots of a tile: row and source element
-  int prow[PW], pcol[PW];
+  // Copies of tile t: this lane's 16-byte slots of it are (wave + 4 i) 64 + lane.  Their tile rows (times 4) and byte
+  // offsets in the source rows, packed: a register more and the loop spills, whose reloads wait for the copies.
+  uint32_t piece[PW];
 #pragma unroll
   for (int i = 0; i < PW; ++i) {
-    const int qs = (wave + 4 * i) * kWave + lane, r = qs / LY::CPRP, pc = qs - r * LY::CPRP;
-    prow[i] = min(r, BN - 1);
-    pcol[i] = pc < LY::CPR ? 8 * (pc ^ LY::flip(r)) : 0;
+    const int qs = (wave + 4 * i) * kWave + lane, r = min(qs / LY::CPRP, BN - 1), pc = qs - qs / LY::CPRP * LY::CPRP;
+    piece[i] = 4u * r | (pc < LY::CPR ? 16u * (pc ^ LY::flip(r)) : 0u) << 16;
   }
-  auto stage = [&](int t) __attribute__((always_inline)) {
-    const int b = t & 1;
+  auto stage = [&](uint16_t* sK, uint16_t* sV, int t) __attribute__((always_inline)) {
+    const uint32_t lk = lds_addr(sK) + wave * kWave * 16, lv = lds_addr(sV) + wave * kWave * 16;
 #pragma unroll
     for (int i = 0; i < PW; ++i) {
       const int n = wave + 4 * i;
       if (i < PW - 1 || PIECES % 4 == 0 || n < PIECES) {
-        const size_t off = (size_t)sRow[t * BN + prow[i]] * D + pcol[i];
-        dma_b128_global(a.kc + off, lds_addr(sK[b]) + n * kWave * 16);
-        dma_b128_global(a.vc + off, lds_addr(sV[b]) + n * kWave * 16);
+        const uint32_t r = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(sRow + t * BN) + (piece[i] & 0xffffu));
+        const size_t off = (size_t)r * (2 * D) + (piece[i] >> 16);
+        dma_b128_global((const char*)a.kc + off, lk + i * 4 * kWave * 16);
+        dma_b128_global((const char*)a.vc + off, lv + i * 4 * kWave * 16);
       }
     }
   };
-
-  auto compute = [&](int t, int cnt) __attribute__((always_inline)) {
-    const uint16_t* cK = sK[t & 1];
-    const uint16_t* cV = sV[t & 1];
+  // `all`: every row of the workgroup sees every entry of the tile
+  auto compute = [&](const uint16_t* cK, const uint16_t* cV, int t, bool all) __attribute__((always_inline)) {
     f32x16 s[NKB];
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb) {
@@ -421,76 +540,45 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) s[kb] = mfma32(lds_read_b128(cK + 32 * kb * PITCH + LY::row_at(rl, ks)), qreg[ks], s[kb]);
     }
-    // whether every row of the wave sees every entry of the tile
-    const int p = sPos[t * BN + (BN == 64 ? lane : col)];
-    const bool full = __ballot(seen(p, wlo) && seen(p, whi)) == ~0ull;
-    if (!full) {
+    if (!all) {
+      const int p = sPos[t * BN + (BN == 64 ? lane : col)];
+      if (__ballot(seen<SHARED>(a, p, wlo) && seen<SHARED>(a, p, whi)) != ~0ull) {
 #pragma unroll
-      for (int kb = 0; kb < NKB; ++kb)
+        for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const int4 e = *reinterpret_cast<const int4*>(&sPos[t * BN + 32 * kb + 8 * q4 + 4 * half]);
-          if (!seen(e.x, at)) s[kb][4 * q4] = -INFINITY;
-          if (!seen(e.y, at)) s[kb][4 * q4 + 1] = -INFINITY;
-          if (!seen(e.z, at)) s[kb][4 * q4 + 2] = -INFINITY;
-          if (!seen(e.w, at)) s[kb][4 * q4 + 3] = -INFINITY;
-        }
-    }
-    float mx = -INFINITY;
-#pragma unroll
-    for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-    if (__ballot(mx > thr)) {
-      const float m_new = fmaxf(m_run, fmaxf(mx, wave_xor32(mx)) * a.scale_log2);
-      const float alpha = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-      l_run *= alpha;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[d][r] *= alpha;
-      m_run = m_new;
-      m_use = m_run == -INFINITY ? 0.f : m_run;
-      thr = (m_run + 8.f) * inv_scale_log2;
-    }
-    float ls = 0.f;
-#pragma unroll
-    for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][r], a.scale_log2, -m_use));
-        s[kb][r] = e;
-        ls += e;
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const int4 e = *reinterpret_cast<const int4*>(&sPos[t * BN + 32 * kb + 8 * q4 + 4 * half]);
+            if (!seen<SHARED>(a, e.x, at)) s[kb][4 * q4] = -INFINITY;
+            if (!seen<SHARED>(a, e.y, at)) s[kb][4 * q4 + 1] = -INFINITY;
+            if (!seen<SHARED>(a, e.z, at)) s[kb][4 * q4 + 2] = -INFINITY;
+            if (!seen<SHARED>(a, e.w, at)) s[kb][4 * q4 + 3] = -INFINITY;
+          }
       }
-    l_run += ls;
-#pragma unroll
-    for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        const bf16x8 pb = pack8(s[kb], 8 * t2);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) acc[d] = mfma32(tr_operand<D, true>(cV, 32 * kb + 16 * t2, 32 * d, tl, th), pb, acc[d]);
-      }
+    }
+    st.template add<NKB>(s, cV, tl, th, a.scale_log2);
   };
 
-  for (long long base = un.c0; base < un.c1; base += kRowsPick) {
-    // the slots of the next 1,024 places that some row sees, in the table's order
-    int slot[LOOK], pos[LOOK];
+  for (int base = un.c0; base < un.c1; base += PICK) {
+    // the slots of the next places that some row sees, in the table's order
+    int slot[LOOK], pos[LOOK], blk[LOOK];
     unsigned long long vis[LOOK];
 #pragma unroll
     for (int k = 0; k < LOOK; ++k) {
-      const long long c = base + k * 256 + tid;
-      const int blk = (int)(c / a.BS), e = c < un.c1 ? trow[blk] : -1;
-      slot[k] = (unsigned)e < (unsigned)a.num_blocks ? e * a.BS + (int)(c - (long long)blk * a.BS) : -1;
+      const int c = base + k * 256 + tid, b = block_of(a, c);
+      blk[k] = c < un.c1 ? trow[b] : -1;
+      slot[k] = (unsigned)blk[k] < (unsigned)a.num_blocks ? blk[k] * a.BS + (c - b * a.BS) : -1;
     }
 #pragma unroll
     for (int k = 0; k < LOOK; ++k) pos[k] = slot[k] >= 0 ? a.slot_pos[slot[k]] : -1;
     if (base != un.c0) __syncthreads();   // the lists are read
+    int all = 0;
 #pragma unroll
     for (int k = 0; k < LOOK; ++k) {
-      vis[k] = __ballot(pos[k] >= 0 && (SHARED || (pos[k] <= hi && (a.window == 0 || lo - pos[k] < a.window || pos[k] < a.sinks))));
+      vis[k] = __ballot(seen_by_some<SHARED>(a, pos[k], lo, hi));
+      if (!SHARED) all += __builtin_popcountll(vis[k] & __ballot(seen<SHARED>(a, pos[k], lo) && seen<SHARED>(a, pos[k], hi)));
       if (lane == 0) sCnt[k * 4 + wave] = __builtin_popcountll(vis[k]);
     }
+    if (!SHARED && lane == 0) sAll[wave] = all;
     __syncthreads();
     int cnt = 0, mine[LOOK];
 #pragma unroll
@@ -502,12 +590,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
       }
     cnt = __builtin_amdgcn_readfirstlane(cnt);
     if (cnt == 0) continue;
-    const int ntile = (cnt + BN - 1) / BN;
+    const bool full = SHARED || __builtin_amdgcn_readfirstlane(sAll[0] + sAll[1] + sAll[2] + sAll[3]) == cnt;
+    const int ntile = (cnt + BN - 1) / BN, last = cnt % BN ? ntile - 1 : ntile;   // the tile that is not full
 #pragma unroll
     for (int k = 0; k < LOOK; ++k)
       if ((vis[k] >> lane) & 1ull) {
-        const int i = mine[k] + __builtin_popcountll(vis[k] & ((1ull << lane) - 1ull)), blk = slot[k] / a.BS;
-        const uint32_t r = ((uint32_t)blk * a.Hkv + g) * a.BS + (slot[k] - blk * a.BS);
+        const int i = mine[k] + __builtin_popcountll(vis[k] & ((1ull << lane) - 1ull));
+        const uint32_t r = ((uint32_t)blk[k] * a.Hkv + g) * a.BS + (slot[k] - blk[k] * a.BS);
         sRow[i] = r;
         sPos[i] = SHARED ? 0 : pos[k];
         if (i == cnt - 1)   // the last tile's places behind it repeat it, and nobody sees them
@@ -517,45 +606,184 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
           }
       }
     __syncthreads();
-    stage(0);
-    for (int t = 0; t < ntile; ++t) {
+    auto step = [&](uint16_t* cK, uint16_t* cV, uint16_t* nK, uint16_t* nV, int t) __attribute__((always_inline)) {
       wait_vm();
       __syncthreads();   // tile t is there, and nobody reads tile t - 1 any more
-      if (t + 1 < ntile) stage(t + 1);
-      if (t == ntile - 1 && cnt % BN) {   // V of the places behind the last entry: their factor is 0, and must stay it
-        for (int x = tid; x < (ntile * BN - cnt) * (PITCH / 8); x += 256)
-          *reinterpret_cast<uint4*>(&sV[t & 1][(BN - (ntile * BN - cnt)) * PITCH + 8 * x]) = make_uint4(0u, 0u, 0u, 0u);
+      if (t + 1 < ntile) stage(nK, nV, t + 1);
+      if (t == last) {   // V of the places behind the last entry: their factor is 0, and must stay it
+        const int n = cnt - t * BN;
+        for (int x = tid; x < (BN - n) * (PITCH / 2); x += 256) reinterpret_cast<uint32_t*>(cV + n * PITCH)[x] = 0u;
         __syncthreads();
       }
-      if (wave_ok) compute(t, cnt);
+      if (wave_ok) compute(cK, cV, t, full && t != last);
+    };
+    stage(sK0, sV0, 0);
+    for (int t = 0;;) {
+      step(sK0, sV0, sK1, sV1, t);
+      if (++t >= ntile) break;
+      step(sK1, sV1, sK0, sV0, t);
+      if (++t >= ntile) break;
     }
   }
+  st.finish(a, un, row_of<SHARED>(a, un, g, row), g, row, half);
+}
 
-  const float l_tot = halves_sum(l_run);
-  if (!row_ok) return;
-  if (un.part < 0) {
-    const float inv = l_tot <= 0.f ? 0.f : 1.f / l_tot;
-    uint16_t* orow = a.o + ((size_t)tok * a.Hq + h) * D;
+// A narrow unit, 32 rows at most, is one wave, with its own tiles of 32 entries (double-buffered; D = 128: 40 KB of LDS,
+// so that four share a CU, one a SIMD).  Every global read of its loop is a copy to LDS, so all of them complete in
+// issue order under one counter: step n issues the K and V copies of tile n + 1, waits until only these are
+// outstanding, asks for the next piece of what the tiles after it need, and computes tile n.  That is, for 192 places
+// of the table at a time, in consecutive steps: their table entries; the positions of the slots these name; and, when
+// the list of slots to gather runs short, the slots that some row sees are added to it (a ring of 256).
+constexpr int kNarrowPick = 192, kNarrowRing = 256;
+template <int D, bool SHARED>
+__global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
+  using LY = Lay<D, true>;
+  constexpr int KS = D / 16, BN = 32, PITCH = LY::PITCH, TILE = BN * PITCH, NP = kNarrowPick / kWave;
+  constexpr int SLOTS = BN * LY::CPRP, NI = (SLOTS + kWave - 1) / kWave, OPS = 2 * NI;   // copies of a tile
+  __shared__ __attribute__((aligned(1024))) uint16_t sK[2 * TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t sV[2 * TILE];
+  __shared__ __attribute__((aligned(256))) int sTab[kNarrowPick];
+  __shared__ __attribute__((aligned(256))) int sSlot[kNarrowPick];
+  __shared__ __attribute__((aligned(16))) uint32_t sRow[kNarrowRing];
+  __shared__ __attribute__((aligned(16))) int sPos[kNarrowRing];
+  static_assert(kNarrowRing >= kNarrowPick + 2 * BN, "what is left of the last places, the tile in work, new ones");
+
+  const int lane = threadIdx.x, half = lane >> 5, col = lane & 31;
+  const int uidx = blockIdx.x / a.Hkv, g = blockIdx.x - uidx * a.Hkv;
+  const Unit un = a.units[a.max_units[0] + uidx];
+  if (un.s < 0) return;
+  const auto rl = LY::row_lane(lane);
+  const int tl = LY::tr_lo(lane), th = LY::tr_hi(lane);
+  const RowLane rw = row_of<SHARED>(a, un, g, col);
+  bf16x8 qreg[KS];
+  {
+    const uint16_t* qrow = a.q + ((size_t)rw.tok * a.Hq + rw.h) * D + 8 * half;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
-        *reinterpret_cast<uint2*>(orow + 32 * d + 8 * q4 + 4 * half) =
-            pack4_bf16(acc[d][4 * q4] * inv, acc[d][4 * q4 + 1] * inv, acc[d][4 * q4 + 2] * inv, acc[d][4 * q4 + 3] * inv);
-    if (half == 0) a.lse[(size_t)tok * a.Hq + h] = l_tot <= 0.f ? -INFINITY : (m_run + __log2f(l_tot)) * 0.6931471805599453f;
-    return;
+    for (int ks = 0; ks < KS; ++ks) qreg[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qrow + 16 * ks));
   }
-  const size_t pidx = (size_t)un.part + (size_t)g * un.rows + row;
-  float* dst = a.part + pidx * D;
-  if (!(l_tot <= 0.f)) {   // else O is left unwritten (the merge skips it)
+  const int lo = SHARED ? rw.at : wave_min(rw.at), hi = SHARED ? rw.at : wave_max(rw.at);
+  RowState<D> st;
+  st.init();
+  const int* trow = a.table + (size_t)un.s * a.max_blocks;
+
+  int prow[NI], pcol[NI];   // this lane's 16-byte slots of a tile: row (-1: none), source element
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
-        *reinterpret_cast<float4*>(dst + 32 * d + 8 * q4 + 4 * half) =
-            make_float4(acc[d][4 * q4], acc[d][4 * q4 + 1], acc[d][4 * q4 + 2], acc[d][4 * q4 + 3]);
+  for (int i = 0; i < NI; ++i) {
+    const int qs = i * kWave + lane, r = qs / LY::CPRP, pc = qs - r * LY::CPRP;
+    prow[i] = qs < SLOTS ? r : -1;
+    pcol[i] = qs < SLOTS && pc < LY::CPR ? 8 * (pc ^ LY::flip(r)) : 0;
   }
-  if (half == 0) a.part_ml[pidx] = make_float2(m_run, l_tot);
+  unsigned tail = 0;             // entries listed so far
+  int next = un.c0, asked = 0;   // first place not asked for; first one of those in work
+  int stage = 0;                 // of these: 0 none, 1 table entries asked for, 2 positions asked for, 3 there
+  auto place = [&](int k) __attribute__((always_inline)) { return (int)min((long long)asked + k * kWave + lane, un.c1 - 1ll); };
+  auto ask_table = [&]() __attribute__((always_inline)) {
+    asked = next;
+    next = (int)min((long long)next + kNarrowPick, (long long)un.c1);
+#pragma unroll
+    for (int k = 0; k < NP; ++k) dma_b32_global(trow + block_of(a, place(k)), lds_addr(&sTab[k * kWave]));
+    stage = 1;
+  };
+  // the slot of a place, by its landed table entry (-1: an entry outside the cache)
+  auto slot_of = [&](int k, int& blk) __attribute__((always_inline)) {
+    const int c = place(k);
+    blk = sTab[k * kWave + lane];
+    return (unsigned)blk < (unsigned)a.num_blocks ? blk * a.BS + (c - block_of(a, c) * a.BS) : -1;
+  };
+  auto ask_pos = [&]() __attribute__((always_inline)) {
+    int blk, slot[NP];
+#pragma unroll
+    for (int k = 0; k < NP; ++k) slot[k] = slot_of(k, blk);
+#pragma unroll
+    for (int k = 0; k < NP; ++k) dma_b32_global(a.slot_pos + max(slot[k], 0), lds_addr(&sSlot[k * kWave]));
+    stage = 2;
+  };
+  auto enlist = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      int blk;
+      const int slot = slot_of(k, blk), pos = sSlot[k * kWave + lane];
+      const bool vis = asked + k * kWave + lane < next && slot >= 0 && seen_by_some<SHARED>(a, pos, lo, hi);
+      const unsigned long long m = __ballot(vis);
+      if (vis) {
+        const unsigned i = (tail + __builtin_popcountll(m & ((1ull << lane) - 1ull))) % kNarrowRing;
+        sRow[i] = ((uint32_t)blk * a.Hkv + g) * a.BS + (slot - blk * a.BS);
+        if (!SHARED) sPos[i] = pos;
+      }
+      tail = __builtin_amdgcn_readfirstlane(tail + __builtin_popcountll(m));
+    }
+    stage = 0;
+  };
+  // Entries from `head` on that make the next tile; lists more where they are short of one.
+  auto ready = [&](unsigned head) __attribute__((always_inline)) {
+    if (tail - head < BN && stage == 3) enlist();
+    while (tail - head < BN && (stage > 0 || next < un.c1)) {   // at the start, and where places show few entries
+      if (stage == 0) ask_table();
+      if (stage == 1) {
+        wait_vm_le<0>();
+        ask_pos();
+      }
+      wait_vm_le<0>();
+      enlist();
+    }
+    return min(tail - head, (unsigned)BN);
+  };
+  auto gather = [&](int b, unsigned head, int n) __attribute__((always_inline)) {
+    uint32_t r[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) r[i] = sRow[(head + min(max(prow[i], 0), n - 1)) % kNarrowRing];   // past the last: it again
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (i * kWave + kWave <= SLOTS || prow[i] >= 0) {
+        const size_t off = (size_t)r[i] * D + pcol[i];
+        dma_b128_global(a.kc + off, lds_addr(sK + b * TILE) + i * kWave * 16);
+        dma_b128_global(a.vc + off, lds_addr(sV + b * TILE) + i * kWave * 16);
+      }
+  };
+
+  wait_vm_le<0>();   // Q is in: no compiler-visible load stays pending in the loop
+  unsigned head = 0;
+  int n = (int)ready(0), b = 0;
+  if (n > 0) gather(0, 0, n);
+  while (n > 0) {
+    const int n1 = n == BN ? (int)ready(head + BN) : 0;
+    if (n1 > 0) {
+      gather(b ^ 1, head + BN, n1);
+      wait_vm_le<OPS>();
+    } else {
+      wait_vm_le<0>();
+    }
+    if (stage == 0 && next < un.c1) ask_table();
+    else if (stage == 1) ask_pos();
+    else if (stage == 2) stage = 3;
+    const uint16_t* cK = sK + b * TILE;
+    uint16_t* cV = sV + b * TILE;
+    f32x16 s[1] = {f32x16{}};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s[0] = mfma32(lds_read_b128(cK + LY::row_at(rl, ks)), qreg[ks], s[0]);
+    if (n < BN) {   // V of the places behind the last entry: their factor is 0, and must stay it
+      for (int x = lane; x < (BN - n) * (PITCH / 8); x += kWave)
+        *reinterpret_cast<uint4*>(&cV[n * PITCH + 8 * x]) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    const int p = SHARED ? 0 : sPos[(head + col) % kNarrowRing];
+    if (__ballot(col < n && (SHARED || (seen<SHARED>(a, p, lo) && seen<SHARED>(a, p, hi)))) != ~0ull) {
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int i = 8 * q4 + 4 * half;
+        int4 e = make_int4(0, 0, 0, 0);
+        if (!SHARED) e = *reinterpret_cast<const int4*>(&sPos[(head + i) % kNarrowRing]);   // head: a multiple of 32
+        if (!(i < n && seen<SHARED>(a, e.x, rw.at))) s[0][4 * q4] = -INFINITY;
+        if (!(i + 1 < n && seen<SHARED>(a, e.y, rw.at))) s[0][4 * q4 + 1] = -INFINITY;
+        if (!(i + 2 < n && seen<SHARED>(a, e.z, rw.at))) s[0][4 * q4 + 2] = -INFINITY;
+        if (!(i + 3 < n && seen<SHARED>(a, e.w, rw.at))) s[0][4 * q4 + 3] = -INFINITY;
+      }
+    }
+    st.template add<1>(s, cV, tl, th, a.scale_log2);
+    head += BN;
+    n = n1;
+    b ^= 1;
+  }
+  st.finish(a, un, rw, g, col, half);
 }
 
 // ---------------------------------------------------------------- the merge
@@ -563,102 +791,122 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
 // sequence's splits.  D / 4 lanes read one partial result as float4.
 template <int D, bool SHARED>
 __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
-  constexpr int LPS = D / 4, PER = kWave / LPS;
+  constexpr int LPS = D / 4, PER = kWave / LPS, UNROLL = 4;
   const int lane = threadIdx.x & 63;
-  const long long r = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= (long long)a.ntok * a.Hq) return;
-  const int tok = (int)(r / a.Hq), h = (int)(r - (long long)tok * a.Hq), g = h / a.G;
-  Parts set[2] = {};
-  long long at[2] = {};
-  int s = tok;
-  if (!SHARED) {   // the sequence of the token: the last one that begins at or before it
-    s = 0;
-    for (int step = 1 << (31 - __builtin_clz(a.S)); step > 0; step >>= 1)
-      if (s + step < a.S && a.cu[s + step] <= tok) s += step;
-    const int t0 = min(max(a.cu[s], 0), a.ntok), t1 = min(max(a.cu[s + 1], t0), a.ntok);
-    if (tok < t0 || tok >= t1) return;
-    set[0] = a.own[s];
-    if (set[0].n == 0) return;   // written by its unit
-    at[0] = (long long)(tok - t0) * a.G;
-  } else {
-    set[0] = a.own[s];
-    const int grp = a.prefix_group[s];
-    if ((unsigned)grp < (unsigned)a.groups) {
-      set[1] = a.prefix[grp];
-      at[1] = (long long)a.rank[s] * a.G;
+  if (!SHARED && a.parts[0] == 0) return;   // every row is written by its unit
+  const long long all = (long long)a.ntok * a.Hq;
+  for (long long r = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); r < all; r += (long long)gridDim.x * 4) {
+    const int tok = (int)(r / a.Hq), h = (int)(r - (long long)tok * a.Hq), g = h / a.G;
+    Parts set[2] = {};
+    long long at[2] = {};
+    if (!SHARED) {   // the sequence of the token: the last one that begins at or before it
+      int s = 0;
+      for (int step = 1 << (31 - __builtin_clz(a.S)); step > 0; step >>= 1)
+        if (s + step < a.S && a.cu[s + step] <= tok) s += step;
+      const int t0 = min(max(a.cu[s], 0), a.ntok), t1 = min(max(a.cu[s + 1], t0), a.ntok);
+      if (tok < t0 || tok >= t1) continue;
+      set[0] = a.own[s];
+      if (set[0].n == 0) continue;   // written by its unit
+      at[0] = (long long)(tok - t0) * a.G;
+    } else {
+      set[0] = a.own[tok];
+      const int grp = a.prefix_group[tok];
+      if ((unsigned)grp < (unsigned)a.groups) {
+        set[1] = a.prefix[grp];
+        at[1] = (long long)a.rank[tok] * a.G;
+      }
     }
-  }
 #pragma unroll
-  for (int k = 0; k < 2; ++k) at[k] += set[k].part + (long long)g * set[k].rows + (h - g * a.G);
-  const int n = set[0].n + set[1].n;
-  auto where = [&](int i) {
-    return i < set[0].n ? at[0] + (long long)i * a.Hkv * set[0].rows : at[1] + (long long)(i - set[0].n) * a.Hkv * set[1].rows;
-  };
-  float M = -INFINITY;
-  for (int i = lane; i < n; i += kWave) {
-    const float2 v = a.part_ml[where(i)];
-    if (!(v.y <= 0.f)) M = fmaxf(M, v.x);
-  }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
-  float L = 0.f;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = lane / LPS; i < n; i += PER) {
-    const long long w = where(i);
-    const float2 v = a.part_ml[w];
-    if (!(v.y <= 0.f)) {
-      const float f = __builtin_amdgcn_exp2f(v.x - M);
-      const float4 y = reinterpret_cast<const float4*>(a.part + w * D)[lane & (LPS - 1)];
-      L += v.y * f;
-      x.x += y.x * f;
-      x.y += y.y * f;
-      x.z += y.z * f;
-      x.w += y.w * f;
+    for (int k = 0; k < 2; ++k) at[k] += set[k].part + (long long)g * set[k].rows + (h - g * a.G);
+    const int n = set[0].n + set[1].n;
+    auto where = [&](int i) {
+      return i < set[0].n ? at[0] + (long long)i * a.Hkv * set[0].rows : at[1] + (long long)(i - set[0].n) * a.Hkv * set[1].rows;
+    };
+    float M = -INFINITY;
+    for (int i = lane; i < n; i += kWave) {
+      const float2 v = a.part_ml[where(i)];
+      if (!(v.y <= 0.f)) M = fmaxf(M, v.x);
     }
-  }
 #pragma unroll
-  for (int off = LPS; off < kWave; off <<= 1) {
-    L += __shfl_xor(L, off);
-    x.x += __shfl_xor(x.x, off);
-    x.y += __shfl_xor(x.y, off);
-    x.z += __shfl_xor(x.z, off);
-    x.w += __shfl_xor(x.w, off);
-  }
-  if (lane < LPS) {
-    const float inv = L <= 0.f ? 0.f : 1.f / L;
-    reinterpret_cast<uint2*>(a.o + r * D)[lane] = pack4_bf16(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
-    if (lane == 0) a.lse[r] = L <= 0.f ? -INFINITY : (M + __log2f(L)) * 0.6931471805599453f;
+    for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+    float L = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = lane / LPS; i0 < n; i0 += UNROLL * PER) {
+      float2 v[UNROLL];
+      float4 y[UNROLL];
+#pragma unroll
+      for (int k = 0; k < UNROLL; ++k) {   // the last ones again behind the end
+        const long long w = where(min(i0 + k * PER, n - 1));
+        v[k] = a.part_ml[w];
+        y[k] = reinterpret_cast<const float4*>(a.part + w * D)[lane & (LPS - 1)];
+      }
+#pragma unroll
+      for (int k = 0; k < UNROLL; ++k)
+        if (i0 + k * PER < n && !(v[k].y <= 0.f)) {
+          const float f = __builtin_amdgcn_exp2f(v[k].x - M);
+          L += v[k].y * f;
+          x.x += y[k].x * f;
+          x.y += y[k].y * f;
+          x.z += y[k].z * f;
+          x.w += y[k].w * f;
+        }
+    }
+#pragma unroll
+    for (int off = LPS; off < kWave; off <<= 1) {
+      L += __shfl_xor(L, off);
+      x.x += __shfl_xor(x.x, off);
+      x.y += __shfl_xor(x.y, off);
+      x.z += __shfl_xor(x.z, off);
+      x.w += __shfl_xor(x.w, off);
+    }
+    if (lane < LPS) {
+      const float inv = L <= 0.f ? 0.f : 1.f / L;
+      reinterpret_cast<uint2*>(a.o + r * D)[lane] = pack4_bf16(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+      if (lane == 0) a.lse[r] = L <= 0.f ? -INFINITY : (M + __log2f(L)) * 0.6931471805599453f;
+    }
   }
 }
 
 // ---------------------------------------------------------------- launchers
 static size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Units per KV head that fill the chip: three workgroups a CU.
-static int rows_want(int Hkv) { return (3 * 256 + Hkv - 1) / Hkv; }
+// Units per KV head that fill the chip: three wide ones a CU, four narrow ones (D = 64: seven).
+static int rows_want(int Hkv, int D, bool wide) { return ((wide ? 3 : D == 128 ? 4 : 7) * 256 + Hkv - 1) / Hkv; }
 // Sizes of a call's workspace, in this order.
 struct RowsSpace {
-  long long units, part;   // units per KV head; partial rows
-  size_t rank, count, base, list, first, own, prefix, unit, rows, ml;
-  size_t bytes() const { return rank + count + base + list + first + own + prefix + unit + rows + ml; }
+  long long units[2], part;   // units per KV head, wide and narrow; partial rows
+  size_t parts, rank, list, count, base, jobs, own, prefix, unit, rows, ml;
+  size_t bytes() const { return parts + rank + list + count + base + jobs + own + prefix + unit + rows + ml; }
 };
-// Row blocks: at most one a job beside the full ones.  Partial rows: one for every row of every job, and what the splits
-// of half a round of units take.
+static bool plans_small(const PagedRows& p) { return p.S <= kPlanSmall && p.groups <= kPlanSmall; }
+// Row blocks of wide jobs: one for every 128 rows, and one more a job (of 33 rows at least; SHARED: groups, and sequences
+// by themselves if they have so many q-heads).  Splits add no more than `want` units of a kind (rows_plan_kernel), and a
+// job has none of fewer than kLeastTiles tiles.  Partial rows: those of every job once and of the units that splits add;
+// for new tokens only those of jobs that are split, each into two at least, so twice those of the added units.
 static RowsSpace rows_space(const PagedRows& p) {
   RowsSpace x{};
-  const long long G = p.Hq / p.Hkv, want = rows_want(p.Hkv);
-  const long long tokens = p.shared ? p.S : p.ntok, jobs = (long long)p.S + p.groups;
-  const long long blocks = (p.shared ? p.S : 0) + tokens * G / kRowBlock + (p.shared ? p.groups : p.S);
-  x.units = std::max(want, blocks + want / 2);
-  x.part = ((p.shared ? 2 : 1) * tokens * G + want * kRowBlock) * p.Hkv;
+  const long long G = p.Hq / p.Hkv, tokens = p.shared ? p.S : p.ntok, all = tokens * G;
+  const long long width = ((long long)p.max_blocks * p.block_size + 31) / 32, splits = (width + kLeastTiles - 1) / kLeastTiles;
+  const long long wide_jobs = std::min<long long>(p.shared ? p.groups : p.S, all / kNarrowRows) + (p.shared && G > kNarrowRows ? p.S : 0);
+  const long long blocks[2] = {all > kNarrowRows ? all / kWideRows + wide_jobs : 0, (p.shared ? (long long)p.groups : 0) + p.S};
+  long long added = 0;
+  for (int k = 0; k < 2; ++k) {
+    const long long want = rows_want(p.Hkv, p.D, k == 0);
+    x.units[k] = std::min(blocks[k] * splits, std::max(want, blocks[k] + want / 2));
+    added += std::min(want, x.units[k]) * (k == 0 ? kWideRows : kNarrowRows);
+  }
+  x.part = (p.shared ? 2 * all + added : 2 * added) * p.Hkv;
+  x.parts = 256;
   if (p.shared) {
     x.rank = x.list = round256((size_t)p.S * sizeof(int));
-    x.count = x.base = round256((size_t)p.groups * sizeof(int));
     x.prefix = round256((size_t)p.groups * sizeof(Parts));
   }
-  x.first = round256((size_t)(jobs + 1) * sizeof(int));
+  if (!plans_small(p)) {
+    if (p.shared) x.count = x.base = round256((size_t)p.groups * sizeof(int));
+    x.jobs = round256(4 * ((size_t)p.S + p.groups + 1) * sizeof(int));
+  }
   x.own = round256((size_t)p.S * sizeof(Parts));
-  x.unit = round256((size_t)x.units * sizeof(Unit));
+  x.unit = round256((size_t)(x.units[0] + x.units[1]) * sizeof(Unit));
   x.rows = round256((size_t)x.part * p.D * sizeof(float));
   x.ml = round256((size_t)x.part * sizeof(float2));
   return x;
@@ -667,19 +915,25 @@ size_t paged_rows_ws_bytes(const PagedRows& p) { return rows_space(p).bytes(); }
 bool paged_rows_fit(const PagedRows& p) {
   const RowsSpace x = rows_space(p);
   const long long rows = (long long)(p.shared ? p.S : p.ntok) * p.Hq;
-  return x.units * p.Hkv <= 0x7fffffffll / 256 && x.part <= 0x7fffffffll && rows <= (1ll << 26) - 4;
+  return std::max(x.units[0], x.units[1]) * p.Hkv <= 0x7fffffffll / 256 && x.part <= 0x7fffffffll && rows <= (1ll << 26) - 4;
 }
 
 template <int D, bool SHARED>
 static hipError_t launch_rows(const PagedRows& p, const RowsArgs& a) {
-  hipLaunchKernelGGL(rows_plan_kernel<SHARED>, dim3(1), dim3(kPlanThreads), 0, p.stream, a);
+  if (plans_small(p)) hipLaunchKernelGGL((rows_plan_kernel<SHARED, kWave>), dim3(1), dim3(kWave), 0, p.stream, a);
+  else hipLaunchKernelGGL((rows_plan_kernel<SHARED, 1024>), dim3(1), dim3(1024), 0, p.stream, a);
   prof_begin(SHARED ? "paged_decode_shared" : "paged_extend", p.stream);
-  hipLaunchKernelGGL((rows_kernel<D, SHARED>), dim3((unsigned)(a.max_units * a.Hkv)), dim3(256), 0, p.stream, a);
+  if (a.max_units[0])
+    hipLaunchKernelGGL((rows_wide_kernel<D, SHARED>), dim3((unsigned)((long long)a.max_units[0] * a.Hkv)), dim3(256), 0,
+                       p.stream, a);
+  hipLaunchKernelGGL((rows_narrow_kernel<D, SHARED>), dim3((unsigned)((long long)a.max_units[1] * a.Hkv)), dim3(64), 0,
+                     p.stream, a);
   prof_end(p.stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const long long rows = (long long)a.ntok * a.Hq;
-  hipLaunchKernelGGL((rows_merge_kernel<D, SHARED>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, p.stream, a);
+  hipLaunchKernelGGL((rows_merge_kernel<D, SHARED>), dim3((unsigned)std::min((rows + 3) / 4, 4096ll)), dim3(256), 0,
+                     p.stream, a);
   return hipGetLastError();
 }
 
@@ -707,6 +961,7 @@ hipError_t launch_paged_rows(const PagedRows& p) {
   a.max_blocks = p.max_blocks;
   a.BS = p.block_size;
   a.num_blocks = p.num_blocks;
+  a.shift = p.block_size & (p.block_size - 1) ? -1 : __builtin_ctz((unsigned)p.block_size);
   a.window = p.window;
   a.sinks = p.sinks;
   a.scale_log2 = p.scale * 1.4426950408889634f;
@@ -716,19 +971,22 @@ hipError_t launch_paged_rows(const PagedRows& p) {
     w += bytes;
     return at;
   };
+  a.parts = (int*)take(x.parts);
   a.rank = (int*)take(x.rank);
+  a.list = (int*)take(x.list);
   a.count = (int*)take(x.count);
   a.base = (int*)take(x.base);
-  a.list = (int*)take(x.list);
-  a.first = (int*)take(x.first);
+  a.jobs = (int*)take(x.jobs);
   a.own = (Parts*)take(x.own);
   a.prefix = (Parts*)take(x.prefix);
   a.units = (Unit*)take(x.unit);
   a.part = (float*)take(x.rows);
   a.part_ml = (float2*)take(x.ml);
-  a.max_units = (int)x.units;
   a.max_part = x.part;
-  a.want = rows_want(p.Hkv);
+  for (int k = 0; k < 2; ++k) {
+    a.max_units[k] = (int)x.units[k];
+    a.want[k] = rows_want(p.Hkv, p.D, k == 0);
+  }
   if (p.shared) return p.D == 128 ? launch_rows<128, true>(p, a) : launch_rows<64, true>(p, a);
   return p.D == 128 ? launch_rows<128, false>(p, a) : launch_rows<64, false>(p, a);
 }

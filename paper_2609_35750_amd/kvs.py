@@ -88,10 +88,10 @@ SIGNATURES = {
     "kvs_paged_decode_ex": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _F, _I, _I,
                                  _P, _Z, _P]),
     "kvs_paged_copy": (_I, [_P, _P, _I, _P, _P, _P, _P, _I, _I, _I, _I, _I, _P]),
-    "kvs_paged_decode_shared_workspace": (_Z, [_I, _I, _I, _I, _I]),
+    "kvs_paged_decode_shared_workspace": (_Z, [_I, _I, _I, _I, _I, _I, _I]),
     "kvs_paged_decode_shared": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _F, _P, _Z,
                                      _P]),
-    "kvs_paged_extend_workspace": (_Z, [_I, _I, _I, _I, _I]),
+    "kvs_paged_extend_workspace": (_Z, [_I, _I, _I, _I, _I, _I, _I]),
     "kvs_paged_extend": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _F, _I, _I, _P, _Z,
                               _P]),
     "kvs_paged_decode_workspace": (_Z, [_I, _I, _I, _I, _I, _I]),

@@ -339,7 +339,7 @@ def kvs_paged_decode_shared(q, k_cache, v_cache, slot_pos, block_table, seq_bloc
     if prefix_blocks.dim() != 1 or prefix_blocks.numel() < 1:
         raise ValueError("prefix_blocks must be [groups], one group at least")
     groups = prefix_blocks.numel()
-    need = lib.kvs_paged_decode_shared_workspace(S, groups, Hq, Hkv, D)
+    need = lib.kvs_paged_decode_shared_workspace(S, groups, Hq, Hkv, D, block_table.shape[1], bs)
     ws = _workspace(need, q.device)
     with _on(q):
         _check("kvs_paged_decode_shared", lib.kvs_paged_decode_shared(
@@ -367,7 +367,7 @@ def kvs_paged_extend(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, q_p
         raise ValueError("q_pos must be [Ntot] and cu_seqlens [S + 1]")
     if window is not None and window < 1:
         raise ValueError("window must be >= 1 (None: no window)")
-    need = lib.kvs_paged_extend_workspace(S, n, Hq, Hkv, D)
+    need = lib.kvs_paged_extend_workspace(S, n, Hq, Hkv, D, block_table.shape[1], bs)
     ws = _workspace(need, q.device)
     with _on(q):
         _check("kvs_paged_extend", lib.kvs_paged_extend(

@@ -322,8 +322,8 @@ def test_refusals_of_each(paged):
     assert _extend(lib, pos=None) == _extend(lib, cu=None) == k.KVS_ERR_NULL
     assert _extend(lib, n=0, q=None, pos=None, cu=None, ws=None, ws_bytes=0) == k.KVS_OK
     for bad in ((0, 1, 1, 64), (1, 0, 1, 64), (1, 1, 0, 64), (1, 1, 1, 0)):
-        assert lib.kvs_paged_decode_shared_workspace(bad[0], 1, bad[1], bad[2], bad[3]) == 0
-        assert lib.kvs_paged_extend_workspace(bad[0], 5, bad[1], bad[2], bad[3]) == 0
+        assert lib.kvs_paged_decode_shared_workspace(bad[0], 1, bad[1], bad[2], bad[3], 4, 16) == 0
+        assert lib.kvs_paged_extend_workspace(bad[0], 5, bad[1], bad[2], bad[3], 4, 16) == 0
 
     def copy(src=FAKE, dst=FAKE, n=3, kc=FAKE, pos=FAKE, move=0, nb=10, bs=16, Hkv=2, D=64):
         return lib.kvs_paged_copy(src, dst, n, kc, FAKE, pos, None, move, nb, bs, Hkv, D, None)
