@@ -199,6 +199,15 @@ __device__ __forceinline__ void dma_b128_global(const void* src, uint32_t lds) {
       : "v"(src), "s"(lds)
       : "memory");
 }
+// The same for bytes that other waves read too.
+__device__ __forceinline__ void dma_b128_cached(const void* src, uint32_t lds) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(src), "s"(lds)
+      : "memory");
+}
 // Asynchronous copy of 4 bytes from this lane's own global address to LDS byte
 // address lds + 4 l.
 __device__ __forceinline__ void dma_b32_global(const void* src, uint32_t lds) {

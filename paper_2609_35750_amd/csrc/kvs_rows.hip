@@ -72,15 +72,21 @@ constexpr int rows_bn() { return D == 128 ? 32 : 64; }   // keys of a tile of wi
 constexpr int kLeastTiles = 4;    // of a unit, in 32-key tiles
 constexpr int kPlanSmall = 256;   // sequences, and groups, that one wave plans, in LDS
 
-// What a unit is, as its workgroups read it.
+// What the plan weighs for wide units: with w tiles of work for each place on the chip the last unit ends about half the
+// longest unit behind w, and one of a split job costs as much as these tiles more, for its partial results.
+constexpr float kSplitTiles = 20.f;
+constexpr int kChunk = 64;        // places of a table that are skipped or looked at together
+
+// What a unit is, as its workgroups read it: the chunks k, k + n, k + 2 n, ... of the places [c0, c1) of a table, so that
+// a run of places that its rows do not see falls on all units of the job alike.
 struct Unit {
   int s;          // sequence whose table is read; -1: no such unit
-  int c0, c1;     // places of the table
+  int c0, c1;
+  int split;      // k | n << 16
   int rows;       // of the job
   int tok;        // first token of the job, or of its members' list
-  int row0;       // first row of the unit
+  int row0;       // first row of the unit; | 1: token i of the job is list[tok + i], else tok + i
   int part;       // first row of its partial results (KV head 0); -1: O and LSE are written
-  int listed;     // whether token i of the job is list[tok + i], else tok + i
 };
 static_assert(sizeof(Unit) == 32, "two 16-byte loads");
 
@@ -110,13 +116,14 @@ struct RowsArgs {
   int* list;        // [S] members, group by group
   int* count;       // [groups] members, and
   int* base;        // [groups] the first of them in `list` (more than kPlanSmall sequences or groups)
-  int* jobs;        // [4][jobs + 1] tiles, rows, first wide and narrow unit (the same)
+  int* jobs;        // [4][jobs] tiles, rows, first wide and narrow unit (the same)
   Parts* own;       // [S] of each sequence
   Parts* prefix;    // [groups] of each group
   Unit* units;      // [max_units[0] + max_units[1]]: wide, narrow
   float* part;      // [max_part][D]
   float2* part_ml;  // [max_part]: m (log2 units), l
-  int* parts;       // number of partial rows
+  int* parts;       // [1] whether there are partial rows
+  int2* stats;      // [S][ceil(max_blocks BS / kChunk)] least and greatest position in each chunk of a table (window > 0)
   long long max_part;
   int max_units[2];
   int want[2];      // units per KV head that fill the chip
@@ -153,83 +160,57 @@ __device__ __forceinline__ long long block_scan(int x, long long& from, int* buf
   return before;
 }
 
-// One workgroup; one wave for up to 256 sequences and groups, with what it knows of them in LDS.  All jobs of a kind are
-// cut into runs of the same size, about the smallest for which the units are as many as fill the chip (and half as many
-// on top of the row blocks, where these do).  Bound by latency.
-template <bool SHARED, int NT>
-__global__ void __launch_bounds__(NT) rows_plan_kernel(RowsArgs a) {
-  constexpr bool SMALL = NT == kWave;
+__device__ __forceinline__ int chunks_of(int places) { return (int)(((unsigned)places + kChunk - 1) / kChunk); }
+
+// Positions in the chunks of the tables, a wave a chunk at a time: (least, greatest), of none (INT_MAX, -1).
+__device__ __forceinline__ void chunk_stats(const RowsArgs& a, int first, int waves) {
+  const int lane = threadIdx.x & 63, each = chunks_of(a.max_blocks * a.BS);
+  for (long long i = first; i < (long long)a.S * each; i += waves) {
+    const int s = (int)(i / each), c = (int)(i - (long long)s * each) * kChunk + lane;
+    const int n = min(max(a.nblk[s], 0), a.max_blocks) * a.BS, b = block_of(a, c);
+    const int e = c < n ? a.table[(size_t)s * a.max_blocks + b] : -1;
+    const int p = (unsigned)e < (unsigned)a.num_blocks ? a.slot_pos[e * a.BS + (c - b * a.BS)] : -1;
+    const int lo = wave_min(p < 0 ? INT_MAX : p), hi = wave_max(p);
+    if (lane == 0) a.stats[i] = make_int2(lo, hi);
+  }
+}
+
+// The plan, by workgroup 0: for up to 256 sequences and groups one wave makes it, with what it knows of them in LDS, and
+// all of them write the units.  The jobs of a kind are cut into runs of the same size, about the smallest for which the
+// units are as many as fill the chip (and half as many on top of the row blocks, where these do).  Bound by latency.
+// Under a window the other workgroups take the positions of the tables' chunks.
+template <bool SHARED, bool SMALL>
+__global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs a) {
+  constexpr int NT = SMALL ? 512 : 1024, PT = SMALL ? kWave : NT;   // threads; those that plan
   constexpr int CAP = SMALL ? kPlanSmall : 1, JOBS = SHARED ? 2 * CAP : CAP;
-  __shared__ int sJobs[4 * JOBS + 2], sGroup[SHARED ? 6 * CAP : 1];
+  __shared__ int sJobs[4 * JOBS], sGroup[SHARED ? 6 * CAP : 1], sPart[JOBS];
   __shared__ Job sJob[JOBS];
-  __shared__ int sPart[JOBS];
-  __shared__ int buf[NT / kWave], sTop[2][NT / kWave];
+  __shared__ int buf[PT / kWave], sTop[2][PT / kWave], sRun[2], sUnits[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, J = SHARED ? a.groups + a.S : a.S;
+  if (blockIdx.x > 0) {
+    chunk_stats(a, (blockIdx.x - 1) * (NT / kWave) + wave, (gridDim.x - 1) * (NT / kWave));
+    return;
+  }
   int* tiles = SMALL ? sJobs : a.jobs;
   int* rows = SMALL ? sJobs + JOBS : a.jobs + J;
   // units of the jobs in front of each, wide and narrow ones counted apart
-  int* first[2] = {SMALL ? sJobs + 2 * JOBS : a.jobs + 2 * J, SMALL ? sJobs + 3 * JOBS + 1 : a.jobs + 3 * J + 1};
+  int* first[2] = {SMALL ? sJobs + 2 * JOBS : a.jobs + 2 * J, SMALL ? sJobs + 3 * JOBS : a.jobs + 3 * J};
   int* count = SMALL ? sGroup : a.count;
   int* base = SMALL ? sGroup + CAP : a.base;
   int* rank = SMALL ? sGroup + 2 * CAP : a.rank;
   int* list = SMALL ? sGroup + 3 * CAP : a.list;
-  // a sequence's blocks and group, SMALL: read once
-  int* sBlocks = sGroup + 4 * CAP;
+  int* sBlocks = sGroup + 4 * CAP;   // SMALL: a sequence's blocks and group, read once
   int* sOf = sGroup + 5 * CAP;
+  auto sync = [&]() {
+    if (SMALL) {
+      __threadfence_block();
+      __builtin_amdgcn_wave_barrier();
+    } else {
+      __syncthreads();
+    }
+  };
   auto blocks_of = [&](int s) { return SMALL && SHARED ? sBlocks[s] : min(max(a.nblk[s], 0), a.max_blocks); };
   auto group_of = [&](int s) { return SMALL ? sOf[s] : a.prefix_group[s]; };
-  if (SHARED) {
-    for (int g = tid; g < a.groups; g += NT) count[g] = 0;
-    if (SMALL) {
-      constexpr int N = SMALL ? CAP / NT : 1;
-      int nb[N], gr[N];   // all reads at once
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        nb[k] = k * NT + tid < a.S ? a.nblk[k * NT + tid] : 0;
-        gr[k] = k * NT + tid < a.S ? a.prefix_group[k * NT + tid] : -1;
-      }
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        sBlocks[k * NT + tid] = min(max(nb[k], 0), a.max_blocks);
-        sOf[k * NT + tid] = gr[k];
-      }
-    }
-    __syncthreads();
-    if (wave == 0)   // ranks in the sequences' order: 64 of them at a time, group by group of those among them
-      for (int s0 = 0; s0 < a.S; s0 += kWave) {
-        const int s = s0 + lane, g = s < a.S ? group_of(s) : -1;
-        unsigned long long todo = __ballot((unsigned)g < (unsigned)a.groups);
-        while (todo) {
-          const int g1 = __builtin_amdgcn_readlane(g, __builtin_ctzll(todo));
-          const unsigned long long same = __ballot(g == g1);
-          const int before = count[g1];
-          if (g == g1) rank[s] = before + __builtin_popcountll(same & ((1ull << lane) - 1ull));
-          if (lane == 0) count[g1] = before + __builtin_popcountll(same);
-          __threadfence_block();
-          todo &= ~same;
-        }
-      }
-    __syncthreads();
-    long long from = 0;
-    for (int g0 = 0; g0 < a.groups; g0 += NT) {
-      const int g = g0 + tid;
-      const int x = (int)block_scan<NT>(g < a.groups ? count[g] : 0, from, buf);
-      if (g < a.groups) base[g] = x;
-    }
-    __syncthreads();
-    for (int s = tid; s < a.S; s += NT) {
-      const int g = group_of(s);
-      if ((unsigned)g < (unsigned)a.groups) {
-        const int r = rank[s], i = base[g] + r;
-        list[i] = s;
-        if (SMALL) {
-          a.list[i] = s;
-          a.rank[s] = r;
-        }
-      }
-    }
-    __syncthreads();
-  }
   // blocks of group g's prefix
   auto prefix_of = [&](int g) { return count[g] < 2 ? 0 : min(max(a.prefix_blocks[g], 0), blocks_of(list[base[g]])); };
   // job j: the groups first, then the sequences
@@ -241,100 +222,195 @@ __global__ void __launch_bounds__(NT) rows_plan_kernel(RowsArgs a) {
     }
     const int s = SHARED ? j - a.groups : j, blocks = blocks_of(s);
     if (SHARED) {
-      const int g = group_of(s), b = (unsigned)g < (unsigned)a.groups ? min(prefix_of(g), blocks) : 0;
+      const int g = group_of(s);
+      int b = 0;
+      if ((unsigned)g < (unsigned)a.groups) b = min(SMALL ? sJob[g].c1 / a.BS : prefix_of(g), blocks);
       return Job{s, b * a.BS, blocks * a.BS, a.G, s, 0};
     }
     const int t0 = min(max(a.cu[s], 0), a.ntok), t1 = min(max(a.cu[s + 1], t0), a.ntok);
     return Job{s, 0, blocks * a.BS, (t1 - t0) * a.G, t0, 0};
   };
-  int top[2] = {1, 1};
-  long long least[2] = {0, 0};
-  for (int j0 = 0; j0 < J; j0 += NT) {
-    const int j = j0 + tid;
-    const Job x = j < J ? job_of(j) : Job{0, 0, 0, 0, 0, 0};
-    const int t = plan_tiles(x.c1 - x.c0), k = is_wide(x.rows) ? 0 : 1;
-    if (j < J) {
-      tiles[j] = t;
-      rows[j] = x.rows;
-      if (SMALL) sJob[j] = x;
-    }
-    top[0] = max(top[0], k == 0 ? t : 0);
-    top[1] = max(top[1], k == 1 ? t : 0);
-    block_scan<NT>(k == 0 ? row_blocks(x.rows) : 0, least[0], buf);
-    block_scan<NT>(k == 1 ? row_blocks(x.rows) : 0, least[1], buf);
-  }
+  if (!SMALL || wave == 0) {
+    if (SHARED) {
+      for (int g = tid; g < a.groups; g += PT) count[g] = 0;
+      if (SMALL) {
+        constexpr int N = SMALL ? CAP / PT : 1;
+        int nb[N], gr[N];   // all reads at once
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    top[k] = wave_max(top[k]);
-    if (lane == 0) sTop[k][wave] = top[k];
-  }
-  __syncthreads();
-  int C[2];
-  float rC[2];
+        for (int k = 0; k < N; ++k) {
+          nb[k] = k * PT + tid < a.S ? a.nblk[k * PT + tid] : 0;
+          gr[k] = k * PT + tid < a.S ? a.prefix_group[k * PT + tid] : -1;
+        }
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    for (int w = 0; w < NT / kWave; ++w) top[k] = max(top[k], sTop[k][w]);
-    // bisection to within an eighth; every wave the same.  The whole of the longest job always fits.
-    const long long most = min((long long)a.max_units[k], max((long long)a.want[k], least[k] + a.want[k] / 2));
-    auto fits = [&](int c) {
-      const float rc = __builtin_amdgcn_rcpf((float)c);
-      long long units = 0;
-      for (int j0 = 0; j0 < J; j0 += kWave) {
-        const int j = j0 + lane, r = j < J ? rows[j] : 0;
-        const long long u = j < J && is_wide(r) == (k == 0) ? (long long)job_splits<SHARED>(tiles[j], r, c, rc) * row_blocks(r) : 0;
-        units += wave_last(wave_scan((int)min(u, 1ll << 24)));   // more than `most` at any rate
+        for (int k = 0; k < N; ++k) {
+          sBlocks[k * PT + tid] = min(max(nb[k], 0), a.max_blocks);
+          sOf[k * PT + tid] = gr[k];
+        }
       }
-      return units <= most;
-    };
-    int lo = min(kLeastTiles, top[k]), hi = top[k];
-    if (fits(lo)) hi = lo;
-    while (hi - lo > 1 + (hi >> 3)) {
-      const int c = lo + (hi - lo) / 2;
-      if (fits(c)) hi = c;
-      else lo = c;
+      sync();
+      if (wave == 0)   // ranks in the sequences' order: 64 of them at a time, group by group of those among them
+        for (int s0 = 0; s0 < a.S; s0 += kWave) {
+          const int s = s0 + lane, g = s < a.S ? group_of(s) : -1;
+          unsigned long long todo = __ballot((unsigned)g < (unsigned)a.groups);
+          while (todo) {
+            const int g1 = __builtin_amdgcn_readlane(g, __builtin_ctzll(todo));
+            const unsigned long long same = __ballot(g == g1);
+            const int before = count[g1];
+            if (g == g1) rank[s] = before + __builtin_popcountll(same & ((1ull << lane) - 1ull));
+            if (lane == 0) count[g1] = before + __builtin_popcountll(same);
+            __threadfence_block();
+            todo &= ~same;
+          }
+        }
+      sync();
+      long long from = 0;
+      for (int g0 = 0; g0 < a.groups; g0 += PT) {
+        const int g = g0 + tid;
+        const int x = (int)block_scan<PT>(g < a.groups ? count[g] : 0, from, buf);
+        if (g < a.groups) base[g] = x;
+      }
+      sync();
+      for (int s = tid; s < a.S; s += PT) {
+        const int g = group_of(s);
+        if ((unsigned)g < (unsigned)a.groups) {
+          const int r = rank[s], i = base[g] + r;
+          list[i] = s;
+          if (SMALL) {
+            a.list[i] = s;
+            a.rank[s] = r;
+          }
+        }
+      }
+      sync();
     }
-    C[k] = hi;
-    rC[k] = __builtin_amdgcn_rcpf((float)hi);
-  }
-  // first units of the jobs, wide and narrow ones counted apart, their first partial rows, and the units themselves
-  long long units0[2] = {0, 0}, part0 = 0;
-  for (int j0 = 0; j0 < J; j0 += NT) {
-    const int j = j0 + tid, r = j < J ? rows[j] : 0, k = is_wide(r) ? 0 : 1;
-    const int n = job_splits<SHARED>(j < J ? tiles[j] : 0, r, C[k], rC[k]), u = n * row_blocks(r);
-    const long long uw = block_scan<NT>(k == 0 ? u : 0, units0[0], buf);
-    const long long un = block_scan<NT>(k == 1 ? u : 0, units0[1], buf);
-    const long long pn = block_scan<NT>(SHARED || n > 1 ? n * r : 0, part0, buf);
-    if (j < J) {
-      first[0][j] = (int)min(uw, (long long)INT_MAX);
-      first[1][j] = (int)min(un, (long long)INT_MAX);
-      const Parts parts = {(int)(pn * a.Hkv), r, SHARED || n > 1 ? n : 0};
-      if (SMALL) sPart[j] = parts.part;
-      if (SHARED && j < a.groups) a.prefix[j] = parts;
-      else a.own[SHARED ? j - a.groups : j] = parts;
+    int top[2] = {1, 1};
+    long long least[2] = {0, 0};
+    // the groups in turns of their own: the sequences' jobs begin where they end
+    for (int j0 = 0; j0 < J; j0 += PT) {
+      const int ends = SHARED && j0 < a.groups ? min(a.groups, j0 + PT) : min(J, j0 + PT), j = j0 + tid;
+      const bool mine = j < ends;
+      const Job x = mine ? job_of(j) : Job{0, 0, 0, 0, 0, 0};
+      const int k = is_wide(x.rows) ? 0 : 1;
+      int places = x.c1 - x.c0;
+      if (!SHARED && a.window > 0) places = (int)min((long long)places, (long long)a.window + a.sinks + x.rows / a.G);
+      const int t = plan_tiles(places);
+      if (mine) {
+        tiles[j] = t;
+        rows[j] = x.rows;
+        if (SMALL) sJob[j] = x;
+      }
+      top[0] = max(top[0], k == 0 ? t : 0);
+      top[1] = max(top[1], k == 1 ? t : 0);
+      block_scan<PT>(k == 0 ? row_blocks(x.rows) : 0, least[0], buf);
+      block_scan<PT>(k == 1 ? row_blocks(x.rows) : 0, least[1], buf);
+      if (SHARED && j0 < a.groups) {
+        j0 = ends - PT;
+        sync();
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      top[k] = wave_max(top[k]);
+      if (lane == 0) sTop[k][wave] = top[k];
+    }
+    sync();
+    int C[2];
+    float rC[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      for (int w = 0; w < PT / kWave; ++w) top[k] = max(top[k], sTop[k][w]);
+      // units of runs of c tiles, and those among them of jobs that are split; every wave the same
+      auto count_units = [&](int c, long long& split) {
+        const float rc = __builtin_amdgcn_rcpf((float)c);
+        long long units = 0;
+        split = 0;
+        for (int j0 = 0; j0 < J; j0 += kWave) {
+          const int j = j0 + lane, r = j < J ? rows[j] : 0;
+          const int n = j < J && is_wide(r) == (k == 0) ? job_splits<SHARED>(tiles[j], r, c, rc) : 0;
+          const int u = (int)min((long long)n * row_blocks(r), 1ll << 24);   // more than `most` at any rate
+          units += wave_last(wave_scan(u));
+          split += wave_last(wave_scan(n > 1 ? u : 0));
+        }
+        return units;
+      };
+      long long split;
+      int lo = min(kLeastTiles, top[k]), hi = top[k];   // the whole of the longest job always fits
+      if (least[k] == 0) {
+        hi = lo;
+      } else if (k == 0) {
+        float best = INFINITY;
+        for (int i = 0; i < 14; ++i) {
+          const int n = i < 4 ? i + 1 : i & 1 ? 4 << ((i - 3) >> 1) : 6 << ((i - 4) >> 1), c = (top[0] + n - 1) / n;   // 1 .. 4, 6, 8, 12, ...
+          if (n > 1 && c < lo) break;
+          const long long units = count_units(c, split);
+          const float cost = (float)split * kSplitTiles / (float)a.want[0] + 0.5f * (float)c;
+          if (units <= a.max_units[0] && cost < best) {
+            best = cost;
+            hi = c;
+          }
+        }
+      } else {   // as many as fill the chip, and half as many on top of the jobs where these do; to within an eighth
+        const long long most = min((long long)a.max_units[1], max((long long)a.want[1], least[1] + a.want[1] / 2));
+        if (count_units(lo, split) <= most) hi = lo;
+        while (hi - lo > 1 + (hi >> 3)) {
+          const int c = lo + (hi - lo) / 2;
+          if (count_units(c, split) <= most) hi = c;
+          else lo = c;
+        }
+      }
+      C[k] = hi;
+      rC[k] = __builtin_amdgcn_rcpf((float)hi);
+    }
+    // first units of the jobs, wide and narrow ones counted apart, and their first partial rows
+    long long units0[2] = {0, 0}, part0 = 0;
+    for (int j0 = 0; j0 < J; j0 += PT) {
+      const int j = j0 + tid, r = j < J ? rows[j] : 0, k = is_wide(r) ? 0 : 1;
+      const int n = job_splits<SHARED>(j < J ? tiles[j] : 0, r, C[k], rC[k]), u = n * row_blocks(r);
+      const long long uw = block_scan<PT>(k == 0 ? u : 0, units0[0], buf);
+      const long long un = block_scan<PT>(k == 1 ? u : 0, units0[1], buf);
+      const long long pn = block_scan<PT>(SHARED || n > 1 ? n * r : 0, part0, buf);
+      if (j < J) {
+        first[0][j] = (int)min(uw, (long long)INT_MAX);
+        first[1][j] = (int)min(un, (long long)INT_MAX);
+        const Parts parts = {(int)(pn * a.Hkv), r, SHARED || n > 1 ? n : 0};
+        if (SMALL) sPart[j] = parts.part;
+        if (SHARED && j < a.groups) a.prefix[j] = parts;
+        else a.own[SHARED ? j - a.groups : j] = parts;
+      }
+    }
+    // offsets that overlap (only where cu_seqlens decreases) may ask for more than there is: nothing is computed then
+    const bool fit = units0[0] <= a.max_units[0] && units0[1] <= a.max_units[1] && part0 * a.Hkv <= a.max_part;
+    if (tid == 0) {
+      a.parts[0] = fit && part0 > 0;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        sRun[k] = C[k];
+        sUnits[k] = fit ? (int)units0[k] : 0;
+      }
     }
   }
-  // offsets that overlap (only where cu_seqlens decreases) may ask for more than there is: nothing is computed then
-  const bool fit = units0[0] <= a.max_units[0] && units0[1] <= a.max_units[1] && part0 * a.Hkv <= a.max_part;
-  if (tid == 0) a.parts[0] = fit && part0 > 0;
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
-    for (int u = tid; u < (fit ? (int)units0[k] : 0); u += NT) {
+  for (int k = 0; k < 2; ++k) {
+    const int all = sUnits[k], c = sRun[k];
+    const float rc = __builtin_amdgcn_rcpf((float)c);
+    Unit* out = a.units + (k == 0 ? 0 : a.max_units[0]);
+    for (int u = tid; u < a.max_units[k]; u += NT) {
+      if (u >= all) {
+        out[u].s = -1;
+        continue;
+      }
       int j = 0;   // the last job that begins at or before u: those without a unit of this kind begin where the next one does
       for (int step = 1 << (31 - __builtin_clz(J)); step > 0; step >>= 1)
         if (j + step < J && first[k][j + step] <= u) j += step;
       const Job b = SMALL ? sJob[j] : job_of(j);
-      const int nb = row_blocks(b.rows), n = job_splits<SHARED>(tiles[j], b.rows, C[k], rC[k]), i = u - first[k][j];
+      const int nb = row_blocks(b.rows), n = job_splits<SHARED>(tiles[j], b.rows, c, rc), i = u - first[k][j];
       const int sp = nb == 1 ? i : i / nb, rb = nb - 1 - (i - sp * nb);   // the last rows see most: first
       const int part = SMALL ? sPart[j] : SHARED && j < a.groups ? a.prefix[j].part : a.own[SHARED ? j - a.groups : j].part;
-      const long long per = (((long long)b.c1 - b.c0 + 31) / 32 + n - 1) / n * 32;
-      a.units[(k == 0 ? 0 : a.max_units[0]) + u] = {
-          b.s, (int)min(b.c0 + per * sp, (long long)b.c1), (int)min(b.c0 + per * (sp + 1), (long long)b.c1), b.rows, b.tok,
-          rb * kWideRows, SHARED || n > 1 ? part + sp * a.Hkv * b.rows : -1, b.listed};
+      out[u] = {b.s, b.c0, b.c1, sp | n << 16, b.rows, b.tok, rb * kWideRows | b.listed,
+                SHARED || n > 1 ? part + sp * a.Hkv * b.rows : -1};
     }
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-    for (int u = (fit ? (int)units0[k] : 0) + tid; u < a.max_units[k]; u += NT) a.units[(k ? a.max_units[0] : 0) + u].s = -1;
+  }
 }
 
 // ---------------------------------------------------------------- the units
@@ -348,7 +424,7 @@ template <bool SHARED>
 __device__ __forceinline__ RowLane row_of(const RowsArgs& a, const Unit& un, int g, int row) {
   const int r = min(row, un.rows - 1), i = r / a.G;   // lanes past the last row repeat it
   RowLane x;
-  x.tok = un.listed ? a.list[un.tok + i] : un.tok + i;
+  x.tok = un.row0 & 1 ? a.list[un.tok + i] : un.tok + i;
   x.h = g * a.G + r - i * a.G;
   x.at = SHARED ? INT_MAX - 1 : max(a.q_pos[x.tok], -1);
   x.ok = row < un.rows;
@@ -363,6 +439,45 @@ template <bool SHARED>
 __device__ __forceinline__ bool seen_by_some(const RowsArgs& a, int p, int lo, int hi) {
   return p >= 0 && (SHARED || (p <= hi && (a.window == 0 || lo - p < a.window || p < a.sinks)));
 }
+
+// The chunks of a unit that its rows (at positions in [lo, hi]) may see something of, 64 of the unit's at a time as a
+// mask; wave-uniform.
+template <bool SHARED>
+struct ChunkWalker {
+  unsigned long long mask;
+  int ord, ords, at, k, n;   // next of the unit's chunks; their number; the mask's first one
+  __device__ __forceinline__ void init(const Unit& un) {
+    k = un.split & 0xffff;
+    n = un.split >> 16;
+    const int chunks = chunks_of(un.c1 - un.c0);
+    ords = chunks > k ? (chunks - k + n - 1) / n : 0;
+    ord = at = 0;
+    mask = 0;
+  }
+  // the next 64
+  __device__ __forceinline__ void look(const RowsArgs& a, const Unit& un, int lo, int hi, int lane) {
+    at = ord;
+    bool see = ord + lane < ords;
+    if (!SHARED && a.window > 0 && see) {
+      const int2 p = a.stats[(size_t)un.s * chunks_of(a.max_blocks * a.BS) + (ord + lane) * n + k];
+      see = p.x <= hi && (p.y > lo - a.window || p.x < a.sinks);
+    }
+    mask = __ballot(see);
+    ord += 64;
+  }
+  // whether there is another one
+  __device__ __forceinline__ bool more(const RowsArgs& a, const Unit& un, int lo, int hi, int lane) {
+    while (mask == 0 && ord < ords) look(a, un, lo, hi, lane);
+    return mask != 0;
+  }
+  // the place of the table that the next one begins at; past the unit's last place if there is none
+  __device__ __forceinline__ int next(const Unit& un) {
+    const int c = un.c0 + ((at + __builtin_ctzll(mask | 1ull << 63)) * n + k) * kChunk;
+    const bool some = mask != 0;
+    mask &= mask - 1ull;
+    return some ? c : un.c1;
+  }
+};
 
 // The running softmax of 32 rows (a lane's column) and their sums of V.
 template <int D>
@@ -458,7 +573,8 @@ constexpr int rows_look() { return SHARED ? 1024 : 512; }
 // double-buffered, each tile read by the four waves.  Scores are S^T = K Q^T
 // (keys on M, rows on N), so that a lane holds 16 scores of one row; softmax and
 // the products with V as in the forward of the eviction mask.
-template <int D, bool SHARED>
+// FAR: caches of 4 GiB or more, whose rows need 64-bit addresses of their own; else a copy takes one addition.
+template <int D, bool SHARED, bool FAR>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) rows_wide_kernel(RowsArgs a) {
   using LY = Lay<D, true>;
   constexpr int KS = D / 16, BN = rows_bn<D>(), NKB = BN / 32, PITCH = LY::PITCH, TILE = BN * PITCH;
@@ -468,7 +584,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
   __shared__ __attribute__((aligned(1024))) uint16_t sK1[TILE];
   __shared__ __attribute__((aligned(1024))) uint16_t sV0[TILE];
   __shared__ __attribute__((aligned(1024))) uint16_t sV1[TILE];
-  __shared__ __attribute__((aligned(16))) uint32_t sRow[PICK];   // rows [block][KV head][row] of the listed slots
+  __shared__ __attribute__((aligned(16))) uint32_t sRow[PICK];   // rows [block][KV head][row] of the listed slots (not FAR: in bytes)
   __shared__ __attribute__((aligned(16))) int sPos[PICK];        // and their positions; INT_MAX: nothing there
   __shared__ int sCnt[LOOK * 4], sAll[4], sMin[4], sMax[4];
 
@@ -478,8 +594,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
   if (un.s < 0) return;
   const auto rl = LY::row_lane(lane);
   const int tl = LY::tr_lo(lane), th = LY::tr_hi(lane);
-  const int row = un.row0 + 32 * wave + col;
-  const bool wave_ok = un.row0 + 32 * wave < un.rows;
+  const int row0 = (un.row0 & ~1) + 32 * wave, row = row0 + col;
+  const bool wave_ok = row0 < un.rows;
   int at;   // this lane's row sees entries up to there
   bf16x8 qreg[KS];
   {
@@ -499,7 +615,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 4; ++w)
-      if (un.row0 + 32 * w < un.rows) {
+      if ((un.row0 & ~1) + 32 * w < un.rows) {
         lo = min(lo, sMin[w]);
         hi = max(hi, sMax[w]);
       }
@@ -525,9 +641,15 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
       const int n = wave + 4 * i;
       if (i < PW - 1 || PIECES % 4 == 0 || n < PIECES) {
         const uint32_t r = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(sRow + t * BN) + (piece[i] & 0xffffu));
-        const size_t off = (size_t)r * (2 * D) + (piece[i] >> 16);
-        dma_b128_global((const char*)a.kc + off, lk + i * 4 * kWave * 16);
-        dma_b128_global((const char*)a.vc + off, lv + i * 4 * kWave * 16);
+        if (FAR) {
+          const size_t off = (size_t)r * (2 * D) + (piece[i] >> 16);
+          dma_b128_cached((const char*)a.kc + off, lk + i * 4 * kWave * 16);
+          dma_b128_cached((const char*)a.vc + off, lv + i * 4 * kWave * 16);
+        } else {
+          const uint32_t off = r + (piece[i] >> 16);
+          dma_b128(a.kc, off, lk + i * 4 * kWave * 16);
+          dma_b128(a.vc, off, lv + i * 4 * kWave * 16);
+        }
       }
     }
   };
@@ -558,19 +680,30 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
     st.template add<NKB>(s, cV, tl, th, a.scale_log2);
   };
 
-  for (int base = un.c0; base < un.c1; base += PICK) {
+  ChunkWalker<SHARED> walk;
+  walk.init(un);
+  bool again = false;
+  while (walk.ord < walk.ords)
+  for (walk.look(a, un, lo, hi, lane); walk.mask; again = true) {
     // the slots of the next places that some row sees, in the table's order
     int slot[LOOK], pos[LOOK], blk[LOOK];
     unsigned long long vis[LOOK];
 #pragma unroll
     for (int k = 0; k < LOOK; ++k) {
-      const int c = base + k * 256 + tid, b = block_of(a, c);
+      int c = un.c1;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int x = walk.next(un);
+        if (w == wave) c = x;
+      }
+      c += lane;
+      const int b = block_of(a, c);
       blk[k] = c < un.c1 ? trow[b] : -1;
       slot[k] = (unsigned)blk[k] < (unsigned)a.num_blocks ? blk[k] * a.BS + (c - b * a.BS) : -1;
     }
 #pragma unroll
     for (int k = 0; k < LOOK; ++k) pos[k] = slot[k] >= 0 ? a.slot_pos[slot[k]] : -1;
-    if (base != un.c0) __syncthreads();   // the lists are read
+    if (again) __syncthreads();   // the lists are read
     int all = 0;
 #pragma unroll
     for (int k = 0; k < LOOK; ++k) {
@@ -596,7 +729,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
     for (int k = 0; k < LOOK; ++k)
       if ((vis[k] >> lane) & 1ull) {
         const int i = mine[k] + __builtin_popcountll(vis[k] & ((1ull << lane) - 1ull));
-        const uint32_t r = ((uint32_t)blk[k] * a.Hkv + g) * a.BS + (slot[k] - blk[k] * a.BS);
+        const uint32_t r = (((uint32_t)blk[k] * a.Hkv + g) * a.BS + (slot[k] - blk[k] * a.BS)) * (FAR ? 1u : 2u * D);
         sRow[i] = r;
         sPos[i] = SHARED ? 0 : pos[k];
         if (i == cnt - 1)   // the last tile's places behind it repeat it, and nobody sees them
@@ -654,6 +787,9 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
   if (un.s < 0) return;
   const auto rl = LY::row_lane(lane);
   const int tl = LY::tr_lo(lane), th = LY::tr_hi(lane);
+  const int* trow = a.table + (size_t)un.s * a.max_blocks;
+  ChunkWalker<SHARED> walk;
+  walk.init(un);
   const RowLane rw = row_of<SHARED>(a, un, g, col);
   bf16x8 qreg[KS];
   {
@@ -664,7 +800,6 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
   const int lo = SHARED ? rw.at : wave_min(rw.at), hi = SHARED ? rw.at : wave_max(rw.at);
   RowState<D> st;
   st.init();
-  const int* trow = a.table + (size_t)un.s * a.max_blocks;
 
   int prow[NI], pcol[NI];   // this lane's 16-byte slots of a tile: row (-1: none), source element
 #pragma unroll
@@ -673,20 +808,20 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
     prow[i] = qs < SLOTS ? r : -1;
     pcol[i] = qs < SLOTS && pc < LY::CPR ? 8 * (pc ^ LY::flip(r)) : 0;
   }
-  unsigned tail = 0;             // entries listed so far
-  int next = un.c0, asked = 0;   // first place not asked for; first one of those in work
-  int stage = 0;                 // of these: 0 none, 1 table entries asked for, 2 positions asked for, 3 there
-  auto place = [&](int k) __attribute__((always_inline)) { return (int)min((long long)asked + k * kWave + lane, un.c1 - 1ll); };
+  unsigned tail = 0;   // entries listed so far
+  int place[NP];       // first places of the chunks in work
+  int stage = 0;       // of these: 0 none, 1 table entries asked for, 2 positions asked for, 3 there
   auto ask_table = [&]() __attribute__((always_inline)) {
-    asked = next;
-    next = (int)min((long long)next + kNarrowPick, (long long)un.c1);
 #pragma unroll
-    for (int k = 0; k < NP; ++k) dma_b32_global(trow + block_of(a, place(k)), lds_addr(&sTab[k * kWave]));
+    for (int k = 0; k < NP; ++k) {
+      place[k] = walk.next(un);
+      dma_b32_global(trow + block_of(a, min(place[k] + lane, un.c1 - 1)), lds_addr(&sTab[k * kWave]));
+    }
     stage = 1;
   };
   // the slot of a place, by its landed table entry (-1: an entry outside the cache)
   auto slot_of = [&](int k, int& blk) __attribute__((always_inline)) {
-    const int c = place(k);
+    const int c = min(place[k] + lane, un.c1 - 1);
     blk = sTab[k * kWave + lane];
     return (unsigned)blk < (unsigned)a.num_blocks ? blk * a.BS + (c - block_of(a, c) * a.BS) : -1;
   };
@@ -703,7 +838,7 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
     for (int k = 0; k < NP; ++k) {
       int blk;
       const int slot = slot_of(k, blk), pos = sSlot[k * kWave + lane];
-      const bool vis = asked + k * kWave + lane < next && slot >= 0 && seen_by_some<SHARED>(a, pos, lo, hi);
+      const bool vis = place[k] + lane < un.c1 && slot >= 0 && seen_by_some<SHARED>(a, pos, lo, hi);
       const unsigned long long m = __ballot(vis);
       if (vis) {
         const unsigned i = (tail + __builtin_popcountll(m & ((1ull << lane) - 1ull))) % kNarrowRing;
@@ -717,7 +852,7 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
   // Entries from `head` on that make the next tile; lists more where they are short of one.
   auto ready = [&](unsigned head) __attribute__((always_inline)) {
     if (tail - head < BN && stage == 3) enlist();
-    while (tail - head < BN && (stage > 0 || next < un.c1)) {   // at the start, and where places show few entries
+    while (tail - head < BN && (stage > 0 || walk.more(a, un, lo, hi, lane))) {   // at the start, and where places show few entries
       if (stage == 0) ask_table();
       if (stage == 1) {
         wait_vm_le<0>();
@@ -753,7 +888,7 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
     } else {
       wait_vm_le<0>();
     }
-    if (stage == 0 && next < un.c1) ask_table();
+    if (stage == 0 && walk.more(a, un, lo, hi, lane)) ask_table();
     else if (stage == 1) ask_pos();
     else if (stage == 2) stage = 3;
     const uint16_t* cK = sK + b * TILE;
@@ -787,18 +922,37 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
 }
 
 // ---------------------------------------------------------------- the merge
-// One wave a (token, q-head): the partial results of the group's prefix and of the sequence's own part, or of a
-// sequence's splits.  D / 4 lanes read one partial result as float4.
+// A partial result joined to what there is: m, l and four of the sums of V.
+struct Joined {
+  float m, l;
+  float4 x;
+  __device__ __forceinline__ void add(float2 ml, const float4& y) {
+    if (ml.y <= 0.f) return;   // a part without an entry: its sums are unwritten
+    const float top = fmaxf(m, ml.x), f = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), e = __builtin_amdgcn_exp2f(ml.x - top);
+    m = top;
+    l = l * f + ml.y * e;
+    x.x = x.x * f + y.x * e;
+    x.y = x.y * f + y.y * e;
+    x.z = x.z * f + y.z * e;
+    x.w = x.w * f + y.w * e;
+  }
+};
+
+// The partial results of a row: the group's prefix and the sequence's own part (one wave a row, whose halves, or
+// quarters, of D / 4 lanes take the parts in turn), or a sequence's splits (one wave a token and KV head, which take the
+// head's rows in turn: few parts a row, and the token is looked up once).  Bound by the latency of its reads: four parts
+// are asked for at a time.
 template <int D, bool SHARED>
 __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
   constexpr int LPS = D / 4, PER = kWave / LPS, UNROLL = 4;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, sub = lane / LPS;
   if (!SHARED && a.parts[0] == 0) return;   // every row is written by its unit
-  const long long all = (long long)a.ntok * a.Hq;
-  for (long long r = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); r < all; r += (long long)gridDim.x * 4) {
-    const int tok = (int)(r / a.Hq), h = (int)(r - (long long)tok * a.Hq), g = h / a.G;
+  const int per_tok = SHARED ? a.Hq : a.Hkv;
+  const long long all = (long long)a.ntok * per_tok;
+  for (long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); i < all; i += (long long)gridDim.x * 4) {
+    const int tok = (int)(i / per_tok), at = (int)(i - (long long)tok * per_tok), g = SHARED ? at / a.G : at;
     Parts set[2] = {};
-    long long at[2] = {};
+    long long row[2] = {};   // of the first q-head of the KV head
     if (!SHARED) {   // the sequence of the token: the last one that begins at or before it
       int s = 0;
       for (int step = 1 << (31 - __builtin_clz(a.S)); step > 0; step >>= 1)
@@ -807,62 +961,51 @@ __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
       if (tok < t0 || tok >= t1) continue;
       set[0] = a.own[s];
       if (set[0].n == 0) continue;   // written by its unit
-      at[0] = (long long)(tok - t0) * a.G;
+      row[0] = (long long)(tok - t0) * a.G;
     } else {
       set[0] = a.own[tok];
       const int grp = a.prefix_group[tok];
       if ((unsigned)grp < (unsigned)a.groups) {
         set[1] = a.prefix[grp];
-        at[1] = (long long)a.rank[tok] * a.G;
+        row[1] = (long long)a.rank[tok] * a.G;
       }
     }
 #pragma unroll
-    for (int k = 0; k < 2; ++k) at[k] += set[k].part + (long long)g * set[k].rows + (h - g * a.G);
+    for (int k = 0; k < 2; ++k) row[k] += set[k].part + (long long)g * set[k].rows;
     const int n = set[0].n + set[1].n;
-    auto where = [&](int i) {
-      return i < set[0].n ? at[0] + (long long)i * a.Hkv * set[0].rows : at[1] + (long long)(i - set[0].n) * a.Hkv * set[1].rows;
-    };
-    float M = -INFINITY;
-    for (int i = lane; i < n; i += kWave) {
-      const float2 v = a.part_ml[where(i)];
-      if (!(v.y <= 0.f)) M = fmaxf(M, v.x);
-    }
+    for (int r = SHARED ? at - g * a.G : sub; r < a.G; r += SHARED ? a.G : PER) {
+      auto where = [&](int p) {
+        return r + (p < set[0].n ? row[0] + (long long)p * a.Hkv * set[0].rows
+                                 : row[1] + (long long)(p - set[0].n) * a.Hkv * set[1].rows);
+      };
+      constexpr int STEP = SHARED ? PER : 1;
+      Joined x = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+      for (int p0 = SHARED ? sub : 0; p0 < n; p0 += UNROLL * STEP) {
+        float2 v[UNROLL];
+        float4 y[UNROLL];
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
-    float L = 0.f;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = lane / LPS; i0 < n; i0 += UNROLL * PER) {
-      float2 v[UNROLL];
-      float4 y[UNROLL];
-#pragma unroll
-      for (int k = 0; k < UNROLL; ++k) {   // the last ones again behind the end
-        const long long w = where(min(i0 + k * PER, n - 1));
-        v[k] = a.part_ml[w];
-        y[k] = reinterpret_cast<const float4*>(a.part + w * D)[lane & (LPS - 1)];
-      }
-#pragma unroll
-      for (int k = 0; k < UNROLL; ++k)
-        if (i0 + k * PER < n && !(v[k].y <= 0.f)) {
-          const float f = __builtin_amdgcn_exp2f(v[k].x - M);
-          L += v[k].y * f;
-          x.x += y[k].x * f;
-          x.y += y[k].y * f;
-          x.z += y[k].z * f;
-          x.w += y[k].w * f;
+        for (int k = 0; k < UNROLL; ++k) {   // the last one again behind the end
+          const long long w = where(min(p0 + k * STEP, n - 1));
+          v[k] = a.part_ml[w];
+          y[k] = reinterpret_cast<const float4*>(a.part + w * D)[lane & (LPS - 1)];
         }
-    }
 #pragma unroll
-    for (int off = LPS; off < kWave; off <<= 1) {
-      L += __shfl_xor(L, off);
-      x.x += __shfl_xor(x.x, off);
-      x.y += __shfl_xor(x.y, off);
-      x.z += __shfl_xor(x.z, off);
-      x.w += __shfl_xor(x.w, off);
-    }
-    if (lane < LPS) {
-      const float inv = L <= 0.f ? 0.f : 1.f / L;
-      reinterpret_cast<uint2*>(a.o + r * D)[lane] = pack4_bf16(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
-      if (lane == 0) a.lse[r] = L <= 0.f ? -INFINITY : (M + __log2f(L)) * 0.6931471805599453f;
+        for (int k = 0; k < UNROLL; ++k)
+          if (p0 + k * STEP < n) x.add(v[k], y[k]);
+      }
+      if (SHARED)
+#pragma unroll
+        for (int off = LPS; off < kWave; off <<= 1) {
+          const float2 v = make_float2(__shfl_xor(x.m, off), __shfl_xor(x.l, off));
+          const float4 y = make_float4(__shfl_xor(x.x.x, off), __shfl_xor(x.x.y, off), __shfl_xor(x.x.z, off), __shfl_xor(x.x.w, off));
+          x.add(v, y);
+        }
+      if (!SHARED || sub == 0) {
+        const float inv = x.l <= 0.f ? 0.f : 1.f / x.l;
+        const size_t out = (size_t)tok * a.Hq + g * a.G + r;
+        reinterpret_cast<uint2*>(a.o + out * D)[lane & (LPS - 1)] = pack4_bf16(x.x.x * inv, x.x.y * inv, x.x.z * inv, x.x.w * inv);
+        if ((lane & (LPS - 1)) == 0) a.lse[out] = x.l <= 0.f ? -INFINITY : (x.m + __log2f(x.l)) * 0.6931471805599453f;
+      }
     }
   }
 }
@@ -875,14 +1018,16 @@ static int rows_want(int Hkv, int D, bool wide) { return ((wide ? 3 : D == 128 ?
 // Sizes of a call's workspace, in this order.
 struct RowsSpace {
   long long units[2], part;   // units per KV head, wide and narrow; partial rows
-  size_t parts, rank, list, count, base, jobs, own, prefix, unit, rows, ml;
-  size_t bytes() const { return parts + rank + list + count + base + jobs + own + prefix + unit + rows + ml; }
+  size_t parts, rank, list, count, base, jobs, own, prefix, unit, stats, rows, ml;
+  size_t bytes() const { return parts + rank + list + count + base + jobs + own + prefix + unit + stats + rows + ml; }
 };
+static size_t stats_chunks(const PagedRows& p) { return ((size_t)p.max_blocks * p.block_size + kChunk - 1) / kChunk; }
 static bool plans_small(const PagedRows& p) { return p.S <= kPlanSmall && p.groups <= kPlanSmall; }
 // Row blocks of wide jobs: one for every 128 rows, and one more a job (of 33 rows at least; SHARED: groups, and sequences
-// by themselves if they have so many q-heads).  Splits add no more than `want` units of a kind (rows_plan_kernel), and a
-// job has none of fewer than kLeastTiles tiles.  Partial rows: those of every job once and of the units that splits add;
-// for new tokens only those of jobs that are split, each into two at least, so twice those of the added units.
+// by themselves if they have so many q-heads).  A job has no splits of fewer than kLeastTiles tiles; those of wide jobs
+// add no more units than four rounds of them and than three times the row blocks (or one round), those of narrow ones no
+// more than a round.  Partial rows: those of every job once and of the units that splits add; for new tokens only those
+// of jobs that are split, each into two at least, so twice those of the added units.
 static RowsSpace rows_space(const PagedRows& p) {
   RowsSpace x{};
   const long long G = p.Hq / p.Hkv, tokens = p.shared ? p.S : p.ntok, all = tokens * G;
@@ -892,8 +1037,9 @@ static RowsSpace rows_space(const PagedRows& p) {
   long long added = 0;
   for (int k = 0; k < 2; ++k) {
     const long long want = rows_want(p.Hkv, p.D, k == 0);
-    x.units[k] = std::min(blocks[k] * splits, std::max(want, blocks[k] + want / 2));
-    added += std::min(want, x.units[k]) * (k == 0 ? kWideRows : kNarrowRows);
+    const long long more = k == 0 ? std::min(std::max(want, 3 * blocks[0]), 4 * want) : std::max(want - blocks[1], want / 2);
+    x.units[k] = std::min(blocks[k] * splits, blocks[k] + more);
+    added += std::min(more, x.units[k]) * (k == 0 ? kWideRows : kNarrowRows);
   }
   x.part = (p.shared ? 2 * all + added : 2 * added) * p.Hkv;
   x.parts = 256;
@@ -903,10 +1049,11 @@ static RowsSpace rows_space(const PagedRows& p) {
   }
   if (!plans_small(p)) {
     if (p.shared) x.count = x.base = round256((size_t)p.groups * sizeof(int));
-    x.jobs = round256(4 * ((size_t)p.S + p.groups + 1) * sizeof(int));
+    x.jobs = round256(4 * ((size_t)p.S + p.groups) * sizeof(int));
   }
   x.own = round256((size_t)p.S * sizeof(Parts));
   x.unit = round256((size_t)(x.units[0] + x.units[1]) * sizeof(Unit));
+  if (!p.shared) x.stats = round256((size_t)p.S * stats_chunks(p) * sizeof(int2));
   x.rows = round256((size_t)x.part * p.D * sizeof(float));
   x.ml = round256((size_t)x.part * sizeof(float2));
   return x;
@@ -920,18 +1067,22 @@ bool paged_rows_fit(const PagedRows& p) {
 
 template <int D, bool SHARED>
 static hipError_t launch_rows(const PagedRows& p, const RowsArgs& a) {
-  if (plans_small(p)) hipLaunchKernelGGL((rows_plan_kernel<SHARED, kWave>), dim3(1), dim3(kWave), 0, p.stream, a);
-  else hipLaunchKernelGGL((rows_plan_kernel<SHARED, 1024>), dim3(1), dim3(1024), 0, p.stream, a);
+  // under a window also the tables' chunks, 16 waves of them a CU
+  const bool small = plans_small(p);
+  const unsigned looks = !SHARED && p.window > 0 ? (unsigned)std::min((p.S * stats_chunks(p) + 7) / 8, (size_t)512) : 0;
+  if (small) hipLaunchKernelGGL((rows_plan_kernel<SHARED, true>), dim3(1 + looks), dim3(512), 0, p.stream, a);
+  else hipLaunchKernelGGL((rows_plan_kernel<SHARED, false>), dim3(1 + looks), dim3(1024), 0, p.stream, a);
+  const bool far = (long long)p.num_blocks * p.block_size * p.Hkv * (2 * D) >= 1ll << 32;
   prof_begin(SHARED ? "paged_decode_shared" : "paged_extend", p.stream);
   if (a.max_units[0])
-    hipLaunchKernelGGL((rows_wide_kernel<D, SHARED>), dim3((unsigned)((long long)a.max_units[0] * a.Hkv)), dim3(256), 0,
-                       p.stream, a);
+    hipLaunchKernelGGL((far ? rows_wide_kernel<D, SHARED, true> : rows_wide_kernel<D, SHARED, false>),
+                       dim3((unsigned)((long long)a.max_units[0] * a.Hkv)), dim3(256), 0, p.stream, a);
   hipLaunchKernelGGL((rows_narrow_kernel<D, SHARED>), dim3((unsigned)((long long)a.max_units[1] * a.Hkv)), dim3(64), 0,
                      p.stream, a);
   prof_end(p.stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const long long rows = (long long)a.ntok * a.Hq;
+  const long long rows = (long long)a.ntok * (SHARED ? a.Hq : a.Hkv);
   hipLaunchKernelGGL((rows_merge_kernel<D, SHARED>), dim3((unsigned)std::min((rows + 3) / 4, 4096ll)), dim3(256), 0,
                      p.stream, a);
   return hipGetLastError();
@@ -980,6 +1131,7 @@ hipError_t launch_paged_rows(const PagedRows& p) {
   a.own = (Parts*)take(x.own);
   a.prefix = (Parts*)take(x.prefix);
   a.units = (Unit*)take(x.unit);
+  a.stats = (int2*)take(x.stats);
   a.part = (float*)take(x.rows);
   a.part_ml = (float2*)take(x.ml);
   a.max_part = x.part;
