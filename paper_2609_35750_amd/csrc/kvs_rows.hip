@@ -27,6 +27,7 @@ namespace kvs {
 // ---------------------------------------------------------------- copies
 // Slot dst[i] takes the K and V rows of slot src[i], its position and its weight; MOVE: slot src[i] is empty then.
 // 16-byte pieces, one of K and one of V a thread and turn; bound by HBM.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int D>
 __global__ void __launch_bounds__(256) paged_copy_kernel(PagedCopy a) {
   const long long per = (long long)a.Hkv * (D / 8), pieces = a.n * per;
@@ -42,9 +43,10 @@ __global__ void __launch_bounds__(256) paged_copy_kernel(PagedCopy a) {
       return (((long long)(slot / a.block_size) * a.Hkv + h) * a.block_size + slot % a.block_size) * D + 8 * d8;
     };
     const long long x = at(from), y = at(to);
-    const uint4 k = *reinterpret_cast<const uint4*>(kc + x), v = *reinterpret_cast<const uint4*>(vc + x);
-    *reinterpret_cast<uint4*>(kc + y) = k;
-    *reinterpret_cast<uint4*>(vc + y) = v;
+    const u32x4 k = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kc + x));
+    const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vc + x));
+    __builtin_nontemporal_store(k, reinterpret_cast<u32x4*>(kc + y));
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(vc + y));
     if (r == 0) {
       if (a.slot_pos) {
         a.slot_pos[to] = a.slot_pos[from];
@@ -73,8 +75,9 @@ constexpr int kLeastTiles = 4;    // of a unit, in 32-key tiles
 constexpr int kPlanSmall = 256;   // sequences, and groups, that one wave plans, in LDS
 
 // What the plan weighs for wide units: with w tiles of work for each place on the chip the last unit ends about half the
-// longest unit behind w, and one of a split job costs as much as these tiles more, for its partial results.
-constexpr float kSplitTiles = 20.f;
+// longest unit behind w (and no unit before its own end), and 128 rows of partial results, written and read, cost as much
+// as these tiles.
+constexpr float kSplitTiles = 40.f;
 constexpr int kChunk = 64;        // places of a table that are skipped or looked at together
 
 // What a unit is, as its workgroups read it: the chunks k, k + n, k + 2 n, ... of the places [c0, c1) of a table, so that
@@ -185,7 +188,10 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   constexpr int CAP = SMALL ? kPlanSmall : 1, JOBS = SHARED ? 2 * CAP : CAP;
   __shared__ int sJobs[4 * JOBS], sGroup[SHARED ? 6 * CAP : 1], sPart[JOBS];
   __shared__ Job sJob[JOBS];
-  __shared__ int buf[PT / kWave], sTop[2][PT / kWave], sRun[2], sUnits[2];
+  constexpr int NW = NT / kWave, TRIES = 16;
+  __shared__ int buf[PT / kWave], sTop[2][PT / kWave], sRun[2], sUnits[2], sSize[2][TRIES];
+  __shared__ long long sLeast[2], sWork;
+  __shared__ float sCost[2][TRIES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, J = SHARED ? a.groups + a.S : a.S;
   if (blockIdx.x > 0) {
     chunk_stats(a, (blockIdx.x - 1) * (NT / kWave) + wave, (gridDim.x - 1) * (NT / kWave));
@@ -284,7 +290,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       sync();
     }
     int top[2] = {1, 1};
-    long long least[2] = {0, 0};
+    long long least[2] = {0, 0}, work = 0;   // row blocks; tiles of all wide ones
     // the groups in turns of their own: the sequences' jobs begin where they end
     for (int j0 = 0; j0 < J; j0 += PT) {
       const int ends = SHARED && j0 < a.groups ? min(a.groups, j0 + PT) : min(J, j0 + PT), j = j0 + tid;
@@ -302,6 +308,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       top[0] = max(top[0], k == 0 ? t : 0);
       top[1] = max(top[1], k == 1 ? t : 0);
       block_scan<PT>(k == 0 ? row_blocks(x.rows) : 0, least[0], buf);
+      block_scan<PT>(k == 0 ? (int)min((long long)row_blocks(x.rows) * t, 1ll << 24) : 0, work, buf);
       block_scan<PT>(k == 1 ? row_blocks(x.rows) : 0, least[1], buf);
       if (SHARED && j0 < a.groups) {
         j0 = ends - PT;
@@ -314,53 +321,87 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       if (lane == 0) sTop[k][wave] = top[k];
     }
     sync();
-    int C[2];
-    float rC[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       for (int w = 0; w < PT / kWave; ++w) top[k] = max(top[k], sTop[k][w]);
-      // units of runs of c tiles, and those among them of jobs that are split; every wave the same
-      auto count_units = [&](int c, long long& split) {
-        const float rc = __builtin_amdgcn_rcpf((float)c);
-        long long units = 0;
-        split = 0;
-        for (int j0 = 0; j0 < J; j0 += kWave) {
-          const int j = j0 + lane, r = j < J ? rows[j] : 0;
-          const int n = j < J && is_wide(r) == (k == 0) ? job_splits<SHARED>(tiles[j], r, c, rc) : 0;
-          const int u = (int)min((long long)n * row_blocks(r), 1ll << 24);   // more than `most` at any rate
-          units += wave_last(wave_scan(u));
-          split += wave_last(wave_scan(n > 1 ? u : 0));
-        }
-        return units;
-      };
-      long long split;
-      int lo = min(kLeastTiles, top[k]), hi = top[k];   // the whole of the longest job always fits
-      if (least[k] == 0) {
-        hi = lo;
-      } else if (k == 0) {
-        float best = INFINITY;
-        for (int i = 0; i < 14; ++i) {
-          const int n = i < 4 ? i + 1 : i & 1 ? 4 << ((i - 3) >> 1) : 6 << ((i - 4) >> 1), c = (top[0] + n - 1) / n;   // 1 .. 4, 6, 8, 12, ...
-          if (n > 1 && c < lo) break;
-          const long long units = count_units(c, split);
-          const float cost = (float)split * kSplitTiles / (float)a.want[0] + 0.5f * (float)c;
-          if (units <= a.max_units[0] && cost < best) {
-            best = cost;
-            hi = c;
-          }
-        }
-      } else {   // as many as fill the chip, and half as many on top of the jobs where these do; to within an eighth
-        const long long most = min((long long)a.max_units[1], max((long long)a.want[1], least[1] + a.want[1] / 2));
-        if (count_units(lo, split) <= most) hi = lo;
-        while (hi - lo > 1 + (hi >> 3)) {
-          const int c = lo + (hi - lo) / 2;
-          if (count_units(c, split) <= most) hi = c;
-          else lo = c;
-        }
+      if (tid == 0) {
+        sRun[k] = top[k];
+        sLeast[k] = least[k];
       }
-      C[k] = hi;
-      rC[k] = __builtin_amdgcn_rcpf((float)hi);
     }
+    if (tid == 0) sWork = work;
+  }
+  __syncthreads();
+  // The size of the runs, a wave a size at a time.  Wide units: the whole of the longest job and its parts, by their cost.
+  // Narrow ones: the smallest size for which they are as many as fill the chip (and half as many on top of the jobs where
+  // these do), in equal ratios from the least to the whole, then between two of these.  The whole always fits.
+  const int top[2] = {sRun[0], sRun[1]};
+  auto units_of = [&](int k, int c, long long& split) {   // and rows of partial results of jobs that are split
+    const float rc = __builtin_amdgcn_rcpf((float)c);
+    long long units = 0;
+    split = 0;
+    for (int j0 = 0; j0 < J; j0 += kWave) {
+      const int j = j0 + lane, r = j < J ? rows[j] : 0;
+      const int n = j < J && is_wide(r) == (k == 0) ? job_splits<SHARED>(tiles[j], r, c, rc) : 0;
+      units += wave_last(wave_scan((int)min((long long)n * row_blocks(r), 1ll << 24)));   // more than there may be at any rate
+      if (k == 0) split += wave_last(wave_scan(n > 1 ? (int)min((long long)n * r, 1ll << 24) : 0));
+    }
+    return units;
+  };
+  const long long most = min((long long)a.max_units[1], max((long long)a.want[1], sLeast[1] + a.want[1] / 2));
+  const int lo1 = min(kLeastTiles, top[1]);
+  for (int i = wave; i < TRIES; i += NW) {
+    long long split;
+    if (sLeast[0] > 0) {
+      const int n = i < 4 ? i + 1 : i & 1 ? 4 << ((i - 3) >> 1) : 6 << ((i - 4) >> 1);   // 1 .. 4, 6, 8, 12, 16, 24, ...
+      const int c = (top[0] + n - 1) / n;
+      const bool fits = (n == 1 || c >= kLeastTiles) && units_of(0, c, split) <= a.max_units[0];
+      const float place = 1.f / (float)a.want[0];
+      if (lane == 0) {
+        sSize[0][i] = c;
+        sCost[0][i] = !fits ? INFINITY
+                            : fmaxf((float)c, (float)sWork * place + 0.5f * (float)c) + (float)split * (kSplitTiles / kWideRows) * place;
+      }
+    }
+    if (sLeast[1] > 0) {
+      const float ratio = __log2f((float)top[1] / (float)lo1) / (float)(TRIES - 1);
+      const int c = i == TRIES - 1 ? top[1] : min(top[1], max(lo1, (int)((float)lo1 * __builtin_amdgcn_exp2f(ratio * (float)i))));
+      const bool fits = units_of(1, c, split) <= most;
+      if (lane == 0) {
+        sSize[1][i] = c;
+        sCost[1][i] = fits ? 0.f : 1.f;
+      }
+    }
+  }
+  __syncthreads();
+  int C[2] = {top[0], top[1]};
+  if (sLeast[0] > 0) {
+    float best = INFINITY;
+    for (int i = 0; i < TRIES; ++i)
+      if (sCost[0][i] < best) {
+        best = sCost[0][i];
+        C[0] = sSize[0][i];
+      }
+  }
+  if (sLeast[1] > 0) {
+    int i = 0;
+    while (i < TRIES - 1 && sCost[1][i] > 0.f) ++i;
+    const int hi = sSize[1][i], lo = i > 0 ? sSize[1][i - 1] : hi;
+    C[1] = hi;
+    if (hi - lo > 1) {   // the same for all threads
+      __syncthreads();
+      for (int t = wave; t < 8; t += NW) {
+        long long split;
+        const int c = lo + (int)((long long)(hi - lo) * (t + 1) / 8);
+        const bool fits = units_of(1, c, split) <= most;
+        if (lane == 0) sSize[1][t] = fits ? c : INT_MAX;
+      }
+      __syncthreads();
+      for (int t = 0; t < 8; ++t) C[1] = min(C[1], sSize[1][t]);
+    }
+  }
+  const float rC[2] = {__builtin_amdgcn_rcpf((float)C[0]), __builtin_amdgcn_rcpf((float)C[1])};
+  if (!SMALL || wave == 0) {
     // first units of the jobs, wide and narrow ones counted apart, and their first partial rows
     long long units0[2] = {0, 0}, part0 = 0;
     for (int j0 = 0; j0 < J; j0 += PT) {
@@ -384,7 +425,6 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       a.parts[0] = fit && part0 > 0;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        sRun[k] = C[k];
         sUnits[k] = fit ? (int)units0[k] : 0;
       }
     }
@@ -392,8 +432,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const int all = sUnits[k], c = sRun[k];
-    const float rc = __builtin_amdgcn_rcpf((float)c);
+    const int all = sUnits[k];
     Unit* out = a.units + (k == 0 ? 0 : a.max_units[0]);
     for (int u = tid; u < a.max_units[k]; u += NT) {
       if (u >= all) {
@@ -404,7 +443,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       for (int step = 1 << (31 - __builtin_clz(J)); step > 0; step >>= 1)
         if (j + step < J && first[k][j + step] <= u) j += step;
       const Job b = SMALL ? sJob[j] : job_of(j);
-      const int nb = row_blocks(b.rows), n = job_splits<SHARED>(tiles[j], b.rows, c, rc), i = u - first[k][j];
+      const int nb = row_blocks(b.rows), n = job_splits<SHARED>(tiles[j], b.rows, C[k], rC[k]), i = u - first[k][j];
       const int sp = nb == 1 ? i : i / nb, rb = nb - 1 - (i - sp * nb);   // the last rows see most: first
       const int part = SMALL ? sPart[j] : SHARED && j < a.groups ? a.prefix[j].part : a.own[SHARED ? j - a.groups : j].part;
       out[u] = {b.s, b.c0, b.c1, sp | n << 16, b.rows, b.tok, rb * kWideRows | b.listed,
@@ -563,22 +602,22 @@ struct RowState {
   }
 };
 
-// Places of the table that a wide unit looks at together (more of them and new tokens' loop spills registers).
-template <bool SHARED>
-constexpr int rows_look() { return SHARED ? 1024 : 512; }
+constexpr int kWidePick = 512;   // places of the table that a wide unit looks at together (more, and its loop spills registers)
 
-// A wide unit walks its run of the table 512 or 1,024 places at a time: the slots that some
+// A wide unit walks its chunks of the table 512 places at a time: the slots that some
 // row of it sees go to a list in LDS (two dependent reads, for all places at
 // once), and the keys and values of the listed slots are gathered tile by tile,
 // double-buffered, each tile read by the four waves.  Scores are S^T = K Q^T
 // (keys on M, rows on N), so that a lane holds 16 scores of one row; softmax and
-// the products with V as in the forward of the eviction mask.
+// the products with V as in the forward of the eviction mask.  New tokens, whose
+// row blocks are many, have three workgroups a CU and two tiles; the few row
+// blocks of shared prefixes, bound by a tile's latency, two workgroups and three.
 // FAR: caches of 4 GiB or more, whose rows need 64-bit addresses of their own; else a copy takes one addition.
 template <int D, bool SHARED, bool FAR>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) rows_wide_kernel(RowsArgs a) {
   using LY = Lay<D, true>;
   constexpr int KS = D / 16, BN = rows_bn<D>(), NKB = BN / 32, PITCH = LY::PITCH, TILE = BN * PITCH;
-  constexpr int PIECES = BN * LY::CPRP / kWave, PW = (PIECES + 3) / 4, PICK = rows_look<SHARED>(), LOOK = PICK / 256;
+  constexpr int PIECES = BN * LY::CPRP / kWave, PW = (PIECES + 3) / 4, PICK = kWidePick, LOOK = PICK / 256;
   static_assert(BN * LY::CPRP % kWave == 0, "tile must fill whole 64-slot pieces");
   __shared__ __attribute__((aligned(1024))) uint16_t sK0[TILE];
   __shared__ __attribute__((aligned(1024))) uint16_t sK1[TILE];
@@ -1014,7 +1053,9 @@ __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
 static size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Units per KV head that fill the chip: three wide ones a CU, four narrow ones (D = 64: seven).
-static int rows_want(int Hkv, int D, bool wide) { return ((wide ? 3 : D == 128 ? 4 : 7) * 256 + Hkv - 1) / Hkv; }
+static int rows_want(const PagedRows& p, bool wide) {
+  return ((wide ? 3 : p.D == 128 ? 4 : 7) * 256 + p.Hkv - 1) / p.Hkv;
+}
 // Sizes of a call's workspace, in this order.
 struct RowsSpace {
   long long units[2], part;   // units per KV head, wide and narrow; partial rows
@@ -1036,7 +1077,7 @@ static RowsSpace rows_space(const PagedRows& p) {
   const long long blocks[2] = {all > kNarrowRows ? all / kWideRows + wide_jobs : 0, (p.shared ? (long long)p.groups : 0) + p.S};
   long long added = 0;
   for (int k = 0; k < 2; ++k) {
-    const long long want = rows_want(p.Hkv, p.D, k == 0);
+    const long long want = rows_want(p, k == 0);
     const long long more = k == 0 ? std::min(std::max(want, 3 * blocks[0]), 4 * want) : std::max(want - blocks[1], want / 2);
     x.units[k] = std::min(blocks[k] * splits, blocks[k] + more);
     added += std::min(more, x.units[k]) * (k == 0 ? kWideRows : kNarrowRows);
@@ -1137,7 +1178,7 @@ hipError_t launch_paged_rows(const PagedRows& p) {
   a.max_part = x.part;
   for (int k = 0; k < 2; ++k) {
     a.max_units[k] = (int)x.units[k];
-    a.want[k] = rows_want(p.Hkv, p.D, k == 0);
+    a.want[k] = rows_want(p, k == 0);
   }
   if (p.shared) return p.D == 128 ? launch_rows<128, true>(p, a) : launch_rows<64, true>(p, a);
   return p.D == 128 ? launch_rows<128, false>(p, a) : launch_rows<64, false>(p, a);
