@@ -66,12 +66,15 @@ hipError_t launch_paged_copy(const PagedCopy& p) {
 }
 
 // ---------------------------------------------------------------- the plan
-// Jobs of more than 32 rows have units of 128 rows, four waves that share a tile of keys and values; smaller ones
-// units of one wave.  The two kinds run one after the other, each cut so that it fills the chip.
+// Jobs of more than 32 rows have units of 128 rows, four waves that share a tile of keys and values, and are cut into
+// equal runs; smaller ones have units of one wave.  Those are bound by HBM, so what counts is that all waves end together:
+// the smaller jobs' chunks, one job's behind the other's, are dealt to the waves in equal parts, and a wave whose part
+// spans jobs has a unit in each of them.  The two kinds run one after the other, each so that it fills the chip.
 constexpr int kWideRows = 128, kNarrowRows = 32;
 template <int D>
 constexpr int rows_bn() { return D == 128 ? 32 : 64; }   // keys of a tile of wide units
-constexpr int kLeastTiles = 4;    // of a unit, in 32-key tiles
+constexpr int kLeastTiles = 4;    // of a wide unit, in 32-key tiles
+constexpr int kLeastChunks = 1;   // of a wave's part
 constexpr int kPlanSmall = 256;   // sequences, and groups, that one wave plans, in LDS
 
 // What the plan weighs for wide units: with w tiles of work for each place on the chip the last unit ends about half the
@@ -80,8 +83,8 @@ constexpr int kPlanSmall = 256;   // sequences, and groups, that one wave plans,
 constexpr float kSplitTiles = 40.f;
 constexpr int kChunk = 64;        // places of a table that are skipped or looked at together
 
-// What a unit is, as its workgroups read it: the chunks k, k + n, k + 2 n, ... of the places [c0, c1) of a table, so that
-// a run of places that its rows do not see falls on all units of the job alike.
+// What a unit is, as its waves read it: the chunks k, k + n, k + 2 n, ... of the places [c0, c1) of a table, so that a run
+// of places that its rows do not see falls on all units of the job alike.
 struct Unit {
   int s;          // sequence whose table is read; -1: no such unit
   int c0, c1;
@@ -119,17 +122,18 @@ struct RowsArgs {
   int* list;        // [S] members, group by group
   int* count;       // [groups] members, and
   int* base;        // [groups] the first of them in `list` (more than kPlanSmall sequences or groups)
-  int* jobs;        // [4][jobs] tiles, rows, first wide and narrow unit (the same)
+  int* jobs;        // [5][jobs] tiles, rows, first wide and narrow unit, first chunk (the same)
   Parts* own;       // [S] of each sequence
   Parts* prefix;    // [groups] of each group
   Unit* units;      // [max_units[0] + max_units[1]]: wide, narrow
+  int* waves;       // [max_waves + 1] first narrow unit of each wave
   float* part;      // [max_part][D]
   float2* part_ml;  // [max_part]: m (log2 units), l
   int* parts;       // [1] whether there are partial rows
   int2* stats;      // [S][ceil(max_blocks BS / kChunk)] least and greatest position in each chunk of a table (window > 0)
   long long max_part;
-  int max_units[2];
-  int want[2];      // units per KV head that fill the chip
+  int max_units[2], max_waves;
+  int want[2];      // wide units, and waves of narrow ones, per KV head that fill the chip
 };
 
 struct Job {
@@ -138,10 +142,17 @@ struct Job {
 __device__ __forceinline__ int block_of(const RowsArgs& a, int place) { return a.shift >= 0 ? place >> a.shift : place / a.BS; }
 __device__ __forceinline__ bool is_wide(int rows) { return rows > kNarrowRows; }
 __device__ __forceinline__ int row_blocks(int rows) { return is_wide(rows) ? (rows + kWideRows - 1) / kWideRows : rows > 0; }
-// Splits of a job of `tiles` (at most kTileCap) under runs of c tiles.  New tokens that see nothing still have rows to write.
+// Splits of a wide job of `tiles` (at most kTileCap) under runs of c tiles.  New tokens that see nothing still have rows
+// to write.
 template <bool SHARED>
 __device__ __forceinline__ int job_splits(int tiles, int rows, int c, float rc) {
-  return rows == 0 || (SHARED && tiles == 0) ? 0 : unit_count(tiles, c, rc);
+  return !is_wide(rows) || (SHARED && tiles == 0) ? 0 : unit_count(tiles, c, rc);
+}
+// Chunks of a narrow job, as they are dealt.
+template <bool SHARED>
+__device__ __forceinline__ int job_chunks(int tiles, int rows) {
+  const int n = (tiles + 1) / 2;
+  return is_wide(rows) || rows == 0 ? 0 : SHARED ? n : max(n, 1);
 }
 
 // Prefix sums over the workgroup's NT threads, without the own value, on top of `from`, which moves on by their total.
@@ -179,19 +190,18 @@ __device__ __forceinline__ void chunk_stats(const RowsArgs& a, int first, int wa
 }
 
 // The plan, by workgroup 0: for up to 256 sequences and groups one wave makes it, with what it knows of them in LDS, and
-// all of them write the units.  The jobs of a kind are cut into runs of the same size, about the smallest for which the
-// units are as many as fill the chip (and half as many on top of the row blocks, where these do).  Bound by latency.
-// Under a window the other workgroups take the positions of the tables' chunks.
+// all of them try the sizes of wide jobs' runs and write the units.  Bound by latency.  Under a window the other
+// workgroups take the positions of the tables' chunks.
 template <bool SHARED, bool SMALL>
 __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs a) {
   constexpr int NT = SMALL ? 512 : 1024, PT = SMALL ? kWave : NT;   // threads; those that plan
   constexpr int CAP = SMALL ? kPlanSmall : 1, JOBS = SHARED ? 2 * CAP : CAP;
-  __shared__ int sJobs[4 * JOBS], sGroup[SHARED ? 6 * CAP : 1], sPart[JOBS];
+  __shared__ int sJobs[5 * JOBS], sGroup[SHARED ? 6 * CAP : 1], sPart[JOBS];
   __shared__ Job sJob[JOBS];
   constexpr int NW = NT / kWave, TRIES = 16;
-  __shared__ int buf[PT / kWave], sTop[2][PT / kWave], sRun[2], sUnits[2], sSize[2][TRIES];
-  __shared__ long long sLeast[2], sWork;
-  __shared__ float sCost[2][TRIES];
+  __shared__ int buf[PT / kWave], sTop[PT / kWave], sTopWide, sUnits[2], sPer, sSize[TRIES];
+  __shared__ long long sLeast, sWork, sChunks;
+  __shared__ float sCost[TRIES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, J = SHARED ? a.groups + a.S : a.S;
   if (blockIdx.x > 0) {
     chunk_stats(a, (blockIdx.x - 1) * (NT / kWave) + wave, (gridDim.x - 1) * (NT / kWave));
@@ -201,6 +211,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   int* rows = SMALL ? sJobs + JOBS : a.jobs + J;
   // units of the jobs in front of each, wide and narrow ones counted apart
   int* first[2] = {SMALL ? sJobs + 2 * JOBS : a.jobs + 2 * J, SMALL ? sJobs + 3 * JOBS : a.jobs + 3 * J};
+  int* chunk = SMALL ? sJobs + 4 * JOBS : a.jobs + 4 * J;   // chunks of the narrow jobs in front of each
   int* count = SMALL ? sGroup : a.count;
   int* base = SMALL ? sGroup + CAP : a.base;
   int* rank = SMALL ? sGroup + 2 * CAP : a.rank;
@@ -289,126 +300,84 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       }
       sync();
     }
-    int top[2] = {1, 1};
-    long long least[2] = {0, 0}, work = 0;   // row blocks; tiles of all wide ones
+    int top = 1;
+    long long least = 0, work = 0, chunks = 0;   // row blocks and tiles of all wide jobs; chunks of all narrow ones
     // the groups in turns of their own: the sequences' jobs begin where they end
     for (int j0 = 0; j0 < J; j0 += PT) {
       const int ends = SHARED && j0 < a.groups ? min(a.groups, j0 + PT) : min(J, j0 + PT), j = j0 + tid;
       const bool mine = j < ends;
       const Job x = mine ? job_of(j) : Job{0, 0, 0, 0, 0, 0};
-      const int k = is_wide(x.rows) ? 0 : 1;
+      const bool wide = is_wide(x.rows);
       int places = x.c1 - x.c0;
       if (!SHARED && a.window > 0) places = (int)min((long long)places, (long long)a.window + a.sinks + x.rows / a.G);
-      const int t = plan_tiles(places);
+      const int t = wide ? plan_tiles(places) : (int)(((unsigned)places + 31) / 32);
       if (mine) {
         tiles[j] = t;
         rows[j] = x.rows;
         if (SMALL) sJob[j] = x;
       }
-      top[0] = max(top[0], k == 0 ? t : 0);
-      top[1] = max(top[1], k == 1 ? t : 0);
-      block_scan<PT>(k == 0 ? row_blocks(x.rows) : 0, least[0], buf);
-      block_scan<PT>(k == 0 ? (int)min((long long)row_blocks(x.rows) * t, 1ll << 24) : 0, work, buf);
-      block_scan<PT>(k == 1 ? row_blocks(x.rows) : 0, least[1], buf);
+      top = max(top, wide ? t : 0);
+      block_scan<PT>(wide ? row_blocks(x.rows) : 0, least, buf);
+      block_scan<PT>(wide ? (int)min((long long)row_blocks(x.rows) * t, 1ll << 24) : 0, work, buf);
+      const long long c0 = block_scan<PT>(job_chunks<SHARED>(t, x.rows), chunks, buf);
+      if (mine) chunk[j] = (int)min(c0, (long long)INT_MAX);
       if (SHARED && j0 < a.groups) {
         j0 = ends - PT;
         sync();
       }
     }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      top[k] = wave_max(top[k]);
-      if (lane == 0) sTop[k][wave] = top[k];
-    }
+    top = wave_max(top);
+    if (lane == 0) sTop[wave] = top;
     sync();
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      for (int w = 0; w < PT / kWave; ++w) top[k] = max(top[k], sTop[k][w]);
-      if (tid == 0) {
-        sRun[k] = top[k];
-        sLeast[k] = least[k];
-      }
+    for (int w = 0; w < PT / kWave; ++w) top = max(top, sTop[w]);
+    if (tid == 0) {
+      sTopWide = top;
+      sLeast = least;
+      sWork = work;
+      sChunks = chunks;
     }
-    if (tid == 0) sWork = work;
   }
   __syncthreads();
-  // The size of the runs, a wave a size at a time.  Wide units: the whole of the longest job and its parts, by their cost.
-  // Narrow ones: the smallest size for which they are as many as fill the chip (and half as many on top of the jobs where
-  // these do), in equal ratios from the least to the whole, then between two of these.  The whole always fits.
-  const int top[2] = {sRun[0], sRun[1]};
-  auto units_of = [&](int k, int c, long long& split) {   // and rows of partial results of jobs that are split
-    const float rc = __builtin_amdgcn_rcpf((float)c);
-    long long units = 0;
-    split = 0;
-    for (int j0 = 0; j0 < J; j0 += kWave) {
-      const int j = j0 + lane, r = j < J ? rows[j] : 0;
-      const int n = j < J && is_wide(r) == (k == 0) ? job_splits<SHARED>(tiles[j], r, c, rc) : 0;
-      units += wave_last(wave_scan((int)min((long long)n * row_blocks(r), 1ll << 24)));   // more than there may be at any rate
-      if (k == 0) split += wave_last(wave_scan(n > 1 ? (int)min((long long)n * r, 1ll << 24) : 0));
-    }
-    return units;
-  };
-  const long long most = min((long long)a.max_units[1], max((long long)a.want[1], sLeast[1] + a.want[1] / 2));
-  const int lo1 = min(kLeastTiles, top[1]);
-  for (int i = wave; i < TRIES; i += NW) {
-    long long split;
-    if (sLeast[0] > 0) {
+  // The size of the wide jobs' runs: the whole of the longest one, which always fits, or a part of it, by their cost; a
+  // wave a size at a time.
+  int C = sTopWide;
+  if (sLeast > 0) {
+    for (int i = wave; i < TRIES; i += NW) {
       const int n = i < 4 ? i + 1 : i & 1 ? 4 << ((i - 3) >> 1) : 6 << ((i - 4) >> 1);   // 1 .. 4, 6, 8, 12, 16, 24, ...
-      const int c = (top[0] + n - 1) / n;
-      const bool fits = (n == 1 || c >= kLeastTiles) && units_of(0, c, split) <= a.max_units[0];
-      const float place = 1.f / (float)a.want[0];
+      const int c = (sTopWide + n - 1) / n;
+      const float rc = __builtin_amdgcn_rcpf((float)c), place = 1.f / (float)a.want[0];
+      long long units = 0, split = 0;   // split: rows of partial results
+      for (int j0 = 0; j0 < J; j0 += kWave) {
+        const int j = j0 + lane, r = j < J ? rows[j] : 0, m = j < J ? job_splits<SHARED>(tiles[j], r, c, rc) : 0;
+        units += wave_last(wave_scan((int)min((long long)m * row_blocks(r), 1ll << 24)));   // more than there may be at any rate
+        split += wave_last(wave_scan(m > 1 ? (int)min((long long)m * r, 1ll << 24) : 0));
+      }
       if (lane == 0) {
-        sSize[0][i] = c;
-        sCost[0][i] = !fits ? INFINITY
-                            : fmaxf((float)c, (float)sWork * place + 0.5f * (float)c) + (float)split * (kSplitTiles / kWideRows) * place;
+        sSize[i] = c;
+        sCost[i] = (n > 1 && c < kLeastTiles) || units > a.max_units[0]
+                       ? INFINITY
+                       : fmaxf((float)c, (float)sWork * place + 0.5f * (float)c) + (float)split * (kSplitTiles / kWideRows) * place;
       }
     }
-    if (sLeast[1] > 0) {
-      const float ratio = __log2f((float)top[1] / (float)lo1) / (float)(TRIES - 1);
-      const int c = i == TRIES - 1 ? top[1] : min(top[1], max(lo1, (int)((float)lo1 * __builtin_amdgcn_exp2f(ratio * (float)i))));
-      const bool fits = units_of(1, c, split) <= most;
-      if (lane == 0) {
-        sSize[1][i] = c;
-        sCost[1][i] = fits ? 0.f : 1.f;
-      }
-    }
-  }
-  __syncthreads();
-  int C[2] = {top[0], top[1]};
-  if (sLeast[0] > 0) {
+    __syncthreads();
     float best = INFINITY;
     for (int i = 0; i < TRIES; ++i)
-      if (sCost[0][i] < best) {
-        best = sCost[0][i];
-        C[0] = sSize[0][i];
+      if (sCost[i] < best) {
+        best = sCost[i];
+        C = sSize[i];
       }
   }
-  if (sLeast[1] > 0) {
-    int i = 0;
-    while (i < TRIES - 1 && sCost[1][i] > 0.f) ++i;
-    const int hi = sSize[1][i], lo = i > 0 ? sSize[1][i - 1] : hi;
-    C[1] = hi;
-    if (hi - lo > 1) {   // the same for all threads
-      __syncthreads();
-      for (int t = wave; t < 8; t += NW) {
-        long long split;
-        const int c = lo + (int)((long long)(hi - lo) * (t + 1) / 8);
-        const bool fits = units_of(1, c, split) <= most;
-        if (lane == 0) sSize[1][t] = fits ? c : INT_MAX;
-      }
-      __syncthreads();
-      for (int t = 0; t < 8; ++t) C[1] = min(C[1], sSize[1][t]);
-    }
-  }
-  const float rC[2] = {__builtin_amdgcn_rcpf((float)C[0]), __builtin_amdgcn_rcpf((float)C[1])};
+  const float rC = __builtin_amdgcn_rcpf((float)C);
+  const int per = (int)max((long long)kLeastChunks, (sChunks + a.want[1] - 1) / a.want[1]);   // chunks of a wave's part
   if (!SMALL || wave == 0) {
     // first units of the jobs, wide and narrow ones counted apart, and their first partial rows
     long long units0[2] = {0, 0}, part0 = 0;
     for (int j0 = 0; j0 < J; j0 += PT) {
-      const int j = j0 + tid, r = j < J ? rows[j] : 0, k = is_wide(r) ? 0 : 1;
-      const int n = job_splits<SHARED>(j < J ? tiles[j] : 0, r, C[k], rC[k]), u = n * row_blocks(r);
-      const long long uw = block_scan<PT>(k == 0 ? u : 0, units0[0], buf);
-      const long long un = block_scan<PT>(k == 1 ? u : 0, units0[1], buf);
+      const int j = j0 + tid, r = j < J ? rows[j] : 0, t = j < J ? tiles[j] : 0, m = job_chunks<SHARED>(t, r);
+      const int nw = job_splits<SHARED>(t, r, C, rC);
+      const int nn = m > 0 ? (int)(((long long)chunk[j] + m - 1) / per) - chunk[j] / per + 1 : 0, n = nw + nn;
+      const long long uw = block_scan<PT>(nw * row_blocks(r), units0[0], buf);
+      const long long un = block_scan<PT>(nn, units0[1], buf);
       const long long pn = block_scan<PT>(SHARED || n > 1 ? n * r : 0, part0, buf);
       if (j < J) {
         first[0][j] = (int)min(uw, (long long)INT_MAX);
@@ -430,6 +399,13 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
     }
   }
   __syncthreads();
+  // the last job that begins at or before x: those without one of these begin where the next one does
+  auto search = [&](const int* begin, int x) {
+    int j = 0;
+    for (int step = 1 << (31 - __builtin_clz(J)); step > 0; step >>= 1)
+      if (j + step < J && begin[j + step] <= x) j += step;
+    return j;
+  };
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int all = sUnits[k];
@@ -439,16 +415,37 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
         out[u].s = -1;
         continue;
       }
-      int j = 0;   // the last job that begins at or before u: those without a unit of this kind begin where the next one does
-      for (int step = 1 << (31 - __builtin_clz(J)); step > 0; step >>= 1)
-        if (j + step < J && first[k][j + step] <= u) j += step;
+      const int j = search(first[k], u), i = u - first[k][j];
       const Job b = SMALL ? sJob[j] : job_of(j);
-      const int nb = row_blocks(b.rows), n = job_splits<SHARED>(tiles[j], b.rows, C[k], rC[k]), i = u - first[k][j];
-      const int sp = nb == 1 ? i : i / nb, rb = nb - 1 - (i - sp * nb);   // the last rows see most: first
       const int part = SMALL ? sPart[j] : SHARED && j < a.groups ? a.prefix[j].part : a.own[SHARED ? j - a.groups : j].part;
-      out[u] = {b.s, b.c0, b.c1, sp | n << 16, b.rows, b.tok, rb * kWideRows | b.listed,
-                SHARED || n > 1 ? part + sp * a.Hkv * b.rows : -1};
+      int c0 = b.c0, c1 = b.c1, sp, n, row0 = 0;
+      if (k == 0) {
+        const int nb = row_blocks(b.rows);
+        n = job_splits<SHARED>(tiles[j], b.rows, C, rC);
+        sp = nb == 1 ? i : i / nb;
+        row0 = (nb - 1 - (i - sp * nb)) * kWideRows;   // the last rows see most: first
+      } else {
+        const int m = job_chunks<SHARED>(tiles[j], b.rows), w = chunk[j] / per;
+        n = (int)(((long long)chunk[j] + m - 1) / per) - w + 1;
+        sp = i;
+      }
+      const int split = k == 1 && (SHARED || a.window == 0) ? 1 << 16 : sp | n << 16;
+      if (k == 1 && (SHARED || a.window == 0)) {   // the part of wave w + i; under a window an equal part of the chunks
+        const long long x = (long long)(chunk[j] / per + i) * per - chunk[j];
+        c1 = (int)min((long long)c1, c0 + (x + per) * kChunk);
+        c0 = (int)min((long long)c1, c0 + max(x, 0ll) * kChunk);
+      }
+      out[u] = {b.s, c0, c1, split, b.rows, b.tok, row0 | b.listed, SHARED || n > 1 ? part + sp * a.Hkv * b.rows : -1};
     }
+  }
+  for (int w = tid; w <= a.max_waves; w += NT) {
+    const long long x = (long long)w * per;
+    int u = sUnits[1];
+    if (u > 0 && x < sChunks) {
+      const int j = search(chunk, (int)x);
+      u = first[1][j] + w - chunk[j] / per;
+    }
+    a.waves[w] = u;
   }
 }
 
@@ -821,11 +818,12 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
   static_assert(kNarrowRing >= kNarrowPick + 2 * BN, "what is left of the last places, the tile in work, new ones");
 
   const int lane = threadIdx.x, half = lane >> 5, col = lane & 31;
-  const int uidx = blockIdx.x / a.Hkv, g = blockIdx.x - uidx * a.Hkv;
-  const Unit un = a.units[a.max_units[0] + uidx];
-  if (un.s < 0) return;
+  const int widx = blockIdx.x / a.Hkv, g = blockIdx.x - widx * a.Hkv;
   const auto rl = LY::row_lane(lane);
   const int tl = LY::tr_lo(lane), th = LY::tr_hi(lane);
+  const int last = a.waves[widx + 1];
+  for (int uidx = a.waves[widx]; uidx < last; ++uidx) {
+  const Unit un = a.units[a.max_units[0] + uidx];
   const int* trow = a.table + (size_t)un.s * a.max_blocks;
   ChunkWalker<SHARED> walk;
   walk.init(un);
@@ -958,6 +956,7 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
     b ^= 1;
   }
   st.finish(a, un, rw, g, col, half);
+  }
 }
 
 // ---------------------------------------------------------------- the merge
@@ -1058,30 +1057,28 @@ static int rows_want(const PagedRows& p, bool wide) {
 }
 // Sizes of a call's workspace, in this order.
 struct RowsSpace {
-  long long units[2], part;   // units per KV head, wide and narrow; partial rows
-  size_t parts, rank, list, count, base, jobs, own, prefix, unit, stats, rows, ml;
-  size_t bytes() const { return parts + rank + list + count + base + jobs + own + prefix + unit + stats + rows + ml; }
+  long long units[2], waves, part;   // units per KV head, wide and narrow; waves of narrow ones; partial rows
+  size_t parts, rank, list, count, base, jobs, own, prefix, unit, wave, stats, rows, ml;
+  size_t bytes() const { return parts + rank + list + count + base + jobs + own + prefix + unit + wave + stats + rows + ml; }
 };
 static size_t stats_chunks(const PagedRows& p) { return ((size_t)p.max_blocks * p.block_size + kChunk - 1) / kChunk; }
 static bool plans_small(const PagedRows& p) { return p.S <= kPlanSmall && p.groups <= kPlanSmall; }
 // Row blocks of wide jobs: one for every 128 rows, and one more a job (of 33 rows at least; SHARED: groups, and sequences
 // by themselves if they have so many q-heads).  A job has no splits of fewer than kLeastTiles tiles; those of wide jobs
-// add no more units than four rounds of them and than three times the row blocks (or one round), those of narrow ones no
-// more than a round.  Partial rows: those of every job once and of the units that splits add; for new tokens only those
-// of jobs that are split, each into two at least, so twice those of the added units.
+// add no more units than four rounds of them and than three times the row blocks (or one round).  Narrow jobs: a unit
+// each, and one more for every wave's end.  Partial rows: those of every job once and of the units that are added; for
+// new tokens only those of jobs of several units, so twice those of the added ones.
 static RowsSpace rows_space(const PagedRows& p) {
   RowsSpace x{};
   const long long G = p.Hq / p.Hkv, tokens = p.shared ? p.S : p.ntok, all = tokens * G;
-  const long long width = ((long long)p.max_blocks * p.block_size + 31) / 32, splits = (width + kLeastTiles - 1) / kLeastTiles;
+  const long long width = (long long)p.max_blocks * p.block_size, jobs = (p.shared ? (long long)p.groups : 0) + p.S;
   const long long wide_jobs = std::min<long long>(p.shared ? p.groups : p.S, all / kNarrowRows) + (p.shared && G > kNarrowRows ? p.S : 0);
-  const long long blocks[2] = {all > kNarrowRows ? all / kWideRows + wide_jobs : 0, (p.shared ? (long long)p.groups : 0) + p.S};
-  long long added = 0;
-  for (int k = 0; k < 2; ++k) {
-    const long long want = rows_want(p, k == 0);
-    const long long more = k == 0 ? std::min(std::max(want, 3 * blocks[0]), 4 * want) : std::max(want - blocks[1], want / 2);
-    x.units[k] = std::min(blocks[k] * splits, blocks[k] + more);
-    added += std::min(more, x.units[k]) * (k == 0 ? kWideRows : kNarrowRows);
-  }
+  const long long blocks = all > kNarrowRows ? all / kWideRows + wide_jobs : 0, want = rows_want(p, true);
+  const long long more = std::min(std::max(want, 3 * blocks), 4 * want);
+  x.units[0] = std::min(blocks * ((width + 32 * kLeastTiles - 1) / (32 * kLeastTiles)), blocks + more);
+  x.waves = std::min<long long>(rows_want(p, false), jobs * ((width + kChunk * kLeastChunks - 1) / (kChunk * kLeastChunks)));
+  x.units[1] = jobs + x.waves;
+  const long long added = std::min(more, x.units[0]) * kWideRows + x.waves * kNarrowRows;
   x.part = (p.shared ? 2 * all + added : 2 * added) * p.Hkv;
   x.parts = 256;
   if (p.shared) {
@@ -1090,10 +1087,11 @@ static RowsSpace rows_space(const PagedRows& p) {
   }
   if (!plans_small(p)) {
     if (p.shared) x.count = x.base = round256((size_t)p.groups * sizeof(int));
-    x.jobs = round256(4 * ((size_t)p.S + p.groups) * sizeof(int));
+    x.jobs = round256(5 * ((size_t)p.S + p.groups) * sizeof(int));
   }
   x.own = round256((size_t)p.S * sizeof(Parts));
   x.unit = round256((size_t)(x.units[0] + x.units[1]) * sizeof(Unit));
+  x.wave = round256((size_t)(x.waves + 1) * sizeof(int));
   if (!p.shared) x.stats = round256((size_t)p.S * stats_chunks(p) * sizeof(int2));
   x.rows = round256((size_t)x.part * p.D * sizeof(float));
   x.ml = round256((size_t)x.part * sizeof(float2));
@@ -1103,7 +1101,8 @@ size_t paged_rows_ws_bytes(const PagedRows& p) { return rows_space(p).bytes(); }
 bool paged_rows_fit(const PagedRows& p) {
   const RowsSpace x = rows_space(p);
   const long long rows = (long long)(p.shared ? p.S : p.ntok) * p.Hq;
-  return std::max(x.units[0], x.units[1]) * p.Hkv <= 0x7fffffffll / 256 && x.part <= 0x7fffffffll && rows <= (1ll << 26) - 4;
+  return std::max(x.units[0], x.units[1]) * p.Hkv <= 0x7fffffffll / 256 && x.part <= 0x7fffffffll && rows <= (1ll << 26) - 4 &&
+         ((long long)p.S + p.groups) * (long long)stats_chunks(p) <= 0x7fffffffll;
 }
 
 template <int D, bool SHARED>
@@ -1118,7 +1117,7 @@ static hipError_t launch_rows(const PagedRows& p, const RowsArgs& a) {
   if (a.max_units[0])
     hipLaunchKernelGGL((far ? rows_wide_kernel<D, SHARED, true> : rows_wide_kernel<D, SHARED, false>),
                        dim3((unsigned)((long long)a.max_units[0] * a.Hkv)), dim3(256), 0, p.stream, a);
-  hipLaunchKernelGGL((rows_narrow_kernel<D, SHARED>), dim3((unsigned)((long long)a.max_units[1] * a.Hkv)), dim3(64), 0,
+  hipLaunchKernelGGL((rows_narrow_kernel<D, SHARED>), dim3((unsigned)((long long)a.max_waves * a.Hkv)), dim3(64), 0,
                      p.stream, a);
   prof_end(p.stream);
   hipError_t e = hipGetLastError();
@@ -1172,6 +1171,7 @@ hipError_t launch_paged_rows(const PagedRows& p) {
   a.own = (Parts*)take(x.own);
   a.prefix = (Parts*)take(x.prefix);
   a.units = (Unit*)take(x.unit);
+  a.waves = (int*)take(x.wave);
   a.stats = (int2*)take(x.stats);
   a.part = (float*)take(x.rows);
   a.part_ml = (float2*)take(x.ml);
@@ -1180,6 +1180,7 @@ hipError_t launch_paged_rows(const PagedRows& p) {
     a.max_units[k] = (int)x.units[k];
     a.want[k] = rows_want(p, k == 0);
   }
+  a.max_waves = (int)x.waves;
   if (p.shared) return p.D == 128 ? launch_rows<128, true>(p, a) : launch_rows<64, true>(p, a);
   return p.D == 128 ? launch_rows<128, false>(p, a) : launch_rows<64, false>(p, a);
 }
