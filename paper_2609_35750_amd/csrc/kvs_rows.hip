@@ -976,19 +976,22 @@ struct Joined {
   }
 };
 
-// The partial results of a row: the group's prefix and the sequence's own part (one wave a row, whose halves, or
-// quarters, of D / 4 lanes take the parts in turn), or a sequence's splits (one wave a token and KV head, which take the
-// head's rows in turn: few parts a row, and the token is looked up once).  Bound by the latency of its reads: four parts
-// are asked for at a time.
-template <int D, bool SHARED>
+// The partial results of a row: the group's prefix and the sequence's own part, or a sequence's splits.  BLOCK: a
+// workgroup a row, whose groups of D / 4 lanes take the parts in turn (one long sequence has hundreds); else, for many
+// rows of new tokens, which have few parts each, a wave a token and KV head, whose halves (D = 64: quarters) take the
+// head's rows in turn, so that the token is looked up once.  Bound by the latency of its reads: four parts are asked for
+// at a time.
+template <int D, bool SHARED, bool BLOCK>
 __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
   constexpr int LPS = D / 4, PER = kWave / LPS, UNROLL = 4;
-  const int lane = threadIdx.x & 63, sub = lane / LPS;
+  __shared__ float2 sML[BLOCK ? 4 : 1];
+  __shared__ float4 sX[BLOCK ? 4 * LPS : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / LPS, d4 = lane & (LPS - 1);
   if (!SHARED && a.parts[0] == 0) return;   // every row is written by its unit
-  const int per_tok = SHARED ? a.Hq : a.Hkv;
+  const int per_tok = BLOCK ? a.Hq : a.Hkv;
   const long long all = (long long)a.ntok * per_tok;
-  for (long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); i < all; i += (long long)gridDim.x * 4) {
-    const int tok = (int)(i / per_tok), at = (int)(i - (long long)tok * per_tok), g = SHARED ? at / a.G : at;
+  for (long long i = BLOCK ? blockIdx.x : blockIdx.x * 4ll + wave; i < all; i += BLOCK ? gridDim.x : gridDim.x * 4ll) {
+    const int tok = (int)(i / per_tok), at = (int)(i - (long long)tok * per_tok), g = BLOCK ? at / a.G : at;
     Parts set[2] = {};
     long long row[2] = {};   // of the first q-head of the KV head
     if (!SHARED) {   // the sequence of the token: the last one that begins at or before it
@@ -1011,38 +1014,48 @@ __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) row[k] += set[k].part + (long long)g * set[k].rows;
     const int n = set[0].n + set[1].n;
-    for (int r = SHARED ? at - g * a.G : sub; r < a.G; r += SHARED ? a.G : PER) {
+    for (int r = BLOCK ? at - g * a.G : sub; r < a.G; r += BLOCK ? a.G : PER) {
       auto where = [&](int p) {
         return r + (p < set[0].n ? row[0] + (long long)p * a.Hkv * set[0].rows
                                  : row[1] + (long long)(p - set[0].n) * a.Hkv * set[1].rows);
       };
-      constexpr int STEP = SHARED ? PER : 1;
+      constexpr int STEP = BLOCK ? 4 * PER : 1;
       Joined x = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-      for (int p0 = SHARED ? sub : 0; p0 < n; p0 += UNROLL * STEP) {
+      for (int p0 = BLOCK ? wave * PER + sub : 0; p0 < n; p0 += UNROLL * STEP) {
         float2 v[UNROLL];
         float4 y[UNROLL];
 #pragma unroll
         for (int k = 0; k < UNROLL; ++k) {   // the last one again behind the end
           const long long w = where(min(p0 + k * STEP, n - 1));
           v[k] = a.part_ml[w];
-          y[k] = reinterpret_cast<const float4*>(a.part + w * D)[lane & (LPS - 1)];
+          y[k] = reinterpret_cast<const float4*>(a.part + w * D)[d4];
         }
 #pragma unroll
         for (int k = 0; k < UNROLL; ++k)
           if (p0 + k * STEP < n) x.add(v[k], y[k]);
       }
-      if (SHARED)
+      if (BLOCK) {
 #pragma unroll
         for (int off = LPS; off < kWave; off <<= 1) {
           const float2 v = make_float2(__shfl_xor(x.m, off), __shfl_xor(x.l, off));
           const float4 y = make_float4(__shfl_xor(x.x.x, off), __shfl_xor(x.x.y, off), __shfl_xor(x.x.z, off), __shfl_xor(x.x.w, off));
           x.add(v, y);
         }
-      if (!SHARED || sub == 0) {
+        if (sub == 0) {
+          if (d4 == 0) sML[wave] = make_float2(x.m, x.l);
+          sX[wave * LPS + d4] = x.x;
+        }
+        __syncthreads();
+        if (wave == 0)
+#pragma unroll
+          for (int w = 1; w < 4; ++w) x.add(sML[w], sX[w * LPS + d4]);
+        __syncthreads();
+      }
+      if (!BLOCK || (wave == 0 && sub == 0)) {
         const float inv = x.l <= 0.f ? 0.f : 1.f / x.l;
         const size_t out = (size_t)tok * a.Hq + g * a.G + r;
-        reinterpret_cast<uint2*>(a.o + out * D)[lane & (LPS - 1)] = pack4_bf16(x.x.x * inv, x.x.y * inv, x.x.z * inv, x.x.w * inv);
-        if ((lane & (LPS - 1)) == 0) a.lse[out] = x.l <= 0.f ? -INFINITY : (x.m + __log2f(x.l)) * 0.6931471805599453f;
+        reinterpret_cast<uint2*>(a.o + out * D)[d4] = pack4_bf16(x.x.x * inv, x.x.y * inv, x.x.z * inv, x.x.w * inv);
+        if (d4 == 0) a.lse[out] = x.l <= 0.f ? -INFINITY : (x.m + __log2f(x.l)) * 0.6931471805599453f;
       }
     }
   }
@@ -1055,6 +1068,7 @@ static size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 static int rows_want(const PagedRows& p, bool wide) {
   return ((wide ? 3 : p.D == 128 ? 4 : 7) * 256 + p.Hkv - 1) / p.Hkv;
 }
+constexpr long long kBlockRows = 4096;   // rows of new tokens that are merged by a workgroup each
 // Sizes of a call's workspace, in this order.
 struct RowsSpace {
   long long units[2], waves, part;   // units per KV head, wide and narrow; waves of narrow ones; partial rows
@@ -1122,9 +1136,12 @@ static hipError_t launch_rows(const PagedRows& p, const RowsArgs& a) {
   prof_end(p.stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const long long rows = (long long)a.ntok * (SHARED ? a.Hq : a.Hkv);
-  hipLaunchKernelGGL((rows_merge_kernel<D, SHARED>), dim3((unsigned)std::min((rows + 3) / 4, 4096ll)), dim3(256), 0,
-                     p.stream, a);
+  const long long rows = (long long)a.ntok * a.Hq;
+  if (SHARED || rows <= kBlockRows)
+    hipLaunchKernelGGL((rows_merge_kernel<D, SHARED, true>), dim3((unsigned)std::min(rows, 16384ll)), dim3(256), 0, p.stream, a);
+  else
+    hipLaunchKernelGGL((rows_merge_kernel<D, SHARED, SHARED>), dim3((unsigned)std::min((rows / a.G + 3) / 4, 4096ll)), dim3(256),
+                       0, p.stream, a);
   return hipGetLastError();
 }
 
