@@ -66,15 +66,16 @@ hipError_t launch_paged_copy(const PagedCopy& p) {
 }
 
 // ---------------------------------------------------------------- the plan
-// Jobs of more than 32 rows have units of 128 rows, four waves that share a tile of keys and values, and are cut into
+// Jobs of more than 64 rows (D = 64: 32) have units of 128 rows, four waves that share a tile of keys and values, and are cut into
 // equal runs; smaller ones have units of one wave.  Those are bound by HBM, so what counts is that all waves end together:
 // the smaller jobs' chunks, one job's behind the other's, are dealt to the waves in equal parts, and a wave whose part
 // spans jobs has a unit in each of them.  The two kinds run one after the other, each so that it fills the chip.
-constexpr int kWideRows = 128, kNarrowRows = 32;
+constexpr int kWideRows = 128;
+constexpr int narrow_rows(int D) { return D == 128 ? 64 : 32; }   // most rows of a narrow job
 template <int D>
 constexpr int rows_bn() { return D == 128 ? 32 : 64; }   // keys of a tile of wide units
 constexpr int kLeastTiles = 4;    // of a wide unit, in 32-key tiles
-constexpr int kLeastChunks = 1;   // of a wave's part
+constexpr int kStartChunks = 2;   // what beginning a narrow job costs a wave (the latency of six reads), as chunks
 constexpr int kPlanSmall = 256;   // sequences, and groups, that one wave plans, in LDS
 
 // What the plan weighs for wide units: with w tiles of work for each place on the chip the last unit ends about half the
@@ -116,6 +117,7 @@ struct RowsArgs {
   float* lse;
   int S, groups, ntok, Hq, Hkv, G, max_blocks, BS, num_blocks, window, sinks;
   int shift;                  // BS = 1 << shift; -1: BS is no power of two
+  int narrow;                 // narrow_rows(D)
   float scale_log2;
   // workspace
   int* rank;        // [S] SHARED: of a sequence among its group's members
@@ -140,19 +142,19 @@ struct Job {
   int s, c0, c1, rows, tok, listed;
 };
 __device__ __forceinline__ int block_of(const RowsArgs& a, int place) { return a.shift >= 0 ? place >> a.shift : place / a.BS; }
-__device__ __forceinline__ bool is_wide(int rows) { return rows > kNarrowRows; }
-__device__ __forceinline__ int row_blocks(int rows) { return is_wide(rows) ? (rows + kWideRows - 1) / kWideRows : rows > 0; }
+__device__ __forceinline__ bool is_wide(const RowsArgs& a, int rows) { return rows > a.narrow; }
+__device__ __forceinline__ int row_blocks(int rows) { return (rows + kWideRows - 1) / kWideRows; }   // of a wide job
 // Splits of a wide job of `tiles` (at most kTileCap) under runs of c tiles.  New tokens that see nothing still have rows
 // to write.
 template <bool SHARED>
-__device__ __forceinline__ int job_splits(int tiles, int rows, int c, float rc) {
-  return !is_wide(rows) || (SHARED && tiles == 0) ? 0 : unit_count(tiles, c, rc);
+__device__ __forceinline__ int job_splits(const RowsArgs& a, int tiles, int rows, int c, float rc) {
+  return !is_wide(a, rows) || (SHARED && tiles == 0) ? 0 : unit_count(tiles, c, rc);
 }
-// Chunks of a narrow job, as they are dealt.
+// Chunks of a narrow job that are dealt.
 template <bool SHARED>
-__device__ __forceinline__ int job_chunks(int tiles, int rows) {
+__device__ __forceinline__ int job_chunks(const RowsArgs& a, int tiles, int rows) {
   const int n = (tiles + 1) / 2;
-  return is_wide(rows) || rows == 0 ? 0 : SHARED ? n : max(n, 1);
+  return is_wide(a, rows) || rows == 0 ? 0 : SHARED ? n : max(n, 1);
 }
 
 // Prefix sums over the workgroup's NT threads, without the own value, on top of `from`, which moves on by their total.
@@ -211,7 +213,8 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   int* rows = SMALL ? sJobs + JOBS : a.jobs + J;
   // units of the jobs in front of each, wide and narrow ones counted apart
   int* first[2] = {SMALL ? sJobs + 2 * JOBS : a.jobs + 2 * J, SMALL ? sJobs + 3 * JOBS : a.jobs + 3 * J};
-  int* chunk = SMALL ? sJobs + 4 * JOBS : a.jobs + 4 * J;   // chunks of the narrow jobs in front of each
+  // where each narrow job's first chunk lies among all that is dealt
+  int* chunk = SMALL ? sJobs + 4 * JOBS : a.jobs + 4 * J;
   int* count = SMALL ? sGroup : a.count;
   int* base = SMALL ? sGroup + CAP : a.base;
   int* rank = SMALL ? sGroup + 2 * CAP : a.rank;
@@ -307,7 +310,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       const int ends = SHARED && j0 < a.groups ? min(a.groups, j0 + PT) : min(J, j0 + PT), j = j0 + tid;
       const bool mine = j < ends;
       const Job x = mine ? job_of(j) : Job{0, 0, 0, 0, 0, 0};
-      const bool wide = is_wide(x.rows);
+      const bool wide = is_wide(a, x.rows);
       int places = x.c1 - x.c0;
       if (!SHARED && a.window > 0) places = (int)min((long long)places, (long long)a.window + a.sinks + x.rows / a.G);
       const int t = wide ? plan_tiles(places) : (int)(((unsigned)places + 31) / 32);
@@ -319,7 +322,8 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       top = max(top, wide ? t : 0);
       block_scan<PT>(wide ? row_blocks(x.rows) : 0, least, buf);
       block_scan<PT>(wide ? (int)min((long long)row_blocks(x.rows) * t, 1ll << 24) : 0, work, buf);
-      const long long c0 = block_scan<PT>(job_chunks<SHARED>(t, x.rows), chunks, buf);
+      const int m = job_chunks<SHARED>(a, t, x.rows), begin = m > 0 ? kStartChunks : 0;
+      const long long c0 = block_scan<PT>(m + begin, chunks, buf) + begin;
       if (mine) chunk[j] = (int)min(c0, (long long)INT_MAX);
       if (SHARED && j0 < a.groups) {
         j0 = ends - PT;
@@ -348,7 +352,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       const float rc = __builtin_amdgcn_rcpf((float)c), place = 1.f / (float)a.want[0];
       long long units = 0, split = 0;   // split: rows of partial results
       for (int j0 = 0; j0 < J; j0 += kWave) {
-        const int j = j0 + lane, r = j < J ? rows[j] : 0, m = j < J ? job_splits<SHARED>(tiles[j], r, c, rc) : 0;
+        const int j = j0 + lane, r = j < J ? rows[j] : 0, m = j < J ? job_splits<SHARED>(a, tiles[j], r, c, rc) : 0;
         units += wave_last(wave_scan((int)min((long long)m * row_blocks(r), 1ll << 24)));   // more than there may be at any rate
         split += wave_last(wave_scan(m > 1 ? (int)min((long long)m * r, 1ll << 24) : 0));
       }
@@ -368,13 +372,13 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       }
   }
   const float rC = __builtin_amdgcn_rcpf((float)C);
-  const int per = (int)max((long long)kLeastChunks, (sChunks + a.want[1] - 1) / a.want[1]);   // chunks of a wave's part
+  const int per = (int)max(1ll, (sChunks + a.want[1] - 1) / a.want[1]);   // of a wave
   if (!SMALL || wave == 0) {
     // first units of the jobs, wide and narrow ones counted apart, and their first partial rows
     long long units0[2] = {0, 0}, part0 = 0;
     for (int j0 = 0; j0 < J; j0 += PT) {
-      const int j = j0 + tid, r = j < J ? rows[j] : 0, t = j < J ? tiles[j] : 0, m = job_chunks<SHARED>(t, r);
-      const int nw = job_splits<SHARED>(t, r, C, rC);
+      const int j = j0 + tid, r = j < J ? rows[j] : 0, t = j < J ? tiles[j] : 0, m = job_chunks<SHARED>(a, t, r);
+      const int nw = job_splits<SHARED>(a, t, r, C, rC);
       const int nn = m > 0 ? (int)(((long long)chunk[j] + m - 1) / per) - chunk[j] / per + 1 : 0, n = nw + nn;
       const long long uw = block_scan<PT>(nw * row_blocks(r), units0[0], buf);
       const long long un = block_scan<PT>(nn, units0[1], buf);
@@ -421,11 +425,11 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       int c0 = b.c0, c1 = b.c1, sp, n, row0 = 0;
       if (k == 0) {
         const int nb = row_blocks(b.rows);
-        n = job_splits<SHARED>(tiles[j], b.rows, C, rC);
+        n = job_splits<SHARED>(a, tiles[j], b.rows, C, rC);
         sp = nb == 1 ? i : i / nb;
         row0 = (nb - 1 - (i - sp * nb)) * kWideRows;   // the last rows see most: first
       } else {
-        const int m = job_chunks<SHARED>(tiles[j], b.rows), w = chunk[j] / per;
+        const int m = job_chunks<SHARED>(a, tiles[j], b.rows), w = chunk[j] / per;
         n = (int)(((long long)chunk[j] + m - 1) / per) - w + 1;
         sp = i;
       }
@@ -443,7 +447,10 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
     int u = sUnits[1];
     if (u > 0 && x < sChunks) {
       const int j = search(chunk, (int)x);
-      u = first[1][j] + w - chunk[j] / per;
+      const int m = job_chunks<SHARED>(a, tiles[j], rows[j]);
+      u = first[1][j];
+      if (m > 0 && chunk[j] <= x)   // within the job, or behind it, where the next one begins
+        u += (int)min((long long)w, ((long long)chunk[j] + m - 1) / per + 1) - chunk[j] / per;
     }
     a.waves[w] = u;
   }
@@ -527,10 +534,10 @@ struct RowState {
     m = -INFINITY;
     l = 0.f;
   }
-  // NKB blocks of 32 keys: masked scores, V in LDS.  The maximum moves only when a score exceeds it by more than 8 (log2
-  // units): probabilities are at most 2^8 then, and bf16 keeps their relative precision.
+  // NKB blocks of 32 keys: masked scores become their exponentials.  The maximum moves only when a score exceeds it by
+  // more than 8 (log2 units): probabilities are at most 2^8 then, and bf16 keeps their relative precision.
   template <int NKB>
-  __device__ __forceinline__ void add(f32x16 (&s)[NKB], const uint16_t* cV, int tl, int th, float scale_log2) {
+  __device__ __forceinline__ void weigh(f32x16 (&s)[NKB], float scale_log2) {
     float mx = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb)
@@ -557,16 +564,6 @@ struct RowState {
         ls += e;
       }
     l += ls;
-    __builtin_amdgcn_s_setprio(3);
-#pragma unroll
-    for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const bf16x8 pb = pack8(s[kb], 8 * t);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) acc[d] = mfma32(tr_operand<D, true>(cV, 32 * kb + 16 * t, 32 * d, tl, th), pb, acc[d]);
-      }
-    __builtin_amdgcn_s_setprio(0);
   }
   // O and LSE, or the partial results, of row `row`.
   __device__ __forceinline__ void finish(const RowsArgs& a, const Unit& un, const RowLane& rw, int g, int row, int half) {
@@ -713,7 +710,18 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
           }
       }
     }
-    st.template add<NKB>(s, cV, tl, th, a.scale_log2);
+    st.template weigh<NKB>(s, a.scale_log2);
+    __builtin_amdgcn_s_setprio(3);   // the products with V run back to back while other waves weigh
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        const bf16x8 pb = pack8(s[kb], 8 * t2);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+          st.acc[d] = mfma32(tr_operand<D, true>(cV, 32 * kb + 16 * t2, 32 * d, tl, th), pb, st.acc[d]);
+      }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   ChunkWalker<SHARED> walk;
@@ -797,46 +805,50 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
   st.finish(a, un, row_of<SHARED>(a, un, g, row), g, row, half);
 }
 
-// A narrow unit, 32 rows at most, is one wave, with its own tiles of 32 entries (double-buffered; D = 128: 40 KB of LDS,
+// A narrow unit, 64 rows at most (D = 64: 32, where two columns' registers would leave half the waves a CU), is one wave, with its own tiles of 32 entries (double-buffered; D = 128: 40 KB of LDS,
 // so that four share a CU, one a SIMD).  Every global read of its loop is a copy to LDS, so all of them complete in
 // issue order under one counter: step n issues the K and V copies of tile n + 1, waits until only these are
 // outstanding, asks for the next piece of what the tiles after it need, and computes tile n.  That is, for 192 places
 // of the table at a time, in consecutive steps: their table entries; the positions of the slots these name; and, when
 // the list of slots to gather runs short, the slots that some row sees are added to it (a ring of 256).
 constexpr int kNarrowPick = 192, kNarrowRing = 256;
-template <int D, bool SHARED>
-__global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
+template <int D>
+struct NarrowSpace {
+  static constexpr int TILE = 32 * Lay<D, true>::PITCH;
+  uint16_t *k, *v;   // [2][TILE]
+  int *tab, *slot;   // [kNarrowPick]
+  uint32_t* row;     // [kNarrowRing]
+  int* pos;
+};
+// A unit of up to 32 NC rows: operands of K and V are read once for all of them.
+template <int D, bool SHARED, int NC>
+__device__ __forceinline__ void narrow_unit(const RowsArgs& a, const Unit& un, int g, const NarrowSpace<D>& x) {
   using LY = Lay<D, true>;
   constexpr int KS = D / 16, BN = 32, PITCH = LY::PITCH, TILE = BN * PITCH, NP = kNarrowPick / kWave;
   constexpr int SLOTS = BN * LY::CPRP, NI = (SLOTS + kWave - 1) / kWave, OPS = 2 * NI;   // copies of a tile
-  __shared__ __attribute__((aligned(1024))) uint16_t sK[2 * TILE];
-  __shared__ __attribute__((aligned(1024))) uint16_t sV[2 * TILE];
-  __shared__ __attribute__((aligned(256))) int sTab[kNarrowPick];
-  __shared__ __attribute__((aligned(256))) int sSlot[kNarrowPick];
-  __shared__ __attribute__((aligned(16))) uint32_t sRow[kNarrowRing];
-  __shared__ __attribute__((aligned(16))) int sPos[kNarrowRing];
-  static_assert(kNarrowRing >= kNarrowPick + 2 * BN, "what is left of the last places, the tile in work, new ones");
-
+  uint16_t *const sK = x.k, *const sV = x.v;
+  int *const sTab = x.tab, *const sSlot = x.slot, *const sPos = x.pos;
+  uint32_t* const sRow = x.row;
   const int lane = threadIdx.x, half = lane >> 5, col = lane & 31;
-  const int widx = blockIdx.x / a.Hkv, g = blockIdx.x - widx * a.Hkv;
   const auto rl = LY::row_lane(lane);
   const int tl = LY::tr_lo(lane), th = LY::tr_hi(lane);
-  const int last = a.waves[widx + 1];
-  for (int uidx = a.waves[widx]; uidx < last; ++uidx) {
-  const Unit un = a.units[a.max_units[0] + uidx];
   const int* trow = a.table + (size_t)un.s * a.max_blocks;
   ChunkWalker<SHARED> walk;
   walk.init(un);
-  const RowLane rw = row_of<SHARED>(a, un, g, col);
-  bf16x8 qreg[KS];
-  {
+  RowState<D> st[NC];
+  bf16x8 qreg[NC][KS];
+  int at[NC], lo = INT_MAX, hi = -1;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const RowLane rw = row_of<SHARED>(a, un, g, 32 * c + col);
+    at[c] = rw.at;
     const uint16_t* qrow = a.q + ((size_t)rw.tok * a.Hq + rw.h) * D + 8 * half;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qreg[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qrow + 16 * ks));
+    for (int ks = 0; ks < KS; ++ks) qreg[c][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qrow + 16 * ks));
+    lo = min(lo, SHARED ? rw.at : wave_min(rw.at));
+    hi = max(hi, SHARED ? rw.at : wave_max(rw.at));
+    st[c].init();
   }
-  const int lo = SHARED ? rw.at : wave_min(rw.at), hi = SHARED ? rw.at : wave_max(rw.at);
-  RowState<D> st;
-  st.init();
 
   int prow[NI], pcol[NI];   // this lane's 16-byte slots of a tile: row (-1: none), source element
 #pragma unroll
@@ -930,12 +942,18 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
     else if (stage == 2) stage = 3;
     const uint16_t* cK = sK + b * TILE;
     uint16_t* cV = sV + b * TILE;
-    f32x16 s[1] = {f32x16{}};
+    f32x16 s[NC][1];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s[0] = mfma32(lds_read_b128(cK + LY::row_at(rl, ks)), qreg[ks], s[0]);
+    for (int c = 0; c < NC; ++c) s[c][0] = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8 ka = lds_read_b128(cK + LY::row_at(rl, ks));
+#pragma unroll
+      for (int c = 0; c < NC; ++c) s[c][0] = mfma32(ka, qreg[c][ks], s[c][0]);
+    }
     if (n < BN) {   // V of the places behind the last entry: their factor is 0, and must stay it
-      for (int x = lane; x < (BN - n) * (PITCH / 8); x += kWave)
-        *reinterpret_cast<uint4*>(&cV[n * PITCH + 8 * x]) = make_uint4(0u, 0u, 0u, 0u);
+      for (int i = lane; i < (BN - n) * (PITCH / 8); i += kWave)
+        *reinterpret_cast<uint4*>(&cV[n * PITCH + 8 * i]) = make_uint4(0u, 0u, 0u, 0u);
     }
     const int p = SHARED ? 0 : sPos[(head + col) % kNarrowRing];
     if (__ballot(col < n && (SHARED || (seen<SHARED>(a, p, lo) && seen<SHARED>(a, p, hi)))) != ~0ull) {
@@ -944,18 +962,54 @@ __global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
         const int i = 8 * q4 + 4 * half;
         int4 e = make_int4(0, 0, 0, 0);
         if (!SHARED) e = *reinterpret_cast<const int4*>(&sPos[(head + i) % kNarrowRing]);   // head: a multiple of 32
-        if (!(i < n && seen<SHARED>(a, e.x, rw.at))) s[0][4 * q4] = -INFINITY;
-        if (!(i + 1 < n && seen<SHARED>(a, e.y, rw.at))) s[0][4 * q4 + 1] = -INFINITY;
-        if (!(i + 2 < n && seen<SHARED>(a, e.z, rw.at))) s[0][4 * q4 + 2] = -INFINITY;
-        if (!(i + 3 < n && seen<SHARED>(a, e.w, rw.at))) s[0][4 * q4 + 3] = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          if (!(i < n && seen<SHARED>(a, e.x, at[c]))) s[c][0][4 * q4] = -INFINITY;
+          if (!(i + 1 < n && seen<SHARED>(a, e.y, at[c]))) s[c][0][4 * q4 + 1] = -INFINITY;
+          if (!(i + 2 < n && seen<SHARED>(a, e.z, at[c]))) s[c][0][4 * q4 + 2] = -INFINITY;
+          if (!(i + 3 < n && seen<SHARED>(a, e.w, at[c]))) s[c][0][4 * q4 + 3] = -INFINITY;
+        }
       }
     }
-    st.template add<1>(s, cV, tl, th, a.scale_log2);
+    bf16x8 pb[NC][2];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      st[c].template weigh<1>(s[c], a.scale_log2);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) pb[c][t] = pack8(s[c][0], 8 * t);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) {
+        const bf16x8 va = tr_operand<D, true>(cV, 16 * t, 32 * d, tl, th);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) st[c].acc[d] = mfma32(va, pb[c][t], st[c].acc[d]);
+      }
     head += BN;
     n = n1;
     b ^= 1;
   }
-  st.finish(a, un, rw, g, col, half);
+#pragma unroll
+  for (int c = 0; c < NC; ++c) st[c].finish(a, un, row_of<SHARED>(a, un, g, 32 * c + col), g, 32 * c + col, half);
+}
+
+template <int D, bool SHARED>
+__global__ void __launch_bounds__(64) rows_narrow_kernel(RowsArgs a) {
+  constexpr int TILE = NarrowSpace<D>::TILE;
+  __shared__ __attribute__((aligned(1024))) uint16_t sK[2 * TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t sV[2 * TILE];
+  __shared__ __attribute__((aligned(256))) int sTab[kNarrowPick];
+  __shared__ __attribute__((aligned(256))) int sSlot[kNarrowPick];
+  __shared__ __attribute__((aligned(16))) uint32_t sRow[kNarrowRing];
+  __shared__ __attribute__((aligned(16))) int sPos[SHARED ? 4 : kNarrowRing];
+  static_assert(kNarrowRing >= kNarrowPick + 2 * 32, "what is left of the last places, the tile in work, new ones");
+  const int widx = blockIdx.x / a.Hkv, g = blockIdx.x - widx * a.Hkv, last = a.waves[widx + 1];
+  for (int uidx = a.waves[widx]; uidx < last; ++uidx) {
+    const Unit un = a.units[a.max_units[0] + uidx];
+    const NarrowSpace<D> x{sK, sV, sTab, sSlot, sRow, sPos};
+    if (un.rows <= 32) narrow_unit<D, SHARED, 1>(a, un, g, x);
+    else if (D == 128) narrow_unit<D, SHARED, narrow_rows(D) / 32>(a, un, g, x);
   }
 }
 
@@ -1077,22 +1131,22 @@ struct RowsSpace {
 };
 static size_t stats_chunks(const PagedRows& p) { return ((size_t)p.max_blocks * p.block_size + kChunk - 1) / kChunk; }
 static bool plans_small(const PagedRows& p) { return p.S <= kPlanSmall && p.groups <= kPlanSmall; }
-// Row blocks of wide jobs: one for every 128 rows, and one more a job (of 33 rows at least; SHARED: groups, and sequences
-// by themselves if they have so many q-heads).  A job has no splits of fewer than kLeastTiles tiles; those of wide jobs
+// Row blocks of wide jobs: one for every 128 rows, and one more a job (SHARED: groups, and sequences by themselves if they
+// have so many q-heads).  A job has no splits of fewer than kLeastTiles tiles; those of wide jobs
 // add no more units than four rounds of them and than three times the row blocks (or one round).  Narrow jobs: a unit
 // each, and one more for every wave's end.  Partial rows: those of every job once and of the units that are added; for
 // new tokens only those of jobs of several units, so twice those of the added ones.
 static RowsSpace rows_space(const PagedRows& p) {
   RowsSpace x{};
   const long long G = p.Hq / p.Hkv, tokens = p.shared ? p.S : p.ntok, all = tokens * G;
-  const long long width = (long long)p.max_blocks * p.block_size, jobs = (p.shared ? (long long)p.groups : 0) + p.S;
-  const long long wide_jobs = std::min<long long>(p.shared ? p.groups : p.S, all / kNarrowRows) + (p.shared && G > kNarrowRows ? p.S : 0);
-  const long long blocks = all > kNarrowRows ? all / kWideRows + wide_jobs : 0, want = rows_want(p, true);
+  const long long narrow = narrow_rows(p.D), width = (long long)p.max_blocks * p.block_size, jobs = (p.shared ? (long long)p.groups : 0) + p.S;
+  const long long wide_jobs = std::min<long long>(p.shared ? p.groups : p.S, all / narrow) + (p.shared && G > narrow ? p.S : 0);
+  const long long blocks = all > narrow ? all / kWideRows + wide_jobs : 0, want = rows_want(p, true);
   const long long more = std::min(std::max(want, 3 * blocks), 4 * want);
   x.units[0] = std::min(blocks * ((width + 32 * kLeastTiles - 1) / (32 * kLeastTiles)), blocks + more);
-  x.waves = std::min<long long>(rows_want(p, false), jobs * ((width + kChunk * kLeastChunks - 1) / (kChunk * kLeastChunks)));
+  x.waves = std::min<long long>(rows_want(p, false), jobs * ((width + kChunk - 1) / kChunk + kStartChunks));
   x.units[1] = jobs + x.waves;
-  const long long added = std::min(more, x.units[0]) * kWideRows + x.waves * kNarrowRows;
+  const long long added = std::min(more, x.units[0]) * kWideRows + x.waves * narrow;
   x.part = (p.shared ? 2 * all + added : 2 * added) * p.Hkv;
   x.parts = 256;
   if (p.shared) {
@@ -1116,7 +1170,7 @@ bool paged_rows_fit(const PagedRows& p) {
   const RowsSpace x = rows_space(p);
   const long long rows = (long long)(p.shared ? p.S : p.ntok) * p.Hq;
   return std::max(x.units[0], x.units[1]) * p.Hkv <= 0x7fffffffll / 256 && x.part <= 0x7fffffffll && rows <= (1ll << 26) - 4 &&
-         ((long long)p.S + p.groups) * (long long)stats_chunks(p) <= 0x7fffffffll;
+         ((long long)p.S + p.groups) * ((long long)stats_chunks(p) + kStartChunks) <= 0x7fffffffll;
 }
 
 template <int D, bool SHARED>
@@ -1198,6 +1252,7 @@ hipError_t launch_paged_rows(const PagedRows& p) {
     a.want[k] = rows_want(p, k == 0);
   }
   a.max_waves = (int)x.waves;
+  a.narrow = narrow_rows(p.D);
   if (p.shared) return p.D == 128 ? launch_rows<128, true>(p, a) : launch_rows<64, true>(p, a);
   return p.D == 128 ? launch_rows<128, false>(p, a) : launch_rows<64, false>(p, a);
 }
