@@ -76,7 +76,11 @@ template <int D>
 constexpr int rows_bn() { return D == 128 ? 32 : 64; }   // keys of a tile of wide units
 constexpr int kLeastTiles = 4;    // of a wide unit, in 32-key tiles
 constexpr int kStartChunks = 2;   // what beginning a narrow job costs a wave (the latency of six reads), as chunks
-constexpr int kPlanSmall = 256;   // sequences, and groups, that one wave plans, in LDS
+constexpr int kPlanSmall = 256, kPlanGroups = 64;   // sequences and groups that one wave plans, in LDS
+// A group's rows are narrow jobs, by row blocks, up to this many: reading the prefix twice, from the caches, costs less than
+// a launch for wide units (40 sequences behind 114 entries, D = 64, 34 -> 26 us); four blocks of a long one more (64
+// sequences behind 16,384 144 -> 165).
+constexpr int kPrefixBlocks = 2;
 
 // What the plan weighs for wide units: with w tiles of work for each place on the chip the last unit ends about half the
 // longest unit behind w (and no unit before its own end), and 128 rows of partial results, written and read, cost as much
@@ -90,9 +94,10 @@ struct Unit {
   int s;          // sequence whose table is read; -1: no such unit
   int c0, c1;
   int split;      // k | n << 16
-  int rows;       // of the job
+  int rows;       // of the job (a group's narrow one: of its row block)
   int tok;        // first token of the job, or of its members' list
-  int row0;       // first row of the unit; | 1: token i of the job is list[tok + i], else tok + i
+  int row0;       // first row of the unit, counted from token `tok`; | 1: token i is list[tok + i], else tok + i; | 2: other
+                  // units read the same entries
   int part;       // first row of its partial results (KV head 0); -1: O and LSE are written
 };
 static_assert(sizeof(Unit) == 32, "two 16-byte loads");
@@ -126,7 +131,7 @@ struct RowsArgs {
   int* base;        // [groups] the first of them in `list` (more than kPlanSmall sequences or groups)
   int* jobs;        // [5][jobs] tiles, rows, first wide and narrow unit, first chunk (the same)
   Parts* own;       // [S] of each sequence
-  Parts* prefix;    // [groups] of each group
+  Parts* prefix;    // [groups][kPrefixBlocks] of each group's row blocks; the first one has all rows if they are wide
   Unit* units;      // [max_units[0] + max_units[1]]: wide, narrow
   int* waves;       // [max_waves + 1] first narrow unit of each wave
   float* part;      // [max_part][D]
@@ -139,7 +144,7 @@ struct RowsArgs {
 };
 
 struct Job {
-  int s, c0, c1, rows, tok, listed;
+  int s, c0, c1, rows, tok, row0;   // row0: with the flags of Unit
 };
 __device__ __forceinline__ int block_of(const RowsArgs& a, int place) { return a.shift >= 0 ? place >> a.shift : place / a.BS; }
 __device__ __forceinline__ bool is_wide(const RowsArgs& a, int rows) { return rows > a.narrow; }
@@ -197,14 +202,14 @@ __device__ __forceinline__ void chunk_stats(const RowsArgs& a, int first, int wa
 template <bool SHARED, bool SMALL>
 __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs a) {
   constexpr int NT = SMALL ? 512 : 1024, PT = SMALL ? kWave : NT;   // threads; those that plan
-  constexpr int CAP = SMALL ? kPlanSmall : 1, JOBS = SHARED ? 2 * CAP : CAP;
+  constexpr int CAP = SMALL ? kPlanSmall : 1, JOBS = SHARED && SMALL ? kPrefixBlocks * kPlanGroups + CAP : CAP;
   __shared__ int sJobs[5 * JOBS], sGroup[SHARED ? 6 * CAP : 1], sPart[JOBS];
   __shared__ Job sJob[JOBS];
   constexpr int NW = NT / kWave, TRIES = 16;
   __shared__ int buf[PT / kWave], sTop[PT / kWave], sTopWide, sUnits[2], sPer, sSize[TRIES];
   __shared__ long long sLeast, sWork, sChunks;
   __shared__ float sCost[TRIES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, J = SHARED ? a.groups + a.S : a.S;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, GJ = SHARED ? kPrefixBlocks * a.groups : 0, J = GJ + a.S;
   if (blockIdx.x > 0) {
     chunk_stats(a, (blockIdx.x - 1) * (NT / kWave) + wave, (gridDim.x - 1) * (NT / kWave));
     return;
@@ -235,16 +240,18 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   auto prefix_of = [&](int g) { return count[g] < 2 ? 0 : min(max(a.prefix_blocks[g], 0), blocks_of(list[base[g]])); };
   // job j: the groups first, then the sequences
   auto job_of = [&](int j) {
-    if (SHARED && j < a.groups) {
-      const int b = prefix_of(j);
-      if (b == 0) return Job{0, 0, 0, 0, 0, 1};
-      return Job{list[base[j]], 0, b * a.BS, count[j] * a.G, base[j], 1};
+    if (SHARED && j < GJ) {
+      const int g = j / kPrefixBlocks, rb = j % kPrefixBlocks, b = prefix_of(g), all = b ? count[g] * a.G : 0;
+      const bool wide = all > kPrefixBlocks * a.narrow;
+      const int r = wide ? (rb == 0 ? all : 0) : min(max(all - rb * a.narrow, 0), a.narrow);
+      if (r == 0) return Job{0, 0, rb == 0 ? b * a.BS : 0, 0, 0, 0};
+      return Job{list[base[g]], 0, b * a.BS, r, base[g], rb * a.narrow | 1 | (all > a.narrow ? 2 : 0)};
     }
-    const int s = SHARED ? j - a.groups : j, blocks = blocks_of(s);
+    const int s = j - GJ, blocks = blocks_of(s);
     if (SHARED) {
       const int g = group_of(s);
       int b = 0;
-      if ((unsigned)g < (unsigned)a.groups) b = min(SMALL ? sJob[g].c1 / a.BS : prefix_of(g), blocks);
+      if ((unsigned)g < (unsigned)a.groups) b = min(SMALL ? sJob[kPrefixBlocks * g].c1 / a.BS : prefix_of(g), blocks);
       return Job{s, b * a.BS, blocks * a.BS, a.G, s, 0};
     }
     const int t0 = min(max(a.cu[s], 0), a.ntok), t1 = min(max(a.cu[s + 1], t0), a.ntok);
@@ -307,11 +314,11 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
     long long least = 0, work = 0, chunks = 0;   // row blocks and tiles of all wide jobs; chunks of all narrow ones
     // the groups in turns of their own: the sequences' jobs begin where they end
     for (int j0 = 0; j0 < J; j0 += PT) {
-      const int ends = SHARED && j0 < a.groups ? min(a.groups, j0 + PT) : min(J, j0 + PT), j = j0 + tid;
+      const int ends = j0 < GJ ? min(GJ, j0 + PT) : min(J, j0 + PT), j = j0 + tid;
       const bool mine = j < ends;
       const Job x = mine ? job_of(j) : Job{0, 0, 0, 0, 0, 0};
       const bool wide = is_wide(a, x.rows);
-      int places = x.c1 - x.c0;
+      int places = x.rows ? x.c1 - x.c0 : 0;
       if (!SHARED && a.window > 0) places = (int)min((long long)places, (long long)a.window + a.sinks + x.rows / a.G);
       const int t = wide ? plan_tiles(places) : (int)(((unsigned)places + 31) / 32);
       if (mine) {
@@ -325,7 +332,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       const int m = job_chunks<SHARED>(a, t, x.rows), begin = m > 0 ? kStartChunks : 0;
       const long long c0 = block_scan<PT>(m + begin, chunks, buf) + begin;
       if (mine) chunk[j] = (int)min(c0, (long long)INT_MAX);
-      if (SHARED && j0 < a.groups) {
+      if (j0 < GJ) {
         j0 = ends - PT;
         sync();
       }
@@ -388,8 +395,8 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
         first[1][j] = (int)min(un, (long long)INT_MAX);
         const Parts parts = {(int)(pn * a.Hkv), r, SHARED || n > 1 ? n : 0};
         if (SMALL) sPart[j] = parts.part;
-        if (SHARED && j < a.groups) a.prefix[j] = parts;
-        else a.own[SHARED ? j - a.groups : j] = parts;
+        if (j < GJ) a.prefix[j] = parts;
+        else a.own[j - GJ] = parts;
       }
     }
     // offsets that overlap (only where cu_seqlens decreases) may ask for more than there is: nothing is computed then
@@ -421,13 +428,13 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       }
       const int j = search(first[k], u), i = u - first[k][j];
       const Job b = SMALL ? sJob[j] : job_of(j);
-      const int part = SMALL ? sPart[j] : SHARED && j < a.groups ? a.prefix[j].part : a.own[SHARED ? j - a.groups : j].part;
-      int c0 = b.c0, c1 = b.c1, sp, n, row0 = 0;
+      const int part = SMALL ? sPart[j] : j < GJ ? a.prefix[j].part : a.own[j - GJ].part;
+      int c0 = b.c0, c1 = b.c1, sp, n, row0 = b.row0;
       if (k == 0) {
         const int nb = row_blocks(b.rows);
         n = job_splits<SHARED>(a, tiles[j], b.rows, C, rC);
         sp = nb == 1 ? i : i / nb;
-        row0 = (nb - 1 - (i - sp * nb)) * kWideRows;   // the last rows see most: first
+        row0 |= (nb - 1 - (i - sp * nb)) * kWideRows;   // the last rows see most: first
       } else {
         const int m = job_chunks<SHARED>(a, tiles[j], b.rows), w = chunk[j] / per;
         n = (int)(((long long)chunk[j] + m - 1) / per) - w + 1;
@@ -439,7 +446,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
         c1 = (int)min((long long)c1, c0 + (x + per) * kChunk);
         c0 = (int)min((long long)c1, c0 + max(x, 0ll) * kChunk);
       }
-      out[u] = {b.s, c0, c1, split, b.rows, b.tok, row0 | b.listed, SHARED || n > 1 ? part + sp * a.Hkv * b.rows : -1};
+      out[u] = {b.s, c0, c1, split, b.rows, b.tok, row0, SHARED || n > 1 ? part + sp * a.Hkv * b.rows : -1};
     }
   }
   for (int w = tid; w <= a.max_waves; w += NT) {
@@ -464,13 +471,13 @@ struct RowLane {
   bool ok;
 };
 template <bool SHARED>
-__device__ __forceinline__ RowLane row_of(const RowsArgs& a, const Unit& un, int g, int row) {
-  const int r = min(row, un.rows - 1), i = r / a.G;   // lanes past the last row repeat it
+__device__ __forceinline__ RowLane row_of(const RowsArgs& a, const Unit& un, int g, int row, int last) {
+  const int r = min(row, last), i = r / a.G;   // lanes past the last row repeat it
   RowLane x;
   x.tok = un.row0 & 1 ? a.list[un.tok + i] : un.tok + i;
   x.h = g * a.G + r - i * a.G;
   x.at = SHARED ? INT_MAX - 1 : max(a.q_pos[x.tok], -1);
-  x.ok = row < un.rows;
+  x.ok = row <= last;
   return x;
 }
 template <bool SHARED>
@@ -627,12 +634,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
   if (un.s < 0) return;
   const auto rl = LY::row_lane(lane);
   const int tl = LY::tr_lo(lane), th = LY::tr_hi(lane);
-  const int row0 = (un.row0 & ~1) + 32 * wave, row = row0 + col;
+  const int row0 = (un.row0 & ~3) + 32 * wave, row = row0 + col;
   const bool wave_ok = row0 < un.rows;
   int at;   // this lane's row sees entries up to there
   bf16x8 qreg[KS];
   {
-    const RowLane rw = row_of<SHARED>(a, un, g, row);
+    const RowLane rw = row_of<SHARED>(a, un, g, row, un.rows - 1);
     at = rw.at;
     const uint16_t* qrow = a.q + ((size_t)rw.tok * a.Hq + rw.h) * D + 8 * half;
 #pragma unroll
@@ -648,7 +655,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 4; ++w)
-      if ((un.row0 & ~1) + 32 * w < un.rows) {
+      if ((un.row0 & ~3) + 32 * w < un.rows) {
         lo = min(lo, sMin[w]);
         hi = max(hi, sMax[w]);
       }
@@ -802,7 +809,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
       if (++t >= ntile) break;
     }
   }
-  st.finish(a, un, row_of<SHARED>(a, un, g, row), g, row, half);
+  st.finish(a, un, row_of<SHARED>(a, un, g, row, un.rows - 1), g, row, half);
 }
 
 // A narrow unit, 64 rows at most (D = 64: 32, where two columns' registers would leave half the waves a CU), is one wave, with its own tiles of 32 entries (double-buffered; D = 128: 40 KB of LDS,
@@ -837,10 +844,11 @@ __device__ __forceinline__ void narrow_unit(const RowsArgs& a, const Unit& un, i
   walk.init(un);
   RowState<D> st[NC];
   bf16x8 qreg[NC][KS];
+  const int row0 = un.row0 & ~3;
   int at[NC], lo = INT_MAX, hi = -1;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const RowLane rw = row_of<SHARED>(a, un, g, 32 * c + col);
+    const RowLane rw = row_of<SHARED>(a, un, g, row0 + 32 * c + col, row0 + un.rows - 1);
     at[c] = rw.at;
     const uint16_t* qrow = a.q + ((size_t)rw.tok * a.Hq + rw.h) * D + 8 * half;
 #pragma unroll
@@ -920,8 +928,13 @@ __device__ __forceinline__ void narrow_unit(const RowsArgs& a, const Unit& un, i
     for (int i = 0; i < NI; ++i)
       if (i * kWave + kWave <= SLOTS || prow[i] >= 0) {
         const size_t off = (size_t)r[i] * D + pcol[i];
-        dma_b128_global(a.kc + off, lds_addr(sK + b * TILE) + i * kWave * 16);
-        dma_b128_global(a.vc + off, lds_addr(sV + b * TILE) + i * kWave * 16);
+        if (SHARED && (un.row0 & 2)) {
+          dma_b128_cached(a.kc + off, lds_addr(sK + b * TILE) + i * kWave * 16);
+          dma_b128_cached(a.vc + off, lds_addr(sV + b * TILE) + i * kWave * 16);
+        } else {
+          dma_b128_global(a.kc + off, lds_addr(sK + b * TILE) + i * kWave * 16);
+          dma_b128_global(a.vc + off, lds_addr(sV + b * TILE) + i * kWave * 16);
+        }
       }
   };
 
@@ -991,7 +1004,8 @@ __device__ __forceinline__ void narrow_unit(const RowsArgs& a, const Unit& un, i
     b ^= 1;
   }
 #pragma unroll
-  for (int c = 0; c < NC; ++c) st[c].finish(a, un, row_of<SHARED>(a, un, g, 32 * c + col), g, 32 * c + col, half);
+  for (int c = 0; c < NC; ++c)
+    st[c].finish(a, un, row_of<SHARED>(a, un, g, row0 + 32 * c + col, row0 + un.rows - 1), g, 32 * c + col, half);
 }
 
 template <int D, bool SHARED>
@@ -1061,8 +1075,14 @@ __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
       set[0] = a.own[tok];
       const int grp = a.prefix_group[tok];
       if ((unsigned)grp < (unsigned)a.groups) {
-        set[1] = a.prefix[grp];
-        row[1] = (long long)a.rank[tok] * a.G;
+        int mine = a.rank[tok] * a.G + at - g * a.G;   // among the group's rows
+        set[1] = a.prefix[kPrefixBlocks * (long long)grp];
+        if (set[1].n > 0 && set[1].rows <= a.narrow) {
+          const int rb = mine / a.narrow;
+          set[1] = a.prefix[kPrefixBlocks * (long long)grp + rb];
+          mine -= rb * a.narrow;
+        }
+        row[1] = mine - (at - g * a.G);
       }
     }
 #pragma unroll
@@ -1130,7 +1150,7 @@ struct RowsSpace {
   size_t bytes() const { return parts + rank + list + count + base + jobs + own + prefix + unit + wave + stats + rows + ml; }
 };
 static size_t stats_chunks(const PagedRows& p) { return ((size_t)p.max_blocks * p.block_size + kChunk - 1) / kChunk; }
-static bool plans_small(const PagedRows& p) { return p.S <= kPlanSmall && p.groups <= kPlanSmall; }
+static bool plans_small(const PagedRows& p) { return p.S <= kPlanSmall && p.groups <= kPlanGroups; }
 // Row blocks of wide jobs: one for every 128 rows, and one more a job (SHARED: groups, and sequences by themselves if they
 // have so many q-heads).  A job has no splits of fewer than kLeastTiles tiles; those of wide jobs
 // add no more units than four rounds of them and than three times the row blocks (or one round).  Narrow jobs: a unit
@@ -1139,9 +1159,10 @@ static bool plans_small(const PagedRows& p) { return p.S <= kPlanSmall && p.grou
 static RowsSpace rows_space(const PagedRows& p) {
   RowsSpace x{};
   const long long G = p.Hq / p.Hkv, tokens = p.shared ? p.S : p.ntok, all = tokens * G;
-  const long long narrow = narrow_rows(p.D), width = (long long)p.max_blocks * p.block_size, jobs = (p.shared ? (long long)p.groups : 0) + p.S;
-  const long long wide_jobs = std::min<long long>(p.shared ? p.groups : p.S, all / narrow) + (p.shared && G > narrow ? p.S : 0);
-  const long long blocks = all > narrow ? all / kWideRows + wide_jobs : 0, want = rows_want(p, true);
+  const long long narrow = narrow_rows(p.D), width = (long long)p.max_blocks * p.block_size, jobs = (p.shared ? (long long)p.groups * kPrefixBlocks : 0) + p.S;
+  const long long most = p.shared ? kPrefixBlocks * narrow : narrow;   // rows of a narrow job, or of a group's
+  const long long wide_jobs = std::min<long long>(p.shared ? p.groups : p.S, all / most) + (p.shared && G > narrow ? p.S : 0);
+  const long long blocks = all > most || (p.shared && G > narrow) ? all / kWideRows + wide_jobs : 0, want = rows_want(p, true);
   const long long more = std::min(std::max(want, 3 * blocks), 4 * want);
   x.units[0] = std::min(blocks * ((width + 32 * kLeastTiles - 1) / (32 * kLeastTiles)), blocks + more);
   x.waves = std::min<long long>(rows_want(p, false), jobs * ((width + kChunk - 1) / kChunk + kStartChunks));
@@ -1151,11 +1172,11 @@ static RowsSpace rows_space(const PagedRows& p) {
   x.parts = 256;
   if (p.shared) {
     x.rank = x.list = round256((size_t)p.S * sizeof(int));
-    x.prefix = round256((size_t)p.groups * sizeof(Parts));
+    x.prefix = round256((size_t)p.groups * kPrefixBlocks * sizeof(Parts));
   }
   if (!plans_small(p)) {
     if (p.shared) x.count = x.base = round256((size_t)p.groups * sizeof(int));
-    x.jobs = round256(5 * ((size_t)p.S + p.groups) * sizeof(int));
+    x.jobs = round256(5 * (size_t)jobs * sizeof(int));
   }
   x.own = round256((size_t)p.S * sizeof(Parts));
   x.unit = round256((size_t)(x.units[0] + x.units[1]) * sizeof(Unit));
@@ -1170,7 +1191,7 @@ bool paged_rows_fit(const PagedRows& p) {
   const RowsSpace x = rows_space(p);
   const long long rows = (long long)(p.shared ? p.S : p.ntok) * p.Hq;
   return std::max(x.units[0], x.units[1]) * p.Hkv <= 0x7fffffffll / 256 && x.part <= 0x7fffffffll && rows <= (1ll << 26) - 4 &&
-         ((long long)p.S + p.groups) * ((long long)stats_chunks(p) + kStartChunks) <= 0x7fffffffll;
+         ((long long)p.S + kPrefixBlocks * (long long)p.groups) * ((long long)stats_chunks(p) + kStartChunks) <= 0x7fffffffll;
 }
 
 template <int D, bool SHARED>

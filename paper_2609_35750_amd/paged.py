@@ -377,6 +377,9 @@ def kvs_paged_extend(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, q_p
     return o, lse
 
 
+_SAVED_BYTES = 96 << 20   # of K and V, from which on decode() reads shared prefixes once
+
+
 class PagedKVCache:
     """Device pools of a streamed paged KV cache plus its native block manager.
 
@@ -389,7 +392,7 @@ class PagedKVCache:
     ``evict_lowest(keep)`` evicts the lowest.
 
     ``fork(src, dst)`` lets an empty sequence share the entries of another one,
-    whose common part ``decode`` then reads once for all; ``extend`` attends
+    whose common part ``decode`` reads once for all where that is faster; ``extend`` attends
     several new tokens a sequence.  ``copy(src, dst)`` gives a sequence entries
     of its own, ``compact()`` brings what evictions have left into fewer blocks.
     """
@@ -405,7 +408,9 @@ class PagedKVCache:
         self.slot_pos = torch.full((num_blocks * block_size,), -1, dtype=torch.int32, device=self.device)
         self.slot_weight = torch.zeros(num_blocks * block_size, dtype=torch.float32, device=self.device) if weights else None
         self._tables = None
+        self._blocks = 0      # in all tables, when they were uploaded
         self._shares = None   # groups of sequences that share a prefix, on the device; None: not known, (): none
+        self._saved = 0       # blocks the groups need not read again
 
     def append(self, seq: int, positions, k_new: torch.Tensor, v_new: torch.Tensor,
                weights: Optional[torch.Tensor] = None) -> np.ndarray:
@@ -521,14 +526,17 @@ class PagedKVCache:
             _check("kvs_bm_tables", lib.kvs_bm_tables(self.bm._h, p, p + 4 * n))
             dev = torch.from_numpy(both).to(self.device)
             self._tables = (dev[:n].view(self.num_seqs, self.max_blocks), dev[n:])
+            self._blocks = int(both[n:].sum())
         return self._tables
 
     def device_groups(self) -> Tuple[torch.Tensor, ...]:
         """(group of every sequence, leading blocks each group has in common); empty if no sequences share their first."""
         if self._shares is None:
             group, blocks = self.bm.groups()
-            self._shares = ()
+            self._shares, self._saved = (), 0
             if blocks.size:
+                members = np.bincount(group[group >= 0], minlength=blocks.size)
+                self._saved = int(((members - 1) * blocks.astype(np.int64)).sum())
                 both = torch.from_numpy(np.concatenate([group, blocks])).to(self.device)
                 self._shares = both[: group.size], both[group.size:]
         return self._shares
@@ -560,7 +568,12 @@ class PagedKVCache:
         table, nblk = self.device_tables()
         if window is None and not accumulate:
             shares = self.device_groups()
-            if shares:
+            # Reading a shared prefix once takes two or three launches more than reading it once a sequence, mostly from the
+            # caches.  32/8 heads, D = 128: 16 sequences behind 4,096 entries with 1,000 of their own 49 -> 36 us, 8 behind
+            # 4,096 with 500 26 -> 25; but 64 behind 1,024 with 1,000 67 -> 73, 8 behind 2,048 with 500 19 -> 23.
+            block_bytes = 4 * self.block_size * self.Hkv * self.D
+            pays = self._saved * block_bytes >= _SAVED_BYTES and 2 * self._saved >= self._blocks
+            if shares and (pays or q.shape[-2] > 32 * self.Hkv):   # groups of more than 32 q-heads: the plain call does not take them
                 return kvs_paged_decode_shared(q, self.k, self.v, self.slot_pos, table, nblk, *shares, softmax_scale, out, lse)
             with _on(self.k):
                 return kvs_paged_decode(q, self.k, self.v, self.slot_pos, table, nblk, softmax_scale, out, lse)

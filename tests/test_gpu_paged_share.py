@@ -77,13 +77,23 @@ class Rollouts:
             at += n
 
 
-def _grouped(pg, groups, alone, Hkv, D, bs, seed):
-    """groups: [(prefix, own entries of each member)]; alone: entries of sequences of their own.  Sequences are shuffled."""
+def _decode(pg, r, q, scale=None):
+    """The decode over shared prefixes, whatever the cache's own choice would be."""
+    c = r.cache
+    groups = c.device_groups()
+    if not groups:
+        groups = (torch.full((len(r.held),), -1, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV))
+    return pg.kvs_paged_decode_shared(q.to(DEV), c.k, c.v, c.slot_pos, *c.device_tables(), *groups, scale)
+
+
+def _grouped(pg, groups, alone, Hkv, D, bs, seed, room=0):
+    """groups: [(prefix, own entries of each member)]; alone: entries of sequences of their own.  Sequences are shuffled.
+    room: entries that any of them may take later."""
     S = sum(len(m) for _, m in groups) + len(alone)
     order = np.random.default_rng(seed).permutation(S).tolist()
     total = sum(p + sum(m) for p, m in groups) + sum(alone)
     longest = max([p + max(m) for p, m in groups] + alone)
-    r = Rollouts(pg, S, total // bs + 3 * S + 5, bs, longest // bs + 4, Hkv, D, seed)
+    r = Rollouts(pg, S, total // bs + (3 + room // bs) * S + 5, bs, (longest + room) // bs + 4, Hkv, D, seed)
     at = 0
     for p, own in groups:
         first = order[at]
@@ -110,6 +120,10 @@ DECODE = [
     ([(100, list(range(0, 40))), (17, [2, 3]), (300, [1, 1, 1])], [9], 20, 4, 128, 64),
     ([(2500, [10, 1300, 0])], [4000], 4, 4, 128, 16),           # one row a KV head and sequence; long runs
     ([(1025, [1023, 1024]), (1024, [1, 1025])], [1, 1023], 64, 1, 128, 16),
+    ([(333, [7] * 13)], [50], 16, 2, 128, 16),                  # two row blocks of one wave's units
+    ([(500, [40] * 9), (77, [1] * 11)], [], 20, 4, 64, 16),
+    ([(90, [3] * 150)], [], 12, 6, 64, 8),                      # 300 rows
+    ([(64, [2, 70]), (9, [1, 1, 5])], [300], 64, 1, 64, 16),    # 64 q-heads a KV head
 ]
 
 
@@ -121,14 +135,70 @@ def test_decode_over_shared_prefixes(pg, case):
     assert len(r.cache.device_groups()[1]) == len(groups)
     q = r.randn(len(r.held), Hq, D)
     scale = 1.0 / math.sqrt(D)
-    o, lse = r.cache.decode(q.to(DEV))
+    o, lse = _decode(pg, r, q)
     r.check_decode("shared", q, o, lse, scale)
+    o2, lse2 = r.cache.decode(q.to(DEV))          # by its own choice
+    r.check_decode("decode", q, o2, lse2, scale)
     # evictions: part of a shared block, a span of shared blocks, own entries; then the groups are others
     big = max(range(len(r.held)), key=lambda s: len(r.held[s]))
     have = sorted(r.held[big])
     r.evict(big, have[:1] + have[len(have) // 3: len(have) // 2])
-    o, lse = r.cache.decode(q.to(DEV), softmax_scale=0.3)
+    o, lse = _decode(pg, r, q, 0.3)
     r.check_decode("shared, evicted", q, o, lse, 0.3)
+
+
+def test_more_sequences_than_one_wave_plans(pg):
+    """300 sequences in 90 groups, and 300 with new tokens."""
+    announce("decode_shared and extend of 300 sequences")
+    rng = np.random.default_rng(2)
+    r = _grouped(pg, [(int(p), rng.integers(0, 30, 3).tolist()) for p in rng.integers(1, 60, 90)], rng.integers(0, 40, 30).tolist(),
+                 2, 64, 8, 77, room=40)
+    S = len(r.held)
+    assert S == 300
+    q = r.randn(S, 6, 64)
+    o, lse = _decode(pg, r, q)
+    r.check_decode("300 sequences", q, o, lse, 0.125)
+    new = rng.choice([0, 1, 2, 40], S, p=[0.2, 0.5, 0.2, 0.1]).tolist()
+    pos = []
+    for s, n in enumerate(new):
+        a = max(r.held[s], default=0) + 1
+        r.append(s, range(a, a + n))
+        pos += range(a, a + n)
+    q = r.randn(len(pos), 6, 64)
+    for window, sinks in ((None, 0), (20, 2)):
+        o, lse = r.cache.extend(q.to(DEV), pos, new, window=window, sinks=sinks)
+        r.check_extend("300 sequences", q, o, lse, 0.125, new, pos, window, sinks)
+
+
+@pytest.mark.parametrize("Hkv,D,G,members", [(8, 128, 4, 40), (4, 64, 8, 3)])
+def test_caches_beyond_4_gib(pg, Hkv, D, G, members):
+    """K and V of 4.3 GB each: entries in the first and the last slots, for units of one wave and of four."""
+    announce(f"decode_shared and extend in a large cache, {Hkv} {D}")
+    bs = 16
+    nb = (4300 << 20) // (bs * Hkv * D * 2)
+    k, v = (torch.empty(nb, Hkv, bs, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    slot_pos = torch.full((nb * bs,), -1, dtype=torch.int32, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    blocks = torch.tensor([0, nb - 1, 1, nb - 2, nb // 2, nb - 3, nb - 4, 7], dtype=torch.int32, device=DEV)
+    for x in (k, v):
+        x[blocks.long()] = torch.randn(8, Hkv, bs, D, generator=g, device=DEV).bfloat16()
+    slot_pos.view(nb, bs)[blocks.long()] = torch.arange(8 * bs, dtype=torch.int32, device=DEV).view(8, bs)
+    S = members
+    table = blocks.expand(S, 8).contiguous()
+    nblk = torch.full((S,), 8, dtype=torch.int32, device=DEV)
+    q = torch.randn(S, Hkv * G, D, generator=g, device=DEV).bfloat16()
+    flat = [x[blocks.long()].transpose(1, 2).reshape(8 * bs, Hkv, D) for x in (k, v)]
+    want = ref.attend(q, *flat, 1 / math.sqrt(D))
+    o, lse = pg.kvs_paged_decode_shared(q, k, v, slot_pos, table, nblk, torch.zeros(S, dtype=torch.int32, device=DEV),
+                                        torch.tensor([5], dtype=torch.int32, device=DEV))
+    ref.check("shared", o, lse, want)
+    one = torch.tensor([0, S], dtype=torch.int32, device=DEV)
+    o, lse = pg.kvs_paged_extend(q, k, v, slot_pos, table[:1].contiguous(), nblk[:1].contiguous(),
+                                 torch.full((S,), 1000, dtype=torch.int32, device=DEV), one)
+    ref.check("extend", o, lse, want)
+    src, dst = torch.arange(bs, dtype=torch.int32, device=DEV), (nb - 5) * bs + torch.arange(bs, dtype=torch.int32, device=DEV)
+    pg.kvs_paged_copy(src, dst, k, v, slot_pos)
+    assert torch.equal(k[nb - 5], k[0]) and torch.equal(v[nb - 5], v[0])
 
 
 def test_everything_is_shared_or_gone(pg):
@@ -140,11 +210,11 @@ def test_everything_is_shared_or_gone(pg):
         r.fork(2, s)
     r.append(5, range(3))
     q = r.randn(6, 4, 64)
-    o, lse = r.cache.decode(q.to(DEV))
+    o, lse = _decode(pg, r, q)
     r.check_decode("all shared", q, o, lse, 0.125)
     for s in (0, 2, 4):
         r.evict(s, sorted(r.held[s]))
-    o, lse = r.cache.decode(q.to(DEV))
+    o, lse = _decode(pg, r, q)
     assert torch.isneginf(lse[[0, 1, 2, 3, 4]]).all() and (o[[0, 1, 2, 3, 4]] == 0).all()
     r.check_decode("all gone", q, o, lse, 0.125)
 
@@ -159,7 +229,7 @@ def test_a_last_block_of_dead_slots_in_a_prefix(pg):
     r.fork(0, 1)
     r.fork(0, 2)
     q = r.randn(3, 8, 128)
-    o, lse = r.cache.decode(q.to(DEV))
+    o, lse = _decode(pg, r, q)
     r.check_decode("dead slots", q, o, lse, 1 / math.sqrt(128))
 
 
@@ -169,7 +239,7 @@ def test_large_and_equal_scores(pg):
     for amp in (0.0, 40.0):
         r = _grouped(pg, [(900, [30, 70, 200])], [], 2, 64, 16, 11)
         q = (r.randn(3, 4, 64).float() * amp).bfloat16()
-        o, lse = r.cache.decode(q.to(DEV))
+        o, lse = _decode(pg, r, q)
         r.check_decode(f"amplitude {amp}", q, o, lse, 0.125)
 
 
@@ -384,3 +454,134 @@ def test_empty_calls(pg):
     r = _grouped(pg, [(60, [20, 6])], [], 2, 64, 16, 41)
     o, lse = r.cache.extend(torch.zeros(0, 4, 64, dtype=torch.bfloat16, device=DEV), [], [0, 0])
     assert o.shape == (0, 4, 64) and lse.shape == (0, 4)
+
+
+@pytest.mark.parametrize("block", [1, 5, 16])
+def test_life_of_two_groups(pg, block):
+    """Rollouts of two prompts as an engine runs them: prompts, forks, chunks of observations, decode steps, spans evicted
+    by some of the members, compaction, branches, releases; every output against what each sequence holds."""
+    announce(f"life of two groups, block size {block}")
+    Hq, Hkv, D, S, seed = 8, 2, 128, 8, 60 + block
+    a = Rollouts(pg, S, 2000 // block + 60, block, 500 // block + 10, Hkv, D, seed)
+    rng = np.random.default_rng(seed)
+    scale = 1 / math.sqrt(D)
+    nxt = [0] * S
+
+    def chunk(lengths):
+        pos = []
+        for s, n in enumerate(lengths):
+            p = list(range(nxt[s], nxt[s] + n))
+            a.append(s, p)
+            pos += p
+            nxt[s] += n
+        if pos:
+            q = a.randn(len(pos), Hq, D)
+            for window, sinks in ((None, 0), (50, 4)):
+                o, lse = a.cache.extend(q.to(DEV), pos, lengths, window=window, sinks=sinks)
+                a.check_extend("chunk", q, o, lse, scale, lengths, pos, window, sinks)
+
+    def step():
+        for s in range(S):
+            if nxt[s]:
+                a.append(s, [nxt[s]])
+                nxt[s] += 1
+        q = a.randn(S, Hq, D)
+        o, lse = _decode(pg, a, q)
+        a.check_decode("step", q, o, lse, scale)
+        o2, lse2 = a.cache.decode(q.to(DEV))
+        a.check_decode("step, plain", q, o2, lse2, scale)
+        at = torch.tensor([max(n - 1, 0) for n in nxt], dtype=torch.int32, device=DEV)
+        o3, lse3 = a.cache.decode(q.to(DEV), positions=at, window=40, sinks=3)
+        for s in range(S):
+            p, k, v = a.kv(s)
+            see = ((int(at[s]) - p < 40) | (p < 3))[None]
+            ref.check("step, window", o3[s:s + 1], lse3[s:s + 1], ref.attend(q[s:s + 1], k, v, scale, see))
+
+    chunk([120, 0, 0, 0, 77, 0, 0, 0])
+    for s in (1, 2, 3):
+        a.fork(0, s)
+        nxt[s] = nxt[0]
+    for s in (5, 6):
+        a.fork(4, s)
+        nxt[s] = nxt[4]
+    step()
+    chunk([30, 1, 0, 64, 9, 33, 0, 0])
+    step()
+    a.evict(1, list(range(16, 48)))            # a span of the prompt, by one member
+    a.evict(3, list(range(5, 9)) + [60])
+    for s in (0, 4):
+        a.evict(s, rng.choice(sorted(a.held[s])[-25:], 10, replace=False).tolist())
+    step()
+    before = [dict(h) for h in a.held]
+    a.cache.compact()
+    assert a.held == before
+    step()
+    a.cache.copy(1, 7)
+    a.held[7], nxt[7] = dict(a.held[1]), nxt[1]
+    step()
+    a.cache.release(2)
+    a.held[2], nxt[2] = {}, 0
+    a.cache.release(4)
+    a.held[4], nxt[4] = {}, 0
+    step()
+    a.fork(5, 4)
+    nxt[4] = nxt[5]
+    chunk([5, 0, 0, 12, 40, 40, 1, 3])
+    for s in range(S):
+        a.cache.release(s)
+    assert a.cache.bm.free_blocks() == a.cache.num_blocks
+    assert (a.cache.slot_pos == -1).all()
+
+
+def test_copies_keep_weights(pg):
+    """A cache that keeps weights: copies take them along, compaction too, and the eviction by them goes on as before."""
+    announce("weights through copies and compaction")
+    Hkv, D, bs = 2, 64, 8
+    r = Rollouts(pg, 3, 60, bs, 30, Hkv, D, 71, weights=True)
+    r.append(0, range(100))
+    w = torch.rand(100)
+    table, n = r.cache.bm.tables()
+    slots = torch.from_numpy((table[0, :n[0], None] * bs + np.arange(bs)).reshape(-1)[:100]).long()
+    r.cache.slot_weight[slots.to(DEV)] = w.to(DEV)
+    r.cache.copy(0, 1)
+    r.held[1] = dict(r.held[0])
+    gone = np.random.default_rng(1).choice(100, 55, replace=False)
+    r.evict(0, gone)
+    r.evict(1, gone)
+    assert r.cache.compact(0) > 0
+    left = sorted(set(range(100)) - set(gone.tolist()))
+    for s in (0, 1):
+        table, n = r.cache.bm.tables()
+        slots = torch.from_numpy((table[s, :n[s], None] * bs + np.arange(bs)).reshape(-1)).long()
+        pos = r.cache.slot_pos.cpu()[slots]
+        assert sorted(pos[pos >= 0].tolist()) == left
+        assert torch.equal(r.cache.slot_weight.cpu()[slots][pos >= 0], w[pos[pos >= 0].long()])
+    out = r.cache.evict_lowest(20)
+    want = sorted(sorted(left, key=lambda p: float(w[p]))[: len(left) - 20])
+    assert sorted(out[0].tolist()) == want and sorted(out[1].tolist()) == want
+
+
+def test_two_streams_at_once(pg):
+    """Calls on two streams at the same time, each with a workspace of its own."""
+    announce("decode_shared and extend on two streams")
+    r = _grouped(pg, [(400, [50, 60, 5, 1])], [200], 2, 128, 16, 81)
+    table, nblk = r.cache.device_tables()
+    group, blocks = r.cache.device_groups()
+    args = (r.cache.k, r.cache.v, r.cache.slot_pos, table, nblk)
+    q = r.randn(5, 16, 128).to(DEV)
+    qe = r.randn(200, 16, 128).to(DEV)
+    cu = torch.tensor([0, 90, 90, 200, 200, 200], dtype=torch.int32, device=DEV)
+    pos = torch.full((200,), 1000, dtype=torch.int32, device=DEV)
+    want = [x.clone() for x in (*pg.kvs_paged_decode_shared(q, *args, group, blocks), *pg.kvs_paged_extend(qe, *args, pos, cu))]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        with torch.cuda.stream(streams[0]):
+            got[0].append(pg.kvs_paged_decode_shared(q, *args, group, blocks))
+        with torch.cuda.stream(streams[1]):
+            got[1].append(pg.kvs_paged_extend(qe, *args, pos, cu))
+    torch.cuda.synchronize()
+    for a, b in zip(*got):
+        for x, y in zip((*a, *b), want):
+            assert torch.equal(x, y)
