@@ -82,9 +82,7 @@ constexpr int kPlanSmall = 256, kPlanGroups = 64;   // sequences and groups that
 // sequences behind 16,384 144 -> 165).
 constexpr int kPrefixBlocks = 2;
 
-// What the plan weighs for wide units: with w tiles of work for each place on the chip the last unit ends about half the
-// longest unit behind w (and no unit before its own end), and 128 rows of partial results, written and read, cost as much
-// as these tiles.
+// What the plan weighs for wide units: 128 rows of partial results, written and read, cost as much as these tiles.
 constexpr float kSplitTiles = 40.f;
 constexpr int kChunk = 64;        // places of a table that are skipped or looked at together
 
@@ -94,7 +92,7 @@ struct Unit {
   int s;          // sequence whose table is read; -1: no such unit
   int c0, c1;
   int split;      // k | n << 16
-  int rows;       // of the job (a group's narrow one: of its row block)
+  int rows;       // of the job (a group's narrow one: of its row block; a cut one: of the row blocks that are cut)
   int tok;        // first token of the job, or of its members' list
   int row0;       // first row of the unit, counted from token `tok`; | 1: token i is list[tok + i], else tok + i; | 2: other
                   // units read the same entries
@@ -102,7 +100,7 @@ struct Unit {
 };
 static_assert(sizeof(Unit) == 32, "two 16-byte loads");
 
-// Partial results of a job: row r of KV head g and split k at part + (k Hkv + g) rows + r.
+// Partial results of a job, of its first `rows` rows: row r of KV head g and split k at part + (k Hkv + g) rows + r.
 struct Parts {
   int part, rows, n;   // n: splits; 0: no partial results
 };
@@ -129,7 +127,7 @@ struct RowsArgs {
   int* list;        // [S] members, group by group
   int* count;       // [groups] members, and
   int* base;        // [groups] the first of them in `list` (more than kPlanSmall sequences or groups)
-  int* jobs;        // [5][jobs] tiles, rows, first wide and narrow unit, first chunk (the same)
+  int* jobs;        // [6][jobs] tiles, rows, first wide and narrow unit, first chunk, first row block (the same)
   Parts* own;       // [S] of each sequence
   Parts* prefix;    // [groups][kPrefixBlocks] of each group's row blocks; the first one has all rows if they are wide
   Unit* units;      // [max_units[0] + max_units[1]]: wide, narrow
@@ -203,10 +201,10 @@ template <bool SHARED, bool SMALL>
 __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs a) {
   constexpr int NT = SMALL ? 512 : 1024, PT = SMALL ? kWave : NT;   // threads; those that plan
   constexpr int CAP = SMALL ? kPlanSmall : 1, JOBS = SHARED && SMALL ? kPrefixBlocks * kPlanGroups + CAP : CAP;
-  __shared__ int sJobs[5 * JOBS], sGroup[SHARED ? 6 * CAP : 1], sPart[JOBS];
+  __shared__ int sJobs[6 * JOBS], sGroup[SHARED ? 6 * CAP : 1], sPart[JOBS];
   __shared__ Job sJob[JOBS];
-  constexpr int NW = NT / kWave, TRIES = 16;
-  __shared__ int buf[PT / kWave], sTop[PT / kWave], sTopWide, sUnits[2], sPer, sSize[TRIES];
+  constexpr int NW = NT / kWave, TRIES = SHARED ? 16 : 24;
+  __shared__ int buf[PT / kWave], sTop[PT / kWave], sTopWide, sUnits[2], sSize[TRIES], sWhole[TRIES];
   __shared__ long long sLeast, sWork, sChunks;
   __shared__ float sCost[TRIES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, GJ = SHARED ? kPrefixBlocks * a.groups : 0, J = GJ + a.S;
@@ -220,6 +218,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   int* first[2] = {SMALL ? sJobs + 2 * JOBS : a.jobs + 2 * J, SMALL ? sJobs + 3 * JOBS : a.jobs + 3 * J};
   // where each narrow job's first chunk lies among all that is dealt
   int* chunk = SMALL ? sJobs + 4 * JOBS : a.jobs + 4 * J;
+  int* block = SMALL ? sJobs + 5 * JOBS : a.jobs + 5 * J;   // row blocks of the wide jobs in front of each
   int* count = SMALL ? sGroup : a.count;
   int* base = SMALL ? sGroup + CAP : a.base;
   int* rank = SMALL ? sGroup + 2 * CAP : a.rank;
@@ -327,11 +326,14 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
         if (SMALL) sJob[j] = x;
       }
       top = max(top, wide ? t : 0);
-      block_scan<PT>(wide ? row_blocks(x.rows) : 0, least, buf);
+      const long long rb0 = block_scan<PT>(wide ? row_blocks(x.rows) : 0, least, buf);
       block_scan<PT>(wide ? (int)min((long long)row_blocks(x.rows) * t, 1ll << 24) : 0, work, buf);
       const int m = job_chunks<SHARED>(a, t, x.rows), begin = m > 0 ? kStartChunks : 0;
       const long long c0 = block_scan<PT>(m + begin, chunks, buf) + begin;
-      if (mine) chunk[j] = (int)min(c0, (long long)INT_MAX);
+      if (mine) {
+        chunk[j] = (int)min(c0, (long long)INT_MAX);
+        block[j] = (int)min(rb0, (long long)INT_MAX);
+      }
       if (j0 < GJ) {
         j0 = ends - PT;
         sync();
@@ -349,25 +351,39 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
     }
   }
   __syncthreads();
-  // The size of the wide jobs' runs: the whole of the longest one, which always fits, or a part of it, by their cost; a
-  // wave a size at a time.
-  int C = sTopWide;
+  // How wide jobs are cut, in tiles of the time that a place on the chip has: all of them into runs of one size, the whole
+  // of the longest, which always fits, or a part of it; or, for new tokens, the row blocks that fill whole rounds left
+  // whole and those behind them cut, so that few rows have partial results and yet the last round is short.  The last
+  // units end about half a unit behind the work's share, and no unit before its own end.  A wave a cut at a time.
+  int C = sTopWide, whole = 0;   // row blocks left whole
+  // of a wide job: its row blocks that are cut (the first ones: a causal row block's last rows see most), and into how many
+  auto cut_of = [&](int j, int c, float rc, int front, int& n) {
+    const int r = rows[j], nb = is_wide(a, r) ? row_blocks(r) : 0, b = nb - min(max(front - block[j], 0), nb);
+    n = b ? job_splits<SHARED>(a, tiles[j], r, c, rc) : 0;
+    return b;
+  };
   if (sLeast > 0) {
+    const long long rounds = sLeast / a.want[0];
     for (int i = wave; i < TRIES; i += NW) {
-      const int n = i < 4 ? i + 1 : i & 1 ? 4 << ((i - 3) >> 1) : 6 << ((i - 4) >> 1);   // 1 .. 4, 6, 8, 12, 16, 24, ...
-      const int c = (sTopWide + n - 1) / n;
-      const float rc = __builtin_amdgcn_rcpf((float)c), place = 1.f / (float)a.want[0];
-      long long units = 0, split = 0;   // split: rows of partial results
+      const int k = i < 16 ? i : i - 15;
+      const int n = k < 4 ? k + 1 : k & 1 ? 4 << ((k - 3) >> 1) : 6 << ((k - 4) >> 1);   // 1 .. 4, 6, 8, 12, 16, 24, ...
+      const int c = (sTopWide + n - 1) / n, front = i < 16 ? 0 : (int)min(rounds * a.want[0], (long long)INT_MAX);
+      const float rc = __builtin_amdgcn_rcpf((float)c), place = 1.f / (float)a.want[0], work = (float)sWork * place;
+      long long units = 0, split = 0;   // behind those left whole; rows of partial results
       for (int j0 = 0; j0 < J; j0 += kWave) {
-        const int j = j0 + lane, r = j < J ? rows[j] : 0, m = j < J ? job_splits<SHARED>(a, tiles[j], r, c, rc) : 0;
-        units += wave_last(wave_scan((int)min((long long)m * row_blocks(r), 1ll << 24)));   // more than there may be at any rate
-        split += wave_last(wave_scan(m > 1 ? (int)min((long long)m * r, 1ll << 24) : 0));
+        const int j = j0 + lane;
+        int m = 0;
+        const int b = j < J ? cut_of(j, c, rc, front, m) : 0;
+        units += wave_last(wave_scan((int)min((long long)m * b, 1ll << 24)));   // more than there may be at any rate
+        split += wave_last(wave_scan(m > 1 ? (int)min((long long)m * min(rows[j], b * kWideRows), 1ll << 24) : 0));
       }
       if (lane == 0) {
+        const float ends = fmaxf(front ? (float)sTopWide : (float)c, work + 0.5f * (float)c);
         sSize[i] = c;
-        sCost[i] = (n > 1 && c < kLeastTiles) || units > a.max_units[0]
+        sWhole[i] = front;
+        sCost[i] = (n > 1 && c < kLeastTiles) || front + units > a.max_units[0] || (i >= 16 && (rounds == 0 || front == sLeast))
                        ? INFINITY
-                       : fmaxf((float)c, (float)sWork * place + 0.5f * (float)c) + (float)split * (kSplitTiles / kWideRows) * place;
+                       : ends + (float)split * (kSplitTiles / kWideRows) * place;
       }
     }
     __syncthreads();
@@ -376,6 +392,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       if (sCost[i] < best) {
         best = sCost[i];
         C = sSize[i];
+        whole = sWhole[i];
       }
   }
   const float rC = __builtin_amdgcn_rcpf((float)C);
@@ -385,15 +402,17 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
     long long units0[2] = {0, 0}, part0 = 0;
     for (int j0 = 0; j0 < J; j0 += PT) {
       const int j = j0 + tid, r = j < J ? rows[j] : 0, t = j < J ? tiles[j] : 0, m = job_chunks<SHARED>(a, t, r);
-      const int nw = job_splits<SHARED>(a, t, r, C, rC);
+      int nw = 0;
+      const int b = j < J ? cut_of(j, C, rC, whole, nw) : 0, nb = is_wide(a, r) ? row_blocks(r) : 0;
       const int nn = m > 0 ? (int)(((long long)chunk[j] + m - 1) / per) - chunk[j] / per + 1 : 0, n = nw + nn;
-      const long long uw = block_scan<PT>(nw * row_blocks(r), units0[0], buf);
+      const int cut_rows = nb ? min(r, b * kWideRows) : r;
+      const long long uw = block_scan<PT>(nb - b + nw * b, units0[0], buf);
       const long long un = block_scan<PT>(nn, units0[1], buf);
-      const long long pn = block_scan<PT>(SHARED || n > 1 ? n * r : 0, part0, buf);
+      const long long pn = block_scan<PT>(SHARED || n > 1 ? n * cut_rows : 0, part0, buf);
       if (j < J) {
         first[0][j] = (int)min(uw, (long long)INT_MAX);
         first[1][j] = (int)min(un, (long long)INT_MAX);
-        const Parts parts = {(int)(pn * a.Hkv), r, SHARED || n > 1 ? n : 0};
+        const Parts parts = {(int)(pn * a.Hkv), cut_rows, SHARED || n > 1 ? n : 0};
         if (SMALL) sPart[j] = parts.part;
         if (j < GJ) a.prefix[j] = parts;
         else a.own[j - GJ] = parts;
@@ -403,10 +422,8 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
     const bool fit = units0[0] <= a.max_units[0] && units0[1] <= a.max_units[1] && part0 * a.Hkv <= a.max_part;
     if (tid == 0) {
       a.parts[0] = fit && part0 > 0;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        sUnits[k] = fit ? (int)units0[k] : 0;
-      }
+      sUnits[0] = fit ? (int)units0[0] : 0;
+      sUnits[1] = fit ? (int)units0[1] : 0;
     }
   }
   __syncthreads();
@@ -429,12 +446,17 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       const int j = search(first[k], u), i = u - first[k][j];
       const Job b = SMALL ? sJob[j] : job_of(j);
       const int part = SMALL ? sPart[j] : j < GJ ? a.prefix[j].part : a.own[j - GJ].part;
-      int c0 = b.c0, c1 = b.c1, sp, n, row0 = b.row0;
-      if (k == 0) {
-        const int nb = row_blocks(b.rows);
-        n = job_splits<SHARED>(a, tiles[j], b.rows, C, rC);
-        sp = nb == 1 ? i : i / nb;
-        row0 |= (nb - 1 - (i - sp * nb)) * kWideRows;   // the last rows see most: first
+      int c0 = b.c0, c1 = b.c1, sp = 0, n, row0 = b.row0, job_rows = b.rows;
+      if (k == 0) {   // the last rows first: they see most
+        const int nb = row_blocks(b.rows), cut = cut_of(j, C, rC, whole, n), x = i - (nb - cut);
+        if (x < 0) {
+          n = 1;
+          row0 |= (nb - 1 - i) * kWideRows;
+        } else {
+          sp = cut == 1 ? x : x / cut;
+          row0 |= (cut - 1 - (x - sp * cut)) * kWideRows;
+          job_rows = min(job_rows, cut * kWideRows);
+        }
       } else {
         const int m = job_chunks<SHARED>(a, tiles[j], b.rows), w = chunk[j] / per;
         n = (int)(((long long)chunk[j] + m - 1) / per) - w + 1;
@@ -446,7 +468,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
         c1 = (int)min((long long)c1, c0 + (x + per) * kChunk);
         c0 = (int)min((long long)c1, c0 + max(x, 0ll) * kChunk);
       }
-      out[u] = {b.s, c0, c1, split, b.rows, b.tok, row0, SHARED || n > 1 ? part + sp * a.Hkv * b.rows : -1};
+      out[u] = {b.s, c0, c1, split, job_rows, b.tok, row0, SHARED || n > 1 ? part + sp * a.Hkv * job_rows : -1};
     }
   }
   for (int w = tid; w <= a.max_waves; w += NT) {
@@ -1062,6 +1084,7 @@ __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
     const int tok = (int)(i / per_tok), at = (int)(i - (long long)tok * per_tok), g = BLOCK ? at / a.G : at;
     Parts set[2] = {};
     long long row[2] = {};   // of the first q-head of the KV head
+    int first = 0;
     if (!SHARED) {   // the sequence of the token: the last one that begins at or before it
       int s = 0;
       for (int step = 1 << (31 - __builtin_clz(a.S)); step > 0; step >>= 1)
@@ -1069,8 +1092,9 @@ __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
       const int t0 = min(max(a.cu[s], 0), a.ntok), t1 = min(max(a.cu[s + 1], t0), a.ntok);
       if (tok < t0 || tok >= t1) continue;
       set[0] = a.own[s];
-      if (set[0].n == 0) continue;   // written by its unit
-      row[0] = (long long)(tok - t0) * a.G;
+      first = (tok - t0) * a.G;
+      if (set[0].n == 0 || first >= set[0].rows) continue;   // written by its unit
+      row[0] = first;
     } else {
       set[0] = a.own[tok];
       const int grp = a.prefix_group[tok];
@@ -1089,6 +1113,7 @@ __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
     for (int k = 0; k < 2; ++k) row[k] += set[k].part + (long long)g * set[k].rows;
     const int n = set[0].n + set[1].n;
     for (int r = BLOCK ? at - g * a.G : sub; r < a.G; r += BLOCK ? a.G : PER) {
+      if (!SHARED && first + r >= set[0].rows) continue;
       auto where = [&](int p) {
         return r + (p < set[0].n ? row[0] + (long long)p * a.Hkv * set[0].rows
                                  : row[1] + (long long)(p - set[0].n) * a.Hkv * set[1].rows);
@@ -1176,7 +1201,7 @@ static RowsSpace rows_space(const PagedRows& p) {
   }
   if (!plans_small(p)) {
     if (p.shared) x.count = x.base = round256((size_t)p.groups * sizeof(int));
-    x.jobs = round256(5 * (size_t)jobs * sizeof(int));
+    x.jobs = round256(6 * (size_t)jobs * sizeof(int));
   }
   x.own = round256((size_t)p.S * sizeof(Parts));
   x.unit = round256((size_t)(x.units[0] + x.units[1]) * sizeof(Unit));
