@@ -201,7 +201,7 @@ template <bool SHARED, bool SMALL>
 __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs a) {
   constexpr int NT = SMALL ? 512 : 1024, PT = SMALL ? kWave : NT;   // threads; those that plan
   constexpr int CAP = SMALL ? kPlanSmall : 1, JOBS = SHARED && SMALL ? kPrefixBlocks * kPlanGroups + CAP : CAP;
-  __shared__ int sJobs[6 * JOBS], sGroup[SHARED ? 6 * CAP : 1], sPart[JOBS];
+  __shared__ int sJobs[6 * JOBS], sGroup[SHARED ? 6 * CAP + kPlanGroups : 1], sPart[JOBS], sSplits[JOBS];
   __shared__ Job sJob[JOBS];
   constexpr int NW = NT / kWave, TRIES = SHARED ? 16 : 24;
   __shared__ int buf[PT / kWave], sTop[PT / kWave], sTopWide, sUnits[2], sSize[TRIES], sWhole[TRIES];
@@ -225,9 +225,10 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   int* list = SMALL ? sGroup + 3 * CAP : a.list;
   int* sBlocks = sGroup + 4 * CAP;   // SMALL: a sequence's blocks and group, read once
   int* sOf = sGroup + 5 * CAP;
+  int* sCommon = sGroup + 6 * CAP;   // SMALL: prefix_blocks
   auto sync = [&]() {
-    if (SMALL) {
-      __threadfence_block();
+    if (SMALL) {   // one wave, whose accesses to LDS take place in order
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     } else {
       __syncthreads();
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   auto blocks_of = [&](int s) { return SMALL && SHARED ? sBlocks[s] : min(max(a.nblk[s], 0), a.max_blocks); };
   auto group_of = [&](int s) { return SMALL ? sOf[s] : a.prefix_group[s]; };
   // blocks of group g's prefix
-  auto prefix_of = [&](int g) { return count[g] < 2 ? 0 : min(max(a.prefix_blocks[g], 0), blocks_of(list[base[g]])); };
+  auto prefix_of = [&](int g) { return count[g] < 2 ? 0 : min(max(SMALL ? sCommon[g] : a.prefix_blocks[g], 0), blocks_of(list[base[g]])); };
   // job j: the groups first, then the sequences
   auto job_of = [&](int j) {
     if (SHARED && j < GJ) {
@@ -262,6 +263,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       if (SMALL) {
         constexpr int N = SMALL ? CAP / PT : 1;
         int nb[N], gr[N];   // all reads at once
+        const int common = tid < a.groups ? a.prefix_blocks[tid] : 0;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
           nb[k] = k * PT + tid < a.S ? a.nblk[k * PT + tid] : 0;
@@ -272,6 +274,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
           sBlocks[k * PT + tid] = min(max(nb[k], 0), a.max_blocks);
           sOf[k * PT + tid] = gr[k];
         }
+        sCommon[tid] = common;
       }
       sync();
       if (wave == 0)   // ranks in the sequences' order: 64 of them at a time, group by group of those among them
@@ -284,7 +287,8 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
             const int before = count[g1];
             if (g == g1) rank[s] = before + __builtin_popcountll(same & ((1ull << lane) - 1ull));
             if (lane == 0) count[g1] = before + __builtin_popcountll(same);
-            __threadfence_block();
+            if (SMALL) sync();
+            else __threadfence_block();
             todo &= ~same;
           }
         }
@@ -299,12 +303,8 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       for (int s = tid; s < a.S; s += PT) {
         const int g = group_of(s);
         if ((unsigned)g < (unsigned)a.groups) {
-          const int r = rank[s], i = base[g] + r;
+          const int i = base[g] + rank[s];
           list[i] = s;
-          if (SMALL) {
-            a.list[i] = s;
-            a.rank[s] = r;
-          }
         }
       }
       sync();
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   };
   if (sLeast > 0) {
     const long long rounds = sLeast / a.want[0];
-    for (int i = wave; i < TRIES; i += NW) {
+    for (int i = wave; i < (rounds > 0 ? TRIES : 16); i += NW) {
       const int k = i < 16 ? i : i - 15;
       const int n = k < 4 ? k + 1 : k & 1 ? 4 << ((k - 3) >> 1) : 6 << ((k - 4) >> 1);   // 1 .. 4, 6, 8, 12, 16, 24, ...
       const int c = (sTopWide + n - 1) / n, front = i < 16 ? 0 : (int)min(rounds * a.want[0], (long long)INT_MAX);
@@ -381,14 +381,14 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
         const float ends = fmaxf(front ? (float)sTopWide : (float)c, work + 0.5f * (float)c);
         sSize[i] = c;
         sWhole[i] = front;
-        sCost[i] = (n > 1 && c < kLeastTiles) || front + units > a.max_units[0] || (i >= 16 && (rounds == 0 || front == sLeast))
+        sCost[i] = (n > 1 && c < kLeastTiles) || front + units > a.max_units[0] || (i >= 16 && front == sLeast)
                        ? INFINITY
                        : ends + (float)split * (kSplitTiles / kWideRows) * place;
       }
     }
     __syncthreads();
     float best = INFINITY;
-    for (int i = 0; i < TRIES; ++i)
+    for (int i = 0; i < (rounds > 0 ? TRIES : 16); ++i)
       if (sCost[i] < best) {
         best = sCost[i];
         C = sSize[i];
@@ -413,9 +413,12 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
         first[0][j] = (int)min(uw, (long long)INT_MAX);
         first[1][j] = (int)min(un, (long long)INT_MAX);
         const Parts parts = {(int)(pn * a.Hkv), cut_rows, SHARED || n > 1 ? n : 0};
-        if (SMALL) sPart[j] = parts.part;
-        if (j < GJ) a.prefix[j] = parts;
-        else a.own[j - GJ] = parts;
+        if (SMALL) {   // stored below
+          sPart[j] = parts.part;
+          sSplits[j] = parts.n;
+        } else {
+          (j < GJ ? a.prefix[j] : a.own[j - GJ]) = parts;
+        }
       }
     }
     // offsets that overlap (only where cu_seqlens decreases) may ask for more than there is: nothing is computed then
@@ -427,6 +430,20 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
     }
   }
   __syncthreads();
+  if (SMALL) {   // what the merge reads
+    for (int j = tid; j < J; j += NT) {
+      int n;
+      const int b = cut_of(j, C, rC, whole, n), r = rows[j];
+      (j < GJ ? a.prefix[j] : a.own[j - GJ]) = {sPart[j], is_wide(a, r) ? min(r, b * kWideRows) : r, sSplits[j]};
+    }
+    for (int s = tid; SHARED && s < a.S; s += NT) {
+      const int g = group_of(s);
+      if ((unsigned)g < (unsigned)a.groups) {
+        a.list[base[g] + rank[s]] = s;
+        a.rank[s] = rank[s];
+      }
+    }
+  }
   // the last job that begins at or before x: those without one of these begin where the next one does
   auto search = [&](const int* begin, int x) {
     int j = 0;
