@@ -66,10 +66,10 @@ hipError_t launch_paged_copy(const PagedCopy& p) {
 }
 
 // ---------------------------------------------------------------- the plan
-// Jobs of more than 64 rows (D = 64: 32) have units of 128 rows, four waves that share a tile of keys and values, and are cut into
-// equal runs; smaller ones have units of one wave.  Those are bound by HBM, so what counts is that all waves end together:
-// the smaller jobs' chunks, one job's behind the other's, are dealt to the waves in equal parts, and a wave whose part
-// spans jobs has a unit in each of them.  The two kinds run one after the other, each so that it fills the chip.
+// Jobs of more than 64 rows (D = 64: 32) have units of 128 rows, four waves that share a tile of keys and values, and are
+// cut into equal runs; smaller ones have units of one wave.  Those are bound by HBM, so what counts is that all waves end
+// together: the smaller jobs' chunks, one job's behind the other's, are dealt to the waves in equal parts, and a wave whose
+// part spans jobs has a unit in each of them.  The two kinds run one after the other, each so that it fills the chip.
 constexpr int kWideRows = 128;
 constexpr int narrow_rows(int D) { return D == 128 ? 64 : 32; }   // most rows of a narrow job
 template <int D>
@@ -136,7 +136,7 @@ struct RowsArgs {
   float2* part_ml;  // [max_part]: m (log2 units), l
   int* parts;       // [1] whether there are partial rows
   int2* stats;      // [S][ceil(max_blocks BS / kChunk)] least and greatest position in each chunk of a table (window > 0)
-  long long max_part;
+  long long max_part, max_split;   // rows of partial results; of those of wide jobs cut into several units
   int max_units[2], max_waves;
   int want[2];      // wide units, and waves of narrow ones, per KV head that fill the chip
 };
@@ -237,7 +237,9 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   auto blocks_of = [&](int s) { return SMALL && SHARED ? sBlocks[s] : min(max(a.nblk[s], 0), a.max_blocks); };
   auto group_of = [&](int s) { return SMALL ? sOf[s] : a.prefix_group[s]; };
   // blocks of group g's prefix
-  auto prefix_of = [&](int g) { return count[g] < 2 ? 0 : min(max(SMALL ? sCommon[g] : a.prefix_blocks[g], 0), blocks_of(list[base[g]])); };
+  auto prefix_of = [&](int g) {
+    return count[g] < 2 ? 0 : min(max(SMALL ? sCommon[g] : a.prefix_blocks[g], 0), blocks_of(list[base[g]]));
+  };
   // job j: the groups first, then the sequences
   auto job_of = [&](int j) {
     if (SHARED && j < GJ) {
@@ -381,7 +383,8 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
         const float ends = fmaxf(front ? (float)sTopWide : (float)c, work + 0.5f * (float)c);
         sSize[i] = c;
         sWhole[i] = front;
-        sCost[i] = (n > 1 && c < kLeastTiles) || front + units > a.max_units[0] || (i >= 16 && front == sLeast)
+        const bool fits = front + units <= a.max_units[0] && split <= a.max_split;
+        sCost[i] = !fits || (n > 1 && c < kLeastTiles) || (i >= 16 && front == sLeast)
                        ? INFINITY
                        : ends + (float)split * (kSplitTiles / kWideRows) * place;
       }
@@ -515,7 +518,7 @@ __device__ __forceinline__ RowLane row_of(const RowsArgs& a, const Unit& un, int
   RowLane x;
   x.tok = un.row0 & 1 ? a.list[un.tok + i] : un.tok + i;
   x.h = g * a.G + r - i * a.G;
-  x.at = SHARED ? INT_MAX - 1 : max(a.q_pos[x.tok], -1);
+  x.at = SHARED ? INT_MAX - 1 : min(max(a.q_pos[x.tok], -1), INT_MAX - 1);   // INT_MAX is nobody's
   x.ok = row <= last;
   return x;
 }
@@ -644,14 +647,11 @@ struct RowState {
 
 constexpr int kWidePick = 512;   // places of the table that a wide unit looks at together (more, and its loop spills registers)
 
-// A wide unit walks its chunks of the table 512 places at a time: the slots that some
-// row of it sees go to a list in LDS (two dependent reads, for all places at
-// once), and the keys and values of the listed slots are gathered tile by tile,
-// double-buffered, each tile read by the four waves.  Scores are S^T = K Q^T
-// (keys on M, rows on N), so that a lane holds 16 scores of one row; softmax and
-// the products with V as in the forward of the eviction mask.  New tokens, whose
-// row blocks are many, have three workgroups a CU and two tiles; the few row
-// blocks of shared prefixes, bound by a tile's latency, two workgroups and three.
+// A wide unit walks its chunks of the table 512 places at a time: the slots that some row of it sees go to a list in LDS
+// (two dependent reads, for all places at once), and the keys and values of the listed slots are gathered tile by tile,
+// double-buffered, each tile read by the four waves.  Scores are S^T = K Q^T (keys on M, rows on N), so that a lane holds 16
+// scores of one row; softmax and the products with V as in the forward of the eviction mask.  Three workgroups a CU, whose
+// registers just do without spills.
 // FAR: caches of 4 GiB or more, whose rows need 64-bit addresses of their own; else a copy takes one addition.
 template <int D, bool SHARED, bool FAR>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) rows_wide_kernel(RowsArgs a) {
@@ -663,11 +663,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
   __shared__ __attribute__((aligned(1024))) uint16_t sK1[TILE];
   __shared__ __attribute__((aligned(1024))) uint16_t sV0[TILE];
   __shared__ __attribute__((aligned(1024))) uint16_t sV1[TILE];
-  __shared__ __attribute__((aligned(16))) uint32_t sRow[PICK];   // rows [block][KV head][row] of the listed slots (not FAR: in bytes)
-  __shared__ __attribute__((aligned(16))) int sPos[PICK];        // and their positions; INT_MAX: nothing there
+  // rows [block][KV head][row] of the listed slots (not FAR: in bytes), and their positions; INT_MAX: nothing there
+  __shared__ __attribute__((aligned(16))) uint32_t sRow[PICK];
+  __shared__ __attribute__((aligned(16))) int sPos[PICK];
   __shared__ int sCnt[LOOK * 4], sAll[4], sMin[4], sMax[4];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int uidx = blockIdx.x / a.Hkv, g = blockIdx.x - uidx * a.Hkv;
   const Unit un = a.units[uidx];
   if (un.s < 0) return;
@@ -773,86 +775,89 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
   ChunkWalker<SHARED> walk;
   walk.init(un);
   bool again = false;
-  while (walk.ord < walk.ords)
-  for (walk.look(a, un, lo, hi, lane); walk.mask; again = true) {
-    // the slots of the next places that some row sees, in the table's order
-    int slot[LOOK], pos[LOOK], blk[LOOK];
-    unsigned long long vis[LOOK];
+  while (walk.ord < walk.ords) {
+    walk.look(a, un, lo, hi, lane);
+    for (; walk.mask; again = true) {
+      // the slots of the next places that some row sees, in the table's order
+      int slot[LOOK], pos[LOOK], blk[LOOK];
+      unsigned long long vis[LOOK];
 #pragma unroll
-    for (int k = 0; k < LOOK; ++k) {
-      int c = un.c1;
+      for (int k = 0; k < LOOK; ++k) {
+        int c = un.c1;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int x = walk.next(un);
-        if (w == wave) c = x;
+        for (int w = 0; w < 4; ++w) {
+          const int x = walk.next(un);
+          if (w == wave) c = x;
+        }
+        c += lane;
+        const int b = block_of(a, c);
+        blk[k] = c < un.c1 ? trow[b] : -1;
+        slot[k] = (unsigned)blk[k] < (unsigned)a.num_blocks ? blk[k] * a.BS + (c - b * a.BS) : -1;
       }
-      c += lane;
-      const int b = block_of(a, c);
-      blk[k] = c < un.c1 ? trow[b] : -1;
-      slot[k] = (unsigned)blk[k] < (unsigned)a.num_blocks ? blk[k] * a.BS + (c - b * a.BS) : -1;
-    }
 #pragma unroll
-    for (int k = 0; k < LOOK; ++k) pos[k] = slot[k] >= 0 ? a.slot_pos[slot[k]] : -1;
-    if (again) __syncthreads();   // the lists are read
-    int all = 0;
+      for (int k = 0; k < LOOK; ++k) pos[k] = slot[k] >= 0 ? a.slot_pos[slot[k]] : -1;
+      if (again) __syncthreads();   // the lists are read
+      int all = 0;
 #pragma unroll
-    for (int k = 0; k < LOOK; ++k) {
-      vis[k] = __ballot(seen_by_some<SHARED>(a, pos[k], lo, hi));
-      if (!SHARED) all += __builtin_popcountll(vis[k] & __ballot(seen<SHARED>(a, pos[k], lo) && seen<SHARED>(a, pos[k], hi)));
-      if (lane == 0) sCnt[k * 4 + wave] = __builtin_popcountll(vis[k]);
-    }
-    if (!SHARED && lane == 0) sAll[wave] = all;
-    __syncthreads();
-    int cnt = 0, mine[LOOK];
-#pragma unroll
-    for (int k = 0; k < LOOK; ++k)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        if (w == wave) mine[k] = cnt;
-        cnt += sCnt[k * 4 + w];
+      for (int k = 0; k < LOOK; ++k) {
+        vis[k] = __ballot(seen_by_some<SHARED>(a, pos[k], lo, hi));
+        if (!SHARED) all += __builtin_popcountll(vis[k] & __ballot(seen<SHARED>(a, pos[k], lo) && seen<SHARED>(a, pos[k], hi)));
+        if (lane == 0) sCnt[k * 4 + wave] = __builtin_popcountll(vis[k]);
       }
-    cnt = __builtin_amdgcn_readfirstlane(cnt);
-    if (cnt == 0) continue;
-    const bool full = SHARED || __builtin_amdgcn_readfirstlane(sAll[0] + sAll[1] + sAll[2] + sAll[3]) == cnt;
-    const int ntile = (cnt + BN - 1) / BN, last = cnt % BN ? ntile - 1 : ntile;   // the tile that is not full
+      if (!SHARED && lane == 0) sAll[wave] = all;
+      __syncthreads();
+      int cnt = 0, mine[LOOK];
 #pragma unroll
-    for (int k = 0; k < LOOK; ++k)
-      if ((vis[k] >> lane) & 1ull) {
-        const int i = mine[k] + __builtin_popcountll(vis[k] & ((1ull << lane) - 1ull));
-        const uint32_t r = (((uint32_t)blk[k] * a.Hkv + g) * a.BS + (slot[k] - blk[k] * a.BS)) * (FAR ? 1u : 2u * D);
-        sRow[i] = r;
-        sPos[i] = SHARED ? 0 : pos[k];
-        if (i == cnt - 1)   // the last tile's places behind it repeat it, and nobody sees them
-          for (int x = cnt; x < ntile * BN; ++x) {
-            sRow[x] = r;
-            sPos[x] = INT_MAX;
-          }
+      for (int k = 0; k < LOOK; ++k)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          if (w == wave) mine[k] = cnt;
+          cnt += sCnt[k * 4 + w];
+        }
+      cnt = __builtin_amdgcn_readfirstlane(cnt);
+      if (cnt == 0) continue;
+      const bool full = SHARED || __builtin_amdgcn_readfirstlane(sAll[0] + sAll[1] + sAll[2] + sAll[3]) == cnt;
+      const int ntile = (cnt + BN - 1) / BN, last = cnt % BN ? ntile - 1 : ntile;   // the tile that is not full
+#pragma unroll
+      for (int k = 0; k < LOOK; ++k)
+        if ((vis[k] >> lane) & 1ull) {
+          const int i = mine[k] + __builtin_popcountll(vis[k] & ((1ull << lane) - 1ull));
+          const uint32_t r = (((uint32_t)blk[k] * a.Hkv + g) * a.BS + (slot[k] - blk[k] * a.BS)) * (FAR ? 1u : 2u * D);
+          sRow[i] = r;
+          sPos[i] = SHARED ? 0 : pos[k];
+          if (i == cnt - 1)   // the last tile's places behind it repeat it, and nobody sees them
+            for (int x = cnt; x < ntile * BN; ++x) {
+              sRow[x] = r;
+              sPos[x] = INT_MAX;
+            }
+        }
+      __syncthreads();
+      auto step = [&](uint16_t* cK, uint16_t* cV, uint16_t* nK, uint16_t* nV, int t) __attribute__((always_inline)) {
+        wait_vm();
+        __syncthreads();   // tile t is there, and nobody reads tile t - 1 any more
+        if (t + 1 < ntile) stage(nK, nV, t + 1);
+        if (t == last) {   // V of the places behind the last entry: their factor is 0, and must stay it
+          const int n = cnt - t * BN;
+          for (int x = tid; x < (BN - n) * (PITCH / 2); x += 256) reinterpret_cast<uint32_t*>(cV + n * PITCH)[x] = 0u;
+          __syncthreads();
+        }
+        if (wave_ok) compute(cK, cV, t, full && t != last);
+      };
+      stage(sK0, sV0, 0);
+      for (int t = 0;;) {
+        step(sK0, sV0, sK1, sV1, t);
+        if (++t >= ntile) break;
+        step(sK1, sV1, sK0, sV0, t);
+        if (++t >= ntile) break;
       }
-    __syncthreads();
-    auto step = [&](uint16_t* cK, uint16_t* cV, uint16_t* nK, uint16_t* nV, int t) __attribute__((always_inline)) {
-      wait_vm();
-      __syncthreads();   // tile t is there, and nobody reads tile t - 1 any more
-      if (t + 1 < ntile) stage(nK, nV, t + 1);
-      if (t == last) {   // V of the places behind the last entry: their factor is 0, and must stay it
-        const int n = cnt - t * BN;
-        for (int x = tid; x < (BN - n) * (PITCH / 2); x += 256) reinterpret_cast<uint32_t*>(cV + n * PITCH)[x] = 0u;
-        __syncthreads();
-      }
-      if (wave_ok) compute(cK, cV, t, full && t != last);
-    };
-    stage(sK0, sV0, 0);
-    for (int t = 0;;) {
-      step(sK0, sV0, sK1, sV1, t);
-      if (++t >= ntile) break;
-      step(sK1, sV1, sK0, sV0, t);
-      if (++t >= ntile) break;
     }
   }
   st.finish(a, un, row_of<SHARED>(a, un, g, row, un.rows - 1), g, row, half);
 }
 
-// A narrow unit, 64 rows at most (D = 64: 32, where two columns' registers would leave half the waves a CU), is one wave, with its own tiles of 32 entries (double-buffered; D = 128: 40 KB of LDS,
-// so that four share a CU, one a SIMD).  Every global read of its loop is a copy to LDS, so all of them complete in
+// A narrow unit, 64 rows at most (D = 64: 32, where two columns' registers would leave half the waves a CU), is one wave,
+// with its own tiles of 32 entries (double-buffered; D = 128: 40 KB of LDS, so that four share a CU, one a SIMD).  Every
+// global read of its loop is a copy to LDS, so all of them complete in
 // issue order under one counter: step n issues the K and V copies of tile n + 1, waits until only these are
 // outstanding, asks for the next piece of what the tiles after it need, and computes tile n.  That is, for 192 places
 // of the table at a time, in consecutive steps: their table entries; the positions of the slots these name; and, when
@@ -947,14 +952,14 @@ __device__ __forceinline__ void narrow_unit(const RowsArgs& a, const Unit& un, i
   };
   // Entries from `head` on that make the next tile; lists more where they are short of one.
   auto ready = [&](unsigned head) __attribute__((always_inline)) {
-    if (tail - head < BN && stage == 3) enlist();
-    while (tail - head < BN && (stage > 0 || walk.more(a, un, lo, hi, lane))) {   // at the start, and where places show few entries
+    while (tail - head < BN && (stage > 0 || walk.more(a, un, lo, hi, lane))) {
+      // what has not been asked for ahead: at the start, and where places show few entries
       if (stage == 0) ask_table();
       if (stage == 1) {
         wait_vm_le<0>();
         ask_pos();
       }
-      wait_vm_le<0>();
+      if (stage == 2) wait_vm_le<0>();
       enlist();
     }
     return min(tail - head, (unsigned)BN);
@@ -978,66 +983,68 @@ __device__ __forceinline__ void narrow_unit(const RowsArgs& a, const Unit& un, i
   };
 
   wait_vm_le<0>();   // Q is in: no compiler-visible load stays pending in the loop
-  unsigned head = 0;
-  int n = (int)ready(0), b = 0;
-  if (n > 0) gather(0, 0, n);
-  while (n > 0) {
-    const int n1 = n == BN ? (int)ready(head + BN) : 0;
+  unsigned head = -BN;   // of the tile in work, n entries; the first turn has none
+  int n = 0, b = 1;
+  for (bool more = true; more;) {
+    const int n1 = n == 0 || n == BN ? (int)ready(head + BN) : 0;   // a tile that is not full is the last
     if (n1 > 0) {
       gather(b ^ 1, head + BN, n1);
       wait_vm_le<OPS>();
     } else {
       wait_vm_le<0>();
     }
+    more = n1 > 0;
     if (stage == 0 && walk.more(a, un, lo, hi, lane)) ask_table();
     else if (stage == 1) ask_pos();
     else if (stage == 2) stage = 3;
-    const uint16_t* cK = sK + b * TILE;
-    uint16_t* cV = sV + b * TILE;
-    f32x16 s[NC][1];
+    if (n > 0) {
+      const uint16_t* cK = sK + b * TILE;
+      uint16_t* cV = sV + b * TILE;
+      f32x16 s[NC][1];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) s[c][0] = f32x16{};
+      for (int c = 0; c < NC; ++c) s[c][0] = f32x16{};
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8 ka = lds_read_b128(cK + LY::row_at(rl, ks));
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 ka = lds_read_b128(cK + LY::row_at(rl, ks));
 #pragma unroll
-      for (int c = 0; c < NC; ++c) s[c][0] = mfma32(ka, qreg[c][ks], s[c][0]);
-    }
-    if (n < BN) {   // V of the places behind the last entry: their factor is 0, and must stay it
-      for (int i = lane; i < (BN - n) * (PITCH / 8); i += kWave)
-        *reinterpret_cast<uint4*>(&cV[n * PITCH + 8 * i]) = make_uint4(0u, 0u, 0u, 0u);
-    }
-    const int p = SHARED ? 0 : sPos[(head + col) % kNarrowRing];
-    if (__ballot(col < n && (SHARED || (seen<SHARED>(a, p, lo) && seen<SHARED>(a, p, hi)))) != ~0ull) {
+        for (int c = 0; c < NC; ++c) s[c][0] = mfma32(ka, qreg[c][ks], s[c][0]);
+      }
+      if (n < BN) {   // V of the places behind the last entry: their factor is 0, and must stay it
+        for (int i = lane; i < (BN - n) * (PITCH / 8); i += kWave)
+          *reinterpret_cast<uint4*>(&cV[n * PITCH + 8 * i]) = make_uint4(0u, 0u, 0u, 0u);
+      }
+      const int p = SHARED ? 0 : sPos[(head + col) % kNarrowRing];
+      if (__ballot(col < n && (SHARED || (seen<SHARED>(a, p, lo) && seen<SHARED>(a, p, hi)))) != ~0ull) {
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const int i = 8 * q4 + 4 * half;
-        int4 e = make_int4(0, 0, 0, 0);
-        if (!SHARED) e = *reinterpret_cast<const int4*>(&sPos[(head + i) % kNarrowRing]);   // head: a multiple of 32
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const int i = 8 * q4 + 4 * half;
+          int4 e = make_int4(0, 0, 0, 0);
+          if (!SHARED) e = *reinterpret_cast<const int4*>(&sPos[(head + i) % kNarrowRing]);   // head: a multiple of 32
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          if (!(i < n && seen<SHARED>(a, e.x, at[c]))) s[c][0][4 * q4] = -INFINITY;
-          if (!(i + 1 < n && seen<SHARED>(a, e.y, at[c]))) s[c][0][4 * q4 + 1] = -INFINITY;
-          if (!(i + 2 < n && seen<SHARED>(a, e.z, at[c]))) s[c][0][4 * q4 + 2] = -INFINITY;
-          if (!(i + 3 < n && seen<SHARED>(a, e.w, at[c]))) s[c][0][4 * q4 + 3] = -INFINITY;
+          for (int c = 0; c < NC; ++c) {
+            if (!(i < n && seen<SHARED>(a, e.x, at[c]))) s[c][0][4 * q4] = -INFINITY;
+            if (!(i + 1 < n && seen<SHARED>(a, e.y, at[c]))) s[c][0][4 * q4 + 1] = -INFINITY;
+            if (!(i + 2 < n && seen<SHARED>(a, e.z, at[c]))) s[c][0][4 * q4 + 2] = -INFINITY;
+            if (!(i + 3 < n && seen<SHARED>(a, e.w, at[c]))) s[c][0][4 * q4 + 3] = -INFINITY;
+          }
         }
       }
-    }
-    bf16x8 pb[NC][2];
+      bf16x8 pb[NC][2];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      st[c].template weigh<1>(s[c], a.scale_log2);
+      for (int c = 0; c < NC; ++c) {
+        st[c].template weigh<1>(s[c], a.scale_log2);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) pb[c][t] = pack8(s[c][0], 8 * t);
-    }
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d) {
-        const bf16x8 va = tr_operand<D, true>(cV, 16 * t, 32 * d, tl, th);
-#pragma unroll
-        for (int c = 0; c < NC; ++c) st[c].acc[d] = mfma32(va, pb[c][t], st[c].acc[d]);
+        for (int t = 0; t < 2; ++t) pb[c][t] = pack8(s[c][0], 8 * t);
       }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+          const bf16x8 va = tr_operand<D, true>(cV, 16 * t, 32 * d, tl, th);
+#pragma unroll
+          for (int c = 0; c < NC; ++c) st[c].acc[d] = mfma32(va, pb[c][t], st[c].acc[d]);
+        }
+    }
     head += BN;
     n = n1;
     b ^= 1;
@@ -1187,21 +1194,24 @@ static int rows_want(const PagedRows& p, bool wide) {
 constexpr long long kBlockRows = 4096;   // rows of new tokens that are merged by a workgroup each
 // Sizes of a call's workspace, in this order.
 struct RowsSpace {
-  long long units[2], waves, part;   // units per KV head, wide and narrow; waves of narrow ones; partial rows
+  long long units[2], waves, split, part;   // units per KV head, wide and narrow; waves of narrow ones; partial rows of cut
+                                            // wide jobs per KV head, and of all
   size_t parts, rank, list, count, base, jobs, own, prefix, unit, wave, stats, rows, ml;
   size_t bytes() const { return parts + rank + list + count + base + jobs + own + prefix + unit + wave + stats + rows + ml; }
 };
 static size_t stats_chunks(const PagedRows& p) { return ((size_t)p.max_blocks * p.block_size + kChunk - 1) / kChunk; }
 static bool plans_small(const PagedRows& p) { return p.S <= kPlanSmall && p.groups <= kPlanGroups; }
 // Row blocks of wide jobs: one for every 128 rows, and one more a job (SHARED: groups, and sequences by themselves if they
-// have so many q-heads).  A job has no splits of fewer than kLeastTiles tiles; those of wide jobs
-// add no more units than four rounds of them and than three times the row blocks (or one round).  Narrow jobs: a unit
-// each, and one more for every wave's end.  Partial rows: those of every job once and of the units that are added; for
-// new tokens only those of jobs of several units, so twice those of the added ones.
+// have so many q-heads).  A job has no splits of fewer than kLeastTiles tiles; those of wide jobs add no more units than
+// four rounds of them and than three times the row blocks (or one round).  Narrow jobs: a unit each, and one more for
+// every wave's end.  Partial rows: of wide jobs 128 a unit (new tokens: only what is cut has any, and the plan cuts no more
+// than twice the units that may be added); of narrow ones those of every job once and of the units that are added, for
+// new tokens, where only jobs of several units have any, twice the latter.
 static RowsSpace rows_space(const PagedRows& p) {
   RowsSpace x{};
   const long long G = p.Hq / p.Hkv, tokens = p.shared ? p.S : p.ntok, all = tokens * G;
-  const long long narrow = narrow_rows(p.D), width = (long long)p.max_blocks * p.block_size, jobs = (p.shared ? (long long)p.groups * kPrefixBlocks : 0) + p.S;
+  const long long narrow = narrow_rows(p.D), width = (long long)p.max_blocks * p.block_size;
+  const long long jobs = (p.shared ? (long long)p.groups * kPrefixBlocks : 0) + p.S;
   const long long most = p.shared ? kPrefixBlocks * narrow : narrow;   // rows of a narrow job, or of a group's
   const long long wide_jobs = std::min<long long>(p.shared ? p.groups : p.S, all / most) + (p.shared && G > narrow ? p.S : 0);
   const long long blocks = all > most || (p.shared && G > narrow) ? all / kWideRows + wide_jobs : 0, want = rows_want(p, true);
@@ -1209,8 +1219,8 @@ static RowsSpace rows_space(const PagedRows& p) {
   x.units[0] = std::min(blocks * ((width + 32 * kLeastTiles - 1) / (32 * kLeastTiles)), blocks + more);
   x.waves = std::min<long long>(rows_want(p, false), jobs * ((width + kChunk - 1) / kChunk + kStartChunks));
   x.units[1] = jobs + x.waves;
-  const long long added = std::min(more, x.units[0]) * kWideRows + x.waves * narrow;
-  x.part = (p.shared ? 2 * all + added : 2 * added) * p.Hkv;
+  x.split = (p.shared ? x.units[0] : 2 * std::min(more, x.units[0])) * kWideRows;
+  x.part = (x.split + (p.shared ? 2 * all + x.waves * narrow : 2 * x.waves * narrow)) * p.Hkv;
   x.parts = 256;
   if (p.shared) {
     x.rank = x.list = round256((size_t)p.S * sizeof(int));
@@ -1310,6 +1320,7 @@ hipError_t launch_paged_rows(const PagedRows& p) {
   a.part = (float*)take(x.rows);
   a.part_ml = (float2*)take(x.ml);
   a.max_part = x.part;
+  a.max_split = x.split;
   for (int k = 0; k < 2; ++k) {
     a.max_units[k] = (int)x.units[k];
     a.want[k] = rows_want(p, k == 0);
