@@ -585,3 +585,52 @@ def test_two_streams_at_once(pg):
     for a, b in zip(*got):
         for x, y in zip((*a, *b), want):
             assert torch.equal(x, y)
+
+
+def test_long_rows_among_many_short_ones(pg):
+    """11 blocks of 128 rows over 262,144 places, which the plan wants to cut into many units, beside 200 jobs of 16 rows,
+    for which row blocks are counted that there are not: what is cut has room for its partial results.  The long table
+    names 64 blocks 64 times, so that softmax gives what it gives over one time, and LSE ln 64 more."""
+    H, D, bs, nb, times, n, S = 64, 64, 64, 64, 64, 1400, 201
+    g = torch.Generator().manual_seed(11)
+    k, v = (torch.randn(nb, H, bs, D, generator=g).bfloat16() for _ in range(2))
+    q = torch.randn(n + 16 * (S - 1), H, D, generator=g).bfloat16()
+    table = torch.zeros(S, nb * times, dtype=torch.int32)
+    table[0] = torch.arange(nb).repeat(times)
+    table[1:, 0] = torch.arange(S - 1) % nb
+    blocks = torch.ones(S, dtype=torch.int32)
+    blocks[0] = nb * times
+    pos = torch.arange(nb * bs, dtype=torch.int32)
+    at = torch.cat([torch.arange(n) + nb * bs - n] + [bs * (i % nb) + bs - 16 + torch.arange(16) for i in range(S - 1)]).int()
+    cu = torch.cat([torch.zeros(1), n + 16 * torch.arange(S)]).int()
+    dev = lambda *x: [t.to(DEV) for t in x]
+    o, lse = torch.full_like(q, float("nan")).to(DEV), torch.full(q.shape[:2], float("nan"), device=DEV)
+    pg.kvs_paged_extend(*dev(q, k, v, pos, table, blocks, at, cu), out=o, lse=lse)
+    assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+    o, lse = o.cpu(), lse.cpu()
+    rows = lambda x, b: x[b].transpose(-3, -2).reshape(-1, H, D)
+    for h in (0, 31, 63):
+        one = slice(h, h + 1)
+        want = ref.attend(q[:n, one], rows(k, slice(None))[:, one], rows(v, slice(None))[:, one], D ** -0.5,
+                          torch.arange(nb * bs)[None] <= at[:n, None])
+        # 64 times as many entries: their sums' share of the bounds, with E <= max |v|
+        more = 2 * nb * bs * times * ref.U
+        want = (want[0], want[1] + math.log(times), want[2] + more * v.float().abs().max().item(), want[3] + more)
+        ref.check(f"long, head {h}", o[:n, one], lse[:n, one], want)
+        for i in (0, 63, 199):
+            r0 = n + 16 * i
+            kb, vb = (rows(x, slice(i % nb, i % nb + 1))[:, one] for x in (k, v))
+            see = torch.arange(bs)[None] + bs * (i % nb) <= at[r0:r0 + 16, None]
+            ref.check(f"short {i}, head {h}", o[r0:r0 + 16, one], lse[r0:r0 + 16, one],
+                      ref.attend(q[r0:r0 + 16, one], kb, vb, D ** -0.5, see))
+
+
+@pytest.mark.parametrize("n,D", [(1, 128), (1, 64), (40, 128), (40, 64)])
+def test_a_position_behind_all_others(pg, n, D):
+    """q_pos INT32_MAX sees every entry, and nothing else: 70 entries leave part of a tile empty, whatever its rows."""
+    r = Rollouts(pg, 1, 8, 16, 8, 2, D, 5)
+    r.append(0, range(70))
+    q = r.randn(n, 8, D)
+    at = [2 ** 31 - 1] * n
+    o, lse = r.cache.extend(q.to(DEV), at, [n])
+    r.check_extend(f"INT32_MAX n={n} D={D}", q, o, lse, D ** -0.5, [n], at)
