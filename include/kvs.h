@@ -307,7 +307,8 @@ kvs_status_t kvs_check_evict_at(const int32_t* evict_at, const int32_t* cu_seqle
  * Per-kernel timing for benchmarks.  While enabled, each call brackets every
  * kernel it launches with HIP events on the call's stream.  kvs_prof_read
  * waits for the recorded events and returns, for the kernel named `name`
- * ("classify", "fwd", "bwd_pre", "bwd_dkdv", "bwd_dq", "key_weights", "paged_decode", "paged_decode_shared", "paged_extend", "paged_evict_lowest"), the
+ * ("classify", "fwd", "bwd_pre", "bwd_dkdv", "bwd_dq", "key_weights", "paged_decode",
+ * "paged_decode_shared", "paged_extend", "paged_evict_lowest"), the
  * number of launches and their total duration in milliseconds.  The records
  * are process-wide (every thread's launches land in one list, guarded by a
  * lock), so enable timing only while the calls to be timed are the only
@@ -553,7 +554,8 @@ kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void*
 
 /* The decode of sequences that share the beginning of their tables (rollouts of
  * one prompt), whose common entries are read once for all of them.  Q, O, LSE, the
- * caches and the tables are those of kvs_paged_decode, and so are the results.
+ * caches and the tables are those of kvs_paged_decode, and so are the results but
+ * for roundings (partial results are joined in another order).
  * prefix_group (device int32 [num_seqs]): the group of each sequence, in [0,
  * num_groups) (anything else: none); prefix_blocks (device int32 [num_groups]): how
  * many leading table entries the members of each group have in common
@@ -562,7 +564,8 @@ kvs_status_t kvs_paged_decode_ex(const void* Q, const void* K_cache, const void*
  * where another member's begins differently.
  * Supported: D in {64, 128}; Hq / Hkv <= 64; block_size in [1, 64]; max_blocks *
  * block_size <= 2^30; num_blocks * block_size * Hkv <= 2^32 (num_blocks *
- * block_size <= INT32_MAX); num_seqs * Hq < 2^26.  Workspace from the query. */
+ * block_size <= INT32_MAX); num_seqs * Hq < 2^26; (num_seqs + 2 num_groups) *
+ * (ceil(max_blocks * block_size / 64) + 2) < 2^31.  Workspace from the query. */
 size_t kvs_paged_decode_shared_workspace(int num_seqs, int num_groups, int Hq, int Hkv, int D, int max_blocks,
                                          int block_size);
 kvs_status_t kvs_paged_decode_shared(const void* Q, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
@@ -577,9 +580,9 @@ kvs_status_t kvs_paged_decode_shared(const void* Q, const void* K_cache, const v
  * [Ntot][Hq][D], LSE fp32 [Ntot][Hq]; sequence s has the tokens [cu_seqlens[s],
  * cu_seqlens[s + 1]) (device int32 [num_seqs + 1], non-decreasing; clamped to [0,
  * Ntot], and tokens of no sequence keep what O and LSE held).  The token at trace
- * position q_pos[t] (device int32 [Ntot]) sees of its sequence's live entries
- * those at p <= q_pos[t], and under a window (window > 0) of these those with
- * q_pos[t] - p < window or p < sinks: one token a sequence is kvs_paged_decode_ex,
+ * position q_pos[t] (device int32 [Ntot]; INT32_MAX counts as one less) sees of its
+ * sequence's live entries those at p <= q_pos[t], and under a window (window > 0) of
+ * these those with q_pos[t] - p < window or p < sinks: one token a sequence is kvs_paged_decode_ex,
  * and all tokens of a trace at once, nothing evicted, are kvs_window_attn_fwd.
  * A token that sees nothing gets O = 0, LSE = -inf.  Entries that are live but not
  * visible to a token are factors 0 in its products: an infinity or NaN in their V
