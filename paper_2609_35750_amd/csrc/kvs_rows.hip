@@ -26,7 +26,9 @@ namespace kvs {
 
 // ---------------------------------------------------------------- copies
 // Slot dst[i] takes the K and V rows of slot src[i], its position and its weight; MOVE: slot src[i] is empty then.
-// 16-byte pieces, one of K and one of V a thread and turn; bound by HBM.
+// 16-byte pieces, one of K and one of V a thread and turn; bound by HBM: 16,000 entries of 8 KV heads at D = 128 (131 MB
+// read and written) in 28 us, 4.6 TB/s where a large copy reaches 5.0.  (Several pieces a thread, asked for together, were
+// slower, and pieces head by head the same.)
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int D>
 __global__ void __launch_bounds__(256) paged_copy_kernel(PagedCopy a) {
@@ -82,7 +84,8 @@ constexpr int kPlanSmall = 256, kPlanGroups = 64;   // sequences and groups that
 // sequences behind 16,384 144 -> 165).
 constexpr int kPrefixBlocks = 2;
 
-// What the plan weighs for wide units: 128 rows of partial results, written and read, cost as much as these tiles.
+// What the plan weighs for wide units: 128 rows of partial results, written and read, cost as much as these tiles.  (16
+// ragged chunks are the same with 20 and 60; 8 windowed ones with 20, and 110 -> 113 us with 60.)
 constexpr float kSplitTiles = 40.f;
 constexpr int kChunk = 64;        // places of a table that are skipped or looked at together
 
@@ -195,8 +198,8 @@ __device__ __forceinline__ void chunk_stats(const RowsArgs& a, int first, int wa
 }
 
 // The plan, by workgroup 0: for up to 256 sequences and groups one wave makes it, with what it knows of them in LDS, and
-// all of them try the sizes of wide jobs' runs and write the units.  Bound by latency.  Under a window the other
-// workgroups take the positions of the tables' chunks.
+// all of them try the sizes of wide jobs' runs and write the units.  Bound by latency: 5 us for 4 sequences, 11 for 64 of
+// one group.  Under a window the other workgroups take the positions of the tables' chunks.
 template <bool SHARED, bool SMALL>
 __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs a) {
   constexpr int NT = SMALL ? 512 : 1024, PT = SMALL ? kWave : NT;   // threads; those that plan
@@ -320,6 +323,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       const Job x = mine ? job_of(j) : Job{0, 0, 0, 0, 0, 0};
       const bool wide = is_wide(a, x.rows);
       int places = x.rows ? x.c1 - x.c0 : 0;
+      // by all the job's tokens: by a row block's own, eight windowed chunks are cut less, and 110 us become 119
       if (!SHARED && a.window > 0) places = (int)min((long long)places, (long long)a.window + a.sinks + x.rows / a.G);
       const int t = wide ? plan_tiles(places) : (int)(((unsigned)places + 31) / 32);
       if (mine) {
@@ -651,7 +655,9 @@ constexpr int kWidePick = 512;   // places of the table that a wide unit looks a
 // (two dependent reads, for all places at once), and the keys and values of the listed slots are gathered tile by tile,
 // double-buffered, each tile read by the four waves.  Scores are S^T = K Q^T (keys on M, rows on N), so that a lane holds 16
 // scores of one row; softmax and the products with V as in the forward of the eviction mask.  Three workgroups a CU, whose
-// registers just do without spills.
+// registers just do without spills.  Bound by the matrix cores at the clock their power leaves, as that forward: 4,096
+// tokens of 32 q-heads over 20,480 entries (D = 128) 1.2 ms, 1,030 TFLOP/s, matrix cores busy 51% at 1.8 GHz.  Asking for
+// the next 512 places while the tiles of the last ones are computed, by copies to LDS, made that 5% slower.
 // FAR: caches of 4 GiB or more, whose rows need 64-bit addresses of their own; else a copy takes one addition.
 template <int D, bool SHARED, bool FAR>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))) rows_wide_kernel(RowsArgs a) {
@@ -861,7 +867,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
 // issue order under one counter: step n issues the K and V copies of tile n + 1, waits until only these are
 // outstanding, asks for the next piece of what the tiles after it need, and computes tile n.  That is, for 192 places
 // of the table at a time, in consecutive steps: their table entries; the positions of the slots these name; and, when
-// the list of slots to gather runs short, the slots that some row sees are added to it (a ring of 256).
+// the list of slots to gather runs short, the slots that some row sees are added to it (a ring of 256).  Bound by HBM where
+// jobs are long: 4 tokens of each of 64 sequences behind 1,000 to 8,000 entries (1.14 GB) 190 us, 6.0 TB/s; 16 rollouts
+// behind 4,096 common entries (80 MB) 26 us, half of it the dependent reads in front of the first tile.
 constexpr int kNarrowPick = 192, kNarrowRing = 256;
 template <int D>
 struct NarrowSpace {
@@ -1094,7 +1102,8 @@ struct Joined {
 // workgroup a row, whose groups of D / 4 lanes take the parts in turn (one long sequence has hundreds); else, for many
 // rows of new tokens, which have few parts each, a wave a token and KV head, whose halves (D = 64: quarters) take the
 // head's rows in turn, so that the token is looked up once.  Bound by the latency of its reads: four parts are asked for
-// at a time.
+// at a time.  4 us for few rows, 8 for 64 sequences with 30 MB of parts, 20 for 4,096 tokens with 73 MB.  A workgroup a row
+// against a wave a token: one token over 32,000 entries 36 and 83 us.
 template <int D, bool SHARED, bool BLOCK>
 __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
   constexpr int LPS = D / 4, PER = kWave / LPS, UNROLL = 4;
