@@ -84,9 +84,11 @@ constexpr int kPlanSmall = 256, kPlanGroups = 64;   // sequences and groups that
 // sequences behind 16,384 144 -> 165).
 constexpr int kPrefixBlocks = 2;
 
-// What the plan weighs for wide units: 128 rows of partial results, written and read, cost as much as these tiles.  (16
-// ragged chunks are the same with 20 and 60; 8 windowed ones with 20, and 110 -> 113 us with 60.)
-constexpr float kSplitTiles = 40.f;
+// What the plan weighs for wide units: 128 rows of partial results, written and read, cost as much as these tiles (16
+// ragged chunks are the same with 40; 64 sequences behind 16,384 entries 145 -> 149 us), and a round that fills a third or two of
+// the places takes these parts of a full one, whose workgroups share their CU by threes (against parts of a half and
+// three quarters, or two thirds and 0.8 as here: 2,048 tokens behind 8,192 entries, D = 64, 231 and 225 us).
+constexpr float kSplitTiles = 20.f, kOneOfThree = 0.65f, kTwoOfThree = 0.8f;
 constexpr int kChunk = 64;        // places of a table that are skipped or looked at together
 
 // What a unit is, as its waves read it: the chunks k, k + n, k + 2 n, ... of the places [c0, c1) of a table, so that a run
@@ -359,8 +361,10 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   __syncthreads();
   // How wide jobs are cut, in tiles of the time that a place on the chip has: all of them into runs of one size, the whole
   // of the longest, which always fits, or a part of it; or, for new tokens, the row blocks that fill whole rounds left
-  // whole and those behind them cut, so that few rows have partial results and yet the last round is short.  The last
-  // units end about half a unit behind the work's share, and no unit before its own end.  A wave a cut at a time.
+  // whole and those behind them cut, so that few rows have partial results and yet the last round is short.  Units of one
+  // size end by rounds, and where they are smaller than the largest the last ones half of what they lack later.  (By the
+  // work's share and half a unit more: 4 chunks of 500 to 900 tokens 144 -> 162 us, 2,048 tokens at D = 64 225 -> 250, 16
+  // ragged chunks 543 -> 558.)  A wave a cut at a time.
   int C = sTopWide, whole = 0;   // row blocks left whole
   // of a wide job: its row blocks that are cut (the first ones: a causal row block's last rows see most), and into how many
   auto cut_of = [&](int j, int c, float rc, int front, int& n) {
@@ -374,17 +378,25 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       const int k = i < 16 ? i : i - 15;
       const int n = k < 4 ? k + 1 : k & 1 ? 4 << ((k - 3) >> 1) : 6 << ((k - 4) >> 1);   // 1 .. 4, 6, 8, 12, 16, 24, ...
       const int c = (sTopWide + n - 1) / n, front = i < 16 ? 0 : (int)min(rounds * a.want[0], (long long)INT_MAX);
-      const float rc = __builtin_amdgcn_rcpf((float)c), place = 1.f / (float)a.want[0], work = (float)sWork * place;
-      long long units = 0, split = 0;   // behind those left whole; rows of partial results
+      const float rc = __builtin_amdgcn_rcpf((float)c), place = 1.f / (float)a.want[0];
+      long long units = 0, split = 0, left = 0;   // behind those left whole; rows of partial results; tiles of those left whole
       for (int j0 = 0; j0 < J; j0 += kWave) {
         const int j = j0 + lane;
         int m = 0;
         const int b = j < J ? cut_of(j, c, rc, front, m) : 0;
         units += wave_last(wave_scan((int)min((long long)m * b, 1ll << 24)));   // more than there may be at any rate
+        if (!SHARED && front > 0) {
+          const int nb = j < J && is_wide(a, rows[j]) ? row_blocks(rows[j]) - b : 0;
+          left += wave_last(wave_scan(nb > 0 ? (int)min((long long)nb * tiles[j], 1ll << 24) : 0));
+        }
         split += wave_last(wave_scan(m > 1 ? (int)min((long long)m * min(rows[j], b * kWideRows), 1ll << 24) : 0));
       }
       if (lane == 0) {
-        const float ends = fmaxf(front ? (float)sTopWide : (float)c, work + 0.5f * (float)c);
+        const float u = (float)units * place, full = floorf(u + 1e-3f), rest = u - full;   // rounds
+        const float last = rest < 1e-3f ? 0.f : rest < 0.334f ? kOneOfThree : rest < 0.667f ? kTwoOfThree : 1.f;
+        const float mean = units > 0 ? (float)(sWork - left) * __builtin_amdgcn_rcpf((float)units) : 0.f;
+        const float least = (full > 0.f ? 1.f : last) * (float)c;
+        const float ends = (float)left * place + fmaxf(least, (full + last) * mean + 0.5f * ((float)c - mean));
         sSize[i] = c;
         sWhole[i] = front;
         const bool fits = front + units <= a.max_units[0] && split <= a.max_split;
