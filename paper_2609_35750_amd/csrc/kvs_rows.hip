@@ -416,6 +416,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
   }
   const float rC = __builtin_amdgcn_rcpf((float)C);
   const int per = (int)max(1ll, (sChunks + a.want[1] - 1) / a.want[1]);   // of a wave
+  auto wave_of = [&](int x) { return (int)((unsigned)x / (unsigned)per); };   // of all that is dealt, less than 2^31
   if (!SMALL || wave == 0) {
     // first units of the jobs, wide and narrow ones counted apart, and their first partial rows
     long long units0[2] = {0, 0}, part0 = 0;
@@ -423,7 +424,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       const int j = j0 + tid, r = j < J ? rows[j] : 0, t = j < J ? tiles[j] : 0, m = job_chunks<SHARED>(a, t, r);
       int nw = 0;
       const int b = j < J ? cut_of(j, C, rC, whole, nw) : 0, nb = is_wide(a, r) ? row_blocks(r) : 0;
-      const int nn = m > 0 ? (int)(((long long)chunk[j] + m - 1) / per) - chunk[j] / per + 1 : 0, n = nw + nn;
+      const int nn = m > 0 ? wave_of(chunk[j] + m - 1) - wave_of(chunk[j]) + 1 : 0, n = nw + nn;
       const int cut_rows = nb ? min(r, b * kWideRows) : r;
       const long long uw = block_scan<PT>(nb - b + nw * b, units0[0], buf);
       const long long un = block_scan<PT>(nn, units0[1], buf);
@@ -494,13 +495,13 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
           job_rows = min(job_rows, cut * kWideRows);
         }
       } else {
-        const int m = job_chunks<SHARED>(a, tiles[j], b.rows), w = chunk[j] / per;
-        n = (int)(((long long)chunk[j] + m - 1) / per) - w + 1;
+        const int m = job_chunks<SHARED>(a, tiles[j], b.rows), w = wave_of(chunk[j]);
+        n = wave_of(chunk[j] + m - 1) - w + 1;
         sp = i;
       }
       const int split = k == 1 && (SHARED || a.window == 0) ? 1 << 16 : sp | n << 16;
       if (k == 1 && (SHARED || a.window == 0)) {   // the part of wave w + i; under a window an equal part of the chunks
-        const long long x = (long long)(chunk[j] / per + i) * per - chunk[j];
+        const long long x = (long long)(wave_of(chunk[j]) + i) * per - chunk[j];
         c1 = (int)min((long long)c1, c0 + (x + per) * kChunk);
         c0 = (int)min((long long)c1, c0 + max(x, 0ll) * kChunk);
       }
@@ -515,7 +516,7 @@ __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs 
       const int m = job_chunks<SHARED>(a, tiles[j], rows[j]);
       u = first[1][j];
       if (m > 0 && chunk[j] <= x)   // within the job, or behind it, where the next one begins
-        u += (int)min((long long)w, ((long long)chunk[j] + m - 1) / per + 1) - chunk[j] / per;
+        u += min(w, wave_of(chunk[j] + m - 1) + 1) - wave_of(chunk[j]);
     }
     a.waves[w] = u;
   }
