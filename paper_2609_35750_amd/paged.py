@@ -303,24 +303,47 @@ def kvs_paged_copy(src, dst, k_cache, v_cache, slot_pos=None, slot_weight=None, 
             nb, bs, Hkv, D, _stream(k_cache)))
 
 
-def _rows_args(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, softmax_scale, out, lse, *more):
-    """Checks shared by the calls with many query rows; returns (O, LSE, scale)."""
-    _check_caches(k_cache, v_cache, slot_pos)
-    if q.dim() != 3 or q.dtype != torch.bfloat16:
+def _rows_args(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, softmax_scale, out, lse, a, b):
+    """Checks shared by the calls with many query rows (a, b: two int32 tensors of the call's own).
+
+    Returns (n, Hq, D, num_blocks, Hkv, block_size, S, max_blocks, O, LSE, scale)."""
+    shape, cache, table = q.shape, k_cache.shape, block_table.shape
+    if len(cache) != 4 or v_cache.shape != cache:
+        raise ValueError("the caches must be [num_blocks, Hkv, block_size, D]")
+    if not k_cache.dtype == v_cache.dtype == torch.bfloat16:
+        raise ValueError("the caches must be bfloat16")
+    nb, Hkv, bs, D = cache
+    if slot_pos.dtype != torch.int32 or slot_pos.numel() != nb * bs:
+        raise ValueError("slot_pos must be int32 with num_blocks * block_size entries")
+    if len(shape) != 3 or q.dtype != torch.bfloat16:
         raise ValueError("q must be bfloat16 [n, Hq, D]")
-    if q.shape[2] != k_cache.shape[3]:
+    n, Hq, Dq = shape
+    if Dq != D:
         raise ValueError("cache shapes do not match q")
-    _int32(block_table, seq_blocks, *more)
-    if block_table.dim() != 2 or seq_blocks.shape != (block_table.shape[0],):
+    if not block_table.dtype == seq_blocks.dtype == a.dtype == b.dtype == torch.int32:
+        raise ValueError("positions, slots, tables and counts must be int32")
+    if len(table) != 2 or seq_blocks.shape != (table[0],):
         raise ValueError("block_table must be [S, max_blocks] and seq_blocks [S]")
-    if out is not None and (out.shape != q.shape or out.dtype != torch.bfloat16):
+    dev = q.get_device()
+    for t in (k_cache, v_cache, slot_pos, block_table, seq_blocks, a, b):
+        if t.get_device() != dev:
+            raise ValueError("tensors must be on one device")
+    if dev < 0:
+        raise ValueError("tensors must be on the GPU")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.shape != shape or out.dtype != torch.bfloat16:
         raise ValueError("O must have q's shape and type")
-    if lse is not None and (lse.shape != q.shape[:2] or lse.dtype != torch.float32):
+    elif out.get_device() != dev:
+        raise ValueError("tensors must be on one device")
+    if lse is None:
+        lse = q.new_empty((n, Hq), dtype=torch.float32)
+    elif lse.shape != (n, Hq) or lse.dtype != torch.float32:
         raise ValueError("LSE must be float32 [n, Hq]")
-    _same_device(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, out, lse, *more)
-    scale = 1.0 / math.sqrt(q.shape[2]) if softmax_scale is None else float(softmax_scale)
-    o = torch.empty_like(q) if out is None else out
-    return o, torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse, scale
+    elif lse.get_device() != dev:
+        raise ValueError("tensors must be on one device")
+    scale = 1.0 / math.sqrt(D) if softmax_scale is None else float(softmax_scale)
+    return n, Hq, D, nb, Hkv, bs, table[0], table[1], out, lse, scale
 
 
 def kvs_paged_decode_shared(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, prefix_group, prefix_blocks,
@@ -330,22 +353,19 @@ def kvs_paged_decode_shared(q, k_cache, v_cache, slot_pos, block_table, seq_bloc
     ``prefix_group`` int32 [S]: the group of each sequence (-1: none); ``prefix_blocks`` int32 [groups]: the leading
     table entries its members have in common, which are read once for all of them.
     """
-    o, lse, scale = _rows_args(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, softmax_scale, out, lse,
-                               prefix_group, prefix_blocks)
-    S, Hq, D = q.shape
-    nb, Hkv, bs, _ = k_cache.shape
-    if block_table.shape[0] != S or prefix_group.shape != (S,):
+    n, Hq, D, nb, Hkv, bs, S, mb, o, lse, scale = _rows_args(q, k_cache, v_cache, slot_pos, block_table, seq_blocks,
+                                                             softmax_scale, out, lse, prefix_group, prefix_blocks)
+    if n != S or prefix_group.shape != (S,):
         raise ValueError("q, block_table and prefix_group must have one row a sequence")
-    if prefix_blocks.dim() != 1 or prefix_blocks.numel() < 1:
-        raise ValueError("prefix_blocks must be [groups], one group at least")
     groups = prefix_blocks.numel()
-    need = lib.kvs_paged_decode_shared_workspace(S, groups, Hq, Hkv, D, block_table.shape[1], bs)
+    if groups < 1 or prefix_blocks.dim() != 1:
+        raise ValueError("prefix_blocks must be [groups], one group at least")
+    need = lib.kvs_paged_decode_shared_workspace(S, groups, Hq, Hkv, D, mb, bs)
     ws = _workspace(need, q.device)
     with _on(q):
         _check("kvs_paged_decode_shared", lib.kvs_paged_decode_shared(
             _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(slot_pos), _ptr(block_table), _ptr(seq_blocks), _ptr(prefix_group),
-            _ptr(prefix_blocks), _ptr(o), _ptr(lse), S, groups, Hq, Hkv, D, nb, bs, block_table.shape[1], scale, _ptr(ws),
-            need, _stream(q)))
+            _ptr(prefix_blocks), _ptr(o), _ptr(lse), S, groups, Hq, Hkv, D, nb, bs, mb, scale, _ptr(ws), need, _stream(q)))
     return o, lse
 
 
@@ -358,21 +378,18 @@ def kvs_paged_extend(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, q_p
     int32 [Ntot]; each sees the live entries at p <= its own position, under a ``window`` (None: none) those less than
     ``window`` behind it and the first ``sinks``.  LSE is float32 [Ntot, Hq].
     """
-    o, lse, scale = _rows_args(q, k_cache, v_cache, slot_pos, block_table, seq_blocks, softmax_scale, out, lse, q_pos,
-                               cu_seqlens)
-    n, Hq, D = q.shape
-    nb, Hkv, bs, _ = k_cache.shape
-    S = block_table.shape[0]
+    n, Hq, D, nb, Hkv, bs, S, mb, o, lse, scale = _rows_args(q, k_cache, v_cache, slot_pos, block_table, seq_blocks,
+                                                             softmax_scale, out, lse, q_pos, cu_seqlens)
     if q_pos.shape != (n,) or cu_seqlens.shape != (S + 1,):
         raise ValueError("q_pos must be [Ntot] and cu_seqlens [S + 1]")
     if window is not None and window < 1:
         raise ValueError("window must be >= 1 (None: no window)")
-    need = lib.kvs_paged_extend_workspace(S, n, Hq, Hkv, D, block_table.shape[1], bs)
+    need = lib.kvs_paged_extend_workspace(S, n, Hq, Hkv, D, mb, bs)
     ws = _workspace(need, q.device)
     with _on(q):
         _check("kvs_paged_extend", lib.kvs_paged_extend(
             _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(slot_pos), _ptr(block_table), _ptr(seq_blocks), _ptr(q_pos),
-            _ptr(cu_seqlens), _ptr(o), _ptr(lse), S, n, Hq, Hkv, D, nb, bs, block_table.shape[1], scale,
+            _ptr(cu_seqlens), _ptr(o), _ptr(lse), S, n, Hq, Hkv, D, nb, bs, mb, scale,
             _i31(window or 0), _i31(sinks), _ptr(ws), need, _stream(q)))
     return o, lse
 
