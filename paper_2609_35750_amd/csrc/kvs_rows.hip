@@ -893,7 +893,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
 // of the table at a time, in consecutive steps: their table entries; the positions of the slots these name; and, when
 // the list of slots to gather runs short, the slots that some row sees are added to it (a ring of 256).  Bound by HBM where
 // jobs are long: 4 tokens of each of 64 sequences behind 1,000 to 8,000 entries (1.14 GB) 190 us, 6.0 TB/s; 16 rollouts
-// behind 4,096 common entries (80 MB) 26 us, half of it the dependent reads in front of the first tile.
+// behind 4,096 common entries (80 MB) 27 us, half of it the dependent reads in front of the first tile.
 constexpr int kNarrowPick = 192, kNarrowRing = 256;
 template <int D>
 struct NarrowSpace {
