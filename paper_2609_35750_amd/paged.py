@@ -275,31 +275,34 @@ def kvs_paged_evict_lowest(slot_weight, slot_pos, block_table, seq_blocks, keep,
     return pos, counts
 
 
-def _check_caches(k_cache, v_cache, slot_pos) -> None:
-    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
-        raise ValueError("the caches must be [num_blocks, Hkv, block_size, D]")
-    if k_cache.dtype != torch.bfloat16 or v_cache.dtype != torch.bfloat16:
-        raise ValueError("the caches must be bfloat16")
-    if slot_pos is not None and (slot_pos.dtype != torch.int32 or slot_pos.numel() != k_cache.shape[0] * k_cache.shape[2]):
-        raise ValueError("slot_pos must be int32 with num_blocks * block_size entries")
-
-
 def kvs_paged_copy(src, dst, k_cache, v_cache, slot_pos=None, slot_weight=None, move: bool = False) -> None:
     """``kvs_paged_copy``: slot ``dst[i]`` takes the entry of slot ``src[i]`` (int32 [n]); ``move`` empties the sources.
 
     With its position where ``slot_pos`` is given, and its weight where ``slot_weight`` is.
     """
-    _check_caches(k_cache, v_cache, slot_pos)
-    nb, Hkv, bs, D = k_cache.shape
-    _int32(src, dst)
-    if src.dim() != 1 or dst.shape != src.shape:
-        raise ValueError("src and dst must be [n]")
+    cache, n = k_cache.shape, src.shape
+    if len(cache) != 4 or v_cache.shape != cache:
+        raise ValueError("the caches must be [num_blocks, Hkv, block_size, D]")
+    if not k_cache.dtype == v_cache.dtype == torch.bfloat16:
+        raise ValueError("the caches must be bfloat16")
+    nb, Hkv, bs, D = cache
+    if slot_pos is not None and (slot_pos.dtype != torch.int32 or slot_pos.numel() != nb * bs):
+        raise ValueError("slot_pos must be int32 with num_blocks * block_size entries")
     if slot_weight is not None and (slot_weight.dtype != torch.float32 or slot_weight.numel() != nb * bs):
         raise ValueError("slot_weight must be float32 with num_blocks * block_size entries")
-    _same_device(k_cache, v_cache, src, dst, slot_pos, slot_weight)
+    if not src.dtype == dst.dtype == torch.int32:
+        raise ValueError("positions, slots, tables and counts must be int32")
+    if len(n) != 1 or dst.shape != n:
+        raise ValueError("src and dst must be [n]")
+    dev = k_cache.get_device()
+    for t in (v_cache, src, dst, slot_pos, slot_weight):
+        if t is not None and t.get_device() != dev:
+            raise ValueError("tensors must be on one device")
+    if dev < 0:
+        raise ValueError("tensors must be on the GPU")
     with _on(k_cache):
         _check("kvs_paged_copy", lib.kvs_paged_copy(
-            _ptr(src), _ptr(dst), src.numel(), _ptr(k_cache), _ptr(v_cache), _ptr(slot_pos), _ptr(slot_weight), int(move),
+            _ptr(src), _ptr(dst), n[0], _ptr(k_cache), _ptr(v_cache), _ptr(slot_pos), _ptr(slot_weight), int(move),
             nb, bs, Hkv, D, _stream(k_cache)))
 
 
