@@ -431,6 +431,7 @@ int BlockManager::compact(int seq, int32_t* from, int32_t* to, int* n, std::stri
 int BlockManager::groups(int32_t* seq_group, int32_t* group_blocks, int* n, std::string* err) const {
   *n = 0;
   for (int s = 0; s < ns_; ++s) seq_group[s] = -1;
+  if (extra_ == 0) return kOk;
   struct Run {
     long long own, inner;   // block reads saved by the run as a group; by the runs inside it
     int first, last, blocks;
@@ -503,7 +504,8 @@ int BlockManager::groups(int32_t* seq_group, int32_t* group_blocks, int* n, std:
 int BlockManager::shared(int seq) const {
   if (seq < 0 || seq >= ns_) return -1;
   int k = 0;
-  for (int blk : blocks_[seq]) k += refs_[blk] > 1;
+  if (extra_ > 0)   // a cache that has not forked asks this at every eviction
+    for (int blk : blocks_[seq]) k += refs_[blk] > 1;
   return k;
 }
 
