@@ -151,10 +151,10 @@ int BlockManager::append(int seq, const int32_t* pos, int n, int32_t* slots, std
 // touches consecutive blocks, so the search for each ends where the last one did, or one behind it.
 std::vector<int>::iterator BlockManager::find_block(int seq, int blk, size_t* at) {
   auto& bl = blocks_[seq];
-  auto it = bl.end();
-  for (size_t i = *at; i < bl.size() && i < *at + 2; ++i)
-    if (bl[i] == blk) it = bl.begin() + i;
-  if (it == bl.end()) it = std::find(bl.begin(), bl.end(), blk);
+  const size_t i = *at;
+  const auto it = i < bl.size() && bl[i] == blk           ? bl.begin() + i
+                  : i + 1 < bl.size() && bl[i + 1] == blk ? bl.begin() + i + 1
+                                                          : std::find(bl.begin(), bl.end(), blk);
   *at = it - bl.begin();
   return it;
 }
@@ -255,6 +255,7 @@ int BlockManager::evict_shared(int seq, const int32_t* pos, int n, int32_t* slot
       if (blocks_[seq].back() == r.fresh) tail_fill_[seq] = r.used;
   }
   size_t at = 0;
+  const bool shared = !taken.empty();
   for (int i = 0; i < n; ++i) {
     const int p = pos[i];
     int* s = map.find(p);
@@ -262,14 +263,16 @@ int BlockManager::evict_shared(int seq, const int32_t* pos, int n, int32_t* slot
     *s = SlotMap::kNone;
     map.count(p, -1);
     const int blk = slot / bs_;
-    const auto t = taken.empty() ? taken.end() : taken.find(blk);
-    if (t == taken.end()) {
-      slots[i] = slot;
-      if (--live_[blk] == 0) drop_block(seq, blk, &at);
-    } else {   // the others keep it
-      slots[i] = -1;
-      if (--t->second == 0 && !which.count(blk)) drop_block(seq, blk, &at);
+    if (shared) {   // the others keep it
+      const auto t = taken.find(blk);
+      if (t != taken.end()) {
+        slots[i] = -1;
+        if (--t->second == 0 && !which.count(blk)) drop_block(seq, blk, &at);
+        continue;
+      }
     }
+    slots[i] = slot;
+    if (--live_[blk] == 0) drop_block(seq, blk, &at);
   }
   return kOk;
 }

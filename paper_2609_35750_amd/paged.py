@@ -428,7 +428,8 @@ class PagedKVCache:
         self.slot_pos = torch.full((num_blocks * block_size,), -1, dtype=torch.int32, device=self.device)
         self.slot_weight = torch.zeros(num_blocks * block_size, dtype=torch.float32, device=self.device) if weights else None
         self._tables = None
-        self._blocks = 0      # in all tables, when they were uploaded
+        self._forks = False   # whether sequences have ever shared blocks
+        self._blocks = None   # of every sequence, when the tables were uploaded
         self._shares = None   # groups of sequences that share a prefix, on the device; None: not known, (): none
         self._saved = 0       # blocks the groups need not read again
 
@@ -486,7 +487,7 @@ class PagedKVCache:
 
     def evict(self, seq: int, positions) -> np.ndarray:
         """Entries of a sequence leave; returns their slots, -1 for those in blocks that other sequences hold too."""
-        if not self.bm.shared(seq) > 0:
+        if not (self._forks and self.bm.shared(seq) > 0):
             slots = self.bm.evict(seq, _i32(positions))
             if slots.size:
                 self._mark_evicted(slots)
@@ -501,7 +502,7 @@ class PagedKVCache:
         return slots
 
     def release(self, seq: int) -> np.ndarray:
-        if self.bm.shared(seq) > 0:
+        if self._forks and self.bm.shared(seq) > 0:
             self._shares = None
         slots = self.bm.release(seq)
         if slots.size:
@@ -519,6 +520,7 @@ class PagedKVCache:
         if self.slot_weight is not None:
             raise ValueError("entries' weights are one sequence's: a cache that keeps them takes copy()")
         self.bm.fork(src, dst)
+        self._forks = True
         self._tables = self._shares = None
 
     def copy(self, src: int, dst: int) -> None:
@@ -546,7 +548,7 @@ class PagedKVCache:
             _check("kvs_bm_tables", lib.kvs_bm_tables(self.bm._h, p, p + 4 * n))
             dev = torch.from_numpy(both).to(self.device)
             self._tables = (dev[:n].view(self.num_seqs, self.max_blocks), dev[n:])
-            self._blocks = int(both[n:].sum())
+            self._blocks = both[n:]
         return self._tables
 
     def device_groups(self) -> Tuple[torch.Tensor, ...]:
@@ -560,6 +562,10 @@ class PagedKVCache:
                 both = torch.from_numpy(np.concatenate([group, blocks])).to(self.device)
                 self._shares = both[: group.size], both[group.size:]
         return self._shares
+
+    def _pays(self) -> bool:
+        saved = self._saved * 4 * self.block_size * self.Hkv * self.D
+        return saved >= _SAVED_BYTES and 2 * self._saved >= int(self._blocks.sum())
 
     def extend(self, q: torch.Tensor, positions, lengths, softmax_scale=None, out=None, lse=None,
                window: Optional[int] = None, sinks: int = 0):
@@ -587,13 +593,12 @@ class PagedKVCache:
         """
         table, nblk = self.device_tables()
         if window is None and not accumulate:
-            shares = self.device_groups()
+            shares = self.device_groups() if self._forks else ()
             # Reading a shared prefix once takes two or three launches more than reading it once a sequence, mostly from the
             # caches.  32/8 heads, D = 128: 16 sequences behind 4,096 entries with 1,000 of their own 49 -> 36 us, 8 behind
             # 4,096 with 500 26 -> 25; but 64 behind 1,024 with 1,000 67 -> 73, 8 behind 2,048 with 500 19 -> 23.
-            block_bytes = 4 * self.block_size * self.Hkv * self.D
-            pays = self._saved * block_bytes >= _SAVED_BYTES and 2 * self._saved >= self._blocks
-            if shares and (pays or q.shape[-2] > 32 * self.Hkv):   # groups of more than 32 q-heads: the plain call does not take them
+            # Groups of more than 32 q-heads the plain call does not take.
+            if shares and (self._pays() or q.shape[-2] > 32 * self.Hkv):
                 return kvs_paged_decode_shared(q, self.k, self.v, self.slot_pos, table, nblk, *shares, softmax_scale, out, lse)
             with _on(self.k):
                 return kvs_paged_decode(q, self.k, self.v, self.slot_pos, table, nblk, softmax_scale, out, lse)
