@@ -432,6 +432,9 @@ class PagedKVCache:
         self._blocks = None   # of every sequence, when the tables were uploaded
         self._shares = None   # groups of sequences that share a prefix, on the device; None: not known, (): none
         self._saved = 0       # blocks the groups need not read again
+        # groups of sequences by themselves; made here, as a captured decode would leave them to its graph's replays
+        self._alone = (torch.full((num_seqs,), -1, dtype=torch.int32, device=self.device),
+                       torch.zeros(1, dtype=torch.int32, device=self.device))
 
     def append(self, seq: int, positions, k_new: torch.Tensor, v_new: torch.Tensor,
                weights: Optional[torch.Tensor] = None) -> np.ndarray:
@@ -589,7 +592,8 @@ class PagedKVCache:
         ``window`` (with ``positions``, the queries' trace positions: a list or an int32 tensor on the GPU) shows each
         query the entries less than ``window`` behind it and the first ``sinks``; without a window every live entry is
         seen, and ``positions`` and ``sinks`` have no effect (layers of both kinds take the same call).  ``accumulate``
-        adds the entries' attention weights to ``slot_weight``.
+        adds the entries' attention weights to ``slot_weight``.  A KV head may have 64 q-heads, with a window or
+        ``accumulate`` 32.
         """
         table, nblk = self.device_tables()
         if window is None and not accumulate:
@@ -597,9 +601,11 @@ class PagedKVCache:
             # Reading a shared prefix once takes two or three launches more than reading it once a sequence, mostly from the
             # caches.  32/8 heads, D = 128: 16 sequences behind 4,096 entries with 1,000 of their own 49 -> 36 us, 8 behind
             # 4,096 with 500 26 -> 25; but 64 behind 1,024 with 1,000 67 -> 73, 8 behind 2,048 with 500 19 -> 23.
-            # Groups of more than 32 q-heads the plain call does not take.
-            if shares and (self._pays() or q.shape[-2] > 32 * self.Hkv):
-                return kvs_paged_decode_shared(q, self.k, self.v, self.slot_pos, table, nblk, *shares, softmax_scale, out, lse)
+            # More than 32 q-heads a KV head the plain call does not take, whatever is shared.
+            many = q.dim() == 3 and q.shape[1] > 32 * self.Hkv
+            if many or (shares and self._pays()):
+                return kvs_paged_decode_shared(q, self.k, self.v, self.slot_pos, table, nblk, *(shares or self._alone),
+                                               softmax_scale, out, lse)
             with _on(self.k):
                 return kvs_paged_decode(q, self.k, self.v, self.slot_pos, table, nblk, softmax_scale, out, lse)
         if accumulate and self.slot_weight is None:
