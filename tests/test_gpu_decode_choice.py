@@ -35,7 +35,7 @@ def taken(pg, request, monkeypatch):
 @pytest.mark.parametrize("case", [share.DECODE[i] for i in (2, 3, 4, 6, 8, 10)], ids=lambda c: f"{len(c[0])}_H{c[2]}x{c[3]}_D{c[4]}")
 def test_decode_over_shared_prefixes(pg, taken, case):
     share.test_decode_over_shared_prefixes(pg, case)
-    assert taken
+    assert taken or case[2] > 32 * case[3]       # which do not ask
 
 
 @pytest.mark.parametrize("block", [1, 5, 16])
