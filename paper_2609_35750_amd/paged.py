@@ -536,10 +536,14 @@ class PagedKVCache:
 
         Blocks it shares, and a last one with room for appends, stay as they are.
         """
-        before = self.bm.free_blocks()
-        todo = [self.bm.compact(s) for s in (range(self.num_seqs) if seq is None else [seq])]
-        self._copy(np.concatenate(todo, axis=1), move=True)
-        self._tables = None
+        before, todo = self.bm.free_blocks(), []
+        try:
+            for s in range(self.num_seqs) if seq is None else [seq]:
+                todo.append(self.bm.compact(s))
+        finally:   # where the manager fails at a sequence, the entries of those in front of it have their new slots
+            self._tables = None
+            if todo:
+                self._copy(np.concatenate(todo, axis=1), move=True)
         return self.bm.free_blocks() - before
 
     def device_tables(self) -> Tuple[torch.Tensor, torch.Tensor]:

@@ -1,7 +1,9 @@
-"""PagedKVCache on the host: which form of the decode it takes (no GPU; the calls into the library are recorded)."""
+"""PagedKVCache on the host: which form of the decode it takes, and that slots hold what the block manager says, also
+behind a call that fails (no GPU; the calls into the library are recorded or done on the CPU)."""
 import contextlib
 import os
 
+import numpy as np
 import pytest
 import torch
 
@@ -78,3 +80,78 @@ def test_saved_reads_decide(paged, decodes, monkeypatch):
     cache._tables = None
     cache.decode(q)
     assert decodes.pop() == ("plain",)
+
+
+class Slots:
+    """A cache whose slots' positions are kept on the CPU."""
+
+    def __init__(self, paged, monkeypatch, S=4):
+        def copy(src, dst, k, v, slot_pos, slot_weight, move):
+            slot_pos[dst.long()] = slot_pos[src.long()]
+            if move:
+                slot_pos[src.long()] = -1
+
+        monkeypatch.setattr(paged, "kvs_paged_copy", copy)
+        self.cache = paged.PagedKVCache(80, 4, S, 30, 2, 64, device="cpu")
+        self.cache._mark_evicted = lambda slots: self.cache.slot_pos.__setitem__(torch.from_numpy(slots).long(), -1)
+        self.held = [set() for _ in range(S)]
+
+    def append(self, s, positions):
+        slots = self.cache.bm.append(s, list(positions))
+        self.cache.slot_pos[torch.from_numpy(slots).long()] = torch.tensor(list(positions), dtype=torch.int32)
+        self.cache._tables = None
+        self.held[s] |= set(positions)
+
+    def evict(self, s, positions):
+        self.cache.evict(s, list(positions))
+        self.held[s] -= set(positions)
+
+    def fork(self, a, b):
+        self.cache.fork(a, b)
+        self.held[b] = set(self.held[a])
+
+    def check(self):
+        """Every sequence's table, as the decode gets it, shows its entries."""
+        table, n = (x.numpy() for x in self.cache.device_tables())
+        for s, want in enumerate(self.held):
+            slots = (table[s, :n[s], None] * 4 + np.arange(4)).reshape(-1)
+            pos = self.cache.slot_pos.numpy()[slots]
+            assert sorted(pos[pos >= 0].tolist()) == sorted(want)
+            assert self.cache.bm.live(s) == len(want)
+
+
+def _sparse(paged, monkeypatch):
+    """Four sequences with entries in half the rows of their blocks."""
+    x = Slots(paged, monkeypatch)
+    for s in range(4):
+        x.append(s, range(40))
+        x.evict(s, range(0, 40, 2))
+    x.check()
+    return x
+
+
+def test_compaction_that_fails_at_a_sequence(paged, monkeypatch):
+    """The manager fails at the third of four sequences: the entries of the first two are where their tables say."""
+    from paper_2609_35750_amd.kvs import KVS_ERR_CAPACITY
+
+    x = _sparse(paged, monkeypatch)
+    compact = x.cache.bm.compact
+
+    def short_of_memory(s):
+        if s == 2:
+            raise paged.KvsError("kvs_bm_compact", KVS_ERR_CAPACITY)
+        return compact(s)
+
+    monkeypatch.setattr(x.cache.bm, "compact", short_of_memory)
+    x.cache.device_tables()
+    with pytest.raises(paged.KvsError):
+        x.cache.compact()
+    x.check()
+
+
+def test_compaction_of_all_sequences(paged, monkeypatch):
+    x = _sparse(paged, monkeypatch)
+    assert x.cache.compact() == 4 * 5
+    x.check()
+    assert x.cache.compact() == 0
+    x.check()
