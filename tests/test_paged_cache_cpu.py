@@ -143,9 +143,10 @@ def test_compaction_that_fails_at_a_sequence(paged, monkeypatch):
         return compact(s)
 
     monkeypatch.setattr(x.cache.bm, "compact", short_of_memory)
-    x.cache.device_tables()
     with pytest.raises(paged.KvsError):
         x.cache.compact()
+    x.check()
+    x.append(0, [40])
     x.check()
 
 
