@@ -495,11 +495,12 @@ class PagedKVCache:
             if slots.size:
                 self._mark_evicted(slots)
         else:   # what stays of a shared block goes to one of the sequence's own
+            room = self._room(self.bm.live(seq))
             slots, pairs = self.bm.evict_shared(seq, positions)
             mine = slots[slots >= 0]
             if mine.size:
                 self._mark_evicted(mine)
-            self._copy(pairs)
+            self._copy(pairs, room)
             self._shares = None
         self._tables = None
         return slots
@@ -513,10 +514,20 @@ class PagedKVCache:
         self._tables = None
         return slots
 
-    def _copy(self, pairs: np.ndarray, move: bool = False) -> None:
-        if pairs.shape[1]:
-            src, dst = torch.from_numpy(np.ascontiguousarray(pairs)).to(self.device)
-            kvs_paged_copy(src, dst, self.k, self.v, self.slot_pos, self.slot_weight, move)
+    def _room(self, entries: int) -> torch.Tensor:
+        """Device memory for slots to copy from and to, asked for before the manager gives entries new slots: without it
+        nothing has changed."""
+        if self.k.is_cuda:
+            with _on(self.k):
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("slots are copied by lists of the host, which a capture does not take")
+        return torch.empty(2 * max(entries, 1), dtype=torch.int32, device=self.device)
+
+    def _copy(self, pairs: np.ndarray, room: torch.Tensor, move: bool = False) -> None:
+        n = pairs.shape[1]
+        if n:
+            room[:2 * n].copy_(torch.from_numpy(pairs.reshape(-1)))
+            kvs_paged_copy(room[:n], room[n:2 * n], self.k, self.v, self.slot_pos, self.slot_weight, move)
 
     def fork(self, src: int, dst: int) -> None:
         """The empty sequence ``dst`` shares the entries of ``src``; what either appends or evicts then is its own."""
@@ -528,7 +539,8 @@ class PagedKVCache:
 
     def copy(self, src: int, dst: int) -> None:
         """The empty sequence ``dst`` gets copies of the entries of ``src``, with their weights, in fresh blocks."""
-        self._copy(self.bm.copy(src, dst))
+        room = self._room(self.bm.live(src))
+        self._copy(self.bm.copy(src, dst), room)
         self._tables = None
 
     def compact(self, seq: Optional[int] = None) -> int:
@@ -536,14 +548,15 @@ class PagedKVCache:
 
         Blocks it shares, and a last one with room for appends, stay as they are.
         """
-        before, todo = self.bm.free_blocks(), []
+        before, todo, seqs = self.bm.free_blocks(), [], range(self.num_seqs) if seq is None else [seq]
+        room = self._room(sum(self.bm.live(s) for s in seqs))
         try:
-            for s in range(self.num_seqs) if seq is None else [seq]:
+            for s in seqs:
                 todo.append(self.bm.compact(s))
         finally:   # where the manager fails at a sequence, the entries of those in front of it have their new slots
             self._tables = None
             if todo:
-                self._copy(np.concatenate(todo, axis=1), move=True)
+                self._copy(np.concatenate(todo, axis=1), room, move=True)
         return self.bm.free_blocks() - before
 
     def device_tables(self) -> Tuple[torch.Tensor, torch.Tensor]:

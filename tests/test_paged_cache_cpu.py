@@ -156,3 +156,37 @@ def test_compaction_of_all_sequences(paged, monkeypatch):
     x.check()
     assert x.cache.compact() == 0
     x.check()
+
+
+@pytest.mark.parametrize("call", ["copy", "compact", "compact one", "evict"])
+def test_a_device_without_memory_for_the_lists(paged, monkeypatch, call):
+    """The lists of slots find no room on the device: manager and slots are as they were, and the call works later."""
+    x = Slots(paged, monkeypatch)
+    x.append(0, range(40))
+    x.evict(0, range(0, 30, 2))
+    x.append(1, range(20))
+    x.fork(1, 2)
+    free = x.cache.bm.free_blocks()
+
+    def run():
+        if call == "copy":
+            x.cache.copy(0, 3)
+            x.held[3] = set(x.held[0])
+        elif call == "evict":
+            x.evict(2, [1, 6])
+        else:
+            x.cache.compact(0 if call == "compact one" else None)
+
+    def full(*a, **k):
+        raise torch.OutOfMemoryError("full")
+
+    with monkeypatch.context() as m:
+        m.setattr(torch, "empty", full)
+        m.setattr(torch.Tensor, "to", full)
+        with pytest.raises(torch.OutOfMemoryError):
+            run()
+    assert x.cache.bm.free_blocks() == free
+    x.append(1, [20])
+    x.check()
+    run()
+    x.check()
