@@ -201,7 +201,8 @@ __device__ __forceinline__ void chunk_stats(const RowsArgs& a, int first, int wa
 
 // The plan, by workgroup 0: for up to 256 sequences and groups one wave makes it, with what it knows of them in LDS, and
 // all of them try the sizes of wide jobs' runs and write the units.  Bound by latency: 5 us for 4 sequences, 11 for 64 of
-// one group.  Under a window the other workgroups take the positions of the tables' chunks.
+// one group, 30 for 256 of 64 groups.  Beyond that the counts are in global memory, and each group among 64 sequences is a
+// round trip there: 104 us for 512 shuffled sequences of 64 groups, 224 for 1,024 of 128.  Under a window the other workgroups take the positions of the tables' chunks.
 template <bool SHARED, bool SMALL>
 __global__ void __launch_bounds__(SMALL ? 512 : 1024) rows_plan_kernel(RowsArgs a) {
   constexpr int NT = SMALL ? 512 : 1024, PT = SMALL ? kWave : NT;   // threads; those that plan
@@ -680,7 +681,8 @@ constexpr int kWidePick = 512;   // places of the table that a wide unit looks a
 // double-buffered, each tile read by the four waves.  Scores are S^T = K Q^T (keys on M, rows on N), so that a lane holds 16
 // scores of one row; softmax and the products with V as in the forward of the eviction mask.  Three workgroups a CU, whose
 // registers just do without spills.  Bound by the matrix cores at the clock their power leaves, as that forward: 4,096
-// tokens of 32 q-heads over 20,480 entries (D = 128) 1.2 ms, 1,030 TFLOP/s, matrix cores busy 51% at 1.8 GHz.  Asking for
+// tokens of 32 q-heads over 20,480 entries (D = 128) 1.21 ms, 993 TFLOP/s, 0.91 of that forward's rate over a trace of 16,384
+// in turns with it, matrix cores busy 52% at 1.85 GHz.  Asking for
 // the next 512 places while the tiles of the last ones are computed, by copies to LDS, made that 5% slower.
 // FAR: caches of 4 GiB or more, whose rows need 64-bit addresses of their own; else a copy takes one addition.
 template <int D, bool SHARED, bool FAR>
@@ -893,7 +895,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3, 3))
 // of the table at a time, in consecutive steps: their table entries; the positions of the slots these name; and, when
 // the list of slots to gather runs short, the slots that some row sees are added to it (a ring of 256).  Bound by HBM where
 // jobs are long: 4 tokens of each of 64 sequences behind 1,000 to 8,000 entries (1.14 GB) 190 us, 6.0 TB/s; 16 rollouts
-// behind 4,096 common entries (80 MB) 27 us, half of it the dependent reads in front of the first tile.
+// behind 4,096 common entries (80 MB) 28 us, half of it the dependent reads in front of the first tile.
 constexpr int kNarrowPick = 192, kNarrowRing = 256;
 template <int D>
 struct NarrowSpace {
@@ -1126,7 +1128,7 @@ struct Joined {
 // workgroup a row, whose groups of D / 4 lanes take the parts in turn (one long sequence has hundreds); else, for many
 // rows of new tokens, which have few parts each, a wave a token and KV head, whose halves (D = 64: quarters) take the
 // head's rows in turn, so that the token is looked up once.  Bound by the latency of its reads: four parts are asked for
-// at a time.  4 us for few rows, 8 for 64 sequences with 30 MB of parts, 20 for 4,096 tokens with 73 MB.  A workgroup a row
+// at a time.  4 us for few rows, 10 for 64 sequences with 39 MB of parts, 17 for 4,096 tokens with 54 MB.  A workgroup a row
 // against a wave a token: one token over 32,000 entries 36 and 83 us.
 template <int D, bool SHARED, bool BLOCK>
 __global__ void __launch_bounds__(256) rows_merge_kernel(RowsArgs a) {
